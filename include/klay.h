@@ -337,6 +337,109 @@ void klay_builder_destroy(klay_builder* b);
 /* Frees index arrays and library-owned workspace.  NULL is allowed. */
 void klay_destroy(klay_circuit* c);
 
+/*
+ * Operators between a network and a circuit's leaf weights.  They need no handle; every call enqueues kernels on `stream` of `device`
+ * (of the calling thread's current device it makes no use, and leaves it as it was), allocates nothing and does not synchronise.
+ * Two calls may overlap if they share no buffer that either writes.
+ */
+
+/* Types of the tensors that a network gives and takes: IEEE single, bfloat16, IEEE half.  All arithmetic is in single. */
+typedef enum { KLAY_F32 = 0, KLAY_BF16 = 1, KLAY_F16 = 2 } klay_dtype;
+
+/* Where row r (0 <= r < rows) of a tensor starts: (r / inner) * outer_stride + (r % inner) * inner_stride elements. */
+typedef struct klay_rows {
+    int64_t inner, outer_stride, inner_stride;
+} klay_rows;
+
+/*
+ * klay_tokens_forward -- log probabilities of given tokens under rows of logits (the weights of literals "the network answers t"):
+ *   p_j = exp(x_j) / sum_i exp(x_i);  logp_k = ln p_{t_k};  neg_k = ln(1 - p_{t_k}), the weight of the negated literal, exact also
+ *   where p rounds to 1;  entropy = - sum_j p_j ln p_j;  the `top` largest logits (equal ones: the lowest index first).
+ *   logits      device [rows, vocab] of `dtype`, the elements of a row next to each other, rows placed by logit_rows
+ *   tokens      device [rows, num_tokens] int64, placed by token_rows and token_stride.  A negative token asks for nothing: its logp and
+ *               neg are 0 and it has no gradient.  A token >= vocab gives NaN.  The same token may be asked for more than once.
+ *   logp, neg   device [rows, num_tokens] fp32; neg may be NULL, logp only where num_tokens = 0
+ *   entropy     device [rows] fp32, or NULL
+ *   stats       device [rows, 4] fp32, what klay_tokens_backward needs of a row, or NULL
+ *   top_logp, top_tokens   device [rows, top] fp32 / int64, best first; NULL where top = 0
+ *   workspace   device, 16-byte aligned, klay_tokens_workspace_bytes(args) bytes; NULL where that is 0
+ * A logit of -inf is a token that is not allowed.  A row of nothing else gives logp = -inf, neg = 0, entropy 0, and no gradient; a NaN or
+ * +inf makes every value of its row NaN (and leaves top_tokens any tokens).
+ * Errors: KLAY_EINVAL (sizes out of range: 1 <= vocab, 0 <= num_tokens <= 1024, 0 <= top <= min(vocab, 64), 0 <= rows < 2^31; null or
+ * unknown arguments), KLAY_ENOMEM (workspace too small), KLAY_EHIP.
+ */
+typedef struct klay_tokens_args {
+    int32_t dtype, device, vocab, num_tokens, top, reserved;
+    int64_t rows;
+    const void* logits;
+    klay_rows logit_rows;
+    const int64_t* tokens;
+    klay_rows token_rows;
+    int64_t token_stride;
+} klay_tokens_args;
+size_t klay_tokens_workspace_bytes(const klay_tokens_args* args);
+klay_status klay_tokens_forward(const klay_tokens_args* args, float* logp, float* neg, float* entropy, float* stats, float* top_logp,
+                                int64_t* top_tokens, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * klay_tokens_backward -- derivative of a klay_tokens_forward with respect to the logits, which must be as they were.
+ *   stats       as written by the forward call (with entropy asked for if dentropy is given)
+ *   dlogp, dneg, dentropy   device, shaped as the outputs; each may be NULL (no adjoint)
+ *   dlogits     device [rows, vocab] contiguous, of `dtype`; every entry is written, rounded once.  An adjoint of exactly 0
+ *               contributes 0, and a row all of whose adjoints are 0 is not read.
+ * The same inputs give the same bits.  Errors: as klay_tokens_forward.
+ */
+klay_status klay_tokens_backward(const klay_tokens_args* args, const float* stats, const float* dlogp, const float* dneg,
+                                 const float* dentropy, void* dlogits, void* stream);
+
+/*
+ * klay_scan_forward -- gated recurrence over sequences in a semiring (Section 4), the value of a chain of AND and OR gates of any length:
+ *   h_t = a_t (x) h_{t-1} (+) x_t:  REAL: a h + x;  LOG: log(exp(a + h) + exp(x));  MAXLOG: max(a + h, x)
+ *   gates, inputs   device [batch, time, channels] of `dtype` (KLAY_F32 in the log-domain semirings), channels next to each other,
+ *               the two other strides in elements
+ *   offsets     NULL: `batch` sequences of `time` steps.  Otherwise batch = 1 and device int64 [sequences + 1]: sequence s is the rows
+ *               offsets[s] .. offsets[s + 1] - 1, ascending, in 0 .. time; it may be empty.  Rows of no sequence get 0 as states.
+ *   row_info    device int32 [time]; required with offsets, for klay_scan_backward, which reads what the forward call wrote
+ *   initial     device fp32 [batch or sequences, channels]: the states before the first steps; NULL: 0 (LOG, MAXLOG: -inf)
+ *   states      device [batch, time, channels] of `dtype`, contiguous: h, each rounded once from fp32
+ *   final       device fp32 [batch or sequences, channels]: the states behind the last steps (of an empty sequence: its initial one); or NULL
+ *   workspace   device, 16-byte aligned, klay_scan_workspace_bytes(args) bytes (for either direction); NULL where that is 0
+ * Offsets that are none (descending, out of range) give undefined values, but no access outside the arrays.
+ * Errors: KLAY_EINVAL, KLAY_ENOMEM (workspace too small), KLAY_EHIP.
+ */
+typedef struct klay_scan_args {
+    int32_t dtype, semiring, device, channels;
+    int64_t batch, time, sequences;
+    const void* gates;
+    const void* inputs;
+    int64_t gates_batch_stride, gates_time_stride, inputs_batch_stride, inputs_time_stride;
+    const int64_t* offsets;
+    int32_t* row_info;
+    const float* initial;
+} klay_scan_args;
+size_t klay_scan_workspace_bytes(const klay_scan_args* args);
+klay_status klay_scan_forward(const klay_scan_args* args, void* states, float* final, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * klay_scan_backward -- derivative of a klay_scan_forward (REAL, LOG) with respect to gates, inputs and initial states.
+ *   args        as for the forward call; REAL does not read inputs (may be NULL)
+ *   states      as written by the forward call
+ *   dstates     device [batch, time, channels] of `dtype`, contiguous, or NULL (no adjoint); dfinal fp32, or NULL
+ *   dgates, dinputs   device [batch, time, channels] of `dtype`, contiguous; dinitial fp32; each may be NULL (not wanted)
+ * A step whose value is log 0 passes nothing down.  Errors: as klay_scan_forward; MAXLOG is not differentiated (KLAY_EINVAL).
+ */
+klay_status klay_scan_backward(const klay_scan_args* args, const void* states, const void* dstates, const float* dfinal, void* dgates,
+                               void* dinputs, float* dinitial, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * klay_scan_step -- one step for `rows` running sequences: state = gates (x) state (+) inputs, in place, and its copy in `dtype`.
+ *   gates, inputs   device [rows, channels] of `dtype`;  state device fp32 [rows, channels];  out [rows, channels] of `dtype` or NULL
+ * Channels next to each other, rows that many elements apart; rows of state and of out must not overlap.
+ */
+klay_status klay_scan_step(int32_t dtype, int32_t semiring, int32_t device, int64_t rows, int32_t channels, const void* gates,
+                           int64_t gates_stride, const void* inputs, int64_t inputs_stride, float* state, int64_t state_stride, void* out,
+                           int64_t out_stride, void* stream);
+
 /* Message of the last failing call on this thread ("" if none). */
 const char* klay_last_error(void);
 

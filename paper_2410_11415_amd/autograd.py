@@ -61,3 +61,21 @@ class CircuitLayer(torch.nn.Module):
             return self.circuit.forward(weights.contiguous(), self.semiring,
                                         neg_weights=None if neg_weights is None else neg_weights.contiguous())
         return _Evaluate.apply(weights, neg_weights, self)
+
+    def from_logits(self, logits, tokens, complement: bool = True):
+        """The circuit on the answers of a network: variable ``g * K + k`` is "position g answers ``tokens[..., g, k]``", its log
+        weight (and with ``complement`` that of its negation; without, a negated literal weighs 1, for circuits that say by themselves
+        that a position answers one thing) comes from ``logits[B, G, V]`` by :func:`token_logprobs`.  ``tokens``: int64 ``[G, K]`` or
+        ``[B, G, K]`` with G * K the circuit's variables; log-domain semirings only.  Gradients go to ``logits``.
+        """
+        from .operators import token_logprobs
+        if self.semiring not in (KLAY_LOG, KLAY_MAXLOG):
+            raise ValueError("from_logits gives log weights: the layer's semiring must be KLAY_LOG or KLAY_MAXLOG")
+        if logits.dim() != 3 or tokens.dim() not in (2, 3) or tokens.shape[-2] != logits.shape[1]:
+            raise ValueError("logits must be [B, G, V] and tokens [G, K] or [B, G, K]")
+        batch, groups = logits.shape[:2]
+        if groups * tokens.shape[-1] != self.circuit.num_vars:
+            raise ValueError("tokens must name %d variables, not %d x %d" % (self.circuit.num_vars, groups, tokens.shape[-1]))
+        r = token_logprobs(logits, tokens.expand(batch, -1, -1) if tokens.dim() == 2 else tokens, complement=complement)
+        weights = r.logp.reshape(batch, -1)
+        return self(weights, r.neg.reshape(batch, -1) if complement else torch.zeros_like(weights))

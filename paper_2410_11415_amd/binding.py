@@ -17,6 +17,7 @@ from . import build as _build
 
 KLAY_OK, KLAY_EINVAL, KLAY_ECYCLE, KLAY_ENOMEM, KLAY_EHIP, KLAY_ESTATE = range(6)
 KLAY_REAL, KLAY_LOG, KLAY_MAXLOG = 0, 1, 2
+KLAY_F32, KLAY_BF16, KLAY_F16 = range(3)
 KLAY_LIT, KLAY_AND, KLAY_OR, KLAY_TRUE, KLAY_FALSE = range(5)
 KLAY_STATIC_WORKSPACE_BYTES = 64 << 20
 KERNEL_CLASSES = ("leaf", "fwd_sum", "fwd_prod", "fwd_lse", "root", "seed", "bwd_sum", "bwd_softmax", "bwd_leaf",
@@ -27,7 +28,8 @@ EXPORTS = ("klay_build", "klay_build_ex", "klay_forward", "klay_backward", "klay
            "klay_layer_csr", "klay_layer_nodes", "klay_workspace_bytes", "klay_set_workspace",
            "klay_set_profiling", "klay_get_profile", "klay_destroy", "klay_last_error", "klay_builder_create",
            "klay_builder_add", "klay_builder_finish", "klay_builder_destroy", "klay_forward_lits", "klay_backward_lits", "klay_root_positions", "klay_forward_f64",
-           "klay_backward_f64", "klay_forward_static", "klay_persistent_layers")
+           "klay_backward_f64", "klay_forward_static", "klay_persistent_layers", "klay_tokens_workspace_bytes", "klay_tokens_forward",
+           "klay_tokens_backward", "klay_scan_workspace_bytes", "klay_scan_forward", "klay_scan_backward", "klay_scan_step")
 
 
 class KlayError(RuntimeError):
@@ -55,6 +57,24 @@ class klay_info_t(ctypes.Structure):
 class klay_profile_t(ctypes.Structure):
     _fields_ = [("ms", ctypes.c_float * len(KERNEL_CLASSES)), ("launches", ctypes.c_int32 * len(KERNEL_CLASSES)),
                 ("alg_bytes", ctypes.c_double * len(KERNEL_CLASSES)), ("min_bytes", ctypes.c_double * len(KERNEL_CLASSES))]
+
+
+class klay_rows(ctypes.Structure):
+    _fields_ = [("inner", ctypes.c_int64), ("outer_stride", ctypes.c_int64), ("inner_stride", ctypes.c_int64)]
+
+
+class klay_tokens_args(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("device", ctypes.c_int32), ("vocab", ctypes.c_int32), ("num_tokens", ctypes.c_int32),
+                ("top", ctypes.c_int32), ("reserved", ctypes.c_int32), ("rows", ctypes.c_int64), ("logits", ctypes.c_void_p),
+                ("logit_rows", klay_rows), ("tokens", ctypes.c_void_p), ("token_rows", klay_rows), ("token_stride", ctypes.c_int64)]
+
+
+class klay_scan_args(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("semiring", ctypes.c_int32), ("device", ctypes.c_int32), ("channels", ctypes.c_int32),
+                ("batch", ctypes.c_int64), ("time", ctypes.c_int64), ("sequences", ctypes.c_int64), ("gates", ctypes.c_void_p),
+                ("inputs", ctypes.c_void_p), ("gates_batch_stride", ctypes.c_int64), ("gates_time_stride", ctypes.c_int64),
+                ("inputs_batch_stride", ctypes.c_int64), ("inputs_time_stride", ctypes.c_int64), ("offsets", ctypes.c_void_p),
+                ("row_info", ctypes.c_void_p), ("initial", ctypes.c_void_p)]
 
 
 _lib = None
@@ -119,6 +139,20 @@ def load():
     lib.klay_set_profiling.argtypes = [vp, i32]
     lib.klay_get_profile.restype = ctypes.c_int
     lib.klay_get_profile.argtypes = [vp, ctypes.POINTER(klay_profile_t)]
+    lib.klay_tokens_workspace_bytes.restype = ctypes.c_size_t
+    lib.klay_tokens_workspace_bytes.argtypes = [ctypes.POINTER(klay_tokens_args)]
+    lib.klay_tokens_forward.restype = ctypes.c_int
+    lib.klay_tokens_forward.argtypes = [ctypes.POINTER(klay_tokens_args), vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.klay_tokens_backward.restype = ctypes.c_int
+    lib.klay_tokens_backward.argtypes = [ctypes.POINTER(klay_tokens_args), vp, vp, vp, vp, vp, vp]
+    lib.klay_scan_workspace_bytes.restype = ctypes.c_size_t
+    lib.klay_scan_workspace_bytes.argtypes = [ctypes.POINTER(klay_scan_args)]
+    lib.klay_scan_forward.restype = ctypes.c_int
+    lib.klay_scan_forward.argtypes = [ctypes.POINTER(klay_scan_args), vp, vp, vp, ctypes.c_size_t, vp]
+    lib.klay_scan_backward.restype = ctypes.c_int
+    lib.klay_scan_backward.argtypes = [ctypes.POINTER(klay_scan_args), vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.klay_scan_step.restype = ctypes.c_int
+    lib.klay_scan_step.argtypes = [i32, i32, i32, i64, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp]
     lib.klay_builder_create.restype = ctypes.c_int
     lib.klay_builder_create.argtypes = [i32, ctypes.POINTER(vp)]
     lib.klay_builder_add.restype = ctypes.c_int
@@ -218,6 +252,40 @@ def klay_builder_finish(builder, device, options: klay_options | None = None):
 
 def klay_builder_destroy(builder):
     load().klay_builder_destroy(builder)
+
+
+def klay_tokens_workspace_bytes(args) -> int:
+    return load().klay_tokens_workspace_bytes(args)
+
+
+def klay_tokens_forward(args, logp_ptr, neg_ptr, entropy_ptr, stats_ptr, top_logp_ptr, top_tokens_ptr, workspace_ptr,
+                        workspace_bytes, stream=0):
+    _check(load().klay_tokens_forward(args, logp_ptr, neg_ptr, entropy_ptr, stats_ptr, top_logp_ptr, top_tokens_ptr,
+                                      workspace_ptr, workspace_bytes, stream))
+
+
+def klay_tokens_backward(args, stats_ptr, dlogp_ptr, dneg_ptr, dentropy_ptr, dlogits_ptr, stream=0):
+    _check(load().klay_tokens_backward(args, stats_ptr, dlogp_ptr, dneg_ptr, dentropy_ptr, dlogits_ptr, stream))
+
+
+def klay_scan_workspace_bytes(args) -> int:
+    return load().klay_scan_workspace_bytes(args)
+
+
+def klay_scan_forward(args, states_ptr, final_ptr, workspace_ptr, workspace_bytes, stream=0):
+    _check(load().klay_scan_forward(args, states_ptr, final_ptr, workspace_ptr, workspace_bytes, stream))
+
+
+def klay_scan_backward(args, states_ptr, dstates_ptr, dfinal_ptr, dgates_ptr, dinputs_ptr, dinitial_ptr, workspace_ptr,
+                       workspace_bytes, stream=0):
+    _check(load().klay_scan_backward(args, states_ptr, dstates_ptr, dfinal_ptr, dgates_ptr, dinputs_ptr, dinitial_ptr,
+                                     workspace_ptr, workspace_bytes, stream))
+
+
+def klay_scan_step(dtype, semiring, device, rows, channels, gates_ptr, gates_stride, inputs_ptr, inputs_stride, state_ptr,
+                   state_stride, out_ptr, out_stride, stream=0):
+    _check(load().klay_scan_step(dtype, semiring, device, rows, channels, gates_ptr, gates_stride, inputs_ptr, inputs_stride,
+                                 state_ptr, state_stride, out_ptr, out_stride, stream))
 
 
 # ---- convenience wrapper --------------------------------------------------------------------

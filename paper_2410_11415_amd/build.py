@@ -9,7 +9,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_DIR = os.path.join(_HERE, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "libklay.so")
-SOURCES = ["klay_api.hip", "layerize.cpp"]
+SOURCES = ["klay_lib.hip", "layerize.cpp"]
 
 
 def hipcc() -> str:

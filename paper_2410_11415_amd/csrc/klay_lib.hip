@@ -1,0 +1,390 @@
+// The library's device code: the circuit evaluator (klay_api.hip) and the operators that need no handle, whose entry points are here.
+// One translation unit, so that all entry points report through the same thread-local message.
+#include "klay_api.hip"
+
+#include "klay_scan.hip.h"
+#include "klay_tokens.hip.h"
+
+namespace {
+
+// Makes `device` current for a call, and the earlier one again afterwards.
+struct OnDevice {
+    int before = -1;
+    bool changed = false;
+    hipError_t status;
+    explicit OnDevice(int device) {
+        status = hipGetDevice(&before);
+        if (status == hipSuccess && before != device) {
+            status = hipSetDevice(device);
+            changed = status == hipSuccess;
+        }
+    }
+    ~OnDevice() {
+        if (changed) (void)hipSetDevice(before);
+    }
+};
+
+// Launch errors come as the launch's own status; what an earlier call has left is none of ours.
+#define KLAY_LAUNCH(kernel, grid, block, stream, ...)                                                    \
+    do {                                                                                                 \
+        (void)hipGetLastError();                                                                         \
+        hipLaunchKernelGGL(kernel, grid, block, 0, static_cast<hipStream_t>(stream), __VA_ARGS__);       \
+        KLAY_HIP(hipGetLastError());                                                                     \
+    } while (0)
+
+constexpr int kComputeUnits = 256;
+constexpr int32_t kMostChannels = 1 << 30;
+bool known_dtype(int32_t t) { return t == KLAY_F32 || t == KLAY_BF16 || t == KLAY_F16; }
+int dtype_bytes(int32_t t) { return t == KLAY_F32 ? 4 : 2; }
+
+// ---- tokens ---------------------------------------------------------------------------------------------------------
+constexpr int32_t kShortRow = 512, kShortestRow = 64;   // rows in the registers of a wave, of a quarter of one
+
+klay_status check_tokens(const klay_tokens_args* a, const char* who) {
+    const std::string name(who);
+    if (!a) return fail(KLAY_EINVAL, name + ": null argument");
+    if (!known_dtype(a->dtype)) return fail(KLAY_EINVAL, name + ": unknown dtype");
+    if (a->vocab < 1 || a->num_tokens < 0 || a->num_tokens > klay::kMaxTokens)
+        return fail(KLAY_EINVAL, name + ": vocab must be >= 1 and num_tokens 0 .. " + std::to_string(klay::kMaxTokens));
+    if (a->top < 0 || a->top > klay::kMaxTop || a->top > a->vocab)
+        return fail(KLAY_EINVAL, name + ": top must be 0 .. min(vocab, " + std::to_string(klay::kMaxTop) + ")");
+    if (a->rows < 0 || a->rows > INT32_MAX) return fail(KLAY_EINVAL, name + ": rows must be 0 .. 2^31 - 1");
+    if (a->rows == 0) return KLAY_OK;
+    if (!a->logits || (a->num_tokens > 0 && !a->tokens)) return fail(KLAY_EINVAL, name + ": null argument");
+    if (a->logit_rows.inner < 1 || a->logit_rows.inner > INT32_MAX ||
+        (a->num_tokens > 0 && (a->token_rows.inner < 1 || a->token_rows.inner > INT32_MAX)))
+        return fail(KLAY_EINVAL, name + ": the inner axis of rows must be 1 .. 2^31 - 1");
+    return KLAY_OK;
+}
+
+// Workgroups per row: one where the rows alone give the chip four workgroups per CU, else so many that they do, each with eight
+// kilobytes of the row or more.
+void token_parts(const klay_tokens_args* a, int32_t* parts, int32_t* part) {
+    const int64_t round = (int64_t)klay::kTokBlock * (16 / dtype_bytes(a->dtype));       // elements that a workgroup takes at a time
+    int64_t n = 1;
+    if (a->rows < 4 * kComputeUnits && a->vocab > kShortRow) {
+        n = std::min<int64_t>((4 * kComputeUnits + a->rows - 1) / a->rows, klay::kMaxParts);
+        n = std::min<int64_t>(n, (a->vocab + 2 * round - 1) / (2 * round));
+    }
+    int64_t size = (a->vocab + n - 1) / n;
+    if (n > 1) size = (size + round - 1) / round * round;
+    *part = (int32_t)std::min<int64_t>(size, INT32_MAX);
+    *parts = (int32_t)((a->vocab + size - 1) / size);
+}
+
+size_t token_lists_at(int64_t rows, int32_t parts) { return (size_t)rows * parts * 4 * sizeof(float); }
+
+klay::TokenArgs token_args(const klay_tokens_args* a) {
+    klay::TokenArgs g{};
+    g.logits = a->logits;
+    g.logit_rows = klay::RowMap{a->logit_rows.outer_stride, a->logit_rows.inner_stride, (int32_t)a->logit_rows.inner};
+    g.tokens = a->tokens;
+    g.token_rows = klay::RowMap{a->token_rows.outer_stride, a->token_rows.inner_stride, (int32_t)std::max<int64_t>(a->token_rows.inner, 1)};
+    g.token_stride = a->token_stride;
+    g.rows = a->rows;
+    g.vocab = a->vocab;
+    g.num_tokens = a->num_tokens;
+    g.top = a->top;
+    return g;
+}
+
+int32_t capped_grid(int64_t units) { return (int32_t)std::min<int64_t>(units, 1 << 20); }
+
+template <typename T, bool ENT, bool TOP>
+klay_status run_tokens(const klay::TokenArgs& g, void* stream) {
+    const dim3 block(klay::kTokBlock);
+    if (g.vocab <= kShortRow) {
+        const int lanes = g.vocab <= kShortestRow ? 16 : 64, per_block = klay::kTokBlock / lanes;
+        const dim3 grid(capped_grid((g.rows + per_block - 1) / per_block));
+        if (lanes == 16) KLAY_LAUNCH((klay::token_short_kernel<T, 16, 4, ENT, TOP>), grid, block, stream, g);
+        else KLAY_LAUNCH((klay::token_short_kernel<T, 64, 8, ENT, TOP>), grid, block, stream, g);
+        return KLAY_OK;
+    }
+    KLAY_LAUNCH((klay::token_row_kernel<T, ENT, TOP>), dim3(capped_grid(g.rows * g.parts)), block, stream, g);
+    if (g.parts > 1) KLAY_LAUNCH((klay::token_join_kernel<T, TOP>), dim3((uint32_t)g.rows), block, stream, g);
+    return KLAY_OK;
+}
+
+template <typename T>
+klay_status run_tokens(const klay::TokenArgs& g, void* stream) {
+    if (g.entropy) return g.top ? run_tokens<T, true, true>(g, stream) : run_tokens<T, true, false>(g, stream);
+    return g.top ? run_tokens<T, false, true>(g, stream) : run_tokens<T, false, false>(g, stream);
+}
+
+template <typename T>
+klay_status run_tokens_back(const klay::TokenArgs& g, void* stream) {
+    const dim3 block(klay::kTokBlock);
+    if (g.vocab <= kShortRow) {
+        const int lanes = g.vocab <= kShortestRow ? 16 : 64, per_block = klay::kTokBlock / lanes;
+        const dim3 grid(capped_grid((g.rows + per_block - 1) / per_block));
+        if (lanes == 16) KLAY_LAUNCH((klay::token_back_short_kernel<T, 16, 4>), grid, block, stream, g);
+        else KLAY_LAUNCH((klay::token_back_short_kernel<T, 64, 8>), grid, block, stream, g);
+        return KLAY_OK;
+    }
+    KLAY_LAUNCH((klay::token_back_kernel<T>), dim3(capped_grid(g.rows * g.parts)), block, stream, g);
+    return KLAY_OK;
+}
+
+// ---- recurrence -----------------------------------------------------------------------------------------------------
+struct ScanPlan {
+    int vec = 1, waves = 4;         // channels per lane; waves per workgroup
+    int32_t chunks = 1, chunk = 0, blocks_c = 1;
+};
+
+klay_status check_scan(const klay_scan_args* a, bool inputs, const char* who) {
+    const std::string name(who);
+    if (!a) return fail(KLAY_EINVAL, name + ": null argument");
+    if (!known_dtype(a->dtype)) return fail(KLAY_EINVAL, name + ": unknown dtype");
+    if (a->semiring != KLAY_REAL && a->semiring != KLAY_LOG && a->semiring != KLAY_MAXLOG) return fail(KLAY_EINVAL, name + ": unknown semiring");
+    if (a->semiring != KLAY_REAL && a->dtype != KLAY_F32) return fail(KLAY_EINVAL, name + ": the log-domain semirings take KLAY_F32 only");
+    if (a->channels < 1 || a->channels > kMostChannels || a->batch < 0 || a->time < 0 || a->time > INT32_MAX || a->batch > INT32_MAX / 8)
+        return fail(KLAY_EINVAL, name + ": channels must be 1 .. 2^30, time 0 .. 2^31 - 1, batch 0 .. 2^28 - 1");
+    if (a->offsets) {
+        if (a->batch != 1) return fail(KLAY_EINVAL, name + ": packed sequences have batch = 1");
+        if (a->sequences < 0 || a->sequences > INT32_MAX / 8) return fail(KLAY_EINVAL, name + ": sequences must be 0 .. 2^28 - 1");
+        if (a->time > 0 && !a->row_info) return fail(KLAY_EINVAL, name + ": packed sequences need row_info");
+    }
+    if (a->batch > 0 && a->time > 0 && (!a->gates || (inputs && !a->inputs))) return fail(KLAY_EINVAL, name + ": null argument");
+    return KLAY_OK;
+}
+
+// Workgroups of four waves fill the chip where batch and channels give four of them per CU; of sixteen waves where they give one; below
+// that the time axis is cut until there are two per CU, in chunks of 256 steps or more.
+ScanPlan scan_plan(const klay_scan_args* a) {
+    ScanPlan p;
+    const bool even = a->dtype != KLAY_F32 && a->channels % 2 == 0;
+    auto blocks = [&](int vec) { return (a->channels + 64 * vec - 1) / (64 * vec); };
+    p.vec = even && blocks(2) * a->batch >= kComputeUnits ? 2 : 1;
+    p.blocks_c = blocks(p.vec);
+    const int64_t n = p.blocks_c * a->batch;
+    if (a->time <= klay::kSteps) p.waves = 1;
+    else if (n >= 4 * kComputeUnits || a->time <= 4 * klay::kSteps) p.waves = 4;
+    else p.waves = 16;
+    p.chunk = (int32_t)a->time;
+    if (n < kComputeUnits && p.waves == 16) {
+        const int64_t tile = (int64_t)p.waves * klay::kSteps;
+        int64_t chunks = std::min<int64_t>((2 * kComputeUnits + n - 1) / n, (a->time + tile - 1) / tile);
+        const int64_t size = ((a->time + chunks - 1) / chunks + tile - 1) / tile * tile;
+        chunks = (a->time + size - 1) / size;
+        if (chunks > 1) {
+            p.chunks = (int32_t)chunks;
+            p.chunk = (int32_t)size;
+        }
+    }
+    return p;
+}
+
+size_t scan_maps(const klay_scan_args* a, const ScanPlan& p) { return (size_t)a->batch * p.chunks * a->channels; }
+size_t scan_bytes(const klay_scan_args* a, const ScanPlan& p) {
+    return p.chunks == 1 ? 0 : scan_maps(a, p) * 8 + (size_t)a->batch * p.chunks * 4;
+}
+
+klay::ScanArgs scan_args(const klay_scan_args* a, const ScanPlan& p, void* workspace) {
+    klay::ScanArgs g{};
+    g.a = a->gates; g.x = a->inputs;
+    g.initial = a->initial;
+    g.rows = a->offsets ? a->row_info : nullptr;
+    g.a_batch = a->gates_batch_stride; g.a_time = a->gates_time_stride;
+    g.x_batch = a->inputs_batch_stride; g.x_time = a->inputs_time_stride;
+    g.time = a->time;
+    g.channels = a->channels;
+    g.chunks = p.chunks; g.chunk = p.chunk; g.blocks_c = p.blocks_c;
+    if (p.chunks > 1) {
+        g.map_a = static_cast<float*>(workspace);
+        g.map_h = g.map_a + scan_maps(a, p);
+        g.map_cut = reinterpret_cast<int32_t*>(g.map_h + scan_maps(a, p));
+    }
+    return g;
+}
+
+template <int S, typename T, int VC, int W>
+klay_status run_scan(const klay::ScanArgs& g, int64_t batch, bool back, void* stream) {
+    const int64_t blocks = batch * g.blocks_c * g.chunks, maps = batch * g.blocks_c * (g.chunks - 1);
+    if (blocks * 64 * W > (int64_t)UINT32_MAX) return fail(KLAY_EINVAL, "klay_scan: batch times channels exceeds one launch");
+    const dim3 block(64, W);
+    if constexpr (S != klay::SEMI_MAX) {
+        if (back) {
+            if constexpr (W == 16)
+                if (maps > 0) KLAY_LAUNCH((klay::scan_back_map_kernel<S, T, VC, W>), dim3((uint32_t)maps), block, stream, g);
+            KLAY_LAUNCH((klay::scan_back_kernel<S, T, VC, W>), dim3((uint32_t)blocks), block, stream, g);
+            return KLAY_OK;
+        }
+    }
+    if constexpr (W == 16)
+        if (maps > 0) KLAY_LAUNCH((klay::scan_map_kernel<S, T, VC, W>), dim3((uint32_t)maps), block, stream, g);
+    KLAY_LAUNCH((klay::scan_kernel<S, T, VC, W>), dim3((uint32_t)blocks), block, stream, g);
+    return KLAY_OK;
+}
+
+template <int S, typename T, int VC>
+klay_status run_scan(const klay::ScanArgs& g, const ScanPlan& p, int64_t batch, bool back, void* stream) {
+    if (p.waves == 1) return run_scan<S, T, VC, 1>(g, batch, back, stream);
+    if (p.waves == 4) return run_scan<S, T, VC, 4>(g, batch, back, stream);
+    return run_scan<S, T, VC, 16>(g, batch, back, stream);
+}
+
+klay_status run_scan(const klay_scan_args* a, const klay::ScanArgs& g, const ScanPlan& p, bool back, void* stream) {
+    using namespace klay;
+    if (a->semiring == KLAY_LOG) return run_scan<SEMI_LOG, f32, 1>(g, p, a->batch, back, stream);
+    if (a->semiring == KLAY_MAXLOG) return run_scan<SEMI_MAX, f32, 1>(g, p, a->batch, back, stream);
+    if (a->dtype == KLAY_F32) return run_scan<SEMI_REAL, f32, 1>(g, p, a->batch, back, stream);
+    if (a->dtype == KLAY_BF16)
+        return p.vec == 2 ? run_scan<SEMI_REAL, bf16, 2>(g, p, a->batch, back, stream) : run_scan<SEMI_REAL, bf16, 1>(g, p, a->batch, back, stream);
+    return p.vec == 2 ? run_scan<SEMI_REAL, f16, 2>(g, p, a->batch, back, stream) : run_scan<SEMI_REAL, f16, 1>(g, p, a->batch, back, stream);
+}
+
+// What the sequences without steps leave: `to` as `from` (null: `none`).
+klay_status fill_states(float* to, const float* from, float none, int64_t count, void* stream) {
+    if (!to || count == 0) return KLAY_OK;
+    KLAY_LAUNCH(klay::scan_fill_kernel, dim3((uint32_t)std::min<int64_t>((count + 255) / 256, 4096)), dim3(256), stream, to, from, none, count);
+    return KLAY_OK;
+}
+
+klay_status scan_workspace(const klay_scan_args* a, const ScanPlan& p, const void* workspace, size_t bytes, const char* who) {
+    const size_t need = scan_bytes(a, p);
+    if (need && (!workspace || bytes < need))
+        return fail(KLAY_ENOMEM, std::string(who) + ": workspace too small: need " + std::to_string(need) + " bytes");
+    if (need && reinterpret_cast<uintptr_t>(workspace) % 16)
+        return fail(KLAY_EINVAL, std::string(who) + ": workspace must be 16-byte aligned");
+    return KLAY_OK;
+}
+
+template <int S, typename T>
+klay_status run_step(const klay::StepArgs& g, bool wide, void* stream) {
+    constexpr int VC = 4;
+    const int64_t lanes = wide ? g.channels / VC : g.channels;
+    const dim3 grid((uint32_t)((lanes + 255) / 256), (uint32_t)std::min<int64_t>(g.batch, 65535));
+    if (wide) KLAY_LAUNCH((klay::step_kernel<S, T, VC>), grid, dim3(256), stream, g);
+    else KLAY_LAUNCH((klay::step_kernel<S, T, 1>), grid, dim3(256), stream, g);
+    return KLAY_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t klay_tokens_workspace_bytes(const klay_tokens_args* a) {
+    if (!a || a->rows < 1 || a->vocab < 1 || !known_dtype(a->dtype) || a->top < 0) return 0;
+    int32_t parts, part;
+    token_parts(a, &parts, &part);
+    return parts == 1 ? 0 : token_lists_at(a->rows, parts) + (size_t)a->rows * parts * a->top * sizeof(uint64_t);
+}
+
+klay_status klay_tokens_forward(const klay_tokens_args* a, float* logp, float* neg, float* entropy, float* stats, float* top_logp,
+                                int64_t* top_tokens, void* workspace, size_t workspace_bytes, void* stream) {
+    const klay_status st = check_tokens(a, "klay_tokens_forward");
+    if (st != KLAY_OK || a->rows == 0) return st;
+    if ((a->num_tokens > 0 && !logp) || (a->top > 0 && (!top_logp || !top_tokens)))
+        return fail(KLAY_EINVAL, "klay_tokens_forward: null argument");
+    klay::TokenArgs g = token_args(a);
+    token_parts(a, &g.parts, &g.part);
+    const size_t need = klay_tokens_workspace_bytes(a);
+    if (need && (!workspace || workspace_bytes < need))
+        return fail(KLAY_ENOMEM, "klay_tokens_forward: workspace too small: need " + std::to_string(need) + " bytes");
+    if (need && reinterpret_cast<uintptr_t>(workspace) % 16)
+        return fail(KLAY_EINVAL, "klay_tokens_forward: workspace must be 16-byte aligned");
+    g.logp = logp; g.neg = neg; g.entropy = entropy;
+    g.stats = reinterpret_cast<klay::RowStats*>(stats);
+    g.top_logp = top_logp; g.top_tokens = top_tokens;
+    g.partial = static_cast<float*>(workspace);
+    g.lists = need ? reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + token_lists_at(a->rows, g.parts)) : nullptr;
+    OnDevice on(a->device);
+    KLAY_HIP(on.status);
+    if (a->dtype == KLAY_F32) return run_tokens<klay::f32>(g, stream);
+    if (a->dtype == KLAY_BF16) return run_tokens<klay::bf16>(g, stream);
+    return run_tokens<klay::f16>(g, stream);
+}
+
+klay_status klay_tokens_backward(const klay_tokens_args* a, const float* stats, const float* dlogp, const float* dneg,
+                                 const float* dentropy, void* dlogits, void* stream) {
+    const klay_status st = check_tokens(a, "klay_tokens_backward");
+    if (st != KLAY_OK || a->rows == 0) return st;
+    if (!stats || !dlogits) return fail(KLAY_EINVAL, "klay_tokens_backward: null argument");
+    klay::TokenArgs g = token_args(a);
+    token_parts(a, &g.parts, &g.part);
+    g.stats = const_cast<klay::RowStats*>(reinterpret_cast<const klay::RowStats*>(stats));
+    g.dlogp = dlogp; g.dneg = dneg; g.dentropy = dentropy;
+    g.dlogits = dlogits;
+    OnDevice on(a->device);
+    KLAY_HIP(on.status);
+    if (a->dtype == KLAY_F32) return run_tokens_back<klay::f32>(g, stream);
+    if (a->dtype == KLAY_BF16) return run_tokens_back<klay::bf16>(g, stream);
+    return run_tokens_back<klay::f16>(g, stream);
+}
+
+size_t klay_scan_workspace_bytes(const klay_scan_args* a) {
+    if (!a || a->batch < 1 || a->time < 1 || a->channels < 1 || !known_dtype(a->dtype)) return 0;
+    return scan_bytes(a, scan_plan(a));
+}
+
+klay_status klay_scan_forward(const klay_scan_args* a, void* states, float* final, void* workspace, size_t workspace_bytes, void* stream) {
+    klay_status st = check_scan(a, true, "klay_scan_forward");
+    if (st != KLAY_OK) return st;
+    const int64_t sequences = a->offsets ? a->sequences : a->batch;
+    const bool rows = a->batch > 0 && a->time > 0;
+    if (rows && !states) return fail(KLAY_EINVAL, "klay_scan_forward: null argument");
+    const ScanPlan p = rows ? scan_plan(a) : ScanPlan();
+    st = scan_workspace(a, p, workspace, workspace_bytes, "klay_scan_forward");
+    if (st != KLAY_OK) return st;
+    OnDevice on(a->device);
+    KLAY_HIP(on.status);
+    if (a->offsets || !rows) {
+        st = fill_states(final, a->initial, a->semiring == KLAY_REAL ? 0.0f : -INFINITY, sequences * a->channels, stream);
+        if (st != KLAY_OK || !rows) return st;
+        KLAY_LAUNCH(klay::scan_rows_kernel, dim3((uint32_t)((a->time + 255) / 256)), dim3(256), stream, a->row_info, a->offsets, a->time,
+                    (int32_t)a->sequences);
+    }
+    klay::ScanArgs g = scan_args(a, p, workspace);
+    g.out = states;
+    g.final = final;
+    return run_scan(a, g, p, false, stream);
+}
+
+klay_status klay_scan_backward(const klay_scan_args* a, const void* states, const void* dstates, const float* dfinal, void* dgates,
+                               void* dinputs, float* dinitial, void* workspace, size_t workspace_bytes, void* stream) {
+    klay_status st = check_scan(a, a && a->semiring == KLAY_LOG, "klay_scan_backward");
+    if (st != KLAY_OK) return st;
+    if (a->semiring == KLAY_MAXLOG) return fail(KLAY_EINVAL, "klay_scan_backward: the (max, +) semiring is not differentiated");
+    const int64_t sequences = a->offsets ? a->sequences : a->batch;
+    const bool rows = a->batch > 0 && a->time > 0;
+    if (rows && !states) return fail(KLAY_EINVAL, "klay_scan_backward: null argument");
+    const ScanPlan p = rows ? scan_plan(a) : ScanPlan();
+    st = scan_workspace(a, p, workspace, workspace_bytes, "klay_scan_backward");
+    if (st != KLAY_OK) return st;
+    OnDevice on(a->device);
+    KLAY_HIP(on.status);
+    if (a->offsets || !rows) {
+        st = fill_states(dinitial, dfinal, 0.0f, sequences * a->channels, stream);
+        if (st != KLAY_OK || !rows) return st;
+    }
+    klay::ScanArgs g = scan_args(a, p, workspace);
+    g.h = states;
+    g.dh = dstates;
+    g.dfinal = dfinal;
+    g.da = dgates; g.dx = dinputs;
+    g.dinitial = dinitial;
+    return run_scan(a, g, p, true, stream);
+}
+
+klay_status klay_scan_step(int32_t dtype, int32_t semiring, int32_t device, int64_t rows, int32_t channels, const void* gates,
+                           int64_t gates_stride, const void* inputs, int64_t inputs_stride, float* state, int64_t state_stride, void* out,
+                           int64_t out_stride, void* stream) {
+    if (!known_dtype(dtype)) return fail(KLAY_EINVAL, "klay_scan_step: unknown dtype");
+    if (semiring != KLAY_REAL && semiring != KLAY_LOG && semiring != KLAY_MAXLOG) return fail(KLAY_EINVAL, "klay_scan_step: unknown semiring");
+    if (semiring != KLAY_REAL && dtype != KLAY_F32) return fail(KLAY_EINVAL, "klay_scan_step: the log-domain semirings take KLAY_F32 only");
+    if (rows < 0 || rows > INT32_MAX || channels < 1 || channels > kMostChannels)
+        return fail(KLAY_EINVAL, "klay_scan_step: rows must be 0 .. 2^31 - 1, channels 1 .. 2^30");
+    if (rows == 0) return KLAY_OK;
+    if (!gates || !inputs || !state) return fail(KLAY_EINVAL, "klay_scan_step: null argument");
+    klay::StepArgs g{gates, inputs, out, state, gates_stride, inputs_stride, out_stride, state_stride, (int32_t)rows, channels};
+    const bool wide = channels % 4 == 0;
+    OnDevice on(device);
+    KLAY_HIP(on.status);
+    if (semiring == KLAY_LOG) return run_step<klay::SEMI_LOG, klay::f32>(g, wide, stream);
+    if (semiring == KLAY_MAXLOG) return run_step<klay::SEMI_MAX, klay::f32>(g, wide, stream);
+    if (dtype == KLAY_F32) return run_step<klay::SEMI_REAL, klay::f32>(g, wide, stream);
+    if (dtype == KLAY_BF16) return run_step<klay::SEMI_REAL, klay::bf16>(g, wide, stream);
+    return run_step<klay::SEMI_REAL, klay::f16>(g, wide, stream);
+}
+
+}  // extern "C"

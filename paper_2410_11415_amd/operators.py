@@ -1,0 +1,289 @@
+"""The operators between a network and a circuit's leaf weights, as differentiable PyTorch functions: log probabilities of given
+tokens (:func:`token_logprobs`) and gated recurrences over sequences in the library's semirings (:func:`gated_scan`, and
+:func:`gated_step` for one step).  Marshalling only, on torch's current stream of the tensors' device: the kernels are those of
+``klay_tokens_*`` and ``klay_scan_*`` (include/klay.h, which says what they compute and refuse).  Results and workspaces are torch
+tensors, so calls may be captured into a graph and made on several streams at once.
+"""
+from __future__ import annotations
+
+from typing import NamedTuple, Optional
+
+import torch
+from torch.autograd.function import once_differentiable
+
+from . import binding as _b
+from .binding import KLAY_LOG, KLAY_MAXLOG, KLAY_REAL
+
+_DTYPES = {torch.float32: _b.KLAY_F32, torch.bfloat16: _b.KLAY_BF16, torch.float16: _b.KLAY_F16}
+_MOST_TOKENS, _MOST_TOP, _MOST_CHANNELS = 1024, 64, 1 << 30
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream(device: int) -> int:
+    """The handle of the device's current stream (without a Stream object where this torch has a function for it)."""
+    return torch.cuda.current_stream(device).cuda_stream if _raw_stream is None else _raw_stream(device)
+
+
+def _check_tensor(t, name, dtypes=None):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(name + " must be a CUDA tensor")
+    if dtypes is not None and t.dtype not in dtypes:
+        raise ValueError("%s must be %s" % (name, " or ".join(str(d).replace("torch.", "") for d in dtypes)))
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _workspace(size, device):
+    return torch.empty(size, dtype=torch.uint8, device=device) if size else None
+
+
+# ---- log probabilities of given tokens ----------------------------------------------------------------------------
+class TokenLogprobs(NamedTuple):
+    """What :func:`token_logprobs` returns; None for what was not asked."""
+    logp: Optional[torch.Tensor]
+    neg: Optional[torch.Tensor]
+    entropy: Optional[torch.Tensor]
+    top_logp: Optional[torch.Tensor]
+    top_tokens: Optional[torch.Tensor]
+
+
+def _rows_of(t):
+    """(t, its leading axes as klay_rows): t itself where at most two strides describe them, else a contiguous copy."""
+    if t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1):
+        return t, _b.klay_rows(max(t.shape[0], 1), 0, t.stride(0))
+    merged = []
+    for n, s in zip(t.shape[:-1], t.stride()[:-1]):
+        if n == 1:
+            continue
+        if merged and merged[-1][1] == n * s:
+            merged[-1] = (merged[-1][0] * n, s)
+        else:
+            merged.append((n, s))
+    if len(merged) > 2:
+        return _rows_of(t.contiguous())
+    merged = [(1, 0)] * (2 - len(merged)) + merged
+    return t, _b.klay_rows(max(merged[1][0], 1), merged[0][1], merged[1][1])
+
+
+def _token_args(logits, tokens, top):
+    if logits.stride(-1) != 1 and logits.shape[-1] != 1:
+        logits = logits.contiguous()
+    logits, logit_rows = _rows_of(logits)
+    tokens, token_rows = (None, _b.klay_rows(1, 0, 0)) if tokens is None else _rows_of(tokens)
+    vocab = logits.shape[-1]
+    args = _b.klay_tokens_args(_DTYPES[logits.dtype], logits.device.index, vocab, 0 if tokens is None else tokens.shape[-1], top, 0,
+                               logits.numel() // vocab, logits.data_ptr(), logit_rows, _ptr(tokens), token_rows,
+                               0 if tokens is None else tokens.stride(-1))
+    return args, (logits, tokens)          # the tensors that args points into
+
+
+def _tokens_forward(logits, tokens, complement, entropy, top, keep):
+    args, alive = _token_args(logits, tokens, top)
+    lead, device = logits.shape[:-1], logits.device
+
+    def new(wanted, *tail, dtype=torch.float32):
+        return torch.empty(lead + tail, dtype=dtype, device=device) if wanted else None
+
+    k = args.num_tokens
+    logp, neg, h = new(tokens is not None, k), new(complement and tokens is not None, k), new(entropy)
+    top_logp, top_tokens = new(top, top), new(top, top, dtype=torch.int64)
+    stats = torch.empty((args.rows, 4), dtype=torch.float32, device=device) if keep else None
+    size = _b.klay_tokens_workspace_bytes(args)
+    work = _workspace(size, device)
+    _b.klay_tokens_forward(args, _ptr(logp), _ptr(neg), _ptr(h), _ptr(stats), _ptr(top_logp), _ptr(top_tokens), _ptr(work), size,
+                           _stream(args.device))
+    del alive
+    return logp, neg, h, top_logp, top_tokens, stats
+
+
+class _TokenLogprobs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, tokens, complement, entropy, top):
+        *out, stats = _tokens_forward(logits, tokens, complement, entropy, top, True)
+        ctx.save_for_backward(logits, tokens, stats)
+        ctx.set_materialize_grads(False)
+        ctx.mark_non_differentiable(*[t for t in out[3:] if t is not None])
+        return tuple(out)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dlogp, dneg, dentropy, _top_logp, _top_tokens):
+        logits, tokens, stats = ctx.saved_tensors
+        args, alive = _token_args(logits, tokens, 0)
+        dlogp, dneg, dentropy = (None if t is None else t.contiguous() for t in (dlogp, dneg, dentropy))
+        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        _b.klay_tokens_backward(args, stats.data_ptr(), _ptr(dlogp), _ptr(dneg), _ptr(dentropy), dlogits.data_ptr(),
+                                _stream(args.device))
+        del alive
+        return dlogits, None, None, None, None
+
+
+def token_logprobs(logits, tokens=None, *, complement=False, entropy=False, top=0) -> TokenLogprobs:
+    """Log probabilities of ``tokens[..., K]`` (int64) under ``logits[..., V]`` (float32, bfloat16 or float16): the log weights
+    of the literals "the network answers t".  Everything returned is float32.
+
+    ``logp[..., K]``; with ``complement`` also ``neg[..., K]`` = log(1 - p), the weights of the negated literals (accurate where p
+    rounds to 1); with ``entropy`` the rows' entropies ``[...]``; with ``top`` = n the n most likely tokens, equal ones by their
+    index, as ``top_logp[..., n]`` and ``top_tokens[..., n]``.  A logit of -inf is a token that is not allowed, a negative token
+    asks for nothing (weight 1 for both literals, log 0; no gradient), a token >= V gives NaN.  ``logp``, ``neg`` and ``entropy``
+    are differentiable with respect to ``logits``; of the alternatives neither is (ask for them as ``tokens``).
+
+    The elements of a row should be next to each other and the rows reachable with two strides (as those of ``logits[:, :-1]``
+    are); anything else is copied first.  At most 1024 tokens and 64 alternatives a row.
+    """
+    _check_tensor(logits, "logits", _DTYPES)
+    if logits.dim() < 1 or logits.shape[-1] < 1:
+        raise ValueError("logits must be [..., V] with V >= 1")
+    if tokens is not None:
+        _check_tensor(tokens, "tokens", (torch.int64,))
+        if tokens.device != logits.device:
+            raise ValueError("tokens must be on the device of logits")
+        if tokens.dim() != logits.dim() or tokens.shape[:-1] != logits.shape[:-1]:
+            raise ValueError("tokens must be [..., K] with the leading axes of logits, %s" % (tuple(logits.shape[:-1]),))
+        if tokens.shape[-1] > _MOST_TOKENS:
+            raise ValueError("tokens must be at most %d a row" % _MOST_TOKENS)
+    elif complement:
+        raise ValueError("complement needs tokens")
+    top = int(top)
+    if logits.shape[-1] >= 1 << 31 or not 0 <= top <= min(_MOST_TOP, logits.shape[-1]):
+        raise ValueError("top must be 0 .. min(V, %d), and V below 2^31" % _MOST_TOP)
+    if torch.is_grad_enabled() and logits.requires_grad:
+        return TokenLogprobs(*_TokenLogprobs.apply(logits, tokens, bool(complement), bool(entropy), top))
+    return TokenLogprobs(*_tokens_forward(logits, tokens, bool(complement), bool(entropy), top, False)[:5])
+
+
+# ---- gated recurrence ---------------------------------------------------------------------------------------------
+def _channels_last(t):
+    return t if t.stride(-1) == 1 or t.shape[-1] == 1 else t.contiguous()
+
+
+def _scan_args(gates, inputs, initial, semiring, offsets, row_info):
+    gates, inputs = _channels_last(gates), None if inputs is None else _channels_last(inputs)
+    packed = offsets is not None
+    batch, time = (1, gates.shape[0]) if packed else gates.shape[:2]
+
+    def strides(t):
+        return (0, 0) if t is None else (0, t.stride(0)) if packed else (t.stride(0), t.stride(1))
+
+    initial = None if initial is None else initial.contiguous()
+    args = _b.klay_scan_args(_DTYPES[gates.dtype], semiring, gates.device.index, gates.shape[-1], batch, time,
+                             offsets.shape[0] - 1 if packed else 0, gates.data_ptr(), _ptr(inputs), *strides(gates), *strides(inputs),
+                             _ptr(offsets), _ptr(row_info), _ptr(initial))
+    return args, (gates, inputs, initial)
+
+
+def _scan_forward(gates, inputs, initial, semiring, offsets):
+    device = gates.device
+    row_info = None if offsets is None else torch.empty(gates.shape[0], dtype=torch.int32, device=device)
+    args, alive = _scan_args(gates, inputs, initial, semiring, offsets, row_info)
+    states = torch.empty(gates.shape, dtype=gates.dtype, device=device)
+    final = torch.empty((args.sequences if offsets is not None else args.batch, args.channels), dtype=torch.float32, device=device)
+    size = _b.klay_scan_workspace_bytes(args)
+    work = _workspace(size, device)
+    _b.klay_scan_forward(args, states.data_ptr(), final.data_ptr(), _ptr(work), size, _stream(args.device))
+    del alive
+    return states, final, row_info
+
+
+class _GatedScan(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, gates, inputs, initial, semiring, offsets):
+        states, final, row_info = _scan_forward(gates, inputs, initial, semiring, offsets)
+        # (the reverse sweep of the real semiring does not read the inputs)
+        ctx.save_for_backward(gates, inputs if semiring == KLAY_LOG else None, initial, offsets, row_info, states)
+        ctx.semiring = semiring
+        ctx.set_materialize_grads(False)
+        return states, final
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dstates, dfinal):
+        gates, inputs, initial, offsets, row_info, states = ctx.saved_tensors
+        if dstates is None and dfinal is None:
+            return None, None, None, None, None
+        args, alive = _scan_args(gates, inputs, initial, ctx.semiring, offsets, row_info)
+        dstates, dfinal = (None if t is None else t.contiguous() for t in (dstates, dfinal))
+        dgates, dinputs = (torch.empty(gates.shape, dtype=gates.dtype, device=gates.device) if need else None
+                           for need in ctx.needs_input_grad[:2])
+        dinitial = torch.empty_like(initial, memory_format=torch.contiguous_format) if ctx.needs_input_grad[2] else None
+        size = _b.klay_scan_workspace_bytes(args)
+        work = _workspace(size, gates.device)
+        _b.klay_scan_backward(args, states.data_ptr(), _ptr(dstates), _ptr(dfinal), _ptr(dgates), _ptr(dinputs), _ptr(dinitial),
+                              _ptr(work), size, _stream(args.device))
+        del alive
+        return dgates, dinputs, dinitial, None, None
+
+
+def _check_recurrence(gates, inputs, semiring):
+    _check_tensor(gates, "gates", _DTYPES)
+    _check_tensor(inputs, "inputs", _DTYPES)
+    if inputs.shape != gates.shape or inputs.dtype != gates.dtype or inputs.device != gates.device:
+        raise ValueError("gates and inputs must have the same shape, type and device")
+    if semiring not in (KLAY_REAL, KLAY_LOG, KLAY_MAXLOG):
+        raise ValueError("unknown semiring")
+    if semiring != KLAY_REAL and gates.dtype != torch.float32:
+        raise ValueError("the log-domain semirings take float32")
+    if gates.dim() < 2 or not 1 <= gates.shape[-1] <= _MOST_CHANNELS:
+        raise ValueError("gates must have 1 .. 2^30 channels")
+
+
+def gated_scan(gates, inputs, initial=None, semiring=KLAY_REAL, offsets=None):
+    """``(states, final)`` of the recurrence h_t = gates_t (x) h_{t-1} (+) inputs_t in a semiring: ``KLAY_REAL`` a h + x (the linear
+    recurrence of a recurrent network), ``KLAY_LOG`` log(exp(a + h) + exp(x)) (a chain of AND and OR gates on log-probabilities),
+    ``KLAY_MAXLOG`` max(a + h, x) (its heaviest proof tree).
+
+    ``gates``, ``inputs``: ``[B, T, C]``, float32, or bfloat16 / float16 in the real semiring; states are kept in float32 and
+    rounded once into ``states`` (of the inputs' type).  ``initial``, ``final``: float32 ``[B, C]``, the states before the first and
+    behind the last step (default: 0, in the log domain -inf).  With ``offsets`` (int64 ``[S + 1]``, ascending) the sequences lie
+    one after the other: ``gates``, ``inputs`` are ``[N, C]``, sequence s is the rows ``offsets[s]`` to ``offsets[s + 1] - 1``, the
+    states are ``[S, C]``; a sequence may be empty, and rows of none get states and gradients of 0.
+
+    Differentiable (``KLAY_REAL``, ``KLAY_LOG``) with respect to gates, inputs and initial, through both results.  The channels
+    should be next to each other; other layouts are copied first.
+    """
+    _check_recurrence(gates, inputs, semiring)
+    if gates.dim() != (3 if offsets is None else 2):
+        raise ValueError("gates and inputs must be [B, T, C], or [N, C] with offsets")
+    if offsets is not None:
+        _check_tensor(offsets, "offsets", (torch.int64,))
+        if offsets.dim() != 1 or offsets.shape[0] < 1 or not offsets.is_contiguous() or offsets.device != gates.device:
+            raise ValueError("offsets must be a contiguous [S + 1] tensor on the device of gates")
+    if initial is not None:
+        _check_tensor(initial, "initial", (torch.float32,))
+        sequences = gates.shape[0] if offsets is None else offsets.shape[0] - 1
+        if initial.shape != (sequences, gates.shape[-1]) or initial.device != gates.device:
+            raise ValueError("initial must be [%d, %d] on the device of gates" % (sequences, gates.shape[-1]))
+    semiring = int(semiring)
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (gates, inputs, initial)):
+        if semiring == KLAY_MAXLOG:
+            raise RuntimeError("the (max, +) semiring is not differentiated; evaluate it under torch.no_grad()")
+        return _GatedScan.apply(gates, inputs, initial, semiring, offsets)
+    return _scan_forward(gates, inputs, initial, semiring, offsets)[:2]
+
+
+def gated_step(gates, inputs, state, semiring=KLAY_REAL, out=None):
+    """One step of :func:`gated_scan` for B running sequences: ``state`` (float32 ``[B, C]``) becomes gates (x) state (+) inputs in
+    place, and a copy of it in the type of ``gates``, ``inputs`` (``[B, C]``) is returned (in ``out``, where given).  Not
+    differentiated: the tensors must not require a gradient while gradients are enabled."""
+    _check_recurrence(gates, inputs, semiring)
+    _check_tensor(state, "state", (torch.float32,))
+    if gates.dim() != 2 or state.shape != gates.shape or state.device != gates.device:
+        raise ValueError("gates, inputs and state must be [B, C] on one device")
+    if out is None:
+        out = torch.empty(gates.shape, dtype=gates.dtype, device=gates.device)
+    elif not isinstance(out, torch.Tensor) or out.shape != gates.shape or out.dtype != gates.dtype or out.device != gates.device:
+        raise ValueError("out must have the shape, type and device of gates")
+    batch, channels = gates.shape
+    for t, name in ((state, "state"), (out, "out")):
+        if (channels > 1 and t.stride(1) != 1) or (batch > 1 and t.stride(0) < channels):
+            raise ValueError(name + " must have its channels next to each other and rows that do not overlap")
+    if torch.is_grad_enabled() and (gates.requires_grad or inputs.requires_grad or state.requires_grad or out.requires_grad):
+        raise RuntimeError("gated_step is not differentiated; call it under torch.no_grad(), or gated_scan")
+    gates, inputs = _channels_last(gates), _channels_last(inputs)
+    device = gates.device.index
+    _b.klay_scan_step(_DTYPES[gates.dtype], int(semiring), device, batch, channels, gates.data_ptr(), gates.stride(0), inputs.data_ptr(),
+                      inputs.stride(0), state.data_ptr(), state.stride(0), out.data_ptr(), out.stride(0), _stream(device))
+    torch.autograd.graph.increment_version((state, out))          # written in place: a graph that has saved them is to notice
+    return out

@@ -1,0 +1,160 @@
+"""The operators as they are used together (GPU): a recurrent layer, its logits, the log probabilities of tokens, a recurrence of
+log-probabilities, the circuit and a loss, forward and backward, against the same program in 64 bits on the CPU; and
+CircuitLayer.from_logits, which leads from logits straight into a circuit."""
+import numpy as np
+import pytest
+import torch
+
+from klay_synth import AND, FALSE, LIT, OR, TRUE, tiny_ddnnf
+from tests.gpu_util import GRAD_TOL, LOG_ATOL
+
+pytestmark = pytest.mark.gpu
+
+
+def circuit_64(c, pos, neg, best=False):
+    """Log value of every root, [B, R], node by node."""
+    kind, lit, ptr, idx, roots = c.arrays()[1:]
+    value = {}
+    for n in c_order(kind, ptr, idx):
+        kids = [value[int(i)] for i in idx[ptr[n]:ptr[n + 1]]]
+        if kind[n] == LIT:
+            v = abs(int(lit[n])) - 1
+            value[n] = (pos if lit[n] > 0 else neg)[:, v]
+        elif kind[n] in (TRUE, FALSE):
+            value[n] = torch.full_like(pos[:, 0], 0.0 if kind[n] == TRUE else -np.inf)
+        else:
+            kids = torch.stack(kids)
+            value[n] = kids.sum(0) if kind[n] == AND else kids.amax(0) if best else torch.logsumexp(kids, 0)
+            assert kind[n] in (AND, OR)
+    return torch.stack([value[int(r)] for r in roots], 1)
+
+
+def c_order(kind, ptr, idx):
+    done, order, stack = set(), [], list(range(len(kind)))
+    while stack:
+        n = stack[-1]
+        todo = [int(i) for i in idx[ptr[n]:ptr[n + 1]] if int(i) not in done]
+        if n in done or not todo:
+            if n not in done:
+                done.add(n)
+                order.append(n)
+            stack.pop()
+        else:
+            stack.extend(todo)
+    return order
+
+
+@pytest.mark.parametrize("complement", [True, False])
+@pytest.mark.parametrize("each", [True, False])
+@pytest.mark.parametrize("vocab", [3, 50, 900])
+def test_from_logits(vocab, each, complement):
+    import paper_2410_11415_amd as klay
+    c = tiny_ddnnf(3, 12, 30)[0]
+    k = klay.Circuit(*c.arrays(), device=0)
+    rng = np.random.default_rng(vocab)
+    B, G, K = 9, 4, 3
+    x = torch.from_numpy(rng.normal(size=(B, G, vocab)) * 2).float()
+    t = torch.from_numpy(np.stack([rng.permutation(vocab)[:K] for _ in range(B * G)]).reshape(B, G, K))
+    t = t if each else t[0]
+    x64 = x.double().requires_grad_(True)
+    lp = torch.log_softmax(x64, -1).gather(2, t.expand(B, G, K)).reshape(B, G * K)
+    lp.retain_grad()
+    ln = torch.log1p(-lp.exp()) if complement else torch.zeros_like(lp)
+    if complement:
+        ln.retain_grad()
+    want = circuit_64(c, lp, ln)
+    weights = torch.from_numpy(rng.normal(size=tuple(want.shape)))
+    (want * weights).sum().backward()
+    logits = x.cuda().requires_grad_(True)
+    got = klay.CircuitLayer(k, klay.KLAY_LOG).from_logits(logits, t.cuda(), complement=complement)
+    assert float((got.detach().cpu().double() - want.detach()).abs().max()) <= LOG_ATOL
+    (got * weights.float().cuda()).sum().backward()
+    # an entry of the gradient is a sum over the position's tokens of the leaf adjoints times factors of at most 1
+    of = torch.clamp(lp.grad.abs(), min=1.0) + (torch.clamp(ln.grad.abs(), min=1.0) if complement else 0.0)
+    tol = GRAD_TOL * of.reshape(B, G, K).sum(-1, keepdim=True)
+    assert bool(((logits.grad.cpu().double() - x64.grad).abs() <= tol).all())
+    with torch.no_grad():
+        best = klay.CircuitLayer(k, klay.KLAY_MAXLOG).from_logits(logits, t.cuda(), complement=complement)
+    assert float((best.cpu().double() - circuit_64(c, lp, ln, best=True).detach()).abs().max()) <= LOG_ATOL
+    k.close()
+
+
+def test_from_logits_with_forbidden_and_unasked_tokens():
+    """a forbidden token's literal is impossible, and an unasked one weighs 1 either way"""
+    import paper_2410_11415_amd as klay
+    c = tiny_ddnnf(5, 12, 20)[0]
+    k = klay.Circuit(*c.arrays(), device=0)
+    x = torch.randn(5, 4, 30)
+    x[:, 1, :10] = -float("inf")
+    t = torch.tensor([[0, 1, 2], [3, 12, 13], [5, -1, 6], [-1, -1, -1]])
+    lp = torch.log_softmax(x.double(), -1).gather(2, t.clamp(min=0).expand(5, 4, 3)).reshape(5, 12)
+    asked = (t >= 0).reshape(12)
+    ln = torch.where(asked, torch.log1p(-lp.exp()), 0.0)
+    lp = torch.where(asked, lp, 0.0)
+    logits = x.cuda().requires_grad_(True)
+    got = klay.CircuitLayer(k).from_logits(logits, t.cuda())
+    want = circuit_64(c, lp, ln)
+    assert torch.equal(torch.isinf(got.detach().cpu()), torch.isinf(want))
+    fine = torch.isfinite(want)
+    assert float((got.detach().cpu().double() - want)[fine].abs().max()) <= LOG_ATOL
+    got.sum().backward()
+    assert torch.isfinite(logits.grad).all() and not logits.grad[:, 3].any()
+    k.close()
+
+
+class Program:
+    """x -> recurrent layer -> logits -> log probability that position t has its token -> by position t it has been seen -> circuit."""
+
+    def __init__(self, seed, batch, channels, vocab):
+        rng = np.random.default_rng(seed)
+        self.c = tiny_ddnnf(1, 12, 30)[0]
+        self.x = rng.normal(size=(batch, 12, channels))
+        self.params = [rng.normal(size=s) / np.sqrt(channels) for s in ((channels, channels), (channels, channels), (channels, vocab))]
+        self.start = rng.normal(size=(batch, channels))
+        self.tokens = rng.integers(0, vocab, size=(12, 1))
+
+    def loss(self, x, start, params, scan, logprobs, circuit):
+        gates, inputs, head = params
+        a = torch.sigmoid(x @ gates + 2.0)
+        states, _ = scan(0, a, x @ inputs, start)
+        logp, neg, entropy = logprobs(states @ head, torch.from_numpy(self.tokens).to(x.device).expand(x.shape[0], 12, 1))
+        # log of "seen at t or before", and of its complement, whose recurrence has no inputs
+        seen, _ = scan(1, neg, logp, None)
+        unseen, _ = scan(1, neg, torch.full_like(neg, -float("inf")), torch.zeros_like(neg[:, 0]))
+        return -circuit(seen[..., 0], unseen[..., 0])[:, 0].mean() - 0.01 * entropy.mean()
+
+
+def test_the_whole_chain():
+    import paper_2410_11415_amd as klay
+    p = Program(0, 4, 24, 40)
+    k = klay.Circuit(*p.c.arrays(), device=0)
+    layer = klay.CircuitLayer(k, klay.KLAY_LOG)
+
+    def scan_64(semiring, a, x, h):
+        h = torch.full_like(x[:, 0], 0.0 if semiring == 0 else -float("inf")) if h is None else h
+        out = []
+        for t in range(x.shape[1]):
+            h = a[:, t] * h + x[:, t] if semiring == 0 else torch.logsumexp(torch.stack([a[:, t] + h, x[:, t]]), 0)
+            out.append(h)
+        return torch.stack(out, 1), h
+
+    def logprobs_64(x, t):
+        lp = torch.log_softmax(x, -1)
+        asked = lp.gather(2, t)
+        return asked, torch.log1p(-asked.exp()), -(lp.exp() * lp).sum(-1)
+
+    def logprobs(x, t):
+        r = klay.token_logprobs(x, t, complement=True, entropy=True)
+        return r.logp, r.neg, r.entropy
+    host = [torch.from_numpy(v).float() for v in [p.x, p.start] + p.params]
+    exact = [t.double().requires_grad_(True) for t in host]
+    want = p.loss(exact[0], exact[1], exact[2:], scan_64, logprobs_64, lambda a, b: circuit_64(p.c, a, b))
+    want.backward()
+    ours = [t.cuda().requires_grad_(True) for t in host]
+    got = p.loss(ours[0], ours[1], ours[2:], lambda s, a, x, h: klay.gated_scan(a, x, h, s), logprobs, layer)
+    got.backward()
+    assert abs(float(got) - float(want)) <= LOG_ATOL + 1e-5 * abs(float(want))
+    # what fp32 does to the matrix products and to every operator is of the order of 1e-6; a wrong term would be of order 1
+    for a, b in zip(ours, exact):
+        assert float((a.grad.cpu().double() - b.grad).norm() / b.grad.norm()) <= 1e-3
+    k.close()
