@@ -396,7 +396,7 @@ klay_status klay_tokens_backward(const klay_tokens_args* args, const float* stat
  * klay_scan_forward -- gated recurrence over sequences in a semiring (Section 4), the value of a chain of AND and OR gates of any length:
  *   h_t = a_t (x) h_{t-1} (+) x_t:  REAL: a h + x;  LOG: log(exp(a + h) + exp(x));  MAXLOG: max(a + h, x)
  *   gates, inputs   device [batch, time, channels] of `dtype` (KLAY_F32 in the log-domain semirings), channels next to each other,
- *               the two other strides in elements
+ *               the two other strides in elements; at most 2^25 channels and 2^25 elements from one time step to the next
  *   offsets     NULL: `batch` sequences of `time` steps.  Otherwise batch = 1 and device int64 [sequences + 1]: sequence s is the rows
  *               offsets[s] .. offsets[s + 1] - 1, ascending, in 0 .. time; it may be empty.  Rows of no sequence get 0 as states.
  *   row_info    device int32 [time]; required with offsets, for klay_scan_backward, which reads what the forward call wrote

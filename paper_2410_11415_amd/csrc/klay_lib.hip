@@ -5,6 +5,8 @@
 #include "klay_scan.hip.h"
 #include "klay_tokens.hip.h"
 
+#include <initializer_list>
+
 namespace {
 
 // Makes `device` current for a call, and the earlier one again afterwards.
@@ -33,7 +35,7 @@ struct OnDevice {
     } while (0)
 
 constexpr int kComputeUnits = 256;
-constexpr int32_t kMostChannels = 1 << 30;
+constexpr int32_t kMostChannels = 1 << 25;      // and the most elements from one time step to the next: a wave's rows lie within 32-bit offsets
 bool known_dtype(int32_t t) { return t == KLAY_F32 || t == KLAY_BF16 || t == KLAY_F16; }
 int dtype_bytes(int32_t t) { return t == KLAY_F32 ? 4 : 2; }
 
@@ -138,7 +140,9 @@ klay_status check_scan(const klay_scan_args* a, bool inputs, const char* who) {
     if (a->semiring != KLAY_REAL && a->semiring != KLAY_LOG && a->semiring != KLAY_MAXLOG) return fail(KLAY_EINVAL, name + ": unknown semiring");
     if (a->semiring != KLAY_REAL && a->dtype != KLAY_F32) return fail(KLAY_EINVAL, name + ": the log-domain semirings take KLAY_F32 only");
     if (a->channels < 1 || a->channels > kMostChannels || a->batch < 0 || a->time < 0 || a->time > INT32_MAX || a->batch > INT32_MAX / 8)
-        return fail(KLAY_EINVAL, name + ": channels must be 1 .. 2^30, time 0 .. 2^31 - 1, batch 0 .. 2^28 - 1");
+        return fail(KLAY_EINVAL, name + ": channels must be 1 .. 2^25, time 0 .. 2^31 - 1, batch 0 .. 2^28 - 1");
+    if (a->gates_time_stride < 0 || a->gates_time_stride > kMostChannels || a->inputs_time_stride < 0 || a->inputs_time_stride > kMostChannels)
+        return fail(KLAY_EINVAL, name + ": the time strides must be 0 .. 2^25");
     if (a->offsets) {
         if (a->batch != 1) return fail(KLAY_EINVAL, name + ": packed sequences have batch = 1");
         if (a->sequences < 0 || a->sequences > INT32_MAX / 8) return fail(KLAY_EINVAL, name + ": sequences must be 0 .. 2^28 - 1");
@@ -148,27 +152,37 @@ klay_status check_scan(const klay_scan_args* a, bool inputs, const char* who) {
     return KLAY_OK;
 }
 
-// Workgroups of four waves fill the chip where batch and channels give four of them per CU; of sixteen waves where they give one; below
-// that the time axis is cut until there are two per CU, in chunks of 256 steps or more.
+// All of them multiples of `bytes`?
+bool aligned_to(size_t bytes, std::initializer_list<const void*> all) {
+    uintptr_t bits = 0;
+    for (const void* p : all) bits |= reinterpret_cast<uintptr_t>(p);
+    return bits % bytes == 0;
+}
+
+// Two channels a lane where that leaves two workgroups per CU, and addresses and strides let a lane take both at once (us, one / two: 16 x 4096
+// x 4096 fp32 forward 653 / 554, backward 1113 / 964; 32 x 1024 x 4096 bf16 181 / 169, 329 / 278; 8 x 4096 x 2048 bf16, where it would leave
+// half of the CUs empty, 101 / 126, 175 / 182).  Waves as many as the time steps give work to, eight at most (sixteen: within 5% either way, and the
+// log semiring's reverse sweep runs out of registers).  Where batch and channels give less than one workgroup per two CUs the time
+// axis is cut until there is one per CU (8 x 4096 x 512 LOG forward, chunks of 4096 / 1024 / 682 steps: 146 / 73 / 81 us).
 ScanPlan scan_plan(const klay_scan_args* a) {
     ScanPlan p;
-    const bool even = a->dtype != KLAY_F32 && a->channels % 2 == 0;
+    const int64_t size = dtype_bytes(a->dtype);
     auto blocks = [&](int vec) { return (a->channels + 64 * vec - 1) / (64 * vec); };
-    p.vec = even && blocks(2) * a->batch >= kComputeUnits ? 2 : 1;
+    const bool pairs = a->channels % 2 == 0 && aligned_to(2 * size, {a->gates, a->inputs}) && (a->gates_batch_stride | a->gates_time_stride |
+                       a->inputs_batch_stride | a->inputs_time_stride) % 2 == 0;
+    p.vec = a->semiring == KLAY_REAL && pairs && blocks(2) * a->batch >= 2 * kComputeUnits ? 2 : 1;
     p.blocks_c = blocks(p.vec);
     const int64_t n = p.blocks_c * a->batch;
-    if (a->time <= klay::kSteps) p.waves = 1;
-    else if (n >= 4 * kComputeUnits || a->time <= 4 * klay::kSteps) p.waves = 4;
-    else p.waves = 16;
+    p.waves = a->time <= klay::kSteps ? 1 : a->time <= 4 * klay::kSteps ? 4 : 8;
     p.chunk = (int32_t)a->time;
-    if (n < kComputeUnits && p.waves == 16) {
+    if (n <= kComputeUnits / 2 && p.waves == 8) {
         const int64_t tile = (int64_t)p.waves * klay::kSteps;
-        int64_t chunks = std::min<int64_t>((2 * kComputeUnits + n - 1) / n, (a->time + tile - 1) / tile);
-        const int64_t size = ((a->time + chunks - 1) / chunks + tile - 1) / tile * tile;
-        chunks = (a->time + size - 1) / size;
+        int64_t chunks = std::min<int64_t>(kComputeUnits / n, (a->time + tile - 1) / tile);
+        const int64_t steps = ((a->time + chunks - 1) / chunks + tile - 1) / tile * tile;
+        chunks = (a->time + steps - 1) / steps;
         if (chunks > 1) {
             p.chunks = (int32_t)chunks;
-            p.chunk = (int32_t)size;
+            p.chunk = (int32_t)steps;
         }
     }
     return p;
@@ -177,6 +191,12 @@ ScanPlan scan_plan(const klay_scan_args* a) {
 size_t scan_maps(const klay_scan_args* a, const ScanPlan& p) { return (size_t)a->batch * p.chunks * a->channels; }
 size_t scan_bytes(const klay_scan_args* a, const ScanPlan& p) {
     return p.chunks == 1 ? 0 : scan_maps(a, p) * 8 + (size_t)a->batch * p.chunks * 4;
+}
+
+// One channel a lane after all, for arrays that two at once do not fit (the chunks stay).
+void narrow(ScanPlan* p, const klay_scan_args* a) {
+    p->vec = 1;
+    p->blocks_c = (a->channels + 63) / 64;
 }
 
 klay::ScanArgs scan_args(const klay_scan_args* a, const ScanPlan& p, void* workspace) {
@@ -204,13 +224,13 @@ klay_status run_scan(const klay::ScanArgs& g, int64_t batch, bool back, void* st
     const dim3 block(64, W);
     if constexpr (S != klay::SEMI_MAX) {
         if (back) {
-            if constexpr (W == 16)
+            if constexpr (W == 8)
                 if (maps > 0) KLAY_LAUNCH((klay::scan_back_map_kernel<S, T, VC, W>), dim3((uint32_t)maps), block, stream, g);
             KLAY_LAUNCH((klay::scan_back_kernel<S, T, VC, W>), dim3((uint32_t)blocks), block, stream, g);
             return KLAY_OK;
         }
     }
-    if constexpr (W == 16)
+    if constexpr (W == 8)
         if (maps > 0) KLAY_LAUNCH((klay::scan_map_kernel<S, T, VC, W>), dim3((uint32_t)maps), block, stream, g);
     KLAY_LAUNCH((klay::scan_kernel<S, T, VC, W>), dim3((uint32_t)blocks), block, stream, g);
     return KLAY_OK;
@@ -220,14 +240,15 @@ template <int S, typename T, int VC>
 klay_status run_scan(const klay::ScanArgs& g, const ScanPlan& p, int64_t batch, bool back, void* stream) {
     if (p.waves == 1) return run_scan<S, T, VC, 1>(g, batch, back, stream);
     if (p.waves == 4) return run_scan<S, T, VC, 4>(g, batch, back, stream);
-    return run_scan<S, T, VC, 16>(g, batch, back, stream);
+    return run_scan<S, T, VC, 8>(g, batch, back, stream);
 }
 
 klay_status run_scan(const klay_scan_args* a, const klay::ScanArgs& g, const ScanPlan& p, bool back, void* stream) {
     using namespace klay;
     if (a->semiring == KLAY_LOG) return run_scan<SEMI_LOG, f32, 1>(g, p, a->batch, back, stream);
     if (a->semiring == KLAY_MAXLOG) return run_scan<SEMI_MAX, f32, 1>(g, p, a->batch, back, stream);
-    if (a->dtype == KLAY_F32) return run_scan<SEMI_REAL, f32, 1>(g, p, a->batch, back, stream);
+    if (a->dtype == KLAY_F32)
+        return p.vec == 2 ? run_scan<SEMI_REAL, f32, 2>(g, p, a->batch, back, stream) : run_scan<SEMI_REAL, f32, 1>(g, p, a->batch, back, stream);
     if (a->dtype == KLAY_BF16)
         return p.vec == 2 ? run_scan<SEMI_REAL, bf16, 2>(g, p, a->batch, back, stream) : run_scan<SEMI_REAL, bf16, 1>(g, p, a->batch, back, stream);
     return p.vec == 2 ? run_scan<SEMI_REAL, f16, 2>(g, p, a->batch, back, stream) : run_scan<SEMI_REAL, f16, 1>(g, p, a->batch, back, stream);
@@ -323,7 +344,7 @@ klay_status klay_scan_forward(const klay_scan_args* a, void* states, float* fina
     const int64_t sequences = a->offsets ? a->sequences : a->batch;
     const bool rows = a->batch > 0 && a->time > 0;
     if (rows && !states) return fail(KLAY_EINVAL, "klay_scan_forward: null argument");
-    const ScanPlan p = rows ? scan_plan(a) : ScanPlan();
+    ScanPlan p = rows ? scan_plan(a) : ScanPlan();
     st = scan_workspace(a, p, workspace, workspace_bytes, "klay_scan_forward");
     if (st != KLAY_OK) return st;
     OnDevice on(a->device);
@@ -334,6 +355,7 @@ klay_status klay_scan_forward(const klay_scan_args* a, void* states, float* fina
         KLAY_LAUNCH(klay::scan_rows_kernel, dim3((uint32_t)((a->time + 255) / 256)), dim3(256), stream, a->row_info, a->offsets, a->time,
                     (int32_t)a->sequences);
     }
+    if (!aligned_to(2 * dtype_bytes(a->dtype), {states})) narrow(&p, a);
     klay::ScanArgs g = scan_args(a, p, workspace);
     g.out = states;
     g.final = final;
@@ -348,7 +370,7 @@ klay_status klay_scan_backward(const klay_scan_args* a, const void* states, cons
     const int64_t sequences = a->offsets ? a->sequences : a->batch;
     const bool rows = a->batch > 0 && a->time > 0;
     if (rows && !states) return fail(KLAY_EINVAL, "klay_scan_backward: null argument");
-    const ScanPlan p = rows ? scan_plan(a) : ScanPlan();
+    ScanPlan p = rows ? scan_plan(a) : ScanPlan();
     st = scan_workspace(a, p, workspace, workspace_bytes, "klay_scan_backward");
     if (st != KLAY_OK) return st;
     OnDevice on(a->device);
@@ -357,6 +379,7 @@ klay_status klay_scan_backward(const klay_scan_args* a, const void* states, cons
         st = fill_states(dinitial, dfinal, 0.0f, sequences * a->channels, stream);
         if (st != KLAY_OK || !rows) return st;
     }
+    if (!aligned_to(2 * dtype_bytes(a->dtype), {states, dstates, dgates, dinputs})) narrow(&p, a);
     klay::ScanArgs g = scan_args(a, p, workspace);
     g.h = states;
     g.dh = dstates;
@@ -373,7 +396,7 @@ klay_status klay_scan_step(int32_t dtype, int32_t semiring, int32_t device, int6
     if (semiring != KLAY_REAL && semiring != KLAY_LOG && semiring != KLAY_MAXLOG) return fail(KLAY_EINVAL, "klay_scan_step: unknown semiring");
     if (semiring != KLAY_REAL && dtype != KLAY_F32) return fail(KLAY_EINVAL, "klay_scan_step: the log-domain semirings take KLAY_F32 only");
     if (rows < 0 || rows > INT32_MAX || channels < 1 || channels > kMostChannels)
-        return fail(KLAY_EINVAL, "klay_scan_step: rows must be 0 .. 2^31 - 1, channels 1 .. 2^30");
+        return fail(KLAY_EINVAL, "klay_scan_step: rows must be 0 .. 2^31 - 1, channels 1 .. 2^25");
     if (rows == 0) return KLAY_OK;
     if (!gates || !inputs || !state) return fail(KLAY_EINVAL, "klay_scan_step: null argument");
     klay::StepArgs g{gates, inputs, out, state, gates_stride, inputs_stride, out_stride, state_stride, (int32_t)rows, channels};

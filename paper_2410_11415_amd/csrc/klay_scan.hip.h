@@ -67,182 +67,242 @@ struct ScanArgs {
 // The kSteps rows from t on, as a wave sees them: bit i = row t + i.
 struct Rows {
     uint32_t first, last, live;
-    int32_t seq;            // lane i: sequence of row t + i
-    __device__ __forceinline__ Rows(const ScanArgs& g, int64_t t, int64_t end, int batch) {
-        const int lane = threadIdx.x;
-        int32_t r = kDeadRow;
-        if (lane < kSteps && t + lane < end) {
-            if (g.rows) r = g.rows[t + lane];
-            else r = 4 * batch + (t + lane == 0 ? ROW_FIRST : 0) + (t + lane == g.time - 1 ? ROW_LAST : 0);
+    int32_t info;           // packed, lane i: what row t + i is;  dense: the sequence
+    __device__ __forceinline__ void load(const ScanArgs& g, int64_t t, int64_t end, int32_t batch) {
+        info = batch;
+        if (g.rows) {
+            const int64_t r = t + (threadIdx.x & (kSteps - 1));
+            info = g.rows[r < end ? r : end - 1];
         }
-        seq = r >> 2;
-        live = (uint32_t)__ballot(r >= 0);
-        first = (uint32_t)__ballot(r >= 0 && (r & ROW_FIRST));
-        last = (uint32_t)__ballot(r >= 0 && (r & ROW_LAST));
     }
-    __device__ __forceinline__ int64_t sequence(int i) const { return __builtin_amdgcn_readlane(seq, i); }
+    __device__ __forceinline__ void resolve(const ScanArgs& g, int64_t t, int64_t end) {
+        const int64_t left = end - t;
+        live = left >= kSteps ? kAllSteps : left > 0 ? (1u << left) - 1 : 0;
+        if (g.rows) {
+            first = (uint32_t)__ballot(info >= 0 && (info & ROW_FIRST)) & live;
+            last = (uint32_t)__ballot(info >= 0 && (info & ROW_LAST)) & live;
+            live &= (uint32_t)__ballot(info >= 0);
+        } else {
+            first = t == 0 ? 1u & live : 0;
+            const int64_t behind = g.time - 1 - t;
+            last = behind >= 0 && behind < kSteps ? (1u << behind) & live : 0;
+        }
+    }
+    // all rows in the middle of one sequence: the waves' steps are straight-line code, in which loads of the tile behind stay in flight
+    __device__ __forceinline__ bool plain() const { return live == kAllSteps && (first | last) == 0; }
+    __device__ __forceinline__ int64_t sequence(const ScanArgs& g, int i) const {
+        return g.rows ? __builtin_amdgcn_readlane(info, i) >> 2 : __builtin_amdgcn_readfirstlane(info);
+    }
 };
 
+// Where a lane's channels are.
+struct Place {
+    int32_t batch, c;
+    bool in;
+    uint32_t lane;          // the first one, 0 past the channels
+};
+
+// The rows from t on of an array whose row 0 is at `base`.  Rows past `end` stand for the last one before it (they are not live, and
+// what they load is not used).
+template <int VC, typename T>
+__device__ __forceinline__ void load_rows(Raw<T, VC> (&to)[kSteps], const T* base, int64_t stride, int64_t t, int64_t end, const Place& at) {
+    const int64_t t0 = t < end ? t : end - 1;
+    const uint32_t left = (uint32_t)(end - 1 - t0 < kSteps ? end - 1 - t0 : kSteps), bytes = (uint32_t)stride * sizeof(T);
+    const Stretch from = stretch_at(base + t0 * stride);
+    const uint32_t lane = at.in ? at.lane * (uint32_t)sizeof(T) : kNoLane;
+#pragma unroll
+    for (uint32_t i = 0; i < kSteps; ++i) to[i] = load_raw<VC, T>(from, lane, (i < left ? i : left) * bytes);
+}
+
 template <int VC>
-__device__ __forceinline__ void load_state(float (&h)[VC], const float* states, int64_t seq, const ScanArgs& g, int c, bool in, float none) {
+__device__ __forceinline__ void load_state(float (&h)[VC], const float* states, int64_t seq, const ScanArgs& g, const Place& at, float none) {
 #pragma unroll
     for (int v = 0; v < VC; ++v) h[v] = none;
-    if (states && in) load_elements<VC>(h, states + seq * g.channels + c);
+    if (states && at.in) load_elements<VC>(h, states + seq * g.channels + at.c);
 }
+
+// The workgroup's place: x = channels, then chunks, then the batch.
+template <int VC>
+__device__ __forceinline__ Place place_of(const ScanArgs& g, int32_t chunks, int32_t& chunk) {
+    Place at;
+    const uint32_t rest = blockIdx.x / (uint32_t)g.blocks_c;
+    at.c = (int32_t)((blockIdx.x - rest * (uint32_t)g.blocks_c) * 64 + threadIdx.x) * VC;
+    at.batch = (int32_t)(rest / (uint32_t)chunks);
+    chunk = (int32_t)(rest - (uint32_t)at.batch * (uint32_t)chunks);
+    at.in = at.c < g.channels;
+    at.lane = at.in ? (uint32_t)at.c : 0;
+    return at;
+}
+
+// A workgroup barrier for what the waves exchange in LDS: loads from memory stay in flight.
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// The maps of the W waves of a tile.  Two sets in turn: a wave may write the next tile's while another still reads these.
+template <int VC, int W> struct Maps {
+    float a[2][W][64][VC], h[2][W][64][VC];
+    int32_t cut[2][W];
+    __device__ __forceinline__ void put(int turn, int wave, const float (&A)[VC], const float (&H)[VC], bool is_cut) {
+        const int lane = threadIdx.x;
+#pragma unroll
+        for (int v = 0; v < VC; ++v) { a[turn][wave][lane][v] = A[v]; h[turn][wave][lane][v] = H[v]; }
+        if (lane == 0) cut[turn][wave] = is_cut;
+    }
+    __device__ __forceinline__ uint64_t cuts(int turn) const {
+        const int lane = threadIdx.x;
+        return __ballot(lane < W && cut[turn][lane < W ? lane : 0] != 0);
+    }
+};
 
 // ---- forward ----------------------------------------------------------------------------------------------------
-template <int S, typename T, int VC>
-__device__ __forceinline__ void load_steps(float (&a)[kSteps][VC], float (&x)[kSteps][VC], const ScanArgs& g, int64_t batch, int64_t t,
-                                           int c, bool in, uint32_t live) {
-    const int cs = in ? c : 0;          // lanes past the channels read channel 0: no branch around the loads
-    const T* pa = static_cast<const T*>(g.a) + batch * g.a_batch + t * g.a_time + cs;
-    const T* px = static_cast<const T*>(g.x) + batch * g.x_batch + t * g.x_time + cs;
-    if (live == kAllSteps) {
+template <int S, typename T, int VC> struct Tile {
+    Raw<T, VC> a[kSteps], x[kSteps];
+    Rows rows;
+    __device__ __forceinline__ void load(const ScanArgs& g, int64_t t, int64_t end, const Place& at) {
+        rows.load(g, t, end, at.batch);
+        load_rows<VC, T>(a, static_cast<const T*>(g.a) + at.batch * g.a_batch, g.a_time, t, end, at);
+        load_rows<VC, T>(x, static_cast<const T*>(g.x) + at.batch * g.x_batch, g.x_time, t, end, at);
+    }
+    // rows that are not live become steps that change nothing
+    __device__ __forceinline__ void resolve(const ScanArgs& g, int64_t t, int64_t end) {
+        rows.resolve(g, t, end);
+        if (rows.live == kAllSteps) return;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+            if (!(rows.live >> i & 1)) {
+                a[i] = all_pieces<VC, T>(Ring<S>::one);
+                x[i] = all_pieces<VC, T>(Ring<S>::zero());
+            }
+    }
+    // the map of the steps, (A, H) before them; whether a sequence starts in them
+    __device__ __forceinline__ bool map(float (&A)[VC], float (&H)[VC], const ScanArgs& g, const Place& at) const {
+        return rows.plain() ? map_steps<true>(A, H, g, at) : map_steps<false>(A, H, g, at);
+    }
+    template <bool PLAIN> __device__ __forceinline__ bool map_steps(float (&A)[VC], float (&H)[VC], const ScanArgs& g, const Place& at) const {
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            load_elements<VC>(a[i], pa + i * g.a_time);
-            load_elements<VC>(x[i], px + i * g.x_time);
+            if (!PLAIN && (rows.first >> i & 1)) load_state<VC>(H, g.initial, rows.sequence(g, i), g, at, Ring<S>::zero());
+#pragma unroll
+            for (int v = 0; v < VC; ++v) {
+                const float av = piece<VC, T>(a[i], v);
+                H[v] = Ring<S>::step(av, H[v], piece<VC, T>(x[i], v));
+                A[v] = Ring<S>::times(av, A[v]);
+            }
         }
-        return;
+        return !PLAIN && rows.first != 0;
     }
+    // the steps themselves, from the state h
+    template <bool PLAIN> __device__ __forceinline__ void walk(float (&h)[VC], const ScanArgs& g, int64_t t, int64_t end, const Place& at) const {
+        const Stretch out = stretch_at(static_cast<T*>(g.out) + ((int64_t)at.batch * g.time + t) * g.channels);
+        const uint32_t lane = at.in ? at.lane * (uint32_t)sizeof(T) : kNoLane, row = (uint32_t)g.channels * sizeof(T);
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
+        for (int i = 0; i < kSteps; ++i) {
+            if (!PLAIN && (rows.first >> i & 1)) load_state<VC>(h, g.initial, rows.sequence(g, i), g, at, Ring<S>::zero());
 #pragma unroll
-        for (int v = 0; v < VC; ++v) { a[i][v] = Ring<S>::one; x[i][v] = Ring<S>::zero(); }
-        if (live >> i & 1) {
-            load_elements<VC>(a[i], pa + i * g.a_time);
-            load_elements<VC>(x[i], px + i * g.x_time);
+            for (int v = 0; v < VC; ++v) h[v] = Ring<S>::step(piece<VC, T>(a[i], v), h[v], piece<VC, T>(x[i], v));
+            if (PLAIN || t + i < end) {
+                float y[VC];
+#pragma unroll
+                for (int v = 0; v < VC; ++v) y[v] = PLAIN || (rows.live >> i & 1) ? h[v] : 0.0f;
+                store_row<VC, T>(out, lane, i * row, y);
+            }
+            if (!PLAIN && g.final && (rows.last >> i & 1) && at.in)
+                store_elements<VC>(g.final + rows.sequence(g, i) * g.channels + at.lane, h);
         }
     }
-}
-
-// The map of the steps in registers: (A, H), and whether a sequence starts in them.
-template <int S, int VC>
-__device__ __forceinline__ bool map_of(float (&A)[VC], float (&H)[VC], const float (&a)[kSteps][VC], const float (&x)[kSteps][VC],
-                                       const Rows& rows, const ScanArgs& g, int c, bool in) {
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-        if (rows.first >> i & 1) load_state<VC>(H, g.initial, rows.sequence(i), g, c, in, Ring<S>::zero());
-#pragma unroll
-        for (int v = 0; v < VC; ++v) {
-            H[v] = Ring<S>::step(a[i][v], H[v], x[i][v]);
-            A[v] = Ring<S>::times(a[i][v], A[v]);
-        }
-    }
-    return rows.first != 0;
-}
+};
 
 // Maps of the chunks (those before the last one): every wave a run of its own, joined at the end.
 template <int S, typename T, int VC, int W>
 __global__ void __launch_bounds__(64 * W) scan_map_kernel(ScanArgs g) {
-    __shared__ float sa[W][64][VC], sh[W][64][VC];
-    __shared__ int scut[W];
-    const int lane = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.y);
-    const int bc = blockIdx.x % g.blocks_c;
-    const int64_t rest = blockIdx.x / g.blocks_c;
-    const int chunk = (int)(rest % (g.chunks - 1));
-    const int64_t batch = rest / (g.chunks - 1);
-    const int c = (bc * 64 + lane) * VC;
-    const bool in = c < g.channels;
+    __shared__ Maps<VC, W> maps;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.y), lane = threadIdx.x;
+    int32_t chunk;
+    const Place at = place_of<VC>(g, g.chunks - 1, chunk);
     const int per_wave = g.chunk / W;
     const int64_t begin = (int64_t)chunk * g.chunk + (int64_t)wave * per_wave, end = begin + per_wave;
     float A[VC], H[VC];
     bool cut = false;
 #pragma unroll
     for (int v = 0; v < VC; ++v) { A[v] = Ring<S>::one; H[v] = Ring<S>::zero(); }
+    Tile<S, T, VC> next;
+    next.load(g, begin, end, at);
     for (int64_t t = begin; t < end; t += kSteps) {
-        float a[kSteps][VC], x[kSteps][VC];
-        const Rows rows(g, t, end, (int)batch);
-        load_steps<S, T, VC>(a, x, g, batch, t, c, in, rows.live);
-        cut |= map_of<S, VC>(A, H, a, x, rows, g, c, in);
+        Tile<S, T, VC> now = next;
+        if (t + kSteps < end) next.load(g, t + kSteps, end, at);
+        now.resolve(g, t, end);
+        cut |= now.map(A, H, g, at);
     }
-#pragma unroll
-    for (int v = 0; v < VC; ++v) { sa[wave][lane][v] = A[v]; sh[wave][lane][v] = H[v]; }
-    if (lane == 0) scut[wave] = cut;
+    maps.put(0, wave, A, H, cut);
     __syncthreads();
     if (wave != 0) return;
-    for (int w = 1; w < W; ++w) {
-        const bool wcut = scut[w];
-        cut |= wcut;
+    const uint64_t cuts = maps.cuts(0);
+    for (int w = 1; w < W; ++w)
 #pragma unroll
         for (int v = 0; v < VC; ++v) {
-            H[v] = wcut ? sh[w][lane][v] : Ring<S>::step(sa[w][lane][v], H[v], sh[w][lane][v]);
-            A[v] = Ring<S>::times(sa[w][lane][v], A[v]);
+            H[v] = cuts >> w & 1 ? maps.h[0][w][lane][v] : Ring<S>::step(maps.a[0][w][lane][v], H[v], maps.h[0][w][lane][v]);
+            A[v] = Ring<S>::times(maps.a[0][w][lane][v], A[v]);
         }
+    const int64_t to = (int64_t)at.batch * g.chunks + chunk;
+    if (at.in) {
+        store_elements<VC>(g.map_a + to * g.channels + at.c, A);
+        store_elements<VC>(g.map_h + to * g.channels + at.c, H);
     }
-    const int64_t at = batch * g.chunks + chunk;
-    if (in) {
-        store_elements<VC>(g.map_a + at * g.channels + c, A);
-        store_elements<VC>(g.map_h + at * g.channels + c, H);
-    }
-    if (bc == 0 && lane == 0) g.map_cut[at] = cut;
+    if (at.c == 0) g.map_cut[to] = cuts != 0;
 }
 
 template <int S, typename T, int VC, int W>
 __global__ void __launch_bounds__(64 * W) scan_kernel(ScanArgs g) {
-    __shared__ float sa[2][W][64][VC], sh[2][W][64][VC];
-    __shared__ int scut[2][W];
-    const int lane = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.y);
-    const int bc = blockIdx.x % g.blocks_c;
-    const int64_t rest = blockIdx.x / g.blocks_c;
-    const int chunk = (int)(rest % g.chunks);
-    const int64_t batch = rest / g.chunks;
-    const int c = (bc * 64 + lane) * VC;
-    const bool in = c < g.channels;
+    __shared__ Maps<VC, W> maps;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.y), lane = threadIdx.x;
+    int32_t chunk;
+    const Place at = place_of<VC>(g, g.chunks, chunk);
+    const int64_t begin = (int64_t)chunk * g.chunk, end = g.time < begin + g.chunk ? g.time : begin + g.chunk;
+    Tile<S, T, VC> next;
+    next.load(g, begin + wave * kSteps, end, at);
     float carry[VC];
 #pragma unroll
     for (int v = 0; v < VC; ++v) carry[v] = Ring<S>::zero();
     for (int k = 0; k < chunk; ++k) {
-        const int64_t at = batch * g.chunks + k;
-        float A[VC] = {}, H[VC] = {};
-        if (in) {
-            load_elements<VC>(A, g.map_a + at * g.channels + c);
-            load_elements<VC>(H, g.map_h + at * g.channels + c);
-        }
-        const bool cut = g.map_cut[at];
+        const int64_t from = (int64_t)at.batch * g.chunks + k;
+        float A[VC], H[VC];
+        load_elements<VC>(A, g.map_a + from * g.channels + at.lane);
+        load_elements<VC>(H, g.map_h + from * g.channels + at.lane);
+        const bool cut = g.map_cut[from];
 #pragma unroll
         for (int v = 0; v < VC; ++v) carry[v] = cut ? H[v] : Ring<S>::step(A[v], carry[v], H[v]);
     }
-    const int64_t begin = (int64_t)chunk * g.chunk, end = g.time < begin + g.chunk ? g.time : begin + g.chunk;
     int turn = 0;
     for (int64_t tile = begin; tile < end; tile += W * kSteps, turn ^= 1) {
         const int64_t t = tile + wave * kSteps;
-        float a[kSteps][VC], x[kSteps][VC], A[VC], H[VC];
-        const Rows rows(g, t, end, (int)batch);
-        load_steps<S, T, VC>(a, x, g, batch, t, c, in, rows.live);
+        Tile<S, T, VC> now = next;
+        if (tile + W * kSteps < end) next.load(g, t + W * kSteps, end, at);
+        now.resolve(g, t, end);
+        float A[VC], H[VC], h[VC];
 #pragma unroll
-        for (int v = 0; v < VC; ++v) { A[v] = Ring<S>::one; H[v] = Ring<S>::zero(); }
-        const bool cut = map_of<S, VC>(A, H, a, x, rows, g, c, in);
-        // two sets of maps in turn: a wave may write the next tile's while another still reads these
+        for (int v = 0; v < VC; ++v) { A[v] = Ring<S>::one; H[v] = Ring<S>::zero(); h[v] = carry[v]; }
+        if constexpr (W > 1) {
+            const bool cut = now.map(A, H, g, at);
+            maps.put(turn, wave, A, H, cut);
+            lds_barrier();
+            const uint64_t cuts = maps.cuts(turn);
 #pragma unroll
-        for (int v = 0; v < VC; ++v) { sa[turn][wave][lane][v] = A[v]; sh[turn][wave][lane][v] = H[v]; }
-        if (lane == 0) scut[turn][wave] = cut;
-        __syncthreads();
-        float h[VC];
+            for (int w = 0; w < W; ++w)
 #pragma unroll
-        for (int w = 0; w < W; ++w) {
-            const bool wcut = scut[turn][w];
-#pragma unroll
-            for (int v = 0; v < VC; ++v) {
-                if (w == wave) h[v] = carry[v];
-                carry[v] = wcut ? sh[turn][w][lane][v] : Ring<S>::step(sa[turn][w][lane][v], carry[v], sh[turn][w][lane][v]);
-            }
+                for (int v = 0; v < VC; ++v) {
+                    if (w == wave) h[v] = carry[v];
+                    carry[v] = Ring<S>::step(maps.a[turn][w][lane][v], carry[v], maps.h[turn][w][lane][v]);
+                    if (cuts != 0 && (cuts >> w & 1)) carry[v] = maps.h[turn][w][lane][v];
+                }
         }
-        T* out = static_cast<T*>(g.out) + (batch * g.time + t) * g.channels + c;
+        if (now.rows.plain()) now.template walk<true>(h, g, t, end, at);
+        else now.template walk<false>(h, g, t, end, at);
+        if constexpr (W == 1)
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            if (rows.first >> i & 1) load_state<VC>(h, g.initial, rows.sequence(i), g, c, in, Ring<S>::zero());
-#pragma unroll
-            for (int v = 0; v < VC; ++v) h[v] = Ring<S>::step(a[i][v], h[v], x[i][v]);
-            if (t + i < end && in) {
-                const bool live = rows.live >> i & 1;
-                float y[VC];
-#pragma unroll
-                for (int v = 0; v < VC; ++v) y[v] = live ? h[v] : 0.0f;
-                store_elements<VC>(out + (int64_t)i * g.channels, y);
-                if (g.final && (rows.last >> i & 1)) store_elements<VC>(g.final + rows.sequence(i) * g.channels + c, h);
-            }
-        }
+            for (int v = 0; v < VC; ++v) carry[v] = h[v];
     }
 }
 
@@ -253,8 +313,8 @@ __global__ void __launch_bounds__(64 * W) scan_kernel(ScanArgs g) {
 //         children, taken from the difference z = a + h_{t-1} - x, in which the rounding of h_t does not enter.  A step both of whose
 //         children are impossible passes nothing down, as an OR gate of value log 0 does.
 // Linear in c with the factors w (REAL: a): the same kind of map, joined from the last step to the first.
-// REAL with 16-bit tensors takes h_{t-1} as the forward pass returned it: one rounding of up to 2^-8 (bf16) or 2^-11 (fp16) relative in da,
-// which is rounded as much itself; keeping the states in 32 bits for it would cost 2 N C more bytes in each direction.
+// REAL with 16-bit tensors takes h_{t-1} as the forward pass returned it: one rounding of up to 2^-8 (bf16) or 2^-11 (fp16) relative in
+// da, which is rounded as much itself; keeping the states in 32 bits for it would cost 2 N C more bytes in each direction.
 __device__ __forceinline__ void shares(float& w, float& v, float a, float h, float x) {
     const float p = a + h;
     const float z = p - x;
@@ -266,74 +326,125 @@ __device__ __forceinline__ void shares(float& w, float& v, float a, float h, flo
     if (z != z && p != x) w = v = z;
 }
 
-// a, w: factors of the steps; b: h_{t-1} (REAL), shares of x (LOG); d: dh
-template <int S, typename T, int VC>
-__device__ __forceinline__ void load_steps_back(float (&w)[kSteps][VC], float (&b)[kSteps][VC], float (&d)[kSteps][VC], const ScanArgs& g,
-                                                int64_t batch, int64_t t, int c, bool in, const Rows& rows, bool need_b) {
-    const int cs = in ? c : 0;
-    const T* pa = static_cast<const T*>(g.a) + batch * g.a_batch + t * g.a_time + cs;
-    const T* px = static_cast<const T*>(g.x) + batch * g.x_batch + t * g.x_time + cs;
-    const int64_t at = (batch * g.time + t) * g.channels + cs;
-    const T* ph = static_cast<const T*>(g.h) + at;
-    const T* pd = static_cast<const T*>(g.dh) + at;
-    float x[S == SEMI_LOG ? kSteps : 1][VC];
+template <int S, typename T, int VC> struct BackTile {
+    static constexpr bool kLog = S == SEMI_LOG;
+    Raw<T, VC> a[kSteps], d[kSteps], h[kSteps], x[kLog ? kSteps : 1];      // h: the states before the steps;  LOG, resolved: a = w, x = v
+    Rows rows;
+    // gates_too: h is needed (LOG: for the shares)
+    __device__ __forceinline__ void load(const ScanArgs& g, int64_t t, int64_t end, const Place& at, bool need_h) {
+        rows.load(g, t, end, at.batch);
+        const int64_t states = (int64_t)at.batch * g.time * g.channels;
+        load_rows<VC, T>(a, static_cast<const T*>(g.a) + at.batch * g.a_batch, g.a_time, t, end, at);
+        if (g.dh) load_rows<VC, T>(d, static_cast<const T*>(g.dh) + states, g.channels, t, end, at);
+        if constexpr (kLog) load_rows<VC, T>(x, static_cast<const T*>(g.x) + at.batch * g.x_batch, g.x_time, t, end, at);
+        if (need_h) {
+            // rows t - 1 ..;  row 0 starts a sequence: what is loaded for it is not used
+            const int64_t t0 = t < end ? t : end - 1;
+            const uint32_t left = (uint32_t)(end - 1 - t0 < kSteps ? end - 1 - t0 : kSteps), bytes = (uint32_t)g.channels * sizeof(T);
+            const uint32_t back = t0 > 0 ? 1 : 0, lane = at.in ? at.lane * (uint32_t)sizeof(T) : kNoLane;
+            const Stretch from = stretch_at(static_cast<const T*>(g.h) + states + (t0 - back) * g.channels);
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-        const bool live = rows.live >> i & 1;
-#pragma unroll
-        for (int v = 0; v < VC; ++v) { w[i][v] = S == SEMI_REAL ? 1.0f : 0.0f; b[i][v] = 0.0f; d[i][v] = 0.0f; }
-        if (live) {
-            load_elements<VC>(w[i], pa + i * g.a_time);
-            if (g.dh) load_elements<VC>(d[i], pd + (int64_t)i * g.channels);
-            if constexpr (S == SEMI_LOG) load_elements<VC>(x[i], px + i * g.x_time);
-        }
-        if (need_b) {
-            if (rows.first >> i & 1) load_state<VC>(b[i], g.initial, rows.sequence(i), g, c, in, Ring<S>::zero());
-            else if (live) load_elements<VC>(b[i], ph + (int64_t)(i - 1) * g.channels);
-        }
-    }
-    if constexpr (S == SEMI_LOG) {
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            const bool live = rows.live >> i & 1;
-#pragma unroll
-            for (int v = 0; v < VC; ++v) {
-                float ws = 1.0f, vs = 0.0f;
-                if (live) shares(ws, vs, w[i][v], b[i][v], x[i][v]);
-                w[i][v] = ws;
-                b[i][v] = vs;
+            for (uint32_t i = 0; i < kSteps; ++i) {
+                const uint32_t row = (i < left ? i : left) + back;
+                h[i] = load_raw<VC, T>(from, lane, (row > 0 ? row - 1 : 0) * bytes);
             }
         }
     }
-}
-
-template <int VC>
-__device__ __forceinline__ bool map_of_back(float (&A)[VC], float (&C)[VC], const float (&w)[kSteps][VC], const float (&d)[kSteps][VC],
-                                            const Rows& rows, const ScanArgs& g, int c, bool in) {
+    __device__ __forceinline__ void resolve(const ScanArgs& g, int64_t t, int64_t end, const Place& at) {
+        rows.resolve(g, t, end);
+        if (!g.dh) {
 #pragma unroll
-    for (int i = kSteps - 1; i >= 0; --i) {
-        if (rows.last >> i & 1) load_state<VC>(C, g.dfinal, rows.sequence(i), g, c, in, 0.0f);
+            for (int i = 0; i < kSteps; ++i) d[i] = all_pieces<VC, T>(0.0f);
+        }
+        if (kLog && !rows.plain()) {
 #pragma unroll
-        for (int v = 0; v < VC; ++v) {
-            C[v] = w[i][v] * (d[i][v] + C[v]);
-            A[v] *= w[i][v];
+            for (int i = 0; i < kSteps; ++i)
+                if (rows.first >> i & 1) {
+                    float before[VC];
+                    load_state<VC>(before, g.initial, rows.sequence(g, i), g, at, Ring<S>::zero());
+                    h[i] = all_pieces<VC, T>(before[0]);
+                }
+        }
+        if constexpr (kLog) {
+            static_assert(VC == 1, "the log-domain semirings take one channel a lane");
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                float w, v;
+                shares(w, v, a[i], h[i], x[i]);
+                a[i] = w;
+                x[i] = v;
+            }
+        }
+        if (rows.live != kAllSteps) {
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i)
+                if (!(rows.live >> i & 1)) {
+                    a[i] = all_pieces<VC, T>(1.0f);
+                    d[i] = all_pieces<VC, T>(0.0f);
+                }
         }
     }
-    return rows.last != 0;
-}
+    __device__ __forceinline__ bool map(float (&A)[VC], float (&C)[VC], const ScanArgs& g, const Place& at) const {
+        return rows.plain() ? map_steps<true>(A, C, g, at) : map_steps<false>(A, C, g, at);
+    }
+    template <bool PLAIN> __device__ __forceinline__ bool map_steps(float (&A)[VC], float (&C)[VC], const ScanArgs& g, const Place& at) const {
+#pragma unroll
+        for (int i = kSteps - 1; i >= 0; --i) {
+            if (!PLAIN && (rows.last >> i & 1)) load_state<VC>(C, g.dfinal, rows.sequence(g, i), g, at, 0.0f);
+#pragma unroll
+            for (int v = 0; v < VC; ++v) {
+                const float w = piece<VC, T>(a[i], v);
+                C[v] = w * (piece<VC, T>(d[i], v) + C[v]);
+                A[v] *= w;
+            }
+        }
+        return !PLAIN && rows.last != 0;
+    }
+    // the steps themselves, from the last to the first, from the adjoint c of the state behind them
+    template <bool PLAIN> __device__ __forceinline__ void walk(float (&c)[VC], const ScanArgs& g, int64_t t, int64_t end, const Place& at) const {
+        const int64_t to = ((int64_t)at.batch * g.time + t) * g.channels;
+        const Stretch da = stretch_at(static_cast<T*>(g.da) + to), dx = stretch_at(static_cast<T*>(g.dx) + to);
+        const uint32_t lane = at.in ? at.lane * (uint32_t)sizeof(T) : kNoLane, row = (uint32_t)g.channels * sizeof(T);
+#pragma unroll
+        for (int i = kSteps - 1; i >= 0; --i) {
+            if (!PLAIN && (rows.last >> i & 1)) load_state<VC>(c, g.dfinal, rows.sequence(g, i), g, at, 0.0f);
+            float ya[VC], yx[VC], before[VC];
+            const bool live = PLAIN || (rows.live >> i & 1);
+            if constexpr (!kLog) {
+#pragma unroll
+                for (int v = 0; v < VC; ++v) before[v] = piece<VC, T>(h[i], v);
+                if (!PLAIN && (rows.first >> i & 1)) load_state<VC>(before, g.initial, rows.sequence(g, i), g, at, Ring<S>::zero());
+            }
+#pragma unroll
+            for (int v = 0; v < VC; ++v) {
+                const float gt = piece<VC, T>(d[i], v) + c[v];
+                c[v] = piece<VC, T>(a[i], v) * gt;
+                if constexpr (!kLog) {
+                    ya[v] = live ? gt * before[v] : 0.0f;
+                    yx[v] = live ? gt : 0.0f;
+                } else {
+                    ya[v] = live ? c[v] : 0.0f;
+                    yx[v] = live ? gt * piece<VC, T>(x[i], v) : 0.0f;
+                }
+            }
+            if (PLAIN || t + i < end) {
+                if (g.da) store_row<VC, T>(da, lane, i * row, ya);
+                if (g.dx) store_row<VC, T>(dx, lane, i * row, yx);
+            }
+            if (!PLAIN && g.dinitial && (rows.first >> i & 1) && at.in)
+                store_elements<VC>(g.dinitial + rows.sequence(g, i) * g.channels + at.lane, c);
+        }
+    }
+};
 
 // Maps of the chunks (those behind the first one), each from its last step to its first.
 template <int S, typename T, int VC, int W>
 __global__ void __launch_bounds__(64 * W) scan_back_map_kernel(ScanArgs g) {
-    __shared__ float sa[W][64][VC], sc[W][64][VC];
-    __shared__ int scut[W];
-    const int lane = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.y);
-    const int bc = blockIdx.x % g.blocks_c;
-    const int64_t rest = blockIdx.x / g.blocks_c;
-    const int chunk = 1 + (int)(rest % (g.chunks - 1));
-    const int64_t batch = rest / (g.chunks - 1);
-    const int c = (bc * 64 + lane) * VC;
-    const bool in = c < g.channels;
+    __shared__ Maps<VC, W> maps;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.y), lane = threadIdx.x;
+    int32_t chunk;
+    const Place at = place_of<VC>(g, g.chunks - 1, chunk);
+    ++chunk;
     const int per_wave = g.chunk / W;
     const int64_t begin = (int64_t)chunk * g.chunk + (int64_t)wave * per_wave;
     const int64_t end = g.time < begin + per_wave ? g.time : begin + per_wave;
@@ -341,106 +452,86 @@ __global__ void __launch_bounds__(64 * W) scan_back_map_kernel(ScanArgs g) {
     bool cut = false;
 #pragma unroll
     for (int v = 0; v < VC; ++v) { A[v] = 1.0f; C[v] = 0.0f; }
-    for (int64_t t = begin + per_wave - kSteps; t >= begin; t -= kSteps) {
-        if (t >= end) continue;
-        float w[kSteps][VC], b[kSteps][VC], d[kSteps][VC];
-        const Rows rows(g, t, end, (int)batch);
-        load_steps_back<S, T, VC>(w, b, d, g, batch, t, c, in, rows, S == SEMI_LOG);
-        cut |= map_of_back<VC>(A, C, w, d, rows, g, c, in);
-    }
-#pragma unroll
-    for (int v = 0; v < VC; ++v) { sa[wave][lane][v] = A[v]; sc[wave][lane][v] = C[v]; }
-    if (lane == 0) scut[wave] = cut;
-    __syncthreads();
-    if (wave != W - 1) return;
-    for (int k = W - 2; k >= 0; --k) {
-        const bool wcut = scut[k];
-        cut |= wcut;
-#pragma unroll
-        for (int v = 0; v < VC; ++v) {
-            C[v] = wcut ? sc[k][lane][v] : fmaf(sa[k][lane][v], C[v], sc[k][lane][v]);
-            A[v] *= sa[k][lane][v];
+    if (begin < end) {
+        int64_t t = begin + (end - 1 - begin) / kSteps * kSteps;
+        BackTile<S, T, VC> next;
+        next.load(g, t, end, at, S == SEMI_LOG);
+        for (; t >= begin; t -= kSteps) {
+            BackTile<S, T, VC> now = next;
+            if (t - kSteps >= begin) next.load(g, t - kSteps, end, at, S == SEMI_LOG);
+            now.resolve(g, t, end, at);
+            cut |= now.map(A, C, g, at);
         }
     }
-    const int64_t at = batch * g.chunks + chunk;
-    if (in) {
-        store_elements<VC>(g.map_a + at * g.channels + c, A);
-        store_elements<VC>(g.map_h + at * g.channels + c, C);
+    maps.put(0, wave, A, C, cut);
+    __syncthreads();
+    if (wave != W - 1) return;
+    const uint64_t cuts = maps.cuts(0);
+    for (int w = W - 2; w >= 0; --w)
+#pragma unroll
+        for (int v = 0; v < VC; ++v) {
+            C[v] = cuts >> w & 1 ? maps.h[0][w][lane][v] : fmaf(maps.a[0][w][lane][v], C[v], maps.h[0][w][lane][v]);
+            A[v] *= maps.a[0][w][lane][v];
+        }
+    const int64_t to = (int64_t)at.batch * g.chunks + chunk;
+    if (at.in) {
+        store_elements<VC>(g.map_a + to * g.channels + at.c, A);
+        store_elements<VC>(g.map_h + to * g.channels + at.c, C);
     }
-    if (bc == 0 && lane == 0) g.map_cut[at] = cut;
+    if (at.c == 0) g.map_cut[to] = cuts != 0;
 }
 
 template <int S, typename T, int VC, int W>
 __global__ void __launch_bounds__(64 * W) scan_back_kernel(ScanArgs g) {
-    __shared__ float sa[2][W][64][VC], sc[2][W][64][VC];
-    __shared__ int scut[2][W];
-    const int lane = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.y);
-    const int bc = blockIdx.x % g.blocks_c;
-    const int64_t rest = blockIdx.x / g.blocks_c;
-    const int chunk = (int)(rest % g.chunks);
-    const int64_t batch = rest / g.chunks;
-    const int c = (bc * 64 + lane) * VC;
-    const bool in = c < g.channels;
+    __shared__ Maps<VC, W> maps;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.y), lane = threadIdx.x;
+    int32_t chunk;
+    const Place at = place_of<VC>(g, g.chunks, chunk);
+    const int64_t begin = (int64_t)chunk * g.chunk, end = g.time < begin + g.chunk ? g.time : begin + g.chunk;
+    const bool need_h = S == SEMI_LOG || g.da;
+    const int64_t tiles = (end - begin + W * kSteps - 1) / (W * kSteps);
+    BackTile<S, T, VC> next;
+    next.load(g, begin + (tiles - 1) * (W * kSteps) + wave * kSteps, end, at, need_h);
     float carry[VC];
 #pragma unroll
     for (int v = 0; v < VC; ++v) carry[v] = 0.0f;
     for (int k = g.chunks - 1; k > chunk; --k) {
-        const int64_t at = batch * g.chunks + k;
-        float A[VC] = {}, C[VC] = {};
-        if (in) {
-            load_elements<VC>(A, g.map_a + at * g.channels + c);
-            load_elements<VC>(C, g.map_h + at * g.channels + c);
-        }
-        const bool cut = g.map_cut[at];
+        const int64_t from = (int64_t)at.batch * g.chunks + k;
+        float A[VC], C[VC];
+        load_elements<VC>(A, g.map_a + from * g.channels + at.lane);
+        load_elements<VC>(C, g.map_h + from * g.channels + at.lane);
+        const bool cut = g.map_cut[from];
 #pragma unroll
         for (int v = 0; v < VC; ++v) carry[v] = cut ? C[v] : fmaf(A[v], carry[v], C[v]);
     }
-    const int64_t begin = (int64_t)chunk * g.chunk, end = g.time < begin + g.chunk ? g.time : begin + g.chunk;
-    const int64_t tiles = (end - begin + W * kSteps - 1) / (W * kSteps);
     int turn = 0;
     for (int64_t n = tiles - 1; n >= 0; --n, turn ^= 1) {
         const int64_t t = begin + n * (W * kSteps) + wave * kSteps;
-        float w[kSteps][VC], b[kSteps][VC], d[kSteps][VC], A[VC], C[VC];
-        const Rows rows(g, t, end, (int)batch);
-        load_steps_back<S, T, VC>(w, b, d, g, batch, t, c, in, rows, S == SEMI_LOG || g.da);
+        BackTile<S, T, VC> now = next;
+        if (n > 0) next.load(g, t - W * kSteps, end, at, need_h);
+        now.resolve(g, t, end, at);
+        float A[VC], C[VC], c[VC];
 #pragma unroll
-        for (int v = 0; v < VC; ++v) { A[v] = 1.0f; C[v] = 0.0f; }
-        const bool cut = map_of_back<VC>(A, C, w, d, rows, g, c, in);
+        for (int v = 0; v < VC; ++v) { A[v] = 1.0f; C[v] = 0.0f; c[v] = carry[v]; }
+        if constexpr (W > 1) {
+            const bool cut = now.map(A, C, g, at);
+            maps.put(turn, wave, A, C, cut);
+            lds_barrier();
+            const uint64_t cuts = maps.cuts(turn);
 #pragma unroll
-        for (int v = 0; v < VC; ++v) { sa[turn][wave][lane][v] = A[v]; sc[turn][wave][lane][v] = C[v]; }
-        if (lane == 0) scut[turn][wave] = cut;
-        __syncthreads();
-        float cc[VC];
+            for (int w = W - 1; w >= 0; --w)
 #pragma unroll
-        for (int k = W - 1; k >= 0; --k) {
-            const bool wcut = scut[turn][k];
-#pragma unroll
-            for (int v = 0; v < VC; ++v) {
-                if (k == wave) cc[v] = carry[v];
-                carry[v] = wcut ? sc[turn][k][lane][v] : fmaf(sa[turn][k][lane][v], carry[v], sc[turn][k][lane][v]);
-            }
+                for (int v = 0; v < VC; ++v) {
+                    if (w == wave) c[v] = carry[v];
+                    carry[v] = fmaf(maps.a[turn][w][lane][v], carry[v], maps.h[turn][w][lane][v]);
+                    if (cuts != 0 && (cuts >> w & 1)) carry[v] = maps.h[turn][w][lane][v];
+                }
         }
-        const int64_t at = (batch * g.time + t) * g.channels + c;
-        T* da = static_cast<T*>(g.da) + at;
-        T* dx = static_cast<T*>(g.dx) + at;
+        if (now.rows.plain()) now.template walk<true>(c, g, t, end, at);
+        else now.template walk<false>(c, g, t, end, at);
+        if constexpr (W == 1)
 #pragma unroll
-        for (int i = kSteps - 1; i >= 0; --i) {
-            if (rows.last >> i & 1) load_state<VC>(cc, g.dfinal, rows.sequence(i), g, c, in, 0.0f);
-            float ya[VC], yx[VC];
-            const bool live = rows.live >> i & 1;
-#pragma unroll
-            for (int v = 0; v < VC; ++v) {
-                const float gt = d[i][v] + cc[v];
-                cc[v] = w[i][v] * gt;
-                ya[v] = live ? (S == SEMI_LOG ? cc[v] : gt * b[i][v]) : 0.0f;
-                yx[v] = live ? (S == SEMI_LOG ? gt * b[i][v] : gt) : 0.0f;
-            }
-            if (t + i < end && in) {
-                if (g.da) store_elements<VC>(da + (int64_t)i * g.channels, ya);
-                if (g.dx) store_elements<VC>(dx + (int64_t)i * g.channels, yx);
-                if (g.dinitial && (rows.first >> i & 1)) store_elements<VC>(g.dinitial + rows.sequence(i) * g.channels + c, cc);
-            }
-        }
+            for (int v = 0; v < VC; ++v) carry[v] = c[v];
     }
 }
 

@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace klay {
 
 using f32 = float;
@@ -20,6 +22,71 @@ template <typename T> struct Pieces<T, 1> {
     typedef T Vec;
     typedef T Loose;
 };
+
+// N elements as they are in memory; a single one of 16 bits in a register of its own (two of them packed into one register would make
+// every load wait for the one before it)
+template <typename T, int N> using Raw = std::conditional_t<N == 1 && sizeof(T) == 2, unsigned int, typename Pieces<T, N>::Vec>;
+
+// A stretch of memory that a wave reads or writes row by row: the address is in scalar registers, a lane adds `lane` bytes and a row
+// `row` bytes (a scalar).  A lane with kNoLane reads zeros and writes nothing (the range check of buffer instructions).
+typedef __amdgpu_buffer_rsrc_t Stretch;
+constexpr uint32_t kNoLane = 0xffffffffu, kStretchBytes = 0xf0000000u;
+__device__ __forceinline__ Stretch stretch_at(const void* p) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)kStretchBytes, 0x00020000);
+}
+template <int BYTES> struct Bits;
+template <> struct Bits<2> { typedef unsigned short T; };
+template <> struct Bits<4> { typedef unsigned int T; };
+template <> struct Bits<8> { typedef unsigned int T __attribute__((ext_vector_type(2))); };
+template <> struct Bits<16> { typedef unsigned int T __attribute__((ext_vector_type(4))); };
+
+template <int N, typename T>
+__device__ __forceinline__ Raw<T, N> load_raw(Stretch from, uint32_t lane, uint32_t row) {
+    if constexpr (N * sizeof(T) == 2) return (unsigned int)__builtin_amdgcn_raw_buffer_load_b16(from, lane, row, 0);
+    typename Bits<N * sizeof(T)>::T r;
+    if constexpr (N * sizeof(T) == 4) r = __builtin_amdgcn_raw_buffer_load_b32(from, lane, row, 0);
+    else if constexpr (N * sizeof(T) == 8) r = __builtin_amdgcn_raw_buffer_load_b64(from, lane, row, 0);
+    else if constexpr (N * sizeof(T) == 16) r = __builtin_amdgcn_raw_buffer_load_b128(from, lane, row, 0);
+    if constexpr (N * sizeof(T) > 2) return __builtin_bit_cast(Raw<T, N>, r);
+}
+template <int N, typename T>
+__device__ __forceinline__ void store_row(Stretch to, uint32_t lane, uint32_t row, const float (&x)[N]) {
+    typename Pieces<T, N>::Vec r;
+    if constexpr (N == 1) {
+        r = (T)x[0];
+    } else {
+        typedef float Floats __attribute__((ext_vector_type(N)));
+        Floats f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = x[i];
+        r = __builtin_convertvector(f, typename Pieces<T, N>::Vec);
+    }
+    const auto bits = __builtin_bit_cast(typename Bits<N * sizeof(T)>::T, r);
+    if constexpr (N * sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(bits, to, lane, row, 0);
+    else if constexpr (N * sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(bits, to, lane, row, 0);
+    else if constexpr (N * sizeof(T) == 8) __builtin_amdgcn_raw_buffer_store_b64(bits, to, lane, row, 0);
+    else __builtin_amdgcn_raw_buffer_store_b128(bits, to, lane, row, 0);
+}
+
+template <int N, typename T>
+__device__ __forceinline__ float piece(const Raw<T, N>& r, int v) {
+    if constexpr (N == 1 && sizeof(T) == 2) return (float)__builtin_bit_cast(T, (unsigned short)r);
+    else if constexpr (N == 1) return r;
+    else return (float)r[v];
+}
+template <int N, typename T>
+__device__ __forceinline__ Raw<T, N> all_pieces(float x) {
+    Raw<T, N> r;
+    if constexpr (N == 1 && sizeof(T) == 2) {
+        r = __builtin_bit_cast(unsigned short, (T)x);
+    } else if constexpr (N == 1) {
+        r = x;
+    } else {
+#pragma unroll
+        for (int v = 0; v < N; ++v) r[v] = (T)x;
+    }
+    return r;
+}
 
 template <int N, typename T>
 __device__ __forceinline__ void load_elements(float (&x)[N], const T* p) {

@@ -15,7 +15,7 @@ from . import binding as _b
 from .binding import KLAY_LOG, KLAY_MAXLOG, KLAY_REAL
 
 _DTYPES = {torch.float32: _b.KLAY_F32, torch.bfloat16: _b.KLAY_BF16, torch.float16: _b.KLAY_F16}
-_MOST_TOKENS, _MOST_TOP, _MOST_CHANNELS = 1024, 64, 1 << 30
+_MOST_TOKENS, _MOST_TOP, _MOST_CHANNELS = 1024, 64, 1 << 25
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
@@ -156,7 +156,9 @@ def token_logprobs(logits, tokens=None, *, complement=False, entropy=False, top=
 
 # ---- gated recurrence ---------------------------------------------------------------------------------------------
 def _channels_last(t):
-    return t if t.stride(-1) == 1 or t.shape[-1] == 1 else t.contiguous()
+    """t, or a copy where its channels lie apart (or its time steps further than the kernels reach)"""
+    fits = (t.stride(-1) == 1 or t.shape[-1] == 1) and t.stride(-2) <= _MOST_CHANNELS
+    return t if fits else t.contiguous()
 
 
 def _scan_args(gates, inputs, initial, semiring, offsets, row_info):
@@ -226,7 +228,7 @@ def _check_recurrence(gates, inputs, semiring):
     if semiring != KLAY_REAL and gates.dtype != torch.float32:
         raise ValueError("the log-domain semirings take float32")
     if gates.dim() < 2 or not 1 <= gates.shape[-1] <= _MOST_CHANNELS:
-        raise ValueError("gates must have 1 .. 2^30 channels")
+        raise ValueError("gates must have 1 .. 2^25 channels")
 
 
 def gated_scan(gates, inputs, initial=None, semiring=KLAY_REAL, offsets=None):

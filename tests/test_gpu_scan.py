@@ -82,12 +82,15 @@ def test_shapes(batch, time, channels, semiring, dtype):
     check(a, x, h, semiring, dtype, rng)
 
 
-@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
-@pytest.mark.parametrize("batch,time,channels", [(260, 30, 100), (130, 100, 130), (64, 300, 520), (128, 300, 256)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("batch,time,channels", [(520, 16, 100), (260, 50, 130), (110, 300, 520), (256, 70, 256)])
 def test_two_channels_a_lane(batch, time, channels, dtype):
     rng = np.random.default_rng(channels)
     a, x, h = make((batch, time, channels), batch, REAL, dtype, rng)
     check(a, x, h, REAL, dtype, rng)
+    wide = torch.zeros((batch, time, 2 * channels + 1), dtype=a.dtype, device="cuda")       # the same from odd addresses: one a lane
+    wide[..., 1:channels + 1], wide[..., channels + 1:] = a, x
+    check(a, x, h, REAL, dtype, rng, given=(wide[..., 1:channels + 1], wide[..., channels + 1:]))
 
 
 @pytest.mark.parametrize("semiring", [LOG, MAX])

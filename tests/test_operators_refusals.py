@@ -66,7 +66,7 @@ def test_tokens_outputs_and_workspace():
 
 
 BAD_SCANS = [dict(dtype=7), dict(semiring=3), dict(semiring=-1), dict(semiring=1, dtype=1), dict(semiring=2, dtype=2), dict(channels=0),
-             dict(channels=(1 << 30) + 1), dict(batch=-1), dict(batch=1 << 30), dict(time=-1), dict(time=1 << 31), dict(gates=None),
+             dict(channels=(1 << 25) + 1), dict(gates_time_stride=(1 << 25) + 1), dict(inputs_time_stride=-1), dict(batch=-1), dict(batch=1 << 30), dict(time=-1), dict(time=1 << 31), dict(gates=None),
              dict(offsets=P, row_info=P), dict(offsets=P, batch=1), dict(offsets=P, batch=1, row_info=P, sequences=-1),
              dict(offsets=P, batch=1, row_info=P, sequences=1 << 30)]
 
@@ -100,7 +100,7 @@ def test_scan_outputs_and_workspace():
 
 
 @pytest.mark.parametrize("bad", [dict(dtype=9), dict(semiring=5), dict(semiring=1, dtype=2), dict(rows=-1), dict(rows=1 << 31), dict(channels=0),
-                                 dict(channels=(1 << 30) + 1), dict(gates=None), dict(inputs=None), dict(state=None)])
+                                 dict(channels=(1 << 25) + 1), dict(gates=None), dict(inputs=None), dict(state=None)])
 def test_step_arguments(bad):
     a = dict(dtype=0, semiring=0, device=0, rows=2, channels=4, gates=P, gs=4, inputs=P, xs=4, state=P, ss=4, out=P, os=4)
     a.update(bad)
