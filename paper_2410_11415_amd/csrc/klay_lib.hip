@@ -41,6 +41,9 @@ int dtype_bytes(int32_t t) { return t == KLAY_F32 ? 4 : 2; }
 
 // ---- tokens ---------------------------------------------------------------------------------------------------------
 constexpr int32_t kShortRow = 512, kShortestRow = 64;   // rows in the registers of a wave, of a quarter of one
+// Up to this many bytes a row is a single wave's where there are rows enough (us, four waves / one: 8192 x 8192 bf16 forward 38 / 30,
+// 16384 x 1000 bf16 45 / 19; 4096 x 32768 bf16 48 / 51, backward 112 / 150).
+constexpr int64_t kWaveRow = 16384;
 
 klay_status check_tokens(const klay_tokens_args* a, const char* who) {
     const std::string name(who);
@@ -92,6 +95,8 @@ klay::TokenArgs token_args(const klay_tokens_args* a) {
 
 int32_t capped_grid(int64_t units) { return (int32_t)std::min<int64_t>(units, 1 << 20); }
 
+template <typename T> bool one_wave(const klay::TokenArgs& g) { return g.parts == 1 && g.vocab * (int64_t)sizeof(T) <= kWaveRow; }
+
 template <typename T, bool ENT, bool TOP>
 klay_status run_tokens(const klay::TokenArgs& g, void* stream) {
     const dim3 block(klay::kTokBlock);
@@ -102,7 +107,8 @@ klay_status run_tokens(const klay::TokenArgs& g, void* stream) {
         else KLAY_LAUNCH((klay::token_short_kernel<T, 64, 8, ENT, TOP>), grid, block, stream, g);
         return KLAY_OK;
     }
-    KLAY_LAUNCH((klay::token_row_kernel<T, ENT, TOP>), dim3(capped_grid(g.rows * g.parts)), block, stream, g);
+    if (one_wave<T>(g)) KLAY_LAUNCH((klay::token_row_kernel<T, ENT, TOP, 64>), dim3(capped_grid(g.rows)), dim3(64), stream, g);
+    else KLAY_LAUNCH((klay::token_row_kernel<T, ENT, TOP, klay::kTokBlock>), dim3(capped_grid(g.rows * g.parts)), block, stream, g);
     if (g.parts > 1) KLAY_LAUNCH((klay::token_join_kernel<T, TOP>), dim3((uint32_t)g.rows), block, stream, g);
     return KLAY_OK;
 }
@@ -123,7 +129,8 @@ klay_status run_tokens_back(const klay::TokenArgs& g, void* stream) {
         else KLAY_LAUNCH((klay::token_back_short_kernel<T, 64, 8>), grid, block, stream, g);
         return KLAY_OK;
     }
-    KLAY_LAUNCH((klay::token_back_kernel<T>), dim3(capped_grid(g.rows * g.parts)), block, stream, g);
+    if (one_wave<T>(g)) KLAY_LAUNCH((klay::token_back_kernel<T, 64>), dim3(capped_grid(g.rows)), dim3(64), stream, g);
+    else KLAY_LAUNCH((klay::token_back_kernel<T, klay::kTokBlock>), dim3(capped_grid(g.rows * g.parts)), block, stream, g);
     return KLAY_OK;
 }
 

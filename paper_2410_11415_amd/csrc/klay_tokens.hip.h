@@ -20,7 +20,7 @@
 
 namespace klay {
 
-constexpr int kTokBlock = 256;              // threads per row part
+constexpr int kTokBlock = 256;              // threads of a workgroup: of a row part (64: one wave, for rows that four would not keep busy)
 constexpr int kMaxTop = 64, kMaxTokens = 1024;
 constexpr float kSlack = 8.0f;
 constexpr float kTokLog2e = 1.4426950408889634f, kTokLn2 = 0.6931471805599453f, kTokFltMax = 3.402823466e+38f;
@@ -127,26 +127,32 @@ template <int G> __device__ __forceinline__ float group_sum(float x) {
     return x;
 }
 // All threads get the result; `at` is scratch that no earlier call since the last barrier has used.
-__device__ __forceinline__ float block_max(float x, float* at) {
+template <int THREADS> __device__ __forceinline__ float block_max(float x, float* at) {
     x = group_max<64>(x);
+    if constexpr (THREADS == 64) return x;
     if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = x;
     __syncthreads();
     return fmaxf(fmaxf(at[0], at[1]), fmaxf(at[2], at[3]));
 }
-__device__ __forceinline__ void block_sum2(float& x, float& y, float* at) {
+template <int THREADS> __device__ __forceinline__ void block_sum2(float& x, float& y, float* at) {
     x = group_sum<64>(x);
     y = group_sum<64>(y);
+    if constexpr (THREADS == 64) return;
     if ((threadIdx.x & 63) == 0) { at[threadIdx.x >> 6] = x; at[4 + (threadIdx.x >> 6)] = y; }
     __syncthreads();
     x = (at[0] + at[1]) + (at[2] + at[3]);
     y = (at[4] + at[5]) + (at[6] + at[7]);
 }
 
-// One thread's run over its elements.
-template <bool ENT, bool TOP>
+// One thread's run over its elements.  y = (x - ref) log2 e is one multiply-add, x log2 e - shift with shift = ref log2 e rounded once: what that
+// rounding puts into the terms it also puts into `shift`, relative to which the sums are read (term).  WIDE takes the difference first, for rows whose maximum
+// is so far from 0 that the product would leave the range of fp32 (a row of nothing but the type's lowest value, for one).
+constexpr float kFar = 2e38f;
+template <bool ENT, bool TOP, bool WIDE = false>
 struct Run {
-    float ref = -kTokFltMax, s = 0.0f, t = 0.0f, max = -INFINITY;
+    float ref = WIDE ? -kTokFltMax : -kFar, shift = -kFar * kTokLog2e, s = 0.0f, t = 0.0f, max = -INFINITY;
     int32_t where = -1;           // first element of the vector that holds the maximum
+    __device__ __forceinline__ float term(float x) const { return WIDE ? (x - ref) * kTokLog2e : fmaf(x, kTokLog2e, -shift); }
     template <int N> __device__ __forceinline__ void take(const float (&x)[N], int32_t base) {
         float top = x[0];
 #pragma unroll
@@ -154,49 +160,114 @@ struct Run {
         if constexpr (TOP) where = top > max || where < 0 ? base : where;
         max = fmaxf(max, top);
         if (top > ref + kSlack) {
-            const float to = fmaxf(top, -kTokFltMax);
-            const float d = (to - ref) * kTokLog2e, f = exp2_of(-d);
+#pragma clang fp contract(off)
+            const float to = WIDE ? fmaxf(top, -kTokFltMax) : __builtin_amdgcn_fmed3f(top, -kFar, kFar);
+            const float next = to * kTokLog2e;              // rounded by itself: the terms to come are taken relative to it
+            const float d = WIDE ? (to - ref) * kTokLog2e : next - shift;
+            const float f = exp2_of(-d);
             if constexpr (ENT) t = f > 0.0f ? f * (t - d * s) : 0.0f;
             s *= f;
             ref = to;
+            shift = next;
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float y = (x[i] - ref) * kTokLog2e, e = exp2_of(y);
+            const float y = term(x[i]), e = exp2_of(y);
             s += e;
             if constexpr (ENT) t = fmaf(e, fmaxf(y, -200.0f), t);       // (no term of -inf: 0 times infinity)
         }
     }
 };
 
-// The N elements of thread `thread`'s vector number i in a part that starts at lo.
-template <int N> __device__ __forceinline__ int32_t vector_at(int32_t lo, int32_t i, int32_t thread) { return lo + (i * kTokBlock + thread) * N; }
-
-constexpr int kKeysRoom = kTokBlock * 8 + 256;      // candidates of one round on top of those kept before
-
-struct TopShared {
-    uint64_t keys[kKeysRoom];
-    uint64_t best[kMaxTop];
-    uint64_t column[kTokBlock];
-    int32_t chosen[kMaxTop];
-    uint64_t limit;
-    int32_t count;
+// How the THREADS threads of a workgroup share the elements [lo, hi) of a row: single ones up to the first multiple of 16 bytes (at `p`, element lo), one
+// a thread; vectors of N from `begin` to `full`, thread after thread; single ones behind.  (Vectors from odd addresses on: 4096 x 32771 bf16
+// read at 4.5 TB/s instead of 5.5.)
+template <int N, int THREADS> struct Share {
+    int32_t lo, begin, full, hi, vectors;
+    template <typename T> __device__ __forceinline__ Share(const T* p, int32_t from, int32_t to) {
+        lo = from;
+        hi = to;
+        const int32_t head = (int32_t)((0 - reinterpret_cast<uintptr_t>(p)) & 15) / (int32_t)sizeof(T);
+        begin = from + (head < to - from ? head : to - from);
+        vectors = (to - begin) / N;
+        full = begin + vectors * N;
+    }
+    __device__ __forceinline__ int32_t head() const { return begin - lo; }
+    __device__ __forceinline__ int32_t tail() const { return hi - full; }
+    __device__ __forceinline__ int32_t at(int32_t i, int32_t thread) const { return begin + (i * THREADS + thread) * N; }
+    __device__ __forceinline__ bool in_vector(int32_t j) const { return j >= begin && j < full; }
 };
 
-// Sorts the `top` largest of keys[0 .. count) into best (0 where there are fewer), and leaves them as the only ones in keys.
-__device__ __forceinline__ void keep_best(TopShared& sh, int32_t top) {
-    const int32_t n = sh.count, tid = threadIdx.x;
-    for (int32_t i = tid; i < top; i += kTokBlock) sh.best[i] = 0;
+// Rank of a lane's key among those of its wave (equal ones by their lane).
+__device__ __forceinline__ int32_t rank_in_wave(uint64_t key) {
+    const int32_t lane = threadIdx.x & 63;
+    const uint32_t lo = (uint32_t)key, hi = (uint32_t)(key >> 32);
+    int32_t rank = 0;
+#pragma unroll 16
+    for (int j = 0; j < 64; ++j) {
+        const uint64_t other = (uint64_t)__builtin_amdgcn_readlane(hi, j) << 32 | (uint32_t)__builtin_amdgcn_readlane(lo, j);
+        rank += other > key || (other == key && j < lane);
+    }
+    return rank;
+}
+
+// The first `columns` threads hold the largest key of a column each (or one not above it).  Of the full waves among them the one of
+// rank top / waves has as many above it, so the least of these is reached by `top` keys or more: a lower bound of the top-th largest key (0 where there
+// are too few columns to tell).  Ends with a barrier behind it.
+__device__ __forceinline__ uint64_t bound_of_columns(uint64_t mine, int32_t columns, int32_t top, uint64_t* quota) {
+    const int32_t wave = threadIdx.x >> 6;
+    const int32_t waves = columns < 128 ? 1 : columns >> 6, each = (top + waves - 1) / waves;
+    if (wave < waves && rank_in_wave(mine) == each - 1) quota[wave] = mine;
     __syncthreads();
-    for (int32_t i = tid; i < n; i += kTokBlock) {
+    uint64_t limit = quota[0];
+    for (int w = 1; w < waves; ++w) limit = quota[w] < limit ? quota[w] : limit;
+    return limit;
+}
+
+template <int THREADS> struct TopShared {
+    static constexpr int kRoom = THREADS * 8 + 256;       // candidates of one round on top of those kept before
+    uint64_t keys[kRoom];
+    uint64_t best[kMaxTop];
+    uint64_t quota[THREADS / 64], quota_again[THREADS / 64];
+    int32_t chosen[THREADS];
+    uint64_t limit;
+    int32_t count, columns;
+};
+
+// Sorts the `top` largest of keys[0 .. count) into best (0 where there are fewer).  `again`: leaves them as the only ones in keys.
+template <int THREADS>
+__device__ __forceinline__ void keep_best(TopShared<THREADS>& sh, int32_t top, bool again) {
+    const int32_t tid = threadIdx.x;
+    int32_t n = sh.count;
+    if (n > 256) {            // most of them are out after one look at the columns of keys[tid + 256 j]
+        constexpr int kEach = (TopShared<THREADS>::kRoom + THREADS - 1) / THREADS;
+        uint64_t mine[kEach], most = 0;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            mine[j] = tid + j * THREADS < n ? sh.keys[tid + j * THREADS] : 0;
+            most = mine[j] > most ? mine[j] : most;
+        }
+        const uint64_t limit = bound_of_columns(most, THREADS, top, sh.quota_again);
+        if (tid == 0) sh.count = 0;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+            if (mine[j] != 0 && mine[j] >= limit) sh.keys[atomicAdd(&sh.count, 1)] = mine[j];
+        __syncthreads();
+        n = sh.count;
+    }
+    for (int32_t i = tid; i < n; i += THREADS) {
         const uint64_t mine = sh.keys[i];
         int32_t rank = 0;
+#pragma unroll 4
         for (int32_t j = 0; j < n; ++j) rank += sh.keys[j] > mine;
         if (rank < top) sh.best[rank] = mine;
     }
+    if (n + tid < top) sh.best[n + tid] = 0;
     __syncthreads();
+    if (!again) return;
     const int32_t kept = n < top ? n : top;
-    for (int32_t i = tid; i < kept; i += kTokBlock) sh.keys[i] = sh.best[i];
+    for (int32_t i = tid; i < kept; i += THREADS) sh.keys[i] = sh.best[i];
     if (tid == 0) {
         sh.count = kept;
         if (n >= top && sh.best[top - 1] > sh.limit) sh.limit = sh.best[top - 1];
@@ -204,32 +275,33 @@ __device__ __forceinline__ void keep_best(TopShared& sh, int32_t top) {
     __syncthreads();
 }
 
-// The `top` largest elements of [lo, hi).  The threads' own maxima are given (column); the top-th largest of them is a lower bound
-// of what is sought, and only the columns of the threads above it hold anything that reaches it: those are read again (from the
-// cache), whatever the order of the logits.
-template <typename T, int N>
-__device__ __forceinline__ void top_of_part(TopShared& sh, const T* row, int32_t lo, int32_t hi, uint64_t mine, int32_t top) {
+// The `top` largest elements of [lo, hi).  A thread's own maximum as a key lies between its `low` and its `high`.  Only the columns of threads whose
+// `high` reaches the bound that the `low` give hold anything that does: those are read again (from the cache).
+// However the logits are ordered, a round adds at most 2048 keys, and more than 256 of them are cut to the best ones before the next.
+template <typename T, int N, int THREADS>
+__device__ __forceinline__ void top_of_part(TopShared<THREADS>& sh, const T* row, const Share<N, THREADS>& share, uint64_t low, uint64_t high,
+                                            int32_t top) {
     const int32_t tid = threadIdx.x;
-    const int32_t vectors = (hi - lo) / N, full = lo + vectors * N;
-    sh.column[tid] = mine;
-    if (tid == 0) { sh.limit = 0; sh.count = 0; }
+    if (tid == 0) sh.count = sh.columns = 0;
+    const int32_t singles = share.head() > share.tail() ? share.head() : share.tail();
+    const int32_t columns_in_use = share.vectors >= THREADS ? THREADS : share.vectors > singles ? share.vectors : singles;
+    uint64_t limit = bound_of_columns(low, columns_in_use, top, sh.quota);
+    if (tid == 0) sh.limit = limit;
+    if (high != 0 && high >= limit) sh.chosen[atomicAdd(&sh.columns, 1)] = tid;
     __syncthreads();
-    int32_t rank = 0;
-    for (int32_t j = 0; j < kTokBlock; ++j) {
-        const uint64_t other = sh.column[j];
-        rank += other > mine || (other == mine && j < tid);
+    const int32_t columns = sh.columns;
+    const int32_t deep = (share.vectors + THREADS - 1) / THREADS, work = columns * deep;
+    if (tid < share.head() + share.tail()) {             // the single ones
+        const int32_t j = tid < share.head() ? share.lo + tid : share.full + tid - share.head();
+        const uint64_t key = order_key((float)row[j], (uint32_t)j);
+        if (key >= limit) sh.keys[atomicAdd(&sh.count, 1)] = key;
     }
-    if (rank < top) sh.chosen[rank] = tid;
-    if (rank == top - 1) sh.limit = mine;
-    __syncthreads();
-    const int32_t columns = top < kTokBlock ? top : kTokBlock;
-    const int32_t deep = (vectors + kTokBlock - 1) / kTokBlock, work = columns * deep;
-    for (int32_t w0 = 0; w0 < work + kTokBlock; w0 += kTokBlock) {
-        const uint64_t limit = sh.limit;
+    for (int32_t w0 = 0; w0 < work; w0 += THREADS) {
+        limit = sh.limit;
         const int32_t w = w0 + tid;
         if (w < work) {
-            const int32_t i = w / columns, base = vector_at<N>(lo, i, sh.chosen[w - i * columns]);
-            if (base < full) {
+            const int32_t i = w / columns, base = share.at(i, sh.chosen[w - i * columns]);
+            if (base < share.full) {
                 float x[N];
                 load_elements<N>(x, row + base);
 #pragma unroll
@@ -238,109 +310,155 @@ __device__ __forceinline__ void top_of_part(TopShared& sh, const T* row, int32_t
                     if (key >= limit) sh.keys[atomicAdd(&sh.count, 1)] = key;
                 }
             }
-        } else if (w0 >= work && full + tid < hi) {          // the last round: what is left behind the full vectors
-            const uint64_t key = order_key((float)row[full + tid], (uint32_t)(full + tid));
-            if (key >= limit) sh.keys[atomicAdd(&sh.count, 1)] = key;
         }
         __syncthreads();
+        if (w0 + THREADS >= work) break;
         const bool many = sh.count > 256;
         __syncthreads();
-        if (many) keep_best(sh, top);
+        if (many) keep_best(sh, top, true);
     }
-    keep_best(sh, top);
+    __syncthreads();
+    keep_best(sh, top, false);
 }
 
-// A workgroup per row part.  parts == 1: everything is written here; otherwise the part's sums and its best elements, for join_kernel.
-template <typename T, bool ENT, bool TOP>
-__global__ void __launch_bounds__(kTokBlock) token_row_kernel(TokenArgs g) {
+// What a workgroup finds out about the elements [lo, hi) of a row.
+struct PartSums {
+    float max, sum, rest, weighted;     // sum = 1 + rest, as far as fp32 tells
+};
+template <typename T, bool ENT, bool TOP, int THREADS, bool WIDE>
+__device__ __forceinline__ PartSums sums_of_part(const T* row, const Share<16 / sizeof(T), THREADS>& share, float* scratch, int32_t* owner,
+                                                 uint64_t* low, uint64_t* high) {
     constexpr int N = 16 / sizeof(T), U = 4;
+    const int32_t tid = threadIdx.x, vectors = share.vectors;
+    if (tid == 0) *owner = THREADS;
+    Run<ENT, TOP, WIDE> run;
+    if (tid < share.head()) {
+        const float x[1] = {(float)row[share.lo + tid]};
+        run.take(x, share.lo + tid);
+    }
+    int32_t i = 0;
+    if (U * THREADS <= vectors) {
+        // U vectors a step, the next step's on their way meanwhile
+        Raw<T, N> next[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) next[u] = stream_raw<N>(row + share.at(u, tid));
+        for (;;) {
+            Raw<T, N> now[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) now[u] = next[u];
+            const int32_t at = i;
+            i += U;
+            const bool more = (i + U) * THREADS <= vectors;
+            if (more) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) next[u] = stream_raw<N>(row + share.at(i + u, tid));
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float x[N];
+#pragma unroll
+                for (int q = 0; q < N; ++q) x[q] = piece<N, T>(now[u], q);
+                run.take(x, share.at(at + u, tid));
+            }
+            if (!more) break;
+        }
+    }
+    for (; i * THREADS + tid < vectors; ++i) {
+        float x[N];
+        load_elements<N>(x, row + share.at(i, tid));
+        run.take(x, share.at(i, tid));
+    }
+    if (tid < share.tail()) {
+        const float x[1] = {(float)row[share.full + tid]};
+        run.take(x, share.full + tid);
+    }
+
+    PartSums p;
+    p.max = block_max<THREADS>(run.max, scratch);
+    const float to = fmaxf(p.max, -kTokFltMax);
+    const float d = run.term(to), f = exp2_of(-d);
+    float s = run.s, t = 0.0f;
+    if (s > 0.0f) {                 // (a thread without terms, or one with a NaN, stays as it is)
+        t = ENT && f > 0.0f ? f * (run.t - d * s) : 0.0f;
+        s *= f;
+    }
+    p.sum = s;
+    p.weighted = t;
+    block_sum2<THREADS>(p.sum, p.weighted, scratch + 8);
+    p.rest = p.sum == 0.0f ? 0.0f : p.sum - 1.0f;
+    if (p.sum > 0.0f && p.sum < 1.5f) {
+        // One element holds most of the sum: `sum - 1` would keep little of the others.  Its thread's terms are taken again, without it.
+        if (run.max == p.max) atomicMin(owner, tid);
+        __syncthreads();
+        const int32_t who = *owner;
+        if (tid == who) s = t = 0.0f;
+        const int32_t deep = (vectors - who + THREADS - 1) / THREADS;       // its vectors (none for a thread behind them)
+        for (int32_t v = tid; v < deep; v += THREADS) {
+            float x[N];
+            load_elements<N>(x, row + share.at(v, who));
+#pragma unroll
+            for (int q = 0; q < N; ++q) {
+                const float y = (x[q] - to) * kTokLog2e, e = x[q] == p.max ? 0.0f : exp2_of(y);
+                s += e;
+                t = fmaf(e, fmaxf(y, -200.0f), t);
+            }
+        }
+        if (tid < 2) {              // and its single ones
+            const int32_t j = tid == 0 ? share.lo + who : share.full + who;
+            if (who < (tid == 0 ? share.head() : share.tail()) && (float)row[j] != p.max) {
+                const float y = ((float)row[j] - to) * kTokLog2e, e = exp2_of(y);
+                s += e;
+                t = fmaf(e, fmaxf(y, -200.0f), t);
+            }
+        }
+        p.rest = s;
+        p.weighted = t;
+        block_sum2<THREADS>(p.rest, p.weighted, scratch + 16);
+    }
+    if constexpr (TOP) {
+        // the thread's largest element as a key lies between these two (the vector is known, the place in it is not)
+        *low = *high = 0;
+        if (run.where >= 0) {
+            const int32_t last = share.in_vector(run.where) ? run.where + N - 1 : run.where;
+            *high = order_key(run.max, (uint32_t)run.where);
+            *low = order_key(run.max, (uint32_t)last);
+        }
+    }
+    return p;
+}
+
+// A workgroup per row part.  parts == 1: everything is written here; otherwise the part's sums and its best elements, for the join kernel.
+template <typename T, bool ENT, bool TOP, int THREADS>
+__global__ void __launch_bounds__(THREADS) token_row_kernel(TokenArgs g) {
+    constexpr int N = 16 / sizeof(T);
     __shared__ float scratch[32];
     __shared__ int32_t owner;
-    __shared__ std::conditional_t<TOP, TopShared, int> tops;
+    __shared__ std::conditional_t<TOP, TopShared<THREADS>, int> tops;
     const int32_t tid = threadIdx.x;
     for (int64_t unit = blockIdx.x; unit < g.rows * g.parts; unit += gridDim.x) {
         const int64_t r = unit / g.parts;
         const int32_t part = (int32_t)(unit - r * g.parts);
         const T* row = static_cast<const T*>(g.logits) + g.logit_rows.at(r);
         const int32_t lo = part * g.part, hi = g.vocab - lo < g.part ? g.vocab : lo + g.part;
-        const int32_t vectors = (hi - lo) / N, full = lo + vectors * N;
-        if (tid == 0) owner = kTokBlock;
-        Run<ENT, TOP> run;
-        int32_t i = 0;
-        for (; (i + U) * kTokBlock <= vectors; i += U) {
-            float x[U][N];
-#pragma unroll
-            for (int u = 0; u < U; ++u) load_elements<N>(x[u], row + vector_at<N>(lo, i + u, tid));
-#pragma unroll
-            for (int u = 0; u < U; ++u) run.take(x[u], vector_at<N>(lo, i + u, tid));
-        }
-        for (; i * kTokBlock + tid < vectors; ++i) {
-            float x[N];
-            load_elements<N>(x, row + vector_at<N>(lo, i, tid));
-            run.take(x, vector_at<N>(lo, i, tid));
-        }
-        if (full + tid < hi) {
-            const float x[1] = {(float)row[full + tid]};
-            run.take(x, full + tid);
-        }
-
-        const float max = block_max(run.max, scratch);
-        const float to = fmaxf(max, -kTokFltMax);
-        const float d = (to - run.ref) * kTokLog2e, f = exp2_of(-d);
-        float s = run.s * f, t = ENT && f > 0.0f ? f * (run.t - d * run.s) : 0.0f;
-        if (run.s != run.s) s = run.s;
-        float sum = s, weighted = t;
-        block_sum2(sum, weighted, scratch + 8);
-        float rest = sum - 1.0f;
-        if (sum > 0.0f && sum < 1.5f) {
-            // One element holds most of the sum: `sum - 1` would keep little of the others.  Its thread's terms are taken again, without it.
-            if (run.max == max) atomicMin(&owner, tid);
+        const Share<N, THREADS> share(row + lo, lo, hi);
+        uint64_t low = 0, high = 0;
+        PartSums p = sums_of_part<T, ENT, TOP, THREADS, false>(row, share, scratch, &owner, &low, &high);
+        if (fabsf(p.max) > 0.5f * kFar && fabsf(p.max) < INFINITY) {
             __syncthreads();
-            const int32_t who = owner;
-            if (tid == who) s = t = 0.0f;
-            const int32_t deep = (vectors - who + kTokBlock - 1) / kTokBlock;       // its vectors (none for a thread behind them)
-            for (int32_t v = tid; v < deep; v += kTokBlock) {
-                float x[N];
-                load_elements<N>(x, row + vector_at<N>(lo, v, who));
-#pragma unroll
-                for (int q = 0; q < N; ++q) {
-                    const float y = (x[q] - to) * kTokLog2e, e = x[q] == max ? 0.0f : exp2_of(y);
-                    s += e;
-                    t = fmaf(e, fmaxf(y, -200.0f), t);
-                }
-            }
-            if (tid == 0 && full + who < hi && (float)row[full + who] != max) {
-                const float y = ((float)row[full + who] - to) * kTokLog2e, e = exp2_of(y);
-                s += e;
-                t = fmaf(e, fmaxf(y, -200.0f), t);
-            }
-            rest = s;
-            weighted = t;
-            block_sum2(rest, weighted, scratch + 16);
+            p = sums_of_part<T, ENT, TOP, THREADS, true>(row, share, scratch, &owner, &low, &high);
         }
-        if (sum == 0.0f) rest = 0.0f;
-        const RowSums sums{max, rest, weighted};
-        if constexpr (TOP) {
-            uint64_t mine = 0;
-            if (run.where >= 0) {
-                const int32_t n = run.where < full ? N : 1;
-                for (int32_t q = 0; q < n; ++q) {
-                    const uint64_t key = order_key((float)row[run.where + q], (uint32_t)(run.where + q));
-                    mine = key > mine ? key : mine;
-                }
-            }
-            top_of_part<T, N>(tops, row, lo, hi, mine, g.top);
-        }
+        const RowSums sums{p.max, p.rest, p.weighted};
+        if constexpr (TOP) top_of_part<T, N, THREADS>(tops, row, share, low, high, g.top);
         if (g.parts == 1) {
             const float log_sum = row_log_sum(sums);
-            for (int32_t k = tid; k < g.num_tokens; k += kTokBlock) write_token<T>(g, row, r, k, sums, log_sum);
+            for (int32_t k = tid; k < g.num_tokens; k += THREADS) write_token<T>(g, row, r, k, sums, log_sum);
             if (tid == 0) write_row(g, r, sums, log_sum);
             if constexpr (TOP)
-                if (tid < g.top) write_top(g, r, tid, tops.best[tid], max, log_sum);
+                if (tid < g.top) write_top(g, r, tid, tops.best[tid], p.max, log_sum);
         } else {
             if (tid == 0) {
-                float* p = g.partial + unit * 4;
-                p[0] = max; p[1] = rest; p[2] = weighted;
+                float* to = g.partial + unit * 4;
+                to[0] = p.max; to[1] = p.rest; to[2] = p.weighted;
             }
             if constexpr (TOP)
                 if (tid < g.top) g.lists[unit * g.top + tid] = tops.best[tid];
@@ -356,20 +474,20 @@ template <typename T, bool TOP>
 __global__ void __launch_bounds__(kTokBlock) token_join_kernel(TokenArgs g) {
     __shared__ float scratch[32];
     __shared__ int32_t owner;
-    __shared__ uint64_t keys[TOP ? kMaxParts * kMaxTop : 1], best[TOP ? kMaxTop : 1], heads[TOP ? kMaxParts : 1];
-    __shared__ uint64_t limit;
+    constexpr int kEach = kMaxParts * kMaxTop / kTokBlock;
+    __shared__ uint64_t keys[TOP ? kMaxParts * kMaxTop : 1], best[TOP ? kMaxTop : 1], quota[kTokBlock / 64];
     __shared__ int32_t count;
     const int32_t tid = threadIdx.x, parts = g.parts;
     const int64_t r = blockIdx.x;
     const T* row = static_cast<const T*>(g.logits) + g.logit_rows.at(r);
-    if (tid == 0) { owner = kMaxParts; limit = 0; count = 0; }
+    if (tid == 0) { owner = kMaxParts; count = 0; }
     float m = -INFINITY, rest = 0.0f, weighted = 0.0f;
     if (tid < parts) {
         const float* p = g.partial + (r * parts + tid) * 4;
         m = p[0]; rest = p[1]; weighted = p[2];
     }
     const bool none = m == -INFINITY && rest == 0.0f;
-    const float max = block_max(m, scratch);
+    const float max = block_max<kTokBlock>(m, scratch);
     if (tid < parts && m == max) atomicMin(&owner, tid);
     __syncthreads();
     // the part that holds the maximum keeps its R; the others bring their own maximum's term along
@@ -381,36 +499,24 @@ __global__ void __launch_bounds__(kTokBlock) token_join_kernel(TokenArgs g) {
         t = !none && f > 0.0f ? f * (weighted - d * whole) : 0.0f;
         if (rest != rest) s = rest;
     }
-    block_sum2(s, t, scratch + 8);
+    block_sum2<kTokBlock>(s, t, scratch + 8);
     const RowSums sums{max, s, t};
     const float log_sum = row_log_sum(sums);
     for (int32_t k = tid; k < g.num_tokens; k += kTokBlock) write_token<T>(g, row, r, k, sums, log_sum);
     if (tid == 0) write_row(g, r, sums, log_sum);
     if constexpr (TOP) {
-        // The lists are sorted.  Of the lists' j-th elements the q-th largest, q j >= top, is a lower bound of what is sought.
-        const int32_t top = g.top;
-        int32_t j = 1;
-        while (j * parts < 2 * top && j < top) j *= 2;
-        if (j > top) j = top;
-        const int32_t q = (top + j - 1) / j;
-        const uint64_t* lists = g.lists + r * parts * top;
-        uint64_t head = 0;
-        if (tid < parts) {
-            head = lists[tid * top + j - 1];
-            heads[tid] = head;
+        const int32_t top = g.top, all = parts * top;
+        const uint64_t* lists = g.lists + r * all;
+        uint64_t mine[kEach], most = 0;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            mine[j] = tid + j * kTokBlock < all ? lists[tid + j * kTokBlock] : 0;
+            most = mine[j] > most ? mine[j] : most;
         }
-        __syncthreads();
-        if (tid < parts) {
-            int32_t rank = 0;
-            for (int32_t p = 0; p < parts; ++p) rank += heads[p] > head || (heads[p] == head && p < tid);
-            if (rank == q - 1) limit = head;
-        }
-        __syncthreads();
-        const uint64_t least = limit;
-        for (int32_t p = tid; p < parts * top; p += kTokBlock) {
-            const uint64_t key = lists[p];
-            if (key != 0 && key >= least) keys[atomicAdd(&count, 1)] = key;
-        }
+        const uint64_t limit = bound_of_columns(most, all < kTokBlock ? all : kTokBlock, top, quota);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+            if (mine[j] != 0 && mine[j] >= limit) keys[atomicAdd(&count, 1)] = mine[j];
         __syncthreads();
         const int32_t n = count;
         for (int32_t p = tid; p < n; p += kTokBlock) {
@@ -542,8 +648,8 @@ __device__ __forceinline__ BulkGrad bulk_grad(const RowStats& s, float others, f
 }
 
 // A workgroup per row part, as forward.
-template <typename T>
-__global__ void __launch_bounds__(kTokBlock) token_back_kernel(TokenArgs g) {
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS) token_back_kernel(TokenArgs g) {
     constexpr int N = 16 / sizeof(T);
     __shared__ TokenGrad grads[kMaxTokens];
     __shared__ float scratch[16];
@@ -554,33 +660,40 @@ __global__ void __launch_bounds__(kTokBlock) token_back_kernel(TokenArgs g) {
         const T* row = static_cast<const T*>(g.logits) + g.logit_rows.at(r);
         T* out = static_cast<T*>(g.dlogits) + r * g.vocab;
         const int32_t lo = part * g.part, hi = g.vocab - lo < g.part ? g.vocab : lo + g.part;
-        const int32_t vectors = (hi - lo) / N, full = lo + vectors * N;
+        const Share<N, THREADS> share(out + lo, lo, hi);
         const RowStats s = g.stats[r];
         float others = 0.0f, asked = 0.0f;
-        for (int32_t k = tid; k < K; k += kTokBlock) {
+        for (int32_t k = tid; k < K; k += THREADS) {
             const TokenGrad t = token_grad<T>(g, row, r, k, s);
             grads[k] = t;
             others += t.others;
             asked += t.token >= 0 || t.others != t.others ? 1.0f : 0.0f;
         }
-        block_sum2(others, asked, scratch);
+        block_sum2<THREADS>(others, asked, scratch);
         const float h = g.dentropy ? g.dentropy[r] : 0.0f;
         // a row that nothing was asked of, or that allows nothing, has no gradient, and is not read (it may hold anything)
         const bool live = s.max != -INFINITY && (asked > 0.0f || h != 0.0f);
         const BulkGrad bulk = bulk_grad(s, others, h);
-        for (int32_t i = tid; i < vectors; i += kTokBlock) {
-            float x[N] = {};
-            if (live) {
-                load_elements<N>(x, row + lo + i * N);
+        if (live) {
+            for (int32_t i = 0; i * THREADS + tid < share.vectors; ++i) {
+                const int32_t j = share.at(i, tid);
+                const Raw<T, N> from = stream_raw<N>(row + j);
+                float x[N];
 #pragma unroll
-                for (int q = 0; q < N; ++q) x[q] = bulk.at(x[q]);
+                for (int q = 0; q < N; ++q) x[q] = bulk.at(piece<N, T>(from, q));
+                stream_elements<N>(out + j, x);
             }
-            store_elements<N>(out + lo + i * N, x);
+            if (tid < share.head()) out[share.lo + tid] = (T)bulk.at((float)row[share.lo + tid]);
+            if (tid < share.tail()) out[share.full + tid] = (T)bulk.at((float)row[share.full + tid]);
+        } else {
+            const float zeros[N] = {};
+            for (int32_t i = 0; i * THREADS + tid < share.vectors; ++i) stream_elements<N>(out + share.at(i, tid), zeros);
+            if (tid < share.head()) out[share.lo + tid] = (T)0.0f;
+            if (tid < share.tail()) out[share.full + tid] = (T)0.0f;
         }
-        if (full + tid < hi) out[full + tid] = (T)(live ? bulk.at((float)row[full + tid]) : 0.0f);
         __syncthreads();            // the entries of the tokens are written once more
         if (live) {
-            for (int32_t k = tid; k < K; k += kTokBlock) {
+            for (int32_t k = tid; k < K; k += THREADS) {
                 const int32_t j = grads[k].token;
                 if (j < lo || j >= hi) continue;
                 float itself = 0.0f, rest = 0.0f;
