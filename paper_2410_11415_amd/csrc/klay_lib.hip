@@ -44,6 +44,7 @@ constexpr int32_t kShortRow = 512, kShortestRow = 64;   // rows in the registers
 // Up to this many bytes a row is a single wave's where there are rows enough (us, four waves / one: 8192 x 8192 bf16 forward 38 / 30,
 // 16384 x 1000 bf16 45 / 19; 4096 x 32768 bf16 48 / 51, backward 112 / 150).
 constexpr int64_t kWaveRow = 16384;
+constexpr int64_t kManyRows = 2 * kComputeUnits;        // workgroups that keep the chip busy by themselves
 
 klay_status check_tokens(const klay_tokens_args* a, const char* who) {
     const std::string name(who);
@@ -62,19 +63,37 @@ klay_status check_tokens(const klay_tokens_args* a, const char* who) {
     return KLAY_OK;
 }
 
-// Workgroups per row: one where the rows alone give the chip four workgroups per CU, else so many that they do, each with eight
-// kilobytes of the row or more.
-void token_parts(const klay_tokens_args* a, int32_t* parts, int32_t* part) {
-    const int64_t round = (int64_t)klay::kTokBlock * (16 / dtype_bytes(a->dtype));       // elements that a workgroup takes at a time
-    int64_t n = 1;
-    if (a->rows < 4 * kComputeUnits && a->vocab > kShortRow) {
-        n = std::min<int64_t>((4 * kComputeUnits + a->rows - 1) / a->rows, klay::kMaxParts);
-        n = std::min<int64_t>(n, (a->vocab + 2 * round - 1) / (2 * round));
-    }
-    int64_t size = (a->vocab + n - 1) / n;
-    if (n > 1) size = (size + round - 1) / round * round;
-    *part = (int32_t)std::min<int64_t>(size, INT32_MAX);
-    *parts = (int32_t)((a->vocab + size - 1) / size);
+// How rows longer than kShortRow are shared out: threads of a workgroup, workgroups per row, elements of each.
+struct TokenPlan {
+    int threads = 256;
+    int32_t parts = 1, part = 0;
+};
+
+TokenPlan in_parts(const klay_tokens_args* a, int threads, int64_t parts) {
+    TokenPlan p;
+    p.threads = threads;
+    const int64_t round = (int64_t)threads * (16 / dtype_bytes(a->dtype));       // elements that a workgroup takes at a time
+    int64_t size = (a->vocab + parts - 1) / parts;
+    if (parts > 1) size = (size + round - 1) / round * round;
+    p.part = (int32_t)std::min<int64_t>(size, INT32_MAX);
+    p.parts = (int32_t)((a->vocab + size - 1) / size);
+    return p;
+}
+
+// Many rows: a workgroup each.  Few: sixteen waves each, and several workgroups only where a row is so long that what they save is more
+// than the second launch that joins them costs (a workgroup takes in some 55 GB/s; the join is about 8 us).
+TokenPlan forward_plan(const klay_tokens_args* a) {
+    const int64_t bytes = (int64_t)a->vocab * dtype_bytes(a->dtype);
+    if (a->rows >= kManyRows) return in_parts(a, bytes <= kWaveRow ? 64 : 256, 1);
+    if (bytes <= kWaveRow) return in_parts(a, 256, 1);
+    return in_parts(a, 1024, bytes <= 512 * 1024 ? 1 : std::min<int64_t>((bytes + 262143) / 262144, klay::kMaxParts));
+}
+
+// The gradient's parts need no joining: as many as give the chip four workgroups per CU, of eight kilobytes or more.
+TokenPlan backward_plan(const klay_tokens_args* a) {
+    const int64_t bytes = (int64_t)a->vocab * dtype_bytes(a->dtype);
+    if (a->rows >= kManyRows) return in_parts(a, bytes <= kWaveRow ? 64 : 256, 1);
+    return in_parts(a, 256, std::min<int64_t>((4 * kComputeUnits + a->rows - 1) / a->rows, (bytes + 8191) / 8192));
 }
 
 size_t token_lists_at(int64_t rows, int32_t parts) { return (size_t)rows * parts * 4 * sizeof(float); }
@@ -95,10 +114,8 @@ klay::TokenArgs token_args(const klay_tokens_args* a) {
 
 int32_t capped_grid(int64_t units) { return (int32_t)std::min<int64_t>(units, 1 << 20); }
 
-template <typename T> bool one_wave(const klay::TokenArgs& g) { return g.parts == 1 && g.vocab * (int64_t)sizeof(T) <= kWaveRow; }
-
 template <typename T, bool ENT, bool TOP>
-klay_status run_tokens(const klay::TokenArgs& g, void* stream) {
+klay_status run_tokens(const klay::TokenArgs& g, int threads, void* stream) {
     const dim3 block(klay::kTokBlock);
     if (g.vocab <= kShortRow) {
         const int lanes = g.vocab <= kShortestRow ? 16 : 64, per_block = klay::kTokBlock / lanes;
@@ -107,20 +124,22 @@ klay_status run_tokens(const klay::TokenArgs& g, void* stream) {
         else KLAY_LAUNCH((klay::token_short_kernel<T, 64, 8, ENT, TOP>), grid, block, stream, g);
         return KLAY_OK;
     }
-    if (one_wave<T>(g)) KLAY_LAUNCH((klay::token_row_kernel<T, ENT, TOP, 64>), dim3(capped_grid(g.rows)), dim3(64), stream, g);
-    else KLAY_LAUNCH((klay::token_row_kernel<T, ENT, TOP, klay::kTokBlock>), dim3(capped_grid(g.rows * g.parts)), block, stream, g);
+    const dim3 grid(capped_grid(g.rows * g.parts));
+    if (threads == 64) KLAY_LAUNCH((klay::token_row_kernel<T, ENT, TOP, 64>), grid, dim3(64), stream, g);
+    else if (threads == 256) KLAY_LAUNCH((klay::token_row_kernel<T, ENT, TOP, 256>), grid, dim3(256), stream, g);
+    else KLAY_LAUNCH((klay::token_row_kernel<T, ENT, TOP, 1024>), grid, dim3(1024), stream, g);
     if (g.parts > 1) KLAY_LAUNCH((klay::token_join_kernel<T, TOP>), dim3((uint32_t)g.rows), block, stream, g);
     return KLAY_OK;
 }
 
 template <typename T>
-klay_status run_tokens(const klay::TokenArgs& g, void* stream) {
-    if (g.entropy) return g.top ? run_tokens<T, true, true>(g, stream) : run_tokens<T, true, false>(g, stream);
-    return g.top ? run_tokens<T, false, true>(g, stream) : run_tokens<T, false, false>(g, stream);
+klay_status run_tokens(const klay::TokenArgs& g, int threads, void* stream) {
+    if (g.entropy) return g.top ? run_tokens<T, true, true>(g, threads, stream) : run_tokens<T, true, false>(g, threads, stream);
+    return g.top ? run_tokens<T, false, true>(g, threads, stream) : run_tokens<T, false, false>(g, threads, stream);
 }
 
 template <typename T>
-klay_status run_tokens_back(const klay::TokenArgs& g, void* stream) {
+klay_status run_tokens_back(const klay::TokenArgs& g, int threads, void* stream) {
     const dim3 block(klay::kTokBlock);
     if (g.vocab <= kShortRow) {
         const int lanes = g.vocab <= kShortestRow ? 16 : 64, per_block = klay::kTokBlock / lanes;
@@ -129,8 +148,9 @@ klay_status run_tokens_back(const klay::TokenArgs& g, void* stream) {
         else KLAY_LAUNCH((klay::token_back_short_kernel<T, 64, 8>), grid, block, stream, g);
         return KLAY_OK;
     }
-    if (one_wave<T>(g)) KLAY_LAUNCH((klay::token_back_kernel<T, 64>), dim3(capped_grid(g.rows)), dim3(64), stream, g);
-    else KLAY_LAUNCH((klay::token_back_kernel<T, klay::kTokBlock>), dim3(capped_grid(g.rows * g.parts)), block, stream, g);
+    const dim3 grid(capped_grid(g.rows * g.parts));
+    if (threads == 64) KLAY_LAUNCH((klay::token_back_kernel<T, 64>), grid, dim3(64), stream, g);
+    else KLAY_LAUNCH((klay::token_back_kernel<T, 256>), grid, dim3(256), stream, g);
     return KLAY_OK;
 }
 
@@ -293,8 +313,7 @@ extern "C" {
 
 size_t klay_tokens_workspace_bytes(const klay_tokens_args* a) {
     if (!a || a->rows < 1 || a->vocab < 1 || !known_dtype(a->dtype) || a->top < 0) return 0;
-    int32_t parts, part;
-    token_parts(a, &parts, &part);
+    const int32_t parts = a->vocab <= kShortRow ? 1 : forward_plan(a).parts;
     return parts == 1 ? 0 : token_lists_at(a->rows, parts) + (size_t)a->rows * parts * a->top * sizeof(uint64_t);
 }
 
@@ -305,7 +324,8 @@ klay_status klay_tokens_forward(const klay_tokens_args* a, float* logp, float* n
     if ((a->num_tokens > 0 && !logp) || (a->top > 0 && (!top_logp || !top_tokens)))
         return fail(KLAY_EINVAL, "klay_tokens_forward: null argument");
     klay::TokenArgs g = token_args(a);
-    token_parts(a, &g.parts, &g.part);
+    const TokenPlan plan = a->vocab <= kShortRow ? TokenPlan() : forward_plan(a);
+    g.parts = plan.parts; g.part = plan.part;
     const size_t need = klay_tokens_workspace_bytes(a);
     if (need && (!workspace || workspace_bytes < need))
         return fail(KLAY_ENOMEM, "klay_tokens_forward: workspace too small: need " + std::to_string(need) + " bytes");
@@ -318,9 +338,9 @@ klay_status klay_tokens_forward(const klay_tokens_args* a, float* logp, float* n
     g.lists = need ? reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + token_lists_at(a->rows, g.parts)) : nullptr;
     OnDevice on(a->device);
     KLAY_HIP(on.status);
-    if (a->dtype == KLAY_F32) return run_tokens<klay::f32>(g, stream);
-    if (a->dtype == KLAY_BF16) return run_tokens<klay::bf16>(g, stream);
-    return run_tokens<klay::f16>(g, stream);
+    if (a->dtype == KLAY_F32) return run_tokens<klay::f32>(g, plan.threads, stream);
+    if (a->dtype == KLAY_BF16) return run_tokens<klay::bf16>(g, plan.threads, stream);
+    return run_tokens<klay::f16>(g, plan.threads, stream);
 }
 
 klay_status klay_tokens_backward(const klay_tokens_args* a, const float* stats, const float* dlogp, const float* dneg,
@@ -329,15 +349,16 @@ klay_status klay_tokens_backward(const klay_tokens_args* a, const float* stats, 
     if (st != KLAY_OK || a->rows == 0) return st;
     if (!stats || !dlogits) return fail(KLAY_EINVAL, "klay_tokens_backward: null argument");
     klay::TokenArgs g = token_args(a);
-    token_parts(a, &g.parts, &g.part);
+    const TokenPlan plan = a->vocab <= kShortRow ? TokenPlan() : backward_plan(a);
+    g.parts = plan.parts; g.part = plan.part;
     g.stats = const_cast<klay::RowStats*>(reinterpret_cast<const klay::RowStats*>(stats));
     g.dlogp = dlogp; g.dneg = dneg; g.dentropy = dentropy;
     g.dlogits = dlogits;
     OnDevice on(a->device);
     KLAY_HIP(on.status);
-    if (a->dtype == KLAY_F32) return run_tokens_back<klay::f32>(g, stream);
-    if (a->dtype == KLAY_BF16) return run_tokens_back<klay::bf16>(g, stream);
-    return run_tokens_back<klay::f16>(g, stream);
+    if (a->dtype == KLAY_F32) return run_tokens_back<klay::f32>(g, plan.threads, stream);
+    if (a->dtype == KLAY_BF16) return run_tokens_back<klay::bf16>(g, plan.threads, stream);
+    return run_tokens_back<klay::f16>(g, plan.threads, stream);
 }
 
 size_t klay_scan_workspace_bytes(const klay_scan_args* a) {

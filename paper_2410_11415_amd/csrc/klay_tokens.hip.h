@@ -20,7 +20,7 @@
 
 namespace klay {
 
-constexpr int kTokBlock = 256;              // threads of a workgroup: of a row part (64: one wave, for rows that four would not keep busy)
+constexpr int kTokBlock = 256;              // threads of a workgroup; the kernels over rows also have 64 and 1024 of them
 constexpr int kMaxTop = 64, kMaxTokens = 1024;
 constexpr float kSlack = 8.0f;
 constexpr float kTokLog2e = 1.4426950408889634f, kTokLn2 = 0.6931471805599453f, kTokFltMax = 3.402823466e+38f;
@@ -85,23 +85,41 @@ __device__ __forceinline__ float row_entropy(const RowSums& s) {
 }
 __device__ __forceinline__ float row_logp(float x, float max, float log_sum) { return max == -INFINITY ? -INFINITY : (x - max) - log_sum; }
 
+// What is asked of a row: token k and its logit, loaded before the row is summed (two loads that wait for each other).
+struct Asked {
+    int64_t token;
+    float x;
+};
 template <typename T>
-__device__ __forceinline__ void write_token(const TokenArgs& g, const T* row, int64_t r, int32_t k, const RowSums& s, float log_sum) {
-    const int64_t t = g.tokens[g.token_rows.at(r) + k * g.token_stride];
+__device__ __forceinline__ Asked asked_of(const TokenArgs& g, const T* row, int64_t r, int32_t k) {
+    Asked a{-1, 0.0f};
+    if (k < g.num_tokens) a.token = g.tokens[g.token_rows.at(r) + k * g.token_stride];
+    if (a.token >= 0 && a.token < g.vocab) a.x = (float)row[a.token];
+    return a;
+}
+
+__device__ __forceinline__ void write_token(const TokenArgs& g, int64_t r, int32_t k, const Asked& a, const RowSums& s, float log_sum) {
     float lp = 0.0f, neg = 0.0f;
-    if (t >= g.vocab) {
+    if (a.token >= g.vocab) {
         lp = neg = __int_as_float(0x7fc00000);
-    } else if (t >= 0) {
-        const float x = (float)row[t];
-        lp = row_logp(x, s.max, log_sum) + (log_sum - log_sum);             // (a NaN of the row reaches every token)
+    } else if (a.token >= 0) {
+        lp = row_logp(a.x, s.max, log_sum) + (log_sum - log_sum);             // (a NaN of the row reaches every token)
         if (g.neg) {
             if (row_empty(s)) neg = 0.0f;
-            else if (x == s.max && s.rest < 1.0f) neg = logf(s.rest) - log_sum;
+            else if (a.x == s.max && s.rest < 1.0f) neg = logf(s.rest) - log_sum;
             else neg = log1pf(-expf(lp));
         }
     }
     g.logp[r * g.num_tokens + k] = lp;
     if (g.neg) g.neg[r * g.num_tokens + k] = neg;
+}
+
+// Thread `thread` of `threads` writes its tokens; `first` is what asked_of said about its first one.
+template <typename T>
+__device__ __forceinline__ void write_tokens(const TokenArgs& g, const T* row, int64_t r, int32_t thread, int32_t threads, const Asked& first,
+                                             const RowSums& s, float log_sum) {
+    for (int32_t k = thread; k < g.num_tokens; k += threads)
+        write_token(g, r, k, k == thread ? first : asked_of<T>(g, row, r, k), s, log_sum);
 }
 
 __device__ __forceinline__ void write_row(const TokenArgs& g, int64_t r, const RowSums& s, float log_sum) {
@@ -116,32 +134,59 @@ __device__ __forceinline__ void write_top(const TokenArgs& g, int64_t r, int32_t
 }
 
 // ---- sums over the threads of a workgroup -------------------------------------------------------------------------
+// A value of another lane by the lane's own instruction (a shuffle through LDS takes some hundred cycles): within four lanes, eight, sixteen,
+// then the last lane of one row of sixteen into the next row, and of the first two rows into the others.  Lanes that get none keep `none`.
+template <int CONTROL> __device__ __forceinline__ int from_lane(int none, int x) { return __builtin_amdgcn_update_dpp(none, x, CONTROL, 0xf, 0xf, false); }
+enum : int { LANES_XOR1 = 0xB1, LANES_XOR2 = 0x4E, LANES_HALF_MIRROR = 0x141, LANES_MIRROR = 0x140, LANES_NEXT_ROW = 0x142, LANES_NEXT_HALF = 0x143 };
+template <int CONTROL> __device__ __forceinline__ float with_lane_max(float x) {
+    return fmaxf(x, __int_as_float(from_lane<CONTROL>(__float_as_int(x), __float_as_int(x))));
+}
+template <int CONTROL> __device__ __forceinline__ float with_lane_sum(float x) { return x + __int_as_float(from_lane<CONTROL>(0, __float_as_int(x))); }
+template <int CONTROL> __device__ __forceinline__ uint64_t with_lane_max(uint64_t x) {
+    const uint64_t y = (uint64_t)(uint32_t)from_lane<CONTROL>(0, (int)(x >> 32)) << 32 | (uint32_t)from_lane<CONTROL>(0, (int)x);
+    return y > x ? y : x;
+}
+// Over the G lanes (16 or 64) of a group; all of them get the result.
 template <int G> __device__ __forceinline__ float group_max(float x) {
-#pragma unroll
-    for (int s = G / 2; s > 0; s >>= 1) x = fmaxf(x, __shfl_xor(x, s, 64));
-    return x;
+    x = with_lane_max<LANES_MIRROR>(with_lane_max<LANES_HALF_MIRROR>(with_lane_max<LANES_XOR2>(with_lane_max<LANES_XOR1>(x))));
+    if constexpr (G == 16) return x;
+    x = with_lane_max<LANES_NEXT_HALF>(with_lane_max<LANES_NEXT_ROW>(x));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 template <int G> __device__ __forceinline__ float group_sum(float x) {
-#pragma unroll
-    for (int s = G / 2; s > 0; s >>= 1) x += __shfl_xor(x, s, 64);
-    return x;
+    x = with_lane_sum<LANES_MIRROR>(with_lane_sum<LANES_HALF_MIRROR>(with_lane_sum<LANES_XOR2>(with_lane_sum<LANES_XOR1>(x))));
+    if constexpr (G == 16) return x;
+    x = with_lane_sum<LANES_NEXT_HALF>(with_lane_sum<LANES_NEXT_ROW>(x));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
-// All threads get the result; `at` is scratch that no earlier call since the last barrier has used.
+template <int G> __device__ __forceinline__ uint64_t group_max(uint64_t x) {
+    x = with_lane_max<LANES_MIRROR>(with_lane_max<LANES_HALF_MIRROR>(with_lane_max<LANES_XOR2>(with_lane_max<LANES_XOR1>(x))));
+    if constexpr (G == 16) return x;
+    x = with_lane_max<LANES_NEXT_HALF>(with_lane_max<LANES_NEXT_ROW>(x));
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), 63) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+// All threads get the result; `at` is scratch (a float a wave; two) that no earlier call since the last barrier has used.
+constexpr int kScratch = 16;
 template <int THREADS> __device__ __forceinline__ float block_max(float x, float* at) {
     x = group_max<64>(x);
     if constexpr (THREADS == 64) return x;
     if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = x;
     __syncthreads();
-    return fmaxf(fmaxf(at[0], at[1]), fmaxf(at[2], at[3]));
+    x = at[0];
+#pragma unroll
+    for (int w = 1; w < THREADS / 64; ++w) x = fmaxf(x, at[w]);
+    return x;
 }
 template <int THREADS> __device__ __forceinline__ void block_sum2(float& x, float& y, float* at) {
     x = group_sum<64>(x);
     y = group_sum<64>(y);
     if constexpr (THREADS == 64) return;
-    if ((threadIdx.x & 63) == 0) { at[threadIdx.x >> 6] = x; at[4 + (threadIdx.x >> 6)] = y; }
+    if ((threadIdx.x & 63) == 0) { at[threadIdx.x >> 6] = x; at[kScratch + (threadIdx.x >> 6)] = y; }
     __syncthreads();
-    x = (at[0] + at[1]) + (at[2] + at[3]);
-    y = (at[4] + at[5]) + (at[6] + at[7]);
+    x = at[0];
+    y = at[kScratch];
+#pragma unroll
+    for (int w = 1; w < THREADS / 64; ++w) { x += at[w]; y += at[kScratch + w]; }
 }
 
 // One thread's run over its elements.  y = (x - ref) log2 e is one multiply-add, x log2 e - shift with shift = ref log2 e rounded once: what that
@@ -198,17 +243,23 @@ template <int N, int THREADS> struct Share {
     __device__ __forceinline__ bool in_vector(int32_t j) const { return j >= begin && j < full; }
 };
 
-// Rank of a lane's key among those of its wave (equal ones by their lane).
-__device__ __forceinline__ int32_t rank_in_wave(uint64_t key) {
-    const int32_t lane = threadIdx.x & 63;
+// The key of rank `which` (0: the largest) among those of a wave, of which only zeros are equal.
+__device__ __forceinline__ uint64_t of_rank_in_wave(uint64_t key, int32_t which) {
+    if (which < 8) {
+        for (;; --which) {
+            const uint64_t most = group_max<64>(key);
+            if (which == 0 || most == 0) return most;
+            if (key == most) key = 0;
+        }
+    }
     const uint32_t lo = (uint32_t)key, hi = (uint32_t)(key >> 32);
     int32_t rank = 0;
 #pragma unroll 16
     for (int j = 0; j < 64; ++j) {
         const uint64_t other = (uint64_t)__builtin_amdgcn_readlane(hi, j) << 32 | (uint32_t)__builtin_amdgcn_readlane(lo, j);
-        rank += other > key || (other == key && j < lane);
+        rank += other > key;
     }
-    return rank;
+    return group_max<64>(rank == which ? key : 0);
 }
 
 // The first `columns` threads hold the largest key of a column each (or one not above it).  Of the full waves among them the one of
@@ -217,37 +268,48 @@ __device__ __forceinline__ int32_t rank_in_wave(uint64_t key) {
 __device__ __forceinline__ uint64_t bound_of_columns(uint64_t mine, int32_t columns, int32_t top, uint64_t* quota) {
     const int32_t wave = threadIdx.x >> 6;
     const int32_t waves = columns < 128 ? 1 : columns >> 6, each = (top + waves - 1) / waves;
-    if (wave < waves && rank_in_wave(mine) == each - 1) quota[wave] = mine;
+    if (wave < waves) {
+        const uint64_t key = of_rank_in_wave(mine, each - 1);
+        if ((threadIdx.x & 63) == 0) quota[wave] = key;
+    }
     __syncthreads();
     uint64_t limit = quota[0];
     for (int w = 1; w < waves; ++w) limit = quota[w] < limit ? quota[w] : limit;
     return limit;
 }
 
-template <int THREADS> struct TopShared {
-    static constexpr int kRoom = THREADS * 8 + 256;       // candidates of one round on top of those kept before
-    uint64_t keys[kRoom];
+// Keys in LDS, and the best of them.
+template <int ROOM, int THREADS> struct Best {
+    uint64_t keys[ROOM];
     uint64_t best[kMaxTop];
-    uint64_t quota[THREADS / 64], quota_again[THREADS / 64];
-    int32_t chosen[THREADS];
+    uint64_t quota[THREADS / 64];
     uint64_t limit;
-    int32_t count, columns;
+    int32_t count;
+};
+// Of a row part: the candidates of one round on top of those kept before.
+template <int THREADS> struct TopShared : Best<THREADS * 8 + 256, THREADS> {
+    uint64_t first_quota[THREADS / 64];
+    int32_t chosen[THREADS];
+    int32_t columns;
 };
 
-// Sorts the `top` largest of keys[0 .. count) into best (0 where there are fewer).  `again`: leaves them as the only ones in keys.
-template <int THREADS>
-__device__ __forceinline__ void keep_best(TopShared<THREADS>& sh, int32_t top, bool again) {
+// Sorts the `top` largest of keys[0 .. count) into best (0 where there are fewer; a key of 0 is none).  `again`: leaves them as the only ones in
+// keys, and raises limit to the last of them.
+template <int ROOM, int THREADS>
+__device__ __forceinline__ void keep_best(Best<ROOM, THREADS>& sh, int32_t top, bool again) {
     const int32_t tid = threadIdx.x;
     int32_t n = sh.count;
-    if (n > 256) {            // most of them are out after one look at the columns of keys[tid + 256 j]
-        constexpr int kEach = (TopShared<THREADS>::kRoom + THREADS - 1) / THREADS;
+    if (n > 128) {            // most of them are out after one look at the columns keys[tid], keys[tid + THREADS], ..
+        constexpr int kEach = (ROOM + THREADS - 1) / THREADS;
+        const int32_t each = (n + THREADS - 1) / THREADS;
         uint64_t mine[kEach], most = 0;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            mine[j] = tid + j * THREADS < n ? sh.keys[tid + j * THREADS] : 0;
+            mine[j] = 0;
+            if (j < each) mine[j] = tid + j * THREADS < n ? sh.keys[tid + j * THREADS] : 0;
             most = mine[j] > most ? mine[j] : most;
         }
-        const uint64_t limit = bound_of_columns(most, THREADS, top, sh.quota_again);
+        const uint64_t limit = bound_of_columns(most, n < THREADS ? n : THREADS, top, sh.quota);
         if (tid == 0) sh.count = 0;
         __syncthreads();
 #pragma unroll
@@ -261,7 +323,7 @@ __device__ __forceinline__ void keep_best(TopShared<THREADS>& sh, int32_t top, b
         int32_t rank = 0;
 #pragma unroll 4
         for (int32_t j = 0; j < n; ++j) rank += sh.keys[j] > mine;
-        if (rank < top) sh.best[rank] = mine;
+        if (rank < top && mine != 0) sh.best[rank] = mine;
     }
     if (n + tid < top) sh.best[n + tid] = 0;
     __syncthreads();
@@ -285,7 +347,7 @@ __device__ __forceinline__ void top_of_part(TopShared<THREADS>& sh, const T* row
     if (tid == 0) sh.count = sh.columns = 0;
     const int32_t singles = share.head() > share.tail() ? share.head() : share.tail();
     const int32_t columns_in_use = share.vectors >= THREADS ? THREADS : share.vectors > singles ? share.vectors : singles;
-    uint64_t limit = bound_of_columns(low, columns_in_use, top, sh.quota);
+    uint64_t limit = bound_of_columns(low, columns_in_use, top, sh.first_quota);
     if (tid == 0) sh.limit = limit;
     if (high != 0 && high >= limit) sh.chosen[atomicAdd(&sh.columns, 1)] = tid;
     __syncthreads();
@@ -384,7 +446,7 @@ __device__ __forceinline__ PartSums sums_of_part(const T* row, const Share<16 / 
     }
     p.sum = s;
     p.weighted = t;
-    block_sum2<THREADS>(p.sum, p.weighted, scratch + 8);
+    block_sum2<THREADS>(p.sum, p.weighted, scratch + kScratch);
     p.rest = p.sum == 0.0f ? 0.0f : p.sum - 1.0f;
     if (p.sum > 0.0f && p.sum < 1.5f) {
         // One element holds most of the sum: `sum - 1` would keep little of the others.  Its thread's terms are taken again, without it.
@@ -413,7 +475,7 @@ __device__ __forceinline__ PartSums sums_of_part(const T* row, const Share<16 / 
         }
         p.rest = s;
         p.weighted = t;
-        block_sum2<THREADS>(p.rest, p.weighted, scratch + 16);
+        block_sum2<THREADS>(p.rest, p.weighted, scratch + 3 * kScratch);
     }
     if constexpr (TOP) {
         // the thread's largest element as a key lies between these two (the vector is known, the place in it is not)
@@ -431,7 +493,7 @@ __device__ __forceinline__ PartSums sums_of_part(const T* row, const Share<16 / 
 template <typename T, bool ENT, bool TOP, int THREADS>
 __global__ void __launch_bounds__(THREADS) token_row_kernel(TokenArgs g) {
     constexpr int N = 16 / sizeof(T);
-    __shared__ float scratch[32];
+    __shared__ float scratch[5 * kScratch];
     __shared__ int32_t owner;
     __shared__ std::conditional_t<TOP, TopShared<THREADS>, int> tops;
     const int32_t tid = threadIdx.x;
@@ -441,6 +503,8 @@ __global__ void __launch_bounds__(THREADS) token_row_kernel(TokenArgs g) {
         const T* row = static_cast<const T*>(g.logits) + g.logit_rows.at(r);
         const int32_t lo = part * g.part, hi = g.vocab - lo < g.part ? g.vocab : lo + g.part;
         const Share<N, THREADS> share(row + lo, lo, hi);
+        Asked asked{-1, 0.0f};
+        if (g.parts == 1) asked = asked_of<T>(g, row, r, tid);
         uint64_t low = 0, high = 0;
         PartSums p = sums_of_part<T, ENT, TOP, THREADS, false>(row, share, scratch, &owner, &low, &high);
         if (fabsf(p.max) > 0.5f * kFar && fabsf(p.max) < INFINITY) {
@@ -451,7 +515,7 @@ __global__ void __launch_bounds__(THREADS) token_row_kernel(TokenArgs g) {
         if constexpr (TOP) top_of_part<T, N, THREADS>(tops, row, share, low, high, g.top);
         if (g.parts == 1) {
             const float log_sum = row_log_sum(sums);
-            for (int32_t k = tid; k < g.num_tokens; k += THREADS) write_token<T>(g, row, r, k, sums, log_sum);
+            write_tokens<T>(g, row, r, tid, THREADS, asked, sums, log_sum);
             if (tid == 0) write_row(g, r, sums, log_sum);
             if constexpr (TOP)
                 if (tid < g.top) write_top(g, r, tid, tops.best[tid], p.max, log_sum);
@@ -472,15 +536,20 @@ constexpr int kMaxParts = 64;
 // Joins the parts of a row.
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kTokBlock) token_join_kernel(TokenArgs g) {
-    __shared__ float scratch[32];
+    __shared__ float scratch[5 * kScratch];
     __shared__ int32_t owner;
-    constexpr int kEach = kMaxParts * kMaxTop / kTokBlock;
-    __shared__ uint64_t keys[TOP ? kMaxParts * kMaxTop : 1], best[TOP ? kMaxTop : 1], quota[kTokBlock / 64];
-    __shared__ int32_t count;
+    __shared__ std::conditional_t<TOP, Best<kMaxParts * kMaxTop, kTokBlock>, int> tops;
     const int32_t tid = threadIdx.x, parts = g.parts;
     const int64_t r = blockIdx.x;
     const T* row = static_cast<const T*>(g.logits) + g.logit_rows.at(r);
-    if (tid == 0) { owner = kMaxParts; count = 0; }
+    const Asked asked = asked_of<T>(g, row, r, tid);
+    if (tid == 0) owner = kMaxParts;
+    if constexpr (TOP) {
+        const int32_t all = parts * g.top;
+        const uint64_t* lists = g.lists + r * all;
+        for (int32_t p = tid; p < all; p += kTokBlock) tops.keys[p] = lists[p];
+        if (tid == 0) tops.count = all;
+    }
     float m = -INFINITY, rest = 0.0f, weighted = 0.0f;
     if (tid < parts) {
         const float* p = g.partial + (r * parts + tid) * 4;
@@ -499,34 +568,14 @@ __global__ void __launch_bounds__(kTokBlock) token_join_kernel(TokenArgs g) {
         t = !none && f > 0.0f ? f * (weighted - d * whole) : 0.0f;
         if (rest != rest) s = rest;
     }
-    block_sum2<kTokBlock>(s, t, scratch + 8);
+    block_sum2<kTokBlock>(s, t, scratch + kScratch);
     const RowSums sums{max, s, t};
     const float log_sum = row_log_sum(sums);
-    for (int32_t k = tid; k < g.num_tokens; k += kTokBlock) write_token<T>(g, row, r, k, sums, log_sum);
+    write_tokens<T>(g, row, r, tid, kTokBlock, asked, sums, log_sum);
     if (tid == 0) write_row(g, r, sums, log_sum);
     if constexpr (TOP) {
-        const int32_t top = g.top, all = parts * top;
-        const uint64_t* lists = g.lists + r * all;
-        uint64_t mine[kEach], most = 0;
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-            mine[j] = tid + j * kTokBlock < all ? lists[tid + j * kTokBlock] : 0;
-            most = mine[j] > most ? mine[j] : most;
-        }
-        const uint64_t limit = bound_of_columns(most, all < kTokBlock ? all : kTokBlock, top, quota);
-#pragma unroll
-        for (int j = 0; j < kEach; ++j)
-            if (mine[j] != 0 && mine[j] >= limit) keys[atomicAdd(&count, 1)] = mine[j];
-        __syncthreads();
-        const int32_t n = count;
-        for (int32_t p = tid; p < n; p += kTokBlock) {
-            const uint64_t mine = keys[p];
-            int32_t rank = 0;
-            for (int32_t o = 0; o < n; ++o) rank += keys[o] > mine;
-            if (rank < top) best[rank] = mine;
-        }
-        __syncthreads();
-        if (tid < top) write_top(g, r, tid, best[tid], max, log_sum);
+        keep_best(tops, g.top, false);
+        if (tid < g.top) write_top(g, r, tid, tops.best[tid], max, log_sum);
     }
 }
 
@@ -536,6 +585,7 @@ __global__ void __launch_bounds__(kTokBlock) token_short_kernel(TokenArgs g) {
     const int32_t lane = threadIdx.x % G;
     for (int64_t r = ((int64_t)blockIdx.x * kTokBlock + threadIdx.x) / G; r < g.rows; r += (int64_t)gridDim.x * (kTokBlock / G)) {
         const T* row = static_cast<const T*>(g.logits) + g.logit_rows.at(r);
+        const Asked asked = asked_of<T>(g, row, r, lane);
         float x[E], max = -INFINITY;
 #pragma unroll
         for (int e = 0; e < E; ++e) x[e] = lane + G * e < g.vocab ? (float)row[lane + G * e] : -INFINITY;
@@ -545,11 +595,7 @@ __global__ void __launch_bounds__(kTokBlock) token_short_kernel(TokenArgs g) {
         int32_t first = 1 << 30;
 #pragma unroll
         for (int e = E - 1; e >= 0; --e) first = x[e] == max ? lane + G * e : first;
-#pragma unroll
-        for (int s = G / 2; s > 0; s >>= 1) {
-            const int32_t other = __shfl_xor(first, s, 64);
-            first = other < first ? other : first;
-        }
+        first = (1 << 30) - (int32_t)group_max<G>((uint64_t)((1 << 30) - first));
         const float to = fmaxf(max, -kTokFltMax);
         float rest = 0.0f, weighted = 0.0f;
 #pragma unroll
@@ -567,7 +613,7 @@ __global__ void __launch_bounds__(kTokBlock) token_short_kernel(TokenArgs g) {
         if constexpr (ENT) weighted = group_sum<G>(weighted);
         const RowSums sums{max, rest, weighted};
         const float log_sum = row_log_sum(sums);
-        for (int32_t k = lane; k < g.num_tokens; k += G) write_token<T>(g, row, r, k, sums, log_sum);
+        write_tokens<T>(g, row, r, lane, G, asked, sums, log_sum);
         if (lane == 0) write_row(g, r, sums, log_sum);
         if constexpr (TOP) {
             uint64_t key[E];
@@ -577,11 +623,7 @@ __global__ void __launch_bounds__(kTokBlock) token_short_kernel(TokenArgs g) {
                 uint64_t best = 0;
 #pragma unroll
                 for (int e = 0; e < E; ++e) best = key[e] > best ? key[e] : best;
-#pragma unroll
-                for (int s = G / 2; s > 0; s >>= 1) {
-                    const uint64_t other = __shfl_xor((unsigned long long)best, s, 64);
-                    best = other > best ? other : best;
-                }
+                best = group_max<G>(best);
 #pragma unroll
                 for (int e = 0; e < E; ++e) key[e] = key[e] == best ? 0 : key[e];
                 if (lane == 0) write_top(g, r, k, best, max, log_sum);
@@ -652,7 +694,7 @@ template <typename T, int THREADS>
 __global__ void __launch_bounds__(THREADS) token_back_kernel(TokenArgs g) {
     constexpr int N = 16 / sizeof(T);
     __shared__ TokenGrad grads[kMaxTokens];
-    __shared__ float scratch[16];
+    __shared__ float scratch[2 * kScratch];
     const int32_t tid = threadIdx.x, K = g.num_tokens;
     for (int64_t unit = blockIdx.x; unit < g.rows * g.parts; unit += gridDim.x) {
         const int64_t r = unit / g.parts;

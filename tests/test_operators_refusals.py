@@ -50,7 +50,7 @@ def test_tokens_outputs_and_workspace():
         with pytest.raises(KlayError) as e:
             binding.klay_tokens_backward(tokens_args(), given[0], P, None, None, given[1])
         assert e.value.status == binding.KLAY_EINVAL
-    one = tokens_args(rows=1, vocab=100000, top=5)
+    one = tokens_args(rows=1, vocab=1000000, top=5)
     need = binding.klay_tokens_workspace_bytes(one)
     assert need > 0 and binding.klay_tokens_workspace_bytes(tokens_args()) == 0 == binding.klay_tokens_workspace_bytes(None)
     for at, size, status in ((None, need, binding.KLAY_ENOMEM), (P, need - 1, binding.KLAY_ENOMEM), (P + 4, need, binding.KLAY_EINVAL)):
