@@ -25,5 +25,6 @@ def __getattr__(name):
         return CircuitLayer
     if name in ("TokenLogprobs", "gated_scan", "gated_step", "token_logprobs"):
         from . import operators
-        return getattr(operators, name)
+        globals()[name] = getattr(operators, name)          # (found without this function from now on)
+        return globals()[name]
     raise AttributeError(name)

@@ -35,10 +35,6 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _workspace(size, device):
-    return torch.empty(size, dtype=torch.uint8, device=device) if size else None
-
-
 # ---- log probabilities of given tokens ----------------------------------------------------------------------------
 class TokenLogprobs(NamedTuple):
     """What :func:`token_logprobs` returns; None for what was not asked."""
@@ -51,10 +47,11 @@ class TokenLogprobs(NamedTuple):
 
 def _rows_of(t):
     """(t, its leading axes as klay_rows): t itself where at most two strides describe them, else a contiguous copy."""
-    if t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1):
-        return t, _b.klay_rows(max(t.shape[0], 1), 0, t.stride(0))
+    shape, strides = t.shape, t.stride()
+    if len(shape) == 2:
+        return t, _b.klay_rows(shape[0] or 1, 0, strides[0])
     merged = []
-    for n, s in zip(t.shape[:-1], t.stride()[:-1]):
+    for n, s in zip(shape[:-1], strides[:-1]):
         if n == 1:
             continue
         if merged and merged[-1][1] == n * s:
@@ -64,44 +61,55 @@ def _rows_of(t):
     if len(merged) > 2:
         return _rows_of(t.contiguous())
     merged = [(1, 0)] * (2 - len(merged)) + merged
-    return t, _b.klay_rows(max(merged[1][0], 1), merged[0][1], merged[1][1])
+    return t, _b.klay_rows(merged[1][0] or 1, merged[0][1], merged[1][1])
 
 
 def _token_args(logits, tokens, top):
-    if logits.stride(-1) != 1 and logits.shape[-1] != 1:
+    vocab = logits.shape[-1]
+    if logits.stride(-1) != 1 and vocab != 1:
         logits = logits.contiguous()
     logits, logit_rows = _rows_of(logits)
-    tokens, token_rows = (None, _b.klay_rows(1, 0, 0)) if tokens is None else _rows_of(tokens)
-    vocab = logits.shape[-1]
-    args = _b.klay_tokens_args(_DTYPES[logits.dtype], logits.device.index, vocab, 0 if tokens is None else tokens.shape[-1], top, 0,
-                               logits.numel() // vocab, logits.data_ptr(), logit_rows, _ptr(tokens), token_rows,
-                               0 if tokens is None else tokens.stride(-1))
+    k = stride = pointer = 0
+    token_rows = logit_rows
+    if tokens is not None:
+        tokens, token_rows = _rows_of(tokens)
+        k, stride, pointer = tokens.shape[-1], tokens.stride(-1), tokens.data_ptr()
+    args = _b.klay_tokens_args(_DTYPES[logits.dtype], logits.get_device(), vocab, k, top, 0, logits.numel() // vocab, logits.data_ptr(),
+                               logit_rows, pointer, token_rows, stride)
     return args, (logits, tokens)          # the tensors that args points into
 
 
 def _tokens_forward(logits, tokens, complement, entropy, top, keep):
     args, alive = _token_args(logits, tokens, top)
-    lead, device = logits.shape[:-1], logits.device
-
-    def new(wanted, *tail, dtype=torch.float32):
-        return torch.empty(lead + tail, dtype=dtype, device=device) if wanted else None
-
-    k = args.num_tokens
-    logp, neg, h = new(tokens is not None, k), new(complement and tokens is not None, k), new(entropy)
-    top_logp, top_tokens = new(top, top), new(top, top, dtype=torch.int64)
-    stats = torch.empty((args.rows, 4), dtype=torch.float32, device=device) if keep else None
+    lead, new, k = tuple(logits.shape[:-1]), logits.new_empty, args.num_tokens
+    logp = neg = h = top_logp = top_tokens = stats = None
+    if tokens is not None:
+        logp = new(lead + (k,), dtype=torch.float32)
+        if complement:
+            neg = new(lead + (k,), dtype=torch.float32)
+    if entropy:
+        h = new(lead, dtype=torch.float32)
+    if top:
+        top_logp, top_tokens = new(lead + (top,), dtype=torch.float32), new(lead + (top,), dtype=torch.int64)
+    if keep:
+        stats = new((args.rows, 4), dtype=torch.float32)
     size = _b.klay_tokens_workspace_bytes(args)
-    work = _workspace(size, device)
+    work = new((size,), dtype=torch.uint8) if size else None
     _b.klay_tokens_forward(args, _ptr(logp), _ptr(neg), _ptr(h), _ptr(stats), _ptr(top_logp), _ptr(top_tokens), _ptr(work), size,
                            _stream(args.device))
-    del alive
-    return logp, neg, h, top_logp, top_tokens, stats
+    return logp, neg, h, top_logp, top_tokens, stats, args, alive
+
+
+def _copies(used, given):
+    """used, if some of it is a copy and has to be kept beside what autograd saves; else None"""
+    return None if all(u is g for u, g in zip(used, given)) else used
 
 
 class _TokenLogprobs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, tokens, complement, entropy, top):
-        *out, stats = _tokens_forward(logits, tokens, complement, entropy, top, True)
+        *out, stats, ctx.args, alive = _tokens_forward(logits, tokens, complement, entropy, top, True)
+        ctx.copies = _copies(alive, (logits, tokens))
         ctx.save_for_backward(logits, tokens, stats)
         ctx.set_materialize_grads(False)
         ctx.mark_non_differentiable(*[t for t in out[3:] if t is not None])
@@ -111,12 +119,13 @@ class _TokenLogprobs(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dlogp, dneg, dentropy, _top_logp, _top_tokens):
         logits, tokens, stats = ctx.saved_tensors
-        args, alive = _token_args(logits, tokens, 0)
         dlogp, dneg, dentropy = (None if t is None else t.contiguous() for t in (dlogp, dneg, dentropy))
-        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        args, alive = ctx.args, ctx.copies
+        if alive is None and (args.logits or 0, args.tokens or 0) != (logits.data_ptr(), 0 if tokens is None else tokens.data_ptr()):
+            args, alive = _token_args(logits, tokens, 0)            # what was saved has been put elsewhere
+        dlogits = logits.new_empty(logits.shape)
         _b.klay_tokens_backward(args, stats.data_ptr(), _ptr(dlogp), _ptr(dneg), _ptr(dentropy), dlogits.data_ptr(),
                                 _stream(args.device))
-        del alive
         return dlogits, None, None, None, None
 
 
@@ -150,52 +159,55 @@ def token_logprobs(logits, tokens=None, *, complement=False, entropy=False, top=
     if logits.shape[-1] >= 1 << 31 or not 0 <= top <= min(_MOST_TOP, logits.shape[-1]):
         raise ValueError("top must be 0 .. min(V, %d), and V below 2^31" % _MOST_TOP)
     if torch.is_grad_enabled() and logits.requires_grad:
-        return TokenLogprobs(*_TokenLogprobs.apply(logits, tokens, bool(complement), bool(entropy), top))
-    return TokenLogprobs(*_tokens_forward(logits, tokens, bool(complement), bool(entropy), top, False)[:5])
+        return TokenLogprobs(*_TokenLogprobs.apply(logits, tokens, complement, entropy, top))
+    return TokenLogprobs(*_tokens_forward(logits, tokens, complement, entropy, top, False)[:5])
 
 
 # ---- gated recurrence ---------------------------------------------------------------------------------------------
 def _channels_last(t):
-    """t, or a copy where its channels lie apart (or its time steps further than the kernels reach)"""
-    fits = (t.stride(-1) == 1 or t.shape[-1] == 1) and t.stride(-2) <= _MOST_CHANNELS
-    return t if fits else t.contiguous()
+    """(t, its strides), or those of a copy where its channels lie apart (or its time steps further than the kernels reach)"""
+    strides = t.stride()
+    if (strides[-1] != 1 and t.shape[-1] != 1) or strides[-2] > _MOST_CHANNELS:
+        t = t.contiguous()
+        strides = t.stride()
+    return t, strides
 
 
 def _scan_args(gates, inputs, initial, semiring, offsets, row_info):
-    gates, inputs = _channels_last(gates), None if inputs is None else _channels_last(inputs)
-    packed = offsets is not None
-    batch, time = (1, gates.shape[0]) if packed else gates.shape[:2]
-
-    def strides(t):
-        return (0, 0) if t is None else (0, t.stride(0)) if packed else (t.stride(0), t.stride(1))
-
+    (gates, gs), (inputs, xs) = _channels_last(gates), _channels_last(inputs)
+    shape = gates.shape
     initial = None if initial is None else initial.contiguous()
-    args = _b.klay_scan_args(_DTYPES[gates.dtype], semiring, gates.device.index, gates.shape[-1], batch, time,
-                             offsets.shape[0] - 1 if packed else 0, gates.data_ptr(), _ptr(inputs), *strides(gates), *strides(inputs),
-                             _ptr(offsets), _ptr(row_info), _ptr(initial))
+    if offsets is None:
+        batch, time, channels = shape
+        args = _b.klay_scan_args(_DTYPES[gates.dtype], semiring, gates.get_device(), channels, batch, time, 0, gates.data_ptr(),
+                                 inputs.data_ptr(), gs[0], gs[1], xs[0], xs[1], None, None, _ptr(initial))
+    else:
+        time, channels = shape
+        args = _b.klay_scan_args(_DTYPES[gates.dtype], semiring, gates.get_device(), channels, 1, time, offsets.shape[0] - 1,
+                                 gates.data_ptr(), inputs.data_ptr(), 0, gs[0], 0, xs[0], offsets.data_ptr(), row_info.data_ptr(),
+                                 _ptr(initial))
     return args, (gates, inputs, initial)
 
 
 def _scan_forward(gates, inputs, initial, semiring, offsets):
-    device = gates.device
-    row_info = None if offsets is None else torch.empty(gates.shape[0], dtype=torch.int32, device=device)
+    new = gates.new_empty
+    row_info = None if offsets is None else new((gates.shape[0],), dtype=torch.int32)
     args, alive = _scan_args(gates, inputs, initial, semiring, offsets, row_info)
-    states = torch.empty(gates.shape, dtype=gates.dtype, device=device)
-    final = torch.empty((args.sequences if offsets is not None else args.batch, args.channels), dtype=torch.float32, device=device)
+    states = new(gates.shape)
+    final = new((args.sequences if offsets is not None else args.batch, args.channels), dtype=torch.float32)
     size = _b.klay_scan_workspace_bytes(args)
-    work = _workspace(size, device)
+    work = new((size,), dtype=torch.uint8) if size else None
     _b.klay_scan_forward(args, states.data_ptr(), final.data_ptr(), _ptr(work), size, _stream(args.device))
-    del alive
-    return states, final, row_info
+    return states, final, row_info, args, alive
 
 
 class _GatedScan(torch.autograd.Function):
     @staticmethod
     def forward(ctx, gates, inputs, initial, semiring, offsets):
-        states, final, row_info = _scan_forward(gates, inputs, initial, semiring, offsets)
+        states, final, row_info, ctx.args, alive = _scan_forward(gates, inputs, initial, semiring, offsets)
+        ctx.semiring, ctx.copies = semiring, _copies(alive, (gates, inputs, initial))
         # (the reverse sweep of the real semiring does not read the inputs)
         ctx.save_for_backward(gates, inputs if semiring == KLAY_LOG else None, initial, offsets, row_info, states)
-        ctx.semiring = semiring
         ctx.set_materialize_grads(False)
         return states, final
 
@@ -205,16 +217,18 @@ class _GatedScan(torch.autograd.Function):
         gates, inputs, initial, offsets, row_info, states = ctx.saved_tensors
         if dstates is None and dfinal is None:
             return None, None, None, None, None
-        args, alive = _scan_args(gates, inputs, initial, ctx.semiring, offsets, row_info)
+        args, alive = ctx.args, ctx.copies
+        now = [0 if t is None else t.data_ptr() for t in (gates, inputs, initial, offsets, row_info)]
+        then = [p or 0 for p in (args.gates, args.inputs if inputs is not None else 0, args.initial, args.offsets, args.row_info)]
+        if alive is None and now != then:                           # what was saved has been put elsewhere
+            args, alive = _scan_args(gates, gates if inputs is None else inputs, initial, ctx.semiring, offsets, row_info)
         dstates, dfinal = (None if t is None else t.contiguous() for t in (dstates, dfinal))
-        dgates, dinputs = (torch.empty(gates.shape, dtype=gates.dtype, device=gates.device) if need else None
-                           for need in ctx.needs_input_grad[:2])
-        dinitial = torch.empty_like(initial, memory_format=torch.contiguous_format) if ctx.needs_input_grad[2] else None
+        dgates, dinputs = (gates.new_empty(gates.shape) if need else None for need in ctx.needs_input_grad[:2])
+        dinitial = initial.new_empty(initial.shape) if ctx.needs_input_grad[2] else None
         size = _b.klay_scan_workspace_bytes(args)
-        work = _workspace(size, gates.device)
+        work = gates.new_empty((size,), dtype=torch.uint8) if size else None
         _b.klay_scan_backward(args, states.data_ptr(), _ptr(dstates), _ptr(dfinal), _ptr(dgates), _ptr(dinputs), _ptr(dinitial),
                               _ptr(work), size, _stream(args.device))
-        del alive
         return dgates, dinputs, dinitial, None, None
 
 
@@ -274,18 +288,18 @@ def gated_step(gates, inputs, state, semiring=KLAY_REAL, out=None):
     if gates.dim() != 2 or state.shape != gates.shape or state.device != gates.device:
         raise ValueError("gates, inputs and state must be [B, C] on one device")
     if out is None:
-        out = torch.empty(gates.shape, dtype=gates.dtype, device=gates.device)
+        out = gates.new_empty(gates.shape)
     elif not isinstance(out, torch.Tensor) or out.shape != gates.shape or out.dtype != gates.dtype or out.device != gates.device:
         raise ValueError("out must have the shape, type and device of gates")
     batch, channels = gates.shape
-    for t, name in ((state, "state"), (out, "out")):
-        if (channels > 1 and t.stride(1) != 1) or (batch > 1 and t.stride(0) < channels):
-            raise ValueError(name + " must have its channels next to each other and rows that do not overlap")
+    ss, os = state.stride(), out.stride()
+    if (channels > 1 and (ss[1] != 1 or os[1] != 1)) or (batch > 1 and (ss[0] < channels or os[0] < channels)):
+        raise ValueError("state and out must have their channels next to each other and rows that do not overlap")
     if torch.is_grad_enabled() and (gates.requires_grad or inputs.requires_grad or state.requires_grad or out.requires_grad):
         raise RuntimeError("gated_step is not differentiated; call it under torch.no_grad(), or gated_scan")
-    gates, inputs = _channels_last(gates), _channels_last(inputs)
-    device = gates.device.index
-    _b.klay_scan_step(_DTYPES[gates.dtype], int(semiring), device, batch, channels, gates.data_ptr(), gates.stride(0), inputs.data_ptr(),
-                      inputs.stride(0), state.data_ptr(), state.stride(0), out.data_ptr(), out.stride(0), _stream(device))
+    (gates, gs), (inputs, xs) = _channels_last(gates), _channels_last(inputs)
+    device = gates.get_device()
+    _b.klay_scan_step(_DTYPES[gates.dtype], semiring, device, batch, channels, gates.data_ptr(), gs[0], inputs.data_ptr(), xs[0],
+                      state.data_ptr(), ss[0], out.data_ptr(), os[0], _stream(device))
     torch.autograd.graph.increment_version((state, out))          # written in place: a graph that has saved them is to notice
     return out
