@@ -377,12 +377,12 @@ klay_status klay_scan_forward(const klay_scan_args* a, void* states, float* fina
     if (st != KLAY_OK) return st;
     OnDevice on(a->device);
     KLAY_HIP(on.status);
-    if (a->offsets || !rows) {
-        st = fill_states(final, a->initial, a->semiring == KLAY_REAL ? 0.0f : -INFINITY, sequences * a->channels, stream);
-        if (st != KLAY_OK || !rows) return st;
-        KLAY_LAUNCH(klay::scan_rows_kernel, dim3((uint32_t)((a->time + 255) / 256)), dim3(256), stream, a->row_info, a->offsets, a->time,
-                    (int32_t)a->sequences);
-    }
+    const float none = a->semiring == KLAY_REAL ? 0.0f : -INFINITY;
+    const int64_t ends = final ? sequences * a->channels : 0;
+    if (!rows) return fill_states(final, a->initial, none, ends, stream);
+    if (a->offsets)
+        KLAY_LAUNCH(klay::scan_rows_kernel, dim3((uint32_t)std::min<int64_t>((std::max(a->time, ends) + 255) / 256, 4096)), dim3(256), stream,
+                    a->row_info, a->offsets, a->time, (int32_t)a->sequences, final, a->initial, none, ends);
     if (!aligned_to(2 * dtype_bytes(a->dtype), {states})) narrow(&p, a);
     klay::ScanArgs g = scan_args(a, p, workspace);
     g.out = states;

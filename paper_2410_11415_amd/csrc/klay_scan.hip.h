@@ -157,6 +157,53 @@ template <int VC, int W> struct Maps {
     }
 };
 
+// The state that comes out of the chunks first .. first + count - 1 of a batch entry, taken in rising (BACK: falling) order, from
+// nothing.  Every wave joins a part of their maps, eight loaded at a time; the parts meet in LDS, in set 1 of `maps`.
+template <int S, int VC, int W, bool BACK>
+__device__ __forceinline__ void state_of_chunks(float (&carry)[VC], Maps<VC, W>& maps, const ScanArgs& g, const Place& at, int32_t first, int32_t count) {
+    constexpr int kAtOnce = 8;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.y), lane = threadIdx.x;
+#pragma unroll
+    for (int v = 0; v < VC; ++v) carry[v] = Ring<S>::zero();
+    if (count <= 0) return;
+    const int32_t each = (count + W - 1) / W;
+    const int32_t from = wave * each, to = from + each < count ? from + each : count;
+    float A[VC], H[VC];
+    bool cut = false;
+#pragma unroll
+    for (int v = 0; v < VC; ++v) { A[v] = Ring<S>::one; H[v] = Ring<S>::zero(); }
+    for (int32_t n = from; n < to; n += kAtOnce) {
+        float a[kAtOnce][VC], h[kAtOnce][VC];
+        int32_t c[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int32_t i = n + j < to ? n + j : to - 1;          // (one past the part: again the last one, which is then not taken)
+            const int64_t k = (int64_t)at.batch * g.chunks + first + (BACK ? count - 1 - i : i);
+            load_elements<VC>(a[j], g.map_a + k * g.channels + at.lane);
+            load_elements<VC>(h[j], g.map_h + k * g.channels + at.lane);
+            c[j] = g.map_cut[k];
+        }
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            if (n + j >= to) break;
+            cut |= c[j] != 0;
+#pragma unroll
+            for (int v = 0; v < VC; ++v) {
+                H[v] = c[j] ? h[j][v] : Ring<S>::step(a[j][v], H[v], h[j][v]);
+                A[v] = Ring<S>::times(a[j][v], A[v]);
+            }
+        }
+    }
+    maps.put(1, wave, A, H, cut);
+    lds_barrier();
+    const uint64_t cuts = maps.cuts(1);
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+        for (int v = 0; v < VC; ++v)
+            carry[v] = cuts >> w & 1 ? maps.h[1][w][lane][v] : Ring<S>::step(maps.a[1][w][lane][v], carry[v], maps.h[1][w][lane][v]);
+}
+
 // ---- forward ----------------------------------------------------------------------------------------------------
 template <int S, typename T, int VC> struct Tile {
     Raw<T, VC> a[kSteps], x[kSteps];
@@ -264,17 +311,7 @@ __global__ void __launch_bounds__(64 * W) scan_kernel(ScanArgs g) {
     Tile<S, T, VC> next;
     next.load(g, begin + wave * kSteps, end, at);
     float carry[VC];
-#pragma unroll
-    for (int v = 0; v < VC; ++v) carry[v] = Ring<S>::zero();
-    for (int k = 0; k < chunk; ++k) {
-        const int64_t from = (int64_t)at.batch * g.chunks + k;
-        float A[VC], H[VC];
-        load_elements<VC>(A, g.map_a + from * g.channels + at.lane);
-        load_elements<VC>(H, g.map_h + from * g.channels + at.lane);
-        const bool cut = g.map_cut[from];
-#pragma unroll
-        for (int v = 0; v < VC; ++v) carry[v] = cut ? H[v] : Ring<S>::step(A[v], carry[v], H[v]);
-    }
+    state_of_chunks<S, VC, W, false>(carry, maps, g, at, 0, chunk);
     int turn = 0;
     for (int64_t tile = begin; tile < end; tile += W * kSteps, turn ^= 1) {
         const int64_t t = tile + wave * kSteps;
@@ -493,17 +530,7 @@ __global__ void __launch_bounds__(64 * W) scan_back_kernel(ScanArgs g) {
     BackTile<S, T, VC> next;
     next.load(g, begin + (tiles - 1) * (W * kSteps) + wave * kSteps, end, at, need_h);
     float carry[VC];
-#pragma unroll
-    for (int v = 0; v < VC; ++v) carry[v] = 0.0f;
-    for (int k = g.chunks - 1; k > chunk; --k) {
-        const int64_t from = (int64_t)at.batch * g.chunks + k;
-        float A[VC], C[VC];
-        load_elements<VC>(A, g.map_a + from * g.channels + at.lane);
-        load_elements<VC>(C, g.map_h + from * g.channels + at.lane);
-        const bool cut = g.map_cut[from];
-#pragma unroll
-        for (int v = 0; v < VC; ++v) carry[v] = cut ? C[v] : fmaf(A[v], carry[v], C[v]);
-    }
+    state_of_chunks<SEMI_REAL, VC, W, true>(carry, maps, g, at, chunk + 1, g.chunks - 1 - chunk);
     int turn = 0;
     for (int64_t n = tiles - 1; n >= 0; --n, turn ^= 1) {
         const int64_t t = begin + n * (W * kSteps) + wave * kSteps;
@@ -539,19 +566,23 @@ __global__ void __launch_bounds__(64 * W) scan_back_kernel(ScanArgs g) {
 // Thread n < rows: row n belongs to the first sequence s with offsets[s + 1] > n.  Offsets that are not what they should be (descending,
 // past the rows, negative) give other results, never an access out of range: s is found in [0, sequences], and row 0 reads no row
 // before it.
-__global__ void __launch_bounds__(256) scan_rows_kernel(int32_t* rows, const int64_t* offsets, int64_t count, int32_t sequences) {
-    const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (n >= count) return;
-    int32_t lo = 0, hi = sequences;
-    while (lo < hi) {
-        const int32_t mid = lo + (hi - lo) / 2;
-        if (offsets[mid + 1] > n) hi = mid;
-        else lo = mid + 1;
+// Thread n < states_count: states[n] = from[n], or `none`: what the sequences without rows end with.
+__global__ void __launch_bounds__(256) scan_rows_kernel(int32_t* rows, const int64_t* offsets, int64_t count, int32_t sequences, float* states,
+                                                        const float* from, float none, int64_t states_count) {
+    for (int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x; n < count || n < states_count; n += (int64_t)gridDim.x * 256) {
+        if (n < states_count) states[n] = from ? from[n] : none;
+        if (n >= count) continue;
+        int32_t lo = 0, hi = sequences;
+        while (lo < hi) {
+            const int32_t mid = lo + (hi - lo) / 2;
+            if (offsets[mid + 1] > n) hi = mid;
+            else lo = mid + 1;
+        }
+        int32_t r = kDeadRow;
+        if (lo < sequences && offsets[lo] <= n)
+            r = 4 * lo + (offsets[lo] == n || n == 0 ? ROW_FIRST : 0) + (offsets[lo + 1] == n + 1 ? ROW_LAST : 0);
+        rows[n] = r;
     }
-    int32_t r = kDeadRow;
-    if (lo < sequences && offsets[lo] <= n)
-        r = 4 * lo + (offsets[lo] == n || n == 0 ? ROW_FIRST : 0) + (offsets[lo + 1] == n + 1 ? ROW_LAST : 0);
-    rows[n] = r;
 }
 
 // states[i] = from[i], or `none`
