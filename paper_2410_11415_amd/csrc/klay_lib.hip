@@ -155,9 +155,12 @@ klay_status run_tokens_back(const klay::TokenArgs& g, int threads, void* stream)
 }
 
 // ---- recurrence -----------------------------------------------------------------------------------------------------
+constexpr int64_t kFewChains = kComputeUnits / 2;
+
 struct ScanPlan {
     int vec = 1, waves = 4;         // channels per lane; waves per workgroup
-    int32_t chunks = 1, chunk = 0, blocks_c = 1;
+    int32_t blocks_c = 1;
+    int64_t chains = 1, tiles = 0;  // tiles > 0: a workgroup a tile
 };
 
 klay_status check_scan(const klay_scan_args* a, bool inputs, const char* who) {
@@ -186,44 +189,39 @@ bool aligned_to(size_t bytes, std::initializer_list<const void*> all) {
     return bits % bytes == 0;
 }
 
-// Two channels a lane where that leaves two workgroups per CU, and addresses and strides let a lane take both at once (us, one / two: 16 x 4096
-// x 4096 fp32 forward 653 / 554, backward 1113 / 964; 32 x 1024 x 4096 bf16 181 / 169, 329 / 278; 8 x 4096 x 2048 bf16, where it would leave
-// half of the CUs empty, 101 / 126, 175 / 182).  Waves as many as the time steps give work to, eight at most (sixteen: within 5% either way, and the
-// log semiring's reverse sweep runs out of registers).  Where batch and channels give less than one workgroup per two CUs the time
-// axis is cut until there is one per CU (8 x 4096 x 512 LOG forward, chunks of 4096 / 1024 / 682 steps: 146 / 73 / 81 us).
+// Waves as many as the time steps give work to, eight at most (sixteen: within 5% either way, and the log semiring's reverse sweep runs out of
+// registers).  A workgroup a tile where batch and channels give less than one workgroup per two CUs (us, one for all tiles / one a tile, forward
+// and reverse: 8 x 4096 x 512 LOG 143 / 56, 227 / 97; at the border, 8 x 2048 x 1024 fp32, 56 / 52, 92 / 79; 8 x 4096 x 2048 bf16 94 / 103,
+// 176 / 180).  Two channels a lane, where addresses and strides let a lane take both at once: there, for 16-bit types (one / two: 4 x 4096 x 2048
+// bf16 70 / 59, 92 / 96; 65536 x 512 fp32 93 / 105, 139 / 155); with one workgroup for all tiles, where two workgroups per CU are left (16 x
+// 4096 x 4096 fp32 653 / 554, 1113 / 964; 32 x 1024 x 4096 bf16 181 / 169, 329 / 278; 8 x 4096 x 2048 bf16, where half of the CUs would be without
+// one, 101 / 126, 175 / 182).
 ScanPlan scan_plan(const klay_scan_args* a) {
     ScanPlan p;
     const int64_t size = dtype_bytes(a->dtype);
     auto blocks = [&](int vec) { return (a->channels + 64 * vec - 1) / (64 * vec); };
     const bool pairs = a->channels % 2 == 0 && aligned_to(2 * size, {a->gates, a->inputs}) && (a->gates_batch_stride | a->gates_time_stride |
                        a->inputs_batch_stride | a->inputs_time_stride) % 2 == 0;
-    p.vec = a->semiring == KLAY_REAL && pairs && blocks(2) * a->batch >= 2 * kComputeUnits ? 2 : 1;
-    p.blocks_c = blocks(p.vec);
-    const int64_t n = p.blocks_c * a->batch;
     p.waves = a->time <= klay::kSteps ? 1 : a->time <= 4 * klay::kSteps ? 4 : 8;
-    p.chunk = (int32_t)a->time;
-    if (n <= kComputeUnits / 2 && p.waves == 8) {
-        const int64_t tile = (int64_t)p.waves * klay::kSteps;
-        int64_t chunks = std::min<int64_t>(kComputeUnits / n, (a->time + tile - 1) / tile);
-        const int64_t steps = ((a->time + chunks - 1) / chunks + tile - 1) / tile * tile;
-        chunks = (a->time + steps - 1) / steps;
-        if (chunks > 1) {
-            p.chunks = (int32_t)chunks;
-            p.chunk = (int32_t)steps;
-        }
-    }
+    const bool few = p.waves == 8 && blocks(1) * a->batch <= kFewChains;
+    p.vec = a->semiring == KLAY_REAL && pairs && (few ? size == 2 : blocks(2) * a->batch >= 2 * kComputeUnits) ? 2 : 1;
+    p.blocks_c = blocks(p.vec);
+    p.chains = p.blocks_c * a->batch;
+    if (few) p.tiles = (a->time + p.waves * klay::kSteps - 1) / (p.waves * klay::kSteps);
     return p;
 }
 
-size_t scan_maps(const klay_scan_args* a, const ScanPlan& p) { return (size_t)a->batch * p.chunks * a->channels; }
-size_t scan_bytes(const klay_scan_args* a, const ScanPlan& p) {
-    return p.chunks == 1 ? 0 : scan_maps(a, p) * 8 + (size_t)a->batch * p.chunks * 4;
+// 64-bit words of the workspace: the ticket's, then two per tile and channel, then one per group of tiles and channel
+int64_t map_words(const ScanPlan& p) { return p.chains * p.tiles * 2 * 64 * p.vec; }
+int64_t scan_words(const ScanPlan& p) {
+    return p.tiles == 0 ? 0 : 2 + map_words(p) + p.chains * ((p.tiles + klay::kGroup - 1) / klay::kGroup) * 64 * p.vec;
 }
 
-// One channel a lane after all, for arrays that two at once do not fit (the chunks stay).
+// One channel a lane after all, for arrays that two at once do not fit.
 void narrow(ScanPlan* p, const klay_scan_args* a) {
     p->vec = 1;
     p->blocks_c = (a->channels + 63) / 64;
+    p->chains = p->blocks_c * a->batch;
 }
 
 klay::ScanArgs scan_args(const klay_scan_args* a, const ScanPlan& p, void* workspace) {
@@ -235,61 +233,68 @@ klay::ScanArgs scan_args(const klay_scan_args* a, const ScanPlan& p, void* works
     g.x_batch = a->inputs_batch_stride; g.x_time = a->inputs_time_stride;
     g.time = a->time;
     g.channels = a->channels;
-    g.chunks = p.chunks; g.chunk = p.chunk; g.blocks_c = p.blocks_c;
-    if (p.chunks > 1) {
-        g.map_a = static_cast<float*>(workspace);
-        g.map_h = g.map_a + scan_maps(a, p);
-        g.map_cut = reinterpret_cast<int32_t*>(g.map_h + scan_maps(a, p));
+    g.blocks_c = p.blocks_c;
+    g.chains = (int32_t)p.chains; g.tiles = (int32_t)p.tiles;
+    if (p.tiles > 0) {
+        g.ticket = static_cast<uint32_t*>(workspace);
+        g.words = static_cast<uint64_t*>(workspace) + 2;
+        g.state_words = g.words + map_words(p);
     }
     return g;
 }
 
 template <int S, typename T, int VC, int W>
-klay_status run_scan(const klay::ScanArgs& g, int64_t batch, bool back, void* stream) {
-    const int64_t blocks = batch * g.blocks_c * g.chunks, maps = batch * g.blocks_c * (g.chunks - 1);
-    if (blocks * 64 * W > (int64_t)UINT32_MAX) return fail(KLAY_EINVAL, "klay_scan: batch times channels exceeds one launch");
-    const dim3 block(64, W);
-    if constexpr (S != klay::SEMI_MAX) {
-        if (back) {
-            if constexpr (W == 8)
-                if (maps > 0) KLAY_LAUNCH((klay::scan_back_map_kernel<S, T, VC, W>), dim3((uint32_t)maps), block, stream, g);
-            KLAY_LAUNCH((klay::scan_back_kernel<S, T, VC, W>), dim3((uint32_t)blocks), block, stream, g);
+klay_status run_scan(const klay::ScanArgs& g, const ScanPlan& p, bool back, void* stream) {
+    const dim3 block(64, W), grid((uint32_t)(p.tiles > 0 ? p.chains * p.tiles : p.chains));
+    if constexpr (W == 8) {
+        if (p.tiles > 0) {
+            if constexpr (S != klay::SEMI_MAX)
+                if (back) {
+                    KLAY_LAUNCH((klay::scan_back_chain_kernel<S, T, VC, W>), grid, block, stream, g);
+                    return KLAY_OK;
+                }
+            KLAY_LAUNCH((klay::scan_chain_kernel<S, T, VC, W>), grid, block, stream, g);
             return KLAY_OK;
         }
     }
-    if constexpr (W == 8)
-        if (maps > 0) KLAY_LAUNCH((klay::scan_map_kernel<S, T, VC, W>), dim3((uint32_t)maps), block, stream, g);
-    KLAY_LAUNCH((klay::scan_kernel<S, T, VC, W>), dim3((uint32_t)blocks), block, stream, g);
+    if constexpr (S != klay::SEMI_MAX)
+        if (back) {
+            KLAY_LAUNCH((klay::scan_back_kernel<S, T, VC, W>), grid, block, stream, g);
+            return KLAY_OK;
+        }
+    KLAY_LAUNCH((klay::scan_kernel<S, T, VC, W>), grid, block, stream, g);
     return KLAY_OK;
 }
 
 template <int S, typename T, int VC>
-klay_status run_scan(const klay::ScanArgs& g, const ScanPlan& p, int64_t batch, bool back, void* stream) {
-    if (p.waves == 1) return run_scan<S, T, VC, 1>(g, batch, back, stream);
-    if (p.waves == 4) return run_scan<S, T, VC, 4>(g, batch, back, stream);
-    return run_scan<S, T, VC, 8>(g, batch, back, stream);
+klay_status run_scan(const klay::ScanArgs& g, const ScanPlan& p, bool back, void* stream) {
+    // (a grid times its block has to stay below 2^32 threads)
+    if ((p.tiles > 0 ? p.chains * p.tiles : p.chains) * 64 * p.waves > (int64_t)UINT32_MAX)
+        return fail(KLAY_EINVAL, "klay_scan: batch times channels exceeds one launch");
+    if (p.waves == 1) return run_scan<S, T, VC, 1>(g, p, back, stream);
+    if (p.waves == 4) return run_scan<S, T, VC, 4>(g, p, back, stream);
+    return run_scan<S, T, VC, 8>(g, p, back, stream);
 }
 
 klay_status run_scan(const klay_scan_args* a, const klay::ScanArgs& g, const ScanPlan& p, bool back, void* stream) {
     using namespace klay;
-    if (a->semiring == KLAY_LOG) return run_scan<SEMI_LOG, f32, 1>(g, p, a->batch, back, stream);
-    if (a->semiring == KLAY_MAXLOG) return run_scan<SEMI_MAX, f32, 1>(g, p, a->batch, back, stream);
+    if (a->semiring == KLAY_LOG) return run_scan<SEMI_LOG, f32, 1>(g, p, back, stream);
+    if (a->semiring == KLAY_MAXLOG) return run_scan<SEMI_MAX, f32, 1>(g, p, back, stream);
     if (a->dtype == KLAY_F32)
-        return p.vec == 2 ? run_scan<SEMI_REAL, f32, 2>(g, p, a->batch, back, stream) : run_scan<SEMI_REAL, f32, 1>(g, p, a->batch, back, stream);
+        return p.vec == 2 ? run_scan<SEMI_REAL, f32, 2>(g, p, back, stream) : run_scan<SEMI_REAL, f32, 1>(g, p, back, stream);
     if (a->dtype == KLAY_BF16)
-        return p.vec == 2 ? run_scan<SEMI_REAL, bf16, 2>(g, p, a->batch, back, stream) : run_scan<SEMI_REAL, bf16, 1>(g, p, a->batch, back, stream);
-    return p.vec == 2 ? run_scan<SEMI_REAL, f16, 2>(g, p, a->batch, back, stream) : run_scan<SEMI_REAL, f16, 1>(g, p, a->batch, back, stream);
+        return p.vec == 2 ? run_scan<SEMI_REAL, bf16, 2>(g, p, back, stream) : run_scan<SEMI_REAL, bf16, 1>(g, p, back, stream);
+    return p.vec == 2 ? run_scan<SEMI_REAL, f16, 2>(g, p, back, stream) : run_scan<SEMI_REAL, f16, 1>(g, p, back, stream);
 }
 
-// What the sequences without steps leave: `to` as `from` (null: `none`).
-klay_status fill_states(float* to, const float* from, float none, int64_t count, void* stream) {
-    if (!to || count == 0) return KLAY_OK;
-    KLAY_LAUNCH(klay::scan_fill_kernel, dim3((uint32_t)std::min<int64_t>((count + 255) / 256, 4096)), dim3(256), stream, to, from, none, count);
+klay_status prepare_scan(const klay::PrepareArgs& g, void* stream) {
+    const int64_t most = std::max(std::max(g.count, g.states_count), g.words_count);
+    if (most > 0) KLAY_LAUNCH(klay::scan_prepare_kernel, dim3((uint32_t)std::min<int64_t>((most + 255) / 256, 4096)), dim3(256), stream, g);
     return KLAY_OK;
 }
 
 klay_status scan_workspace(const klay_scan_args* a, const ScanPlan& p, const void* workspace, size_t bytes, const char* who) {
-    const size_t need = scan_bytes(a, p);
+    const size_t need = (size_t)scan_words(p) * sizeof(uint64_t);
     if (need && (!workspace || bytes < need))
         return fail(KLAY_ENOMEM, std::string(who) + ": workspace too small: need " + std::to_string(need) + " bytes");
     if (need && reinterpret_cast<uintptr_t>(workspace) % 16)
@@ -363,7 +368,7 @@ klay_status klay_tokens_backward(const klay_tokens_args* a, const float* stats, 
 
 size_t klay_scan_workspace_bytes(const klay_scan_args* a) {
     if (!a || a->batch < 1 || a->time < 1 || a->channels < 1 || !known_dtype(a->dtype)) return 0;
-    return scan_bytes(a, scan_plan(a));
+    return (size_t)scan_words(scan_plan(a)) * sizeof(uint64_t);
 }
 
 klay_status klay_scan_forward(const klay_scan_args* a, void* states, float* final, void* workspace, size_t workspace_bytes, void* stream) {
@@ -377,12 +382,23 @@ klay_status klay_scan_forward(const klay_scan_args* a, void* states, float* fina
     if (st != KLAY_OK) return st;
     OnDevice on(a->device);
     KLAY_HIP(on.status);
-    const float none = a->semiring == KLAY_REAL ? 0.0f : -INFINITY;
-    const int64_t ends = final ? sequences * a->channels : 0;
-    if (!rows) return fill_states(final, a->initial, none, ends, stream);
-    if (a->offsets)
-        KLAY_LAUNCH(klay::scan_rows_kernel, dim3((uint32_t)std::min<int64_t>((std::max(a->time, ends) + 255) / 256, 4096)), dim3(256), stream,
-                    a->row_info, a->offsets, a->time, (int32_t)a->sequences, final, a->initial, none, ends);
+    klay::PrepareArgs prepare{};
+    prepare.none = a->semiring == KLAY_REAL ? 0.0f : -INFINITY;
+    if (final && (a->offsets || !rows)) {
+        prepare.states = final;
+        prepare.from = a->initial;
+        prepare.states_count = sequences * a->channels;
+    }
+    if (rows && a->offsets) {
+        prepare.rows = a->row_info;
+        prepare.offsets = a->offsets;
+        prepare.count = a->time;
+        prepare.sequences = (int32_t)a->sequences;
+    }
+    prepare.words = static_cast<uint64_t*>(workspace);
+    prepare.words_count = scan_words(p);
+    st = prepare_scan(prepare, stream);
+    if (st != KLAY_OK || !rows) return st;
     if (!aligned_to(2 * dtype_bytes(a->dtype), {states})) narrow(&p, a);
     klay::ScanArgs g = scan_args(a, p, workspace);
     g.out = states;
@@ -403,10 +419,16 @@ klay_status klay_scan_backward(const klay_scan_args* a, const void* states, cons
     if (st != KLAY_OK) return st;
     OnDevice on(a->device);
     KLAY_HIP(on.status);
-    if (a->offsets || !rows) {
-        st = fill_states(dinitial, dfinal, 0.0f, sequences * a->channels, stream);
-        if (st != KLAY_OK || !rows) return st;
+    klay::PrepareArgs prepare{};
+    if (dinitial && (a->offsets || !rows)) {
+        prepare.states = dinitial;
+        prepare.from = dfinal;
+        prepare.states_count = sequences * a->channels;
     }
+    prepare.words = static_cast<uint64_t*>(workspace);
+    prepare.words_count = scan_words(p);
+    st = prepare_scan(prepare, stream);
+    if (st != KLAY_OK || !rows) return st;
     if (!aligned_to(2 * dtype_bytes(a->dtype), {states, dstates, dgates, dinputs})) narrow(&p, a);
     klay::ScanArgs g = scan_args(a, p, workspace);
     g.h = states;
