@@ -89,11 +89,15 @@ TokenPlan forward_plan(const klay_tokens_args* a) {
     return in_parts(a, 1024, bytes <= 512 * 1024 ? 1 : std::min<int64_t>((bytes + 262143) / 262144, klay::kMaxParts));
 }
 
-// The gradient's parts need no joining: as many as give the chip four workgroups per CU, of eight kilobytes or more.
+// The gradient's parts need no joining: workgroups of kBackPart bytes, or less where there would be fewer than four per CU.  (Reads and
+// writes together go faster the smaller the stretch that all workgroups are on: 4096 x 131072 bf16, whole rows / 64 / 32 / 16 KB, 416 / 382 / 352 /
+// 361 us; a plain copy, 256 / 16 KB, 5.3 / 6.1 TB/s.)
+constexpr int64_t kBackPart = 32768;
 TokenPlan backward_plan(const klay_tokens_args* a) {
     const int64_t bytes = (int64_t)a->vocab * dtype_bytes(a->dtype);
-    if (a->rows >= kManyRows) return in_parts(a, bytes <= kWaveRow ? 64 : 256, 1);
-    return in_parts(a, 256, std::min<int64_t>((4 * kComputeUnits + a->rows - 1) / a->rows, (bytes + 8191) / 8192));
+    if (a->rows >= kManyRows && bytes <= kWaveRow) return in_parts(a, 64, 1);
+    const int64_t few = std::min<int64_t>((4 * kComputeUnits + a->rows - 1) / a->rows, (bytes + 8191) / 8192);
+    return in_parts(a, 256, std::max<int64_t>(few, (bytes + kBackPart - 1) / kBackPart));
 }
 
 size_t token_lists_at(int64_t rows, int32_t parts) { return (size_t)rows * parts * 4 * sizeof(float); }

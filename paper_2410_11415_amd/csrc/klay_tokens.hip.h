@@ -692,7 +692,7 @@ __device__ __forceinline__ BulkGrad bulk_grad(const RowStats& s, float others, f
 // A workgroup per row part, as forward.
 template <typename T, int THREADS>
 __global__ void __launch_bounds__(THREADS) token_back_kernel(TokenArgs g) {
-    constexpr int N = 16 / sizeof(T);
+    constexpr int N = 16 / sizeof(T), U = 4;
     __shared__ TokenGrad grads[kMaxTokens];
     __shared__ float scratch[2 * kScratch];
     const int32_t tid = threadIdx.x, K = g.num_tokens;
@@ -703,6 +703,11 @@ __global__ void __launch_bounds__(THREADS) token_back_kernel(TokenArgs g) {
         T* out = static_cast<T*>(g.dlogits) + r * g.vocab;
         const int32_t lo = part * g.part, hi = g.vocab - lo < g.part ? g.vocab : lo + g.part;
         const Share<N, THREADS> share(out + lo, lo, hi);
+        // the first vectors come while the adjoints are looked at (of a row without any in vain)
+        Raw<T, N> next[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (u * THREADS + tid < share.vectors) next[u] = stream_raw<N>(row + share.at(u, tid));
         const RowStats s = g.stats[r];
         float others = 0.0f, asked = 0.0f;
         for (int32_t k = tid; k < K; k += THREADS) {
@@ -713,17 +718,25 @@ __global__ void __launch_bounds__(THREADS) token_back_kernel(TokenArgs g) {
         }
         block_sum2<THREADS>(others, asked, scratch);
         const float h = g.dentropy ? g.dentropy[r] : 0.0f;
-        // a row that nothing was asked of, or that allows nothing, has no gradient, and is not read (it may hold anything)
+        // a row that nothing was asked of, or that allows nothing, has no gradient, whatever it holds
         const bool live = s.max != -INFINITY && (asked > 0.0f || h != 0.0f);
         const BulkGrad bulk = bulk_grad(s, others, h);
         if (live) {
-            for (int32_t i = 0; i * THREADS + tid < share.vectors; ++i) {
-                const int32_t j = share.at(i, tid);
-                const Raw<T, N> from = stream_raw<N>(row + j);
-                float x[N];
+            for (int32_t i = 0; i * THREADS + tid < share.vectors; i += U) {
+                Raw<T, N> now[U];
 #pragma unroll
-                for (int q = 0; q < N; ++q) x[q] = bulk.at(piece<N, T>(from, q));
-                stream_elements<N>(out + j, x);
+                for (int u = 0; u < U; ++u) now[u] = next[u];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if ((i + U + u) * THREADS + tid < share.vectors) next[u] = stream_raw<N>(row + share.at(i + U + u, tid));
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if ((i + u) * THREADS + tid >= share.vectors) break;
+                    float x[N];
+#pragma unroll
+                    for (int q = 0; q < N; ++q) x[q] = bulk.at(piece<N, T>(now[u], q));
+                    stream_elements<N>(out + share.at(i + u, tid), x);
+                }
             }
             if (tid < share.head()) out[share.lo + tid] = (T)bulk.at((float)row[share.lo + tid]);
             if (tid < share.tail()) out[share.full + tid] = (T)bulk.at((float)row[share.full + tid]);

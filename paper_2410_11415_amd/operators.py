@@ -102,7 +102,10 @@ def _tokens_forward(logits, tokens, complement, entropy, top, keep):
 
 def _copies(used, given):
     """used, if some of it is a copy and has to be kept beside what autograd saves; else None"""
-    return None if all(u is g for u, g in zip(used, given)) else used
+    for u, g in zip(used, given):
+        if u is not g:
+            return used
+    return None
 
 
 class _TokenLogprobs(torch.autograd.Function):
@@ -112,7 +115,8 @@ class _TokenLogprobs(torch.autograd.Function):
         ctx.copies = _copies(alive, (logits, tokens))
         ctx.save_for_backward(logits, tokens, stats)
         ctx.set_materialize_grads(False)
-        ctx.mark_non_differentiable(*[t for t in out[3:] if t is not None])
+        if top:
+            ctx.mark_non_differentiable(*out[3:])
         return tuple(out)
 
     @staticmethod
