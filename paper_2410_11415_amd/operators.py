@@ -108,11 +108,16 @@ def _copies(used, given):
     return None
 
 
+def _places(*tensors):
+    """Where tensors are and how they lie: what args made for them stay good for."""
+    return [None if t is None else (t.data_ptr(), t.stride()) for t in tensors]
+
+
 class _TokenLogprobs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, tokens, complement, entropy, top):
         *out, stats, ctx.args, alive = _tokens_forward(logits, tokens, complement, entropy, top, True)
-        ctx.copies = _copies(alive, (logits, tokens))
+        ctx.copies, ctx.places = _copies(alive, (logits, tokens)), _places(logits, tokens)
         ctx.save_for_backward(logits, tokens, stats)
         ctx.set_materialize_grads(False)
         if top:
@@ -125,7 +130,7 @@ class _TokenLogprobs(torch.autograd.Function):
         logits, tokens, stats = ctx.saved_tensors
         dlogp, dneg, dentropy = (None if t is None else t.contiguous() for t in (dlogp, dneg, dentropy))
         args, alive = ctx.args, ctx.copies
-        if alive is None and (args.logits or 0, args.tokens or 0) != (logits.data_ptr(), 0 if tokens is None else tokens.data_ptr()):
+        if alive is None and ctx.places != _places(logits, tokens):
             args, alive = _token_args(logits, tokens, 0)            # what was saved has been put elsewhere
         dlogits = logits.new_empty(logits.shape)
         _b.klay_tokens_backward(args, stats.data_ptr(), _ptr(dlogp), _ptr(dneg), _ptr(dentropy), dlogits.data_ptr(),
@@ -210,8 +215,10 @@ class _GatedScan(torch.autograd.Function):
     def forward(ctx, gates, inputs, initial, semiring, offsets):
         states, final, row_info, ctx.args, alive = _scan_forward(gates, inputs, initial, semiring, offsets)
         ctx.semiring, ctx.copies = semiring, _copies(alive, (gates, inputs, initial))
-        # (the reverse sweep of the real semiring does not read the inputs)
-        ctx.save_for_backward(gates, inputs if semiring == KLAY_LOG else None, initial, offsets, row_info, states)
+        if semiring != KLAY_LOG:
+            inputs = None                                           # not read by the reverse sweep
+        ctx.places = _places(gates, inputs, initial, offsets, row_info)
+        ctx.save_for_backward(gates, inputs, initial, offsets, row_info, states)
         ctx.set_materialize_grads(False)
         return states, final
 
@@ -222,9 +229,7 @@ class _GatedScan(torch.autograd.Function):
         if dstates is None and dfinal is None:
             return None, None, None, None, None
         args, alive = ctx.args, ctx.copies
-        now = [0 if t is None else t.data_ptr() for t in (gates, inputs, initial, offsets, row_info)]
-        then = [p or 0 for p in (args.gates, args.inputs if inputs is not None else 0, args.initial, args.offsets, args.row_info)]
-        if alive is None and now != then:                           # what was saved has been put elsewhere
+        if alive is None and ctx.places != _places(gates, inputs, initial, offsets, row_info):      # what was saved has been put elsewhere
             args, alive = _scan_args(gates, gates if inputs is None else inputs, initial, ctx.semiring, offsets, row_info)
         dstates, dfinal = (None if t is None else t.contiguous() for t in (dstates, dfinal))
         dgates, dinputs = (gates.new_empty(gates.shape) if need else None for need in ctx.needs_input_grad[:2])

@@ -134,6 +134,29 @@ def test_leading_axes():
     assert torch.equal(one.logp, whole.logp[1, 2]) and torch.equal(one.entropy, whole.entropy[1, 2])
 
 
+def test_saved_tensors_that_come_back_with_other_strides():
+    """what autograd saved may lie in the same place another way (hooks that keep it elsewhere meanwhile)"""
+    x = torch.randn(40, 300, device="cuda")
+    tokens = torch.randint(0, 300, (40, 2), device="cuda")
+    results = []
+    for moved in (False, True):
+        base = torch.zeros((40, 310), device="cuda")
+        base[:, :300] = x
+        logits = base[:, :300].requires_grad_(True)
+
+        def unpack(t):
+            if not moved or t.data_ptr() != logits.data_ptr():
+                return t
+            flat = base.detach().flatten()[:x.numel()]
+            flat.copy_(x.flatten())
+            return flat.view(x.shape)
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t, unpack):
+            out = klay().token_logprobs(logits, tokens).logp
+        results.append(torch.autograd.grad(out.sum(), logits)[0])
+    # (rows from other addresses are summed in another order: the shares differ by the roundings of a sum of at most 300 terms)
+    assert (results[0] - results[1]).abs().max() <= 600 * 2.0 ** -24
+
+
 def test_nothing_to_do():
     k = klay()
     r = k.token_logprobs(torch.empty((0, 9), device="cuda", requires_grad=True), torch.empty((0, 2), dtype=torch.int64, device="cuda"), top=3)
