@@ -404,6 +404,8 @@ klay_status klay_tokens_backward(const klay_tokens_args* args, const float* stat
  *   states      device [batch, time, channels] of `dtype`, contiguous: h, each rounded once from fp32
  *   final       device fp32 [batch or sequences, channels]: the states behind the last steps (of an empty sequence: its initial one); or NULL
  *   workspace   device, 16-byte aligned, klay_scan_workspace_bytes(args) bytes (for either direction); NULL where that is 0
+ * Sums are in single.  Products of many gates may leave its range where the states themselves do not (gates above 1 behind a state of 0).
+ * A state that is NaN or infinite (in the log domain: +inf) makes all behind it in its sequence and channel NaN or infinite.
  * Offsets that are none (descending, out of range) give undefined values, but no access outside the arrays.
  * Errors: KLAY_EINVAL, KLAY_ENOMEM (workspace too small), KLAY_EHIP.
  */

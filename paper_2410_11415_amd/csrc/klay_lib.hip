@@ -250,7 +250,7 @@ klay::ScanArgs scan_args(const klay_scan_args* a, const ScanPlan& p, void* works
 template <int S, typename T, int VC, int W>
 klay_status run_scan(const klay::ScanArgs& g, const ScanPlan& p, bool back, void* stream) {
     const dim3 block(64, W), grid((uint32_t)(p.tiles > 0 ? p.chains * p.tiles : p.chains));
-    if constexpr (W == 8) {
+    if constexpr (W == 8 && (VC == 1 || sizeof(T) == 2)) {
         if (p.tiles > 0) {
             if constexpr (S != klay::SEMI_MAX)
                 if (back) {
@@ -310,7 +310,8 @@ template <int S, typename T>
 klay_status run_step(const klay::StepArgs& g, bool wide, void* stream) {
     constexpr int VC = 4;
     const int64_t lanes = wide ? g.channels / VC : g.channels;
-    const dim3 grid((uint32_t)((lanes + 255) / 256), (uint32_t)std::min<int64_t>(g.batch, 65535));
+    const int64_t across = (lanes + 255) / 256;                                       // (a workgroup takes every grid.y-th row)
+    const dim3 grid((uint32_t)across, (uint32_t)std::min<int64_t>(g.batch, std::max<int64_t>(65535 / across, 1)));
     if (wide) KLAY_LAUNCH((klay::step_kernel<S, T, VC>), grid, dim3(256), stream, g);
     else KLAY_LAUNCH((klay::step_kernel<S, T, 1>), grid, dim3(256), stream, g);
     return KLAY_OK;

@@ -48,6 +48,22 @@ template <int S> struct Ring {
     }
 };
 
+// A map's factor A may leave the range of its type where the states do not (gates above 1 behind a state of 0; a large state that falls by 2^-150 and
+// rises again).  So in the real ring it is a * 2^e: for the steps of a wave e = 0 and a is A itself unless that is out of range, from
+// there on 1/2 <= |a| < 1 or a = 0.  (The sums of a log-domain ring need no such thing.)
+template <int S> __device__ __forceinline__ void times_scaled(float& a, int32_t& e, float by, int32_t by_e) {
+    a = Ring<S>::times(by, a);
+    if constexpr (S == SEMI_REAL) {
+        e += by_e + __builtin_amdgcn_frexp_expf(a);
+        a = __builtin_amdgcn_frexp_mantf(a);
+    }
+}
+template <int S> __device__ __forceinline__ float step_scaled(float a, int32_t e, float h, float x) {
+    if constexpr (S == SEMI_REAL) return __builtin_ldexpf(a * h, e) + x;
+    return Ring<S>::step(a, h, x);
+}
+constexpr float kLeastFactor = 0x1p-100f;        // (with room above the smallest number for the products it goes into)
+
 // What a row of the time axis is to its sequence.
 enum : int { ROW_FIRST = 1, ROW_LAST = 2 };
 constexpr int kDeadRow = -1;        // behind the last sequence (or before the first)
@@ -143,19 +159,79 @@ __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// The map of a wave's steps.
+enum Kind : int32_t { PLAIN, CUT, SCALED };     // CUT: h does not depend on what comes in (a sequence starts in the steps);  SCALED: some e != 0
+template <int VC> struct Map {
+    float a[VC], h[VC], least[VC];              // least: the smallest |product| on the way to a
+    int32_t e[VC];
+    Kind kind;
+    // From the product as it was multiplied: is it right?  If not, by mantissas and exponents.
+    template <typename T>
+    __device__ __forceinline__ void scale(const Raw<T, VC> (&gates)[kSteps]) {
+        bool right = true;
+#pragma unroll
+        for (int v = 0; v < VC; ++v) right = right && least[v] >= kLeastFactor && fabsf(a[v]) < INFINITY;
+        if (__ballot(!right) == 0) return;
+        bool fits = true;
+#pragma unroll
+        for (int v = 0; v < VC; ++v) {
+            a[v] = 1.0f;
+            e[v] = 0;
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const float gate = piece<VC, T>(gates[i], v);
+                a[v] *= __builtin_amdgcn_frexp_mantf(gate);
+                e[v] += __builtin_amdgcn_frexp_expf(gate);
+            }
+            int32_t zero = 0;
+            times_scaled<SEMI_REAL>(a[v], zero, 1.0f, 0);
+            e[v] = a[v] == 0.0f ? 0 : e[v] + zero;
+            fits = fits && e[v] > -100 && e[v] <= 128;
+        }
+        if (__ballot(!fits) == 0) {             // (gates of 0, most of the time)
+#pragma unroll
+            for (int v = 0; v < VC; ++v) {
+                a[v] = __builtin_ldexpf(a[v], e[v]);
+                e[v] = 0;
+            }
+        } else {
+            kind = SCALED;
+        }
+    }
+};
+
 // The maps of the W waves of a tile.  Two sets in turn: a wave may write the next tile's while another still reads these.
 template <int VC, int W> struct Maps {
     float a[2][W][64][VC], h[2][W][64][VC];
-    int32_t cut[2][W];
-    __device__ __forceinline__ void put(int turn, int wave, const float (&A)[VC], const float (&H)[VC], bool is_cut) {
+    int32_t e[2][W][64][VC], kind[2][W];        // e is written and read where some map of the tile is SCALED
+    __device__ __forceinline__ void put(int turn, int wave, const Map<VC>& m) {
         const int lane = threadIdx.x;
 #pragma unroll
-        for (int v = 0; v < VC; ++v) { a[turn][wave][lane][v] = A[v]; h[turn][wave][lane][v] = H[v]; }
-        if (lane == 0) cut[turn][wave] = is_cut;
+        for (int v = 0; v < VC; ++v) { a[turn][wave][lane][v] = m.a[v]; h[turn][wave][lane][v] = m.h[v]; }
+        if (m.kind == SCALED)
+#pragma unroll
+            for (int v = 0; v < VC; ++v) e[turn][wave][lane][v] = m.e[v];
+        if (lane == 0) kind[turn][wave] = m.kind;
     }
-    __device__ __forceinline__ uint64_t cuts(int turn) const {
+    // bit w: wave w's map is of that kind
+    __device__ __forceinline__ uint64_t are(int turn, Kind which) const {
         const int lane = threadIdx.x;
-        return __ballot(lane < W && cut[turn][lane < W ? lane : 0] != 0);
+        return __ballot(lane < W && kind[turn][lane < W ? lane : 0] == which);
+    }
+    // The state behind wave w's steps, from the one in front of them.
+    template <int S>
+    __device__ __forceinline__ void pass(float (&state)[VC], int turn, int w, uint64_t cuts, uint64_t scaled) const {
+        const int lane = threadIdx.x;
+#pragma unroll
+        for (int v = 0; v < VC; ++v) {
+            const float A = a[turn][w][lane][v], H = h[turn][w][lane][v];
+            const float h0 = state[v];
+            state[v] = Ring<S>::step(A, h0, H);
+            if ((cuts | scaled) != 0) {
+                if (scaled >> w & 1) state[v] = step_scaled<S>(A, e[turn][w][lane][v], h0, H);
+                if (cuts >> w & 1) state[v] = H;
+            }
+        }
     }
 };
 
@@ -167,7 +243,8 @@ template <int VC, int W> struct Maps {
 // taken up by ticket, a tile waits only for words of tiles with lower tickets, whose workgroups are running then, and a workgroup
 // publishes its map before it waits for anything.
 constexpr int kGroup = 16;
-constexpr uint32_t kMap = 1, kCut = 2;      // a value; an H that does not depend on what comes in (a sequence starts in the tile)
+// (tags: of an H, kMap, or kCut where it does not depend on what comes in; of an A, kMap + its exponent)
+constexpr uint32_t kMap = 1u << 30, kCut = 2u << 30;
 __device__ __forceinline__ void publish(uint64_t* word, float value, uint32_t tag) {
     __hip_atomic_store(word, (uint64_t)tag << 32 | __float_as_uint(value), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
@@ -197,7 +274,7 @@ __device__ __forceinline__ uint32_t take_tile(const ScanArgs& g, uint32_t* share
 // What the waves of a tile share besides their own maps: those of the tiles before it in the group, and the state in front of the tile.
 template <int VC> struct Before {
     float a[kGroup - 1][64][VC], h[kGroup - 1][64][VC], state[64][VC];
-    int32_t cut[kGroup - 1];
+    int32_t e[kGroup - 1][64][VC], cut[kGroup - 1];
     uint32_t ticket;
 };
 
@@ -208,23 +285,22 @@ __device__ __forceinline__ void state_of_wave(float (&h)[VC], Maps<VC, W>& maps,
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.y), lane = threadIdx.x;
     const int32_t group = q / kGroup, inside = q - group * kGroup;
     lds_barrier();
-    const uint64_t cuts = maps.cuts(0);
+    const uint64_t cuts = maps.are(0, CUT), scaled = S == SEMI_REAL ? maps.are(0, SCALED) : 0;
     float A[VC], H[VC];                     // wave 0: the tile's map
+    int32_t E[VC];
     if (wave == 0) {
 #pragma unroll
-        for (int v = 0; v < VC; ++v) { A[v] = Ring<S>::one; H[v] = Ring<S>::zero(); }
+        for (int v = 0; v < VC; ++v) { A[v] = Ring<S>::one; H[v] = Ring<S>::zero(); E[v] = 0; }
 #pragma unroll
         for (int k = 0; k < W; ++k) {
             const int w = BACK ? W - 1 - k : k;
+            maps.template pass<S>(H, 0, w, cuts, scaled);
 #pragma unroll
-            for (int v = 0; v < VC; ++v) {
-                H[v] = cuts >> w & 1 ? maps.h[0][w][lane][v] : Ring<S>::step(maps.a[0][w][lane][v], H[v], maps.h[0][w][lane][v]);
-                A[v] = Ring<S>::times(maps.a[0][w][lane][v], A[v]);
-            }
+            for (int v = 0; v < VC; ++v) times_scaled<S>(A[v], E[v], maps.a[0][w][lane][v], scaled >> w & 1 ? maps.e[0][w][lane][v] : 0);
         }
 #pragma unroll
         for (int v = 0; v < VC; ++v) {
-            publish(map_word<VC>(g, chain, q, 1) + v, A[v], kMap);
+            publish(map_word<VC>(g, chain, q, 1) + v, A[v], kMap + (uint32_t)E[v]);
             publish(map_word<VC>(g, chain, q, 0) + v, H[v], cuts ? kCut : kMap);
         }
     }
@@ -242,22 +318,28 @@ __device__ __forceinline__ void state_of_wave(float (&h)[VC], Maps<VC, W>& maps,
             __builtin_amdgcn_s_sleep(2);
         }
 #pragma unroll
-        for (int v = 0; v < VC; ++v) { before.h[j][lane][v] = value_of(w0[v]); before.a[j][lane][v] = value_of(w1[v]); }
+        for (int v = 0; v < VC; ++v) {
+            before.h[j][lane][v] = value_of(w0[v]);
+            before.a[j][lane][v] = value_of(w1[v]);
+            before.e[j][lane][v] = (int32_t)(tag_of(w1[v]) - kMap);
+        }
         if (lane == 0) before.cut[j] = tag_of(w0[0]) == kCut;
     }
     lds_barrier();
     if (wave == 0) {
         const uint64_t cut_before = __ballot(lane < inside && before.cut[lane < inside ? lane : 0] != 0);
         float a[VC], b[VC];
+        int32_t e[VC];
 #pragma unroll
-        for (int v = 0; v < VC; ++v) { a[v] = Ring<S>::one; b[v] = Ring<S>::zero(); }
+        for (int v = 0; v < VC; ++v) { a[v] = Ring<S>::one; b[v] = Ring<S>::zero(); e[v] = 0; }
 #pragma unroll 5
         for (int32_t j = 0; j < inside; ++j)
 #pragma unroll
             for (int v = 0; v < VC; ++v) {
                 const float aj = before.a[j][lane][v], hj = before.h[j][lane][v];
-                b[v] = cut_before >> j & 1 ? hj : Ring<S>::step(aj, b[v], hj);
-                a[v] = Ring<S>::times(aj, a[v]);
+                const int32_t ej = before.e[j][lane][v];
+                b[v] = cut_before >> j & 1 ? hj : step_scaled<S>(aj, ej, b[v], hj);
+                times_scaled<S>(a[v], e[v], aj, ej);
             }
         if (cut_before == 0) {
             float front[VC];
@@ -275,11 +357,11 @@ __device__ __forceinline__ void state_of_wave(float (&h)[VC], Maps<VC, W>& maps,
                 __builtin_amdgcn_s_sleep(1);
             }
 #pragma unroll
-            for (int v = 0; v < VC; ++v) b[v] = Ring<S>::step(a[v], front[v], b[v]);
+            for (int v = 0; v < VC; ++v) b[v] = step_scaled<S>(a[v], e[v], front[v], b[v]);
         }
         if (inside == kGroup - 1 && q + 1 < g.tiles)
 #pragma unroll
-            for (int v = 0; v < VC; ++v) publish(state_word<VC>(g, chain, group + 1) + v, cuts ? H[v] : Ring<S>::step(A[v], b[v], H[v]), kMap);
+            for (int v = 0; v < VC; ++v) publish(state_word<VC>(g, chain, group + 1) + v, cuts ? H[v] : step_scaled<S>(A[v], E[v], b[v], H[v]), kMap);
 #pragma unroll
         for (int v = 0; v < VC; ++v) before.state[lane][v] = b[v];
     }
@@ -290,9 +372,7 @@ __device__ __forceinline__ void state_of_wave(float (&h)[VC], Maps<VC, W>& maps,
     for (int k = 0; k < W; ++k) {
         const int w = BACK ? W - 1 - k : k;
         if (BACK ? w <= wave : w >= wave) break;
-#pragma unroll
-        for (int v = 0; v < VC; ++v)
-            h[v] = cuts >> w & 1 ? maps.h[0][w][lane][v] : Ring<S>::step(maps.a[0][w][lane][v], h[v], maps.h[0][w][lane][v]);
+        maps.template pass<S>(h, 0, w, cuts, scaled);
     }
 }
 
@@ -316,22 +396,26 @@ template <int S, typename T, int VC> struct Tile {
                 x[i] = all_pieces<VC, T>(Ring<S>::zero());
             }
     }
-    // the map of the steps, (A, H) before them; whether a sequence starts in them
-    __device__ __forceinline__ bool map(float (&A)[VC], float (&H)[VC], const ScanArgs& g, const Place& at) const {
-        return rows.plain() ? map_steps<true>(A, H, g, at) : map_steps<false>(A, H, g, at);
+    __device__ __forceinline__ void map(Map<VC>& m, const ScanArgs& g, const Place& at) const {
+        if (rows.plain()) map_steps<true>(m, g, at);
+        else map_steps<false>(m, g, at);
+        if (S == SEMI_REAL && m.kind != CUT) m.template scale<T>(a);
     }
-    template <bool PLAIN> __device__ __forceinline__ bool map_steps(float (&A)[VC], float (&H)[VC], const ScanArgs& g, const Place& at) const {
+    template <bool PLAIN> __device__ __forceinline__ void map_steps(Map<VC>& m, const ScanArgs& g, const Place& at) const {
+        m.kind = !PLAIN && rows.first != 0 ? CUT : Kind::PLAIN;
+#pragma unroll
+        for (int v = 0; v < VC; ++v) { m.a[v] = Ring<S>::one; m.h[v] = Ring<S>::zero(); m.least[v] = INFINITY; m.e[v] = 0; }
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            if (!PLAIN && (rows.first >> i & 1)) load_state<VC>(H, g.initial, rows.sequence(g, i), g, at, Ring<S>::zero());
+            if (!PLAIN && (rows.first >> i & 1)) load_state<VC>(m.h, g.initial, rows.sequence(g, i), g, at, Ring<S>::zero());
 #pragma unroll
             for (int v = 0; v < VC; ++v) {
                 const float av = piece<VC, T>(a[i], v);
-                H[v] = Ring<S>::step(av, H[v], piece<VC, T>(x[i], v));
-                A[v] = Ring<S>::times(av, A[v]);
+                m.h[v] = Ring<S>::step(av, m.h[v], piece<VC, T>(x[i], v));
+                m.a[v] = Ring<S>::times(av, m.a[v]);
+                if constexpr (S == SEMI_REAL) m.least[v] = fminf(m.least[v], fabsf(m.a[v]));
             }
         }
-        return !PLAIN && rows.first != 0;
     }
     // the steps themselves, from the state h
     template <bool PLAIN> __device__ __forceinline__ void walk(float (&h)[VC], const ScanArgs& g, int64_t t, int64_t end, const Place& at) const {
@@ -358,7 +442,7 @@ template <int S, typename T, int VC> struct Tile {
 template <int S, typename T, int VC, int W>
 __global__ void __launch_bounds__(64 * W) scan_kernel(ScanArgs g) {
     __shared__ Maps<VC, W> maps;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.y), lane = threadIdx.x;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.y);
     const Place at = place_of<VC>(g, blockIdx.x);
     const int64_t end = g.time;
     Tile<S, T, VC> next;
@@ -372,22 +456,22 @@ __global__ void __launch_bounds__(64 * W) scan_kernel(ScanArgs g) {
         Tile<S, T, VC> now = next;
         if (tile + W * kSteps < end) next.load(g, t + W * kSteps, end, at);
         now.resolve(g, t, end);
-        float A[VC], H[VC], h[VC];
+        float h[VC];
 #pragma unroll
-        for (int v = 0; v < VC; ++v) { A[v] = Ring<S>::one; H[v] = Ring<S>::zero(); h[v] = carry[v]; }
+        for (int v = 0; v < VC; ++v) h[v] = carry[v];
         if constexpr (W > 1) {
-            const bool cut = now.map(A, H, g, at);
-            maps.put(turn, wave, A, H, cut);
+            Map<VC> m;
+            now.map(m, g, at);
+            maps.put(turn, wave, m);
             lds_barrier();
-            const uint64_t cuts = maps.cuts(turn);
+            const uint64_t cuts = maps.are(turn, CUT), scaled = S == SEMI_REAL ? maps.are(turn, SCALED) : 0;
 #pragma unroll
-            for (int w = 0; w < W; ++w)
+            for (int w = 0; w < W; ++w) {
 #pragma unroll
-                for (int v = 0; v < VC; ++v) {
+                for (int v = 0; v < VC; ++v)
                     if (w == wave) h[v] = carry[v];
-                    carry[v] = Ring<S>::step(maps.a[turn][w][lane][v], carry[v], maps.h[turn][w][lane][v]);
-                    if (cuts != 0 && (cuts >> w & 1)) carry[v] = maps.h[turn][w][lane][v];
-                }
+                maps.template pass<S>(carry, turn, w, cuts, scaled);
+            }
         }
         if (now.rows.plain()) now.template walk<true>(h, g, t, end, at);
         else now.template walk<false>(h, g, t, end, at);
@@ -410,11 +494,12 @@ __global__ void __launch_bounds__(64 * W) scan_chain_kernel(ScanArgs g) {
     Tile<S, T, VC> now;
     now.load(g, t, end, at);
     now.resolve(g, t, end);
-    float A[VC], H[VC], h[VC];
-#pragma unroll
-    for (int v = 0; v < VC; ++v) { A[v] = Ring<S>::one; H[v] = Ring<S>::zero(); }
-    const bool cut = now.map(A, H, g, at);
-    maps.put(0, wave, A, H, cut);
+    float h[VC];
+    {
+        Map<VC> m;
+        now.map(m, g, at);
+        maps.put(0, wave, m);
+    }
     state_of_wave<S, VC, W, false>(h, maps, before, g, chain, q);
     if (now.rows.plain()) now.template walk<true>(h, g, t, end, at);
     else now.template walk<false>(h, g, t, end, at);
@@ -498,21 +583,26 @@ template <int S, typename T, int VC> struct BackTile {
                 }
         }
     }
-    __device__ __forceinline__ bool map(float (&A)[VC], float (&C)[VC], const ScanArgs& g, const Place& at) const {
-        return rows.plain() ? map_steps<true>(A, C, g, at) : map_steps<false>(A, C, g, at);
+    __device__ __forceinline__ void map(Map<VC>& m, const ScanArgs& g, const Place& at) const {
+        if (rows.plain()) map_steps<true>(m, g, at);
+        else map_steps<false>(m, g, at);
+        if (m.kind != CUT) m.template scale<T>(a);
     }
-    template <bool PLAIN> __device__ __forceinline__ bool map_steps(float (&A)[VC], float (&C)[VC], const ScanArgs& g, const Place& at) const {
+    template <bool PLAIN> __device__ __forceinline__ void map_steps(Map<VC>& m, const ScanArgs& g, const Place& at) const {
+        m.kind = !PLAIN && rows.last != 0 ? CUT : Kind::PLAIN;
+#pragma unroll
+        for (int v = 0; v < VC; ++v) { m.a[v] = 1.0f; m.h[v] = 0.0f; m.least[v] = INFINITY; m.e[v] = 0; }
 #pragma unroll
         for (int i = kSteps - 1; i >= 0; --i) {
-            if (!PLAIN && (rows.last >> i & 1)) load_state<VC>(C, g.dfinal, rows.sequence(g, i), g, at, 0.0f);
+            if (!PLAIN && (rows.last >> i & 1)) load_state<VC>(m.h, g.dfinal, rows.sequence(g, i), g, at, 0.0f);
 #pragma unroll
             for (int v = 0; v < VC; ++v) {
                 const float w = piece<VC, T>(a[i], v);
-                C[v] = w * (piece<VC, T>(d[i], v) + C[v]);
-                A[v] *= w;
+                m.h[v] = w * (piece<VC, T>(d[i], v) + m.h[v]);
+                m.a[v] *= w;
+                m.least[v] = fminf(m.least[v], fabsf(m.a[v]));
             }
         }
-        return !PLAIN && rows.last != 0;
     }
     // the steps themselves, from the last to the first, from the adjoint c of the state behind them
     template <bool PLAIN> __device__ __forceinline__ void walk(float (&c)[VC], const ScanArgs& g, int64_t t, int64_t end, const Place& at) const {
@@ -554,7 +644,7 @@ template <int S, typename T, int VC> struct BackTile {
 template <int S, typename T, int VC, int W>
 __global__ void __launch_bounds__(64 * W) scan_back_kernel(ScanArgs g) {
     __shared__ Maps<VC, W> maps;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.y), lane = threadIdx.x;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.y);
     const Place at = place_of<VC>(g, blockIdx.x);
     const int64_t end = g.time;
     const bool need_h = S == SEMI_LOG || g.da;
@@ -570,22 +660,22 @@ __global__ void __launch_bounds__(64 * W) scan_back_kernel(ScanArgs g) {
         BackTile<S, T, VC> now = next;
         if (n > 0) next.load(g, t - W * kSteps, end, at, need_h);
         now.resolve(g, t, end, at);
-        float A[VC], C[VC], c[VC];
+        float c[VC];
 #pragma unroll
-        for (int v = 0; v < VC; ++v) { A[v] = 1.0f; C[v] = 0.0f; c[v] = carry[v]; }
+        for (int v = 0; v < VC; ++v) c[v] = carry[v];
         if constexpr (W > 1) {
-            const bool cut = now.map(A, C, g, at);
-            maps.put(turn, wave, A, C, cut);
+            Map<VC> m;
+            now.map(m, g, at);
+            maps.put(turn, wave, m);
             lds_barrier();
-            const uint64_t cuts = maps.cuts(turn);
+            const uint64_t cuts = maps.are(turn, CUT), scaled = maps.are(turn, SCALED);
 #pragma unroll
-            for (int w = W - 1; w >= 0; --w)
+            for (int w = W - 1; w >= 0; --w) {
 #pragma unroll
-                for (int v = 0; v < VC; ++v) {
+                for (int v = 0; v < VC; ++v)
                     if (w == wave) c[v] = carry[v];
-                    carry[v] = fmaf(maps.a[turn][w][lane][v], carry[v], maps.h[turn][w][lane][v]);
-                    if (cuts != 0 && (cuts >> w & 1)) carry[v] = maps.h[turn][w][lane][v];
-                }
+                maps.template pass<SEMI_REAL>(carry, turn, w, cuts, scaled);
+            }
         }
         if (now.rows.plain()) now.template walk<true>(c, g, t, end, at);
         else now.template walk<false>(c, g, t, end, at);
@@ -607,11 +697,12 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))
     BackTile<S, T, VC> now;
     now.load(g, t, end, at, S == SEMI_LOG || g.da);
     now.resolve(g, t, end, at);
-    float A[VC], C[VC], c[VC];
-#pragma unroll
-    for (int v = 0; v < VC; ++v) { A[v] = 1.0f; C[v] = 0.0f; }
-    const bool cut = now.map(A, C, g, at);
-    maps.put(0, wave, A, C, cut);
+    float c[VC];
+    {
+        Map<VC> m;
+        now.map(m, g, at);
+        maps.put(0, wave, m);
+    }
     state_of_wave<SEMI_REAL, VC, W, true>(c, maps, before, g, chain, q);
     if (now.rows.plain()) now.template walk<true>(c, g, t, end, at);
     else now.template walk<false>(c, g, t, end, at);

@@ -6,7 +6,7 @@ multiplications (a thread's run over a row, then trees; exponential and scaling 
 """
 import numpy as np
 
-U = 2.0 ** -24
+U, LEAST = 2.0 ** -24, 2.0 ** -149
 #: what a rounding of a value can be off by, relative (half of eps), and below the normal range, absolute
 REL = {"float32": 2.0 ** -24, "bfloat16": 2.0 ** -8, "float16": 2.0 ** -11}
 TINY = {"float32": 1.2e-38, "bfloat16": 1.2e-38, "float16": 2.0 ** -25}
@@ -108,16 +108,21 @@ def scan(s, a, x, h0, dh=None, dfinal=None, dtype="float32"):
     (The gradient of a gate of 16 bits is made with the state before it as the forward pass returned it, rounded to those bits.)
 
     REAL: h_t is a sum of products of at most t gates; a term with n gates has been through at most n + 24 roundings (its gates, the
-    joins of wave, tile and chunk), so |error| <= 2 u (N + 24 M), M = sum |terms|, N = sum n |terms|.
+    joins of wave, tile and chunk), so |error| <= 2 u (N + 24 M), M = sum |terms|, N = sum n |terms|.  A state below the smallest
+    normal number is rounded to a multiple of 2^-149 whatever its size; gates above 1 make these errors grow as they make the terms
+    grow: D = |a| D + 2^-149 a step, 24 D with the joins.  (A sequence that falls to 2^-230 and rises again by 2^200 is lost in 32
+    bits step by step as well: 2^-230 is 0 there.)
     LOG: a step rounds a + h, the maximum and the sum (u |a + h|, u |h| and 4 u for the logarithm of a sum in [1, 2]) and passes the
     error before it on with the share w <= 1; the joins of wave, tile and chunk each add as much again, hence the factor 8."""
     T, C = x.shape
     h, M, N, E = np.zeros((T, C)), np.zeros((T, C)), np.zeros((T, C)), np.zeros((T, C))
     now, m, n, e = h0.copy(), np.abs(h0), np.zeros(C), np.zeros(C)
+    D, d = np.zeros((T, C)), np.zeros(C)
     size = lambda v: np.where(np.isfinite(v), np.abs(v), 0.0)  # noqa: E731
     with np.errstate(all="ignore"):
         for t in range(T):
             if s == REAL:
+                d = np.abs(a[t]) * d + LEAST
                 n, m = np.abs(a[t]) * (n + m) + np.abs(x[t]), np.abs(a[t]) * m + np.abs(x[t])
             before, now = now, _step(s, a[t], now, x[t])
             if s == LOG:
@@ -125,23 +130,23 @@ def scan(s, a, x, h0, dh=None, dfinal=None, dtype="float32"):
                 e = w * (e + U * size(a[t] + before)) + U * (4 + 2 * size(now))
             elif s == MAX:
                 e = e + U * (size(a[t] + before) + size(a[t]))
-            h[t], M[t], N[t], E[t] = now, m, n, e
-    tol = 2 * U * (N + 24 * M) if s == REAL else 8 * E
+            h[t], M[t], N[t], E[t], D[t] = now, m, n, e, d
+    tol = 2 * U * (N + 24 * M) + 24 * D if s == REAL else 8 * E
     out = {"h": h, "h_tol": tol, "final": now, "final_tol": tol[-1] if T else np.zeros(C)}
     if dh is None:
         return out
     da, dx, da_tol, dx_tol = (np.zeros((T, C)) for _ in range(4))
-    c, cm, cn = dfinal.copy(), np.abs(dfinal), np.zeros(C)
+    c, cm, cn, cd = dfinal.copy(), np.abs(dfinal), np.zeros(C), np.zeros(C)
     with np.errstate(all="ignore"):
         for t in range(T - 1, -1, -1):
             prev = h[t - 1] if t else h0
             prev_tol = tol[t - 1] + (REL[dtype] * np.abs(prev) + TINY[dtype] if dtype != "float32" else 0.0) if t else 0.0
             g, gm, gn = dh[t] + c, np.abs(dh[t]) + cm, np.abs(dh[t]) + cn + cm
-            g_tol = 2 * U * (gn + 24 * gm)
+            g_tol = 2 * U * (gn + 24 * gm) + 24 * cd
             if s == REAL:
                 da[t], dx[t] = g * prev, g
                 da_tol[t], dx_tol[t] = g_tol * np.abs(prev) + gm * prev_tol + 4 * U * np.abs(da[t]), g_tol
-                c, cm, cn = a[t] * g, np.abs(a[t]) * gm, np.abs(a[t]) * gn
+                c, cm, cn, cd = a[t] * g, np.abs(a[t]) * gm, np.abs(a[t]) * gn, np.abs(a[t]) * cd + LEAST
             else:
                 w, v = _shares(a[t], prev, x[t])
                 # a share is off by what the difference a + h - x of its logarithms is, and by the six operations that make it
@@ -149,7 +154,7 @@ def scan(s, a, x, h0, dh=None, dfinal=None, dtype="float32"):
                 da[t], dx[t] = g * w, g * v
                 c, cm, cn = g * w, gm * w, (gn + gm * d / U) * w
                 da_tol[t], dx_tol[t] = 2 * U * (cn + 24 * cm), 2 * U * ((gn + gm * d / U) * v + 24 * gm * v)
-    out.update(da=da, dx=dx, da_tol=da_tol, dx_tol=dx_tol, dinitial=c, dinitial_tol=2 * U * (cn + 24 * cm))
+    out.update(da=da, dx=dx, da_tol=da_tol, dx_tol=dx_tol, dinitial=c, dinitial_tol=2 * U * (cn + 24 * cm) + 24 * cd)
     return out
 
 

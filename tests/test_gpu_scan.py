@@ -32,12 +32,12 @@ def make(shape, count, semiring, dtype, rng, impossible=False):
     return torch.from_numpy(a).to(kind).cuda(), torch.from_numpy(x).to(kind).cuda(), torch.from_numpy(h).float().cuda()
 
 
-def check(a, x, h0, semiring, dtype, rng, spans=None, offsets=None, train=True, given=None):
-    """spans: rows of the packed sequences; h0 None: no initial state"""
+def check(a, x, h0, semiring, dtype, rng, spans=None, offsets=None, train=True, given=None, scale=1.0):
+    """spans: rows of the packed sequences; h0 None: no initial state; scale: of the adjoints"""
     train = train and semiring != MAX
-    dh = torch.from_numpy(rng.normal(size=tuple(x.shape))).to(x.dtype).cuda()
+    dh = torch.from_numpy(rng.normal(size=tuple(x.shape)) * scale).to(x.dtype).cuda()
     count = x.shape[0] if spans is None else len(spans)
-    dfinal = torch.from_numpy(rng.normal(size=(count, x.shape[-1]))).float().cuda()
+    dfinal = torch.from_numpy(rng.normal(size=(count, x.shape[-1])) * scale).float().cuda()
     ga, gx = given if given else (a, x)
     leaves = [t.detach().requires_grad_(train) for t in (ga, gx) + (() if h0 is None else (h0,))]
     h, final = klay().gated_scan(leaves[0], leaves[1], leaves[2] if h0 is not None else None, semiring, offsets=offsets)
@@ -139,6 +139,67 @@ def test_a_sequence_does_not_reach_into_the_next(semiring):
         want = ref.scan(semiring, *(t[slice(*spans[s])].double().cpu().numpy() for t in (a, x)), h[s].double().cpu().numpy())
         ref.close(out[slice(*spans[s])].cpu().numpy(), want["h"], want["h_tol"])
         ref.close(alone[0][0].cpu().numpy(), want["h"], want["h_tol"])
+
+
+# Gates above 1: the product of a stretch of them is past the largest number, what they are applied to is as small, or 0.  (Runs of gates up
+# and down by `bits` bits each, 2^200 a run: past a wave's 16 steps, a tile's 128, a group of tiles.)
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("run,bits", [(20, 10.0), (200, 1.0), (400, 0.5)])
+@pytest.mark.parametrize("batch,time,channels", [(1, 4500, 3), (2, 1200, 130), (50, 210, 200), (260, 150, 130), (70, 60, 130)])
+def test_products_out_of_range(batch, time, channels, run, bits, dtype):
+    rng = np.random.default_rng(run + time)
+    kind, tiny = getattr(torch, dtype), 2.0 ** -120
+    shape = (batch, time, channels)
+    up = np.where(np.arange(time) // run % 2 == 0, bits, -bits)[None, :, None]
+    a = 2.0 ** up * rng.uniform(0.97, 1.03, size=shape) * np.where(rng.random(shape) < 0.1, -1.0, 1.0)
+    x = np.where(rng.random(shape) < 0.02, tiny * rng.normal(size=shape), 0.0)
+    h = tiny * rng.normal(size=(batch, channels))
+    x[..., 0], h[..., 0] = 0.0, 0.0                      # a channel of zeros
+    a, x, h = torch.from_numpy(a).to(kind).cuda(), torch.from_numpy(x).to(kind).cuda(), torch.from_numpy(h).float().cuda()
+    check(a, x, h, REAL, dtype, rng, scale=tiny)
+    if batch == 2:                                       # the same as packed sequences, one behind the other
+        rows = lambda t: t.reshape(batch * time, channels)  # noqa: E731
+        cuts = [0, 130, 131, time, time, 2 * time]
+        check(rows(a), rows(x), torch.cat([h, h, h[:1]]), REAL, dtype, rng, list(zip(cuts[:-1], cuts[1:])), torch.tensor(cuts, device="cuda"),
+              scale=tiny)
+
+
+@pytest.mark.parametrize("batch,channels", [(1, 5), (150, 64)])
+def test_what_is_infinite_stays_in_its_channel(batch, channels):
+    rng = np.random.default_rng(batch)
+    a, x, h = make((batch, 2500, channels), batch, REAL, "float32", rng)
+    a = a.abs() + 0.01
+    want = ref.scan(REAL, *(t[0].double().cpu().numpy() for t in (a, x, h)))
+    x[:, 700, 1], a[:, 800, 2], x[:, 900, 3] = float("inf"), float("-inf"), float("nan")
+    out, final = klay().gated_scan(a, x, h)
+    for c, t in ((1, 700), (2, 800), (3, 900)):
+        assert torch.isfinite(out[:, :t, c]).all() and not torch.isfinite(out[:, t:, c]).any() and not torch.isfinite(final[:, c]).any()
+    for c in (0, 4):
+        ref.close(out[0, :, c].cpu().numpy(), want["h"][:, c], want["h_tol"][:, c])
+
+
+@pytest.mark.parametrize("semiring", [REAL, LOG])
+def test_saved_tensors_that_come_back_with_other_strides(semiring):
+    """what autograd saved may lie in the same place another way (hooks that keep it elsewhere meanwhile)"""
+    rng = np.random.default_rng(1)
+    a, x, h = make((3, 200, 6), 3, semiring, "float32", rng)
+    dh = torch.from_numpy(rng.normal(size=a.shape)).float().cuda()
+    results = []
+    for moved in (False, True):
+        base = torch.zeros((3, 201, 6), device="cuda")
+        base[:, :-1] = a
+        gates = base[:, :-1].requires_grad_(True)
+
+        def unpack(t):
+            if not moved or t.data_ptr() != gates.data_ptr():
+                return t
+            flat = base.detach().flatten()[:a.numel()]
+            flat.copy_(a.flatten())
+            return flat.view(a.shape)
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t, unpack):
+            out, _ = klay().gated_scan(gates, x, h, semiring)
+        results.append(torch.autograd.grad(out, gates, dh)[0])
+    assert torch.equal(*results)
 
 
 @pytest.mark.parametrize("semiring,dtype", CASES)
