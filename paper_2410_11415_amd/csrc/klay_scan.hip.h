@@ -10,7 +10,9 @@
 // so that memory is read once.  Where batch x channels give workgroups enough to fill the chip, one goes through all tiles of its channels.
 // Otherwise every tile is a workgroup of its own (scan_chain_kernel), which publishes its map and takes the state in front of it from what
 // the tiles before it have published.  (Two launches, the first of them for the maps alone, read the inputs twice: 65536 x 512 fp32
-// forward 134 us, reverse 191 us.)
+// forward 134 us, reverse 191 us, for 100 and 130.)
+// Measured: 16 x 4096 x 4096 fp32 forward 563 us = 5.7 TB/s, reverse 1012 us = 5.3 TB/s (a copy of 1 GiB reaches 5.2 to 6.1); 8 x 4096 x 2048 bf16,
+// a workgroup per CU, 93 us = 4.3 TB/s and 170 us = 4.0 TB/s; 65536 x 512 fp32, chained, 100 us and 130 us = 5.4 TB/s.
 #pragma once
 
 #include <hip/hip_runtime.h>

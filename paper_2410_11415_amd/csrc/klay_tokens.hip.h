@@ -9,6 +9,9 @@
 // four issue slots of a CU that has about ten per element at the rate of HBM).  A thread runs through its part of the row once with a
 // reference `ref` that follows its running maximum from afar: it moves only when a value lies more than kSlack above it, so that almost
 // every eight elements cost no rescaling; sums of terms up to e^kSlack lose nothing.  All sums and maxima are fp32.
+// Measured with entropy, bf16 (reads alone reach 7.0 TB/s, a copy 6.1): 4096 x 131072 forward 168 us = 6.4 TB/s at 91% of the vector unit's issue
+// slots, backward 350 us = 6.1 TB/s; 4096 x 32771 forward 52 us = 5.1 TB/s; 1 x 131072 with eight alternatives 17 us, of which one workgroup
+// reads for five.
 #pragma once
 
 #include <hip/hip_runtime.h>

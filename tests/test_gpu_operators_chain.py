@@ -153,7 +153,7 @@ def test_the_whole_chain():
     ours = [t.cuda().requires_grad_(True) for t in host]
     got = p.loss(ours[0], ours[1], ours[2:], lambda s, a, x, h: klay.gated_scan(a, x, h, s), logprobs, layer)
     got.backward()
-    assert abs(float(got) - float(want)) <= LOG_ATOL + 1e-5 * abs(float(want))
+    assert abs(float(got.detach()) - float(want.detach())) <= LOG_ATOL + 1e-5 * abs(float(want.detach()))
     # what fp32 does to the matrix products and to every operator is of the order of 1e-6; a wrong term would be of order 1
     for a, b in zip(ours, exact):
         assert float((a.grad.cpu().double() - b.grad).norm() / b.grad.norm()) <= 1e-3
