@@ -342,7 +342,7 @@ __device__ __forceinline__ void keep_best(Best<ROOM, THREADS>& sh, int32_t top, 
 
 // The `top` largest elements of [lo, hi).  A thread's own maximum as a key lies between its `low` and its `high`.  Only the columns of threads whose
 // `high` reaches the bound that the `low` give hold anything that does: those are read again (from the cache).
-// However the logits are ordered, a round adds at most 2048 keys, and more than 256 of them are cut to the best ones before the next.
+// However the logits are ordered, a round adds at most 8 THREADS keys, and more than 256 of them are cut to the best ones before the next.
 template <typename T, int N, int THREADS>
 __device__ __forceinline__ void top_of_part(TopShared<THREADS>& sh, const T* row, const Share<N, THREADS>& share, uint64_t low, uint64_t high,
                                             int32_t top) {
@@ -365,8 +365,9 @@ __device__ __forceinline__ void top_of_part(TopShared<THREADS>& sh, const T* row
         limit = sh.limit;
         const int32_t w = w0 + tid;
         if (w < work) {
-            const int32_t i = w / columns, base = share.at(i, sh.chosen[w - i * columns]);
-            if (base < share.full) {
+            const int32_t i = w / columns, thread = sh.chosen[w - i * columns];
+            if (i * THREADS + thread < share.vectors) {
+                const int32_t base = share.at(i, thread);
                 float x[N];
                 load_elements<N>(x, row + base);
 #pragma unroll

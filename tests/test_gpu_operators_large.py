@@ -85,3 +85,30 @@ def test_step_past_32_bits():
     x[-1] = 3.0
     k.gated_step(a, x, state, out=out)
     assert bool((state[-1] == 4.0).all()) and bool((out[-1] == 4.0).all()) and bool((state[-2] == 2.0).all())
+
+
+def test_the_longest_row():
+    """2^31 - 1 logits: all 0 but a few.  Sums of ones are exact in fp32 up to 2^24 and off by 2^-24 a join above; with what the change of
+    the reference costs (a factor that is off by 2^-22) the logarithm of the sum is off by less than 1e-5."""
+    k = klay()
+    vocab = (1 << 31) - 1
+    x = torch.zeros((1, vocab), dtype=torch.bfloat16, device="cuda")
+    best = [vocab - 1, vocab - 9, 5, vocab // 2, vocab - 4097]
+    value = torch.tensor([20.0, 19.0, 18.0, 17.0, 16.0], dtype=torch.float64)
+    for j, v in zip(best, value.tolist()):
+        x[0, j] = v
+    x.requires_grad_(True)
+    t = torch.tensor([best + [7]], device="cuda")
+    r = k.token_logprobs(x, t, entropy=True, top=6)
+    total = (vocab - 5) + value.exp().sum()
+    lp = torch.cat([value, torch.zeros(1, dtype=torch.float64)]) - total.log()
+    assert float((r.logp[0].detach().cpu().double() - lp).abs().max()) <= 1e-5 + 32 * ref.U
+    entropy = total.log() - (value.exp() * value).sum() / total
+    assert abs(float(r.entropy[0].detach()) - float(entropy)) <= 1e-5 * 32
+    assert r.top_tokens[0].tolist() == best + [0]
+    dx, = torch.autograd.grad(r.logp[:, 0].sum(), x)
+    p = lp.exp()
+    want = torch.tensor([1 - p[0]] + [-q for q in p[1:5]] + [-p[5]], dtype=torch.float64)
+    got = dx[0, torch.tensor(best + [vocab - 2], device="cuda")].cpu().double()
+    assert ((got - want).abs() <= (2.0 ** -8 + 1e-4) * want.abs()).all()
+    assert int((dx[0] == dx[0, 0]).sum()) == vocab - 5 and bool(dx[0, 0] < 0)
