@@ -160,6 +160,7 @@ klay_status run_tokens_back(const klay::TokenArgs& g, int threads, void* stream)
 
 // ---- recurrence -----------------------------------------------------------------------------------------------------
 constexpr int64_t kFewChains = kComputeUnits / 2;
+constexpr int64_t kMostTiles = (1ll << 32) / 512 - 1;  // a launch has less than 2^32 threads;  beyond (2^30 steps of 64 channels) one workgroup takes all tiles of its channels
 
 struct ScanPlan {
     int vec = 1, waves = 4;         // channels per lane; waves per workgroup
@@ -207,11 +208,12 @@ ScanPlan scan_plan(const klay_scan_args* a) {
     const bool pairs = a->channels % 2 == 0 && aligned_to(2 * size, {a->gates, a->inputs}) && (a->gates_batch_stride | a->gates_time_stride |
                        a->inputs_batch_stride | a->inputs_time_stride) % 2 == 0;
     p.waves = a->time <= klay::kSteps ? 1 : a->time <= 4 * klay::kSteps ? 4 : 8;
-    const bool few = p.waves == 8 && blocks(1) * a->batch <= kFewChains;
+    const int64_t tiles = (a->time + p.waves * klay::kSteps - 1) / (p.waves * klay::kSteps);
+    const bool few = p.waves == 8 && blocks(1) * a->batch <= kFewChains && blocks(1) * a->batch * tiles <= kMostTiles;
     p.vec = a->semiring == KLAY_REAL && pairs && (few ? size == 2 : blocks(2) * a->batch >= 2 * kComputeUnits) ? 2 : 1;
     p.blocks_c = blocks(p.vec);
     p.chains = p.blocks_c * a->batch;
-    if (few) p.tiles = (a->time + p.waves * klay::kSteps - 1) / (p.waves * klay::kSteps);
+    if (few) p.tiles = tiles;
     return p;
 }
 
@@ -272,8 +274,8 @@ klay_status run_scan(const klay::ScanArgs& g, const ScanPlan& p, bool back, void
 
 template <int S, typename T, int VC>
 klay_status run_scan(const klay::ScanArgs& g, const ScanPlan& p, bool back, void* stream) {
-    // (a grid times its block has to stay below 2^32 threads)
-    if ((p.tiles > 0 ? p.chains * p.tiles : p.chains) * 64 * p.waves > (int64_t)UINT32_MAX)
+    // (a grid times its block has to stay below 2^32 threads; tiles do by their plan)
+    if (p.tiles == 0 && p.chains * 64 * p.waves > (int64_t)UINT32_MAX)
         return fail(KLAY_EINVAL, "klay_scan: batch times channels exceeds one launch");
     if (p.waves == 1) return run_scan<S, T, VC, 1>(g, p, back, stream);
     if (p.waves == 4) return run_scan<S, T, VC, 4>(g, p, back, stream);

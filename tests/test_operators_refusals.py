@@ -99,6 +99,12 @@ def test_scan_outputs_and_workspace():
         assert e.value.status == status
 
 
+def test_more_tiles_than_a_launch_has_workgroups():
+    """a workgroup a tile (that is what the workspace is for) only where they fit a launch"""
+    for batch, time, some in ((1, 1 << 29, True), (1, (1 << 31) - 1, False), (100, 1 << 23, True), (100, 1 << 24, False)):
+        assert (binding.klay_scan_workspace_bytes(scan_args(batch=batch, time=time)) > 0) == some
+
+
 @pytest.mark.parametrize("bad", [dict(dtype=9), dict(semiring=5), dict(semiring=1, dtype=2), dict(rows=-1), dict(rows=1 << 31), dict(channels=0),
                                  dict(channels=(1 << 25) + 1), dict(gates=None), dict(inputs=None), dict(state=None)])
 def test_step_arguments(bad):
