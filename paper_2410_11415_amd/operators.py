@@ -100,14 +100,8 @@ def _tokens_forward(logits, tokens, complement, entropy, top, keep):
     return logp, neg, h, top_logp, top_tokens, stats, args, alive
 
 
-def _copies(used, given):
-    """used, if some of it is a copy and has to be kept beside what autograd saves; else None"""
-    for u, g in zip(used, given):
-        if u is not g:
-            return used
-    return None
-
-
+# What a forward call's args point into (the tensors given, or the copies made of them) is what its function saves for the reverse call, so that
+# hooks on saved tensors hold all of it, and nothing else keeps it alive.  The args are used again only where every tensor comes back in its place.
 def _places(*tensors):
     """Where tensors are and how they lie: what args made for them stay good for."""
     return [None if t is None else (t.data_ptr(), t.stride()) for t in tensors]
@@ -116,9 +110,9 @@ def _places(*tensors):
 class _TokenLogprobs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, tokens, complement, entropy, top):
-        *out, stats, ctx.args, alive = _tokens_forward(logits, tokens, complement, entropy, top, True)
-        ctx.copies, ctx.places = _copies(alive, (logits, tokens)), _places(logits, tokens)
-        ctx.save_for_backward(logits, tokens, stats)
+        *out, stats, ctx.args, used = _tokens_forward(logits, tokens, complement, entropy, top, True)
+        ctx.places = _places(*used)
+        ctx.save_for_backward(*used, stats)
         ctx.set_materialize_grads(False)
         if top:
             ctx.mark_non_differentiable(*out[3:])
@@ -129,9 +123,9 @@ class _TokenLogprobs(torch.autograd.Function):
     def backward(ctx, dlogp, dneg, dentropy, _top_logp, _top_tokens):
         logits, tokens, stats = ctx.saved_tensors
         dlogp, dneg, dentropy = (None if t is None else t.contiguous() for t in (dlogp, dneg, dentropy))
-        args, alive = ctx.args, ctx.copies
-        if alive is None and ctx.places != _places(logits, tokens):
-            args, alive = _token_args(logits, tokens, 0)            # what was saved has been put elsewhere
+        args = ctx.args
+        if ctx.places != _places(logits, tokens):                   # what was saved has been put elsewhere
+            args, (logits, tokens) = _token_args(logits, tokens, 0)
         dlogits = logits.new_empty(logits.shape)
         _b.klay_tokens_backward(args, stats.data_ptr(), _ptr(dlogp), _ptr(dneg), _ptr(dentropy), dlogits.data_ptr(),
                                 _stream(args.device))
@@ -213,8 +207,8 @@ def _scan_forward(gates, inputs, initial, semiring, offsets):
 class _GatedScan(torch.autograd.Function):
     @staticmethod
     def forward(ctx, gates, inputs, initial, semiring, offsets):
-        states, final, row_info, ctx.args, alive = _scan_forward(gates, inputs, initial, semiring, offsets)
-        ctx.semiring, ctx.copies = semiring, _copies(alive, (gates, inputs, initial))
+        states, final, row_info, ctx.args, (gates, inputs, initial) = _scan_forward(gates, inputs, initial, semiring, offsets)
+        ctx.semiring = semiring
         if semiring != KLAY_LOG:
             inputs = None                                           # not read by the reverse sweep
         ctx.places = _places(gates, inputs, initial, offsets, row_info)
@@ -228,9 +222,9 @@ class _GatedScan(torch.autograd.Function):
         gates, inputs, initial, offsets, row_info, states = ctx.saved_tensors
         if dstates is None and dfinal is None:
             return None, None, None, None, None
-        args, alive = ctx.args, ctx.copies
-        if alive is None and ctx.places != _places(gates, inputs, initial, offsets, row_info):      # what was saved has been put elsewhere
-            args, alive = _scan_args(gates, gates if inputs is None else inputs, initial, ctx.semiring, offsets, row_info)
+        args = ctx.args
+        if ctx.places != _places(gates, inputs, initial, offsets, row_info):       # what was saved has been put elsewhere
+            args, (gates, inputs, initial) = _scan_args(gates, gates if inputs is None else inputs, initial, ctx.semiring, offsets, row_info)
         dstates, dfinal = (None if t is None else t.contiguous() for t in (dstates, dfinal))
         dgates, dinputs = (gates.new_empty(gates.shape) if need else None for need in ctx.needs_input_grad[:2])
         dinitial = initial.new_empty(initial.shape) if ctx.needs_input_grad[2] else None
