@@ -386,7 +386,8 @@ klay_status klay_tokens_forward(const klay_tokens_args* args, float* logp, float
  *   stats       as written by the forward call (with entropy asked for if dentropy is given)
  *   dlogp, dneg, dentropy   device, shaped as the outputs; each may be NULL (no adjoint)
  *   dlogits     device [rows, vocab] contiguous, of `dtype`; every entry is written, rounded once.  An adjoint of exactly 0
- *               contributes 0, and a row all of whose adjoints are 0 gets zeros, whatever it holds.
+ *               contributes 0, and a row all of whose adjoints are 0 gets zeros, whatever it holds; with any other adjoint a row
+ *               that holds a NaN or +inf gets NaN.
  * The same inputs give the same bits.  Errors: as klay_tokens_forward.
  */
 klay_status klay_tokens_backward(const klay_tokens_args* args, const float* stats, const float* dlogp, const float* dneg,

@@ -40,6 +40,8 @@ struct RowMap {
 
 struct RowStats {       // what a backward pass needs of a row
     float max, log_sum, entropy, pad;
+    // nothing but -inf (a row of NaN, or of NaN and -inf, has a log_sum of NaN)
+    __device__ __forceinline__ bool empty() const { return max == -INFINITY && log_sum == 0.0f; }
 };
 
 struct TokenArgs {
@@ -656,7 +658,7 @@ __device__ __forceinline__ TokenGrad token_grad(const TokenArgs& g, const T* row
         out.others = __int_as_float(0x7fc00000);
         return out;
     }
-    const float lp = row_logp((float)row[t], s.max, s.log_sum);
+    const float lp = row_logp((float)row[t], s.max, s.log_sum) + (s.log_sum - s.log_sum);       // (a NaN of the row reaches every token)
     const float p = expf(lp), away = -expm1f(lp);
     out.token = (int32_t)t;
     float w = nk != 0.0f && away > 0.0f ? nk * p / away : 0.0f;
@@ -723,7 +725,7 @@ __global__ void __launch_bounds__(THREADS) token_back_kernel(TokenArgs g) {
         block_sum2<THREADS>(others, asked, scratch);
         const float h = g.dentropy ? g.dentropy[r] : 0.0f;
         // a row that nothing was asked of, or that allows nothing, has no gradient, whatever it holds
-        const bool live = s.max != -INFINITY && (asked > 0.0f || h != 0.0f);
+        const bool live = !s.empty() && (asked > 0.0f || h != 0.0f);
         const BulkGrad bulk = bulk_grad(s, others, h);
         if (live) {
             for (int32_t i = 0; i * THREADS + tid < share.vectors; i += U) {
@@ -787,7 +789,7 @@ __global__ void __launch_bounds__(kTokBlock) token_back_short_kernel(TokenArgs g
         float p[E], y[E], asked = 0.0f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const bool in = lane + G * e < g.vocab && s.max != -INFINITY;
+            const bool in = lane + G * e < g.vocab && !s.empty();
             const float x = in ? (float)row[lane + G * e] : -INFINITY;
             p[e] = in ? bulk.p(x) : 0.0f;
             y[e] = in ? bulk.entropy_at(x) : 0.0f;
@@ -805,7 +807,7 @@ __global__ void __launch_bounds__(kTokBlock) token_back_short_kernel(TokenArgs g
                 for (int e = 0; e < E; ++e) y[e] += lane + G * e == token ? itself : (others != 0.0f ? others * p[e] : 0.0f);
             }
         }
-        const bool live = s.max != -INFINITY && (asked > 0.0f || h != 0.0f);
+        const bool live = !s.empty() && (asked > 0.0f || h != 0.0f);
 #pragma unroll
         for (int e = 0; e < E; ++e)
             if (lane + G * e < g.vocab) out[lane + G * e] = (T)(live ? y[e] : 0.0f);
