@@ -353,8 +353,9 @@ typedef struct klay_rows {
 
 /*
  * klay_tokens_forward -- log probabilities of given tokens under rows of logits (the weights of literals "the network answers t"):
- *   p_j = exp(x_j) / sum_i exp(x_i);  logp_k = ln p_{t_k};  neg_k = ln(1 - p_{t_k}), the weight of the negated literal, exact also
- *   where p rounds to 1;  entropy = - sum_j p_j ln p_j;  the `top` largest logits (equal ones: the lowest index first).
+ *   p_j = exp(x_j) / sum_i exp(x_i);  logp_k = ln p_{t_k};  neg_k = ln(1 - p_{t_k}), the weight of the negated literal, from the other
+ *   tokens' logits also where p rounds to 1 (-inf only where none of them is allowed: finite masks leave a finite weight);
+ *   entropy = - sum_j p_j ln p_j;  the `top` largest logits (equal ones: the lowest index first).
  *   logits      device [rows, vocab] of `dtype`, the elements of a row next to each other, rows placed by logit_rows
  *   tokens      device [rows, num_tokens] int64, placed by token_rows and token_stride.  A negative token asks for nothing: its logp and
  *               neg are 0 and it has no gradient.  A token >= vocab gives NaN.  The same token may be asked for more than once.

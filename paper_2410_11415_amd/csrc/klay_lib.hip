@@ -100,7 +100,7 @@ TokenPlan backward_plan(const klay_tokens_args* a) {
     return in_parts(a, 256, std::max<int64_t>(few, (bytes + kBackPart - 1) / kBackPart));
 }
 
-size_t token_lists_at(int64_t rows, int32_t parts) { return (size_t)rows * parts * 4 * sizeof(float); }
+size_t token_lists_at(int64_t rows, int32_t parts) { return (size_t)rows * parts * klay::kPartial * sizeof(float); }
 
 klay::TokenArgs token_args(const klay_tokens_args* a) {
     klay::TokenArgs g{};

@@ -3,7 +3,9 @@
 //   M = max x, d_j = x_j - M, S = sum e^d_j = 1 + R (R: all terms but the maximum's own), ln S = log1p(R)
 //   logp_k = d_{t_k} - ln S,  neg_k = ln(1 - p_{t_k}),  H = ln S - sum e^d_j d_j / S
 // R is kept apart from the 1 because everything that a sure network answers lives in it: logp of the likely token is -log1p(R) and its
-// neg ln R - log1p(R), both to fp32's relative accuracy, where S itself has rounded R away.
+// neg ln R - log1p(R), both to fp32's relative accuracy, where S itself has rounded R away.  Below 2^-64 (the others more than 44 under the
+// maximum: a very sure network, or finite masks that leave one token) R = e^(M2 - M) R2 is held as M2, the largest of the others, and R2,
+// their sum relative to it, since terms below 2^-126 are lost relative to M (2^31 of them are 2^-31 of an R that is not held so).
 //
 // Bound: memory, one read of the logits; the arithmetic stands close behind (an element of bf16 has 2 bytes, and its exponential takes
 // four issue slots of a CU that has about ten per element at the rate of HBM).  A thread runs through its part of the row once with a
@@ -25,6 +27,7 @@ namespace klay {
 
 constexpr int kTokBlock = 256;              // threads of a workgroup; the kernels over rows also have 64 and 1024 of them
 constexpr int kMaxTop = 64, kMaxTokens = 1024;
+constexpr int kPartial = 8;                 // floats that a row part leaves for the join
 constexpr float kSlack = 8.0f;
 constexpr float kTokLog2e = 1.4426950408889634f, kTokLn2 = 0.6931471805599453f, kTokFltMax = 3.402823466e+38f;
 
@@ -38,10 +41,9 @@ struct RowMap {
     }
 };
 
-struct RowStats {       // what a backward pass needs of a row
-    float max, log_sum, entropy, pad;
-    // nothing but -inf (a row of NaN, or of NaN and -inf, has a log_sum of NaN)
-    __device__ __forceinline__ bool empty() const { return max == -INFINITY && log_sum == 0.0f; }
+// What a backward pass needs of a row.  below < max: a sure row, M2 and R2 in `below` and `sum`; otherwise `below` is +inf and `sum` ln S.
+struct RowStats {
+    float max, sum, entropy, below;
 };
 
 struct TokenArgs {
@@ -57,7 +59,7 @@ struct TokenArgs {
     RowStats* stats;                    // [rows]
     float* top_logp;                    // [rows, top]
     int64_t* top_tokens;
-    float* partial;                     // [rows, parts, 4]: maximum, R, sum e^d d, unused
+    float* partial;                     // [rows, parts, kPartial]: RowSums
     uint64_t* lists;                    // [rows, parts, top]
     // backward
     const float *dlogp, *dneg, *dentropy;
@@ -80,14 +82,18 @@ __device__ __forceinline__ float key_value(uint64_t key) {
 __device__ __forceinline__ uint32_t key_index(uint64_t key) { return ~(uint32_t)key; }
 
 // ---- what is said about a row once its M, R and T = sum e^d d (base 2: sum e^d d log2 e) are known -----------------
+constexpr float kTinyRest = 0x1p-64f;
 struct RowSums {
     float max, rest, weighted;
+    float below = INFINITY, rest_below = 0.0f;       // of a sure row M2 and R2
+    __device__ __forceinline__ bool sure() const { return below < max; }
 };
 __device__ __forceinline__ bool row_empty(const RowSums& s) { return s.max == -INFINITY && s.rest == 0.0f; }
 __device__ __forceinline__ float row_log_sum(const RowSums& s) { return row_empty(s) ? 0.0f : log1pf(s.rest); }
 __device__ __forceinline__ float row_entropy(const RowSums& s) {
     return row_empty(s) ? 0.0f : log1pf(s.rest) - kTokLn2 * s.weighted / (1.0f + s.rest);
 }
+__device__ __forceinline__ float row_log_rest(const RowSums& s) { return s.sure() ? (s.below - s.max) + logf(s.rest_below) : logf(s.rest); }
 __device__ __forceinline__ float row_logp(float x, float max, float log_sum) { return max == -INFINITY ? -INFINITY : (x - max) - log_sum; }
 
 // What is asked of a row: token k and its logit, loaded before the row is summed (two loads that wait for each other).
@@ -111,7 +117,7 @@ __device__ __forceinline__ void write_token(const TokenArgs& g, int64_t r, int32
         lp = row_logp(a.x, s.max, log_sum) + (log_sum - log_sum);             // (a NaN of the row reaches every token)
         if (g.neg) {
             if (row_empty(s)) neg = 0.0f;
-            else if (a.x == s.max && s.rest < 1.0f) neg = logf(s.rest) - log_sum;
+            else if (a.x == s.max && s.rest < 1.0f) neg = row_log_rest(s) - log_sum;
             else neg = log1pf(-expf(lp));
         }
     }
@@ -130,7 +136,7 @@ __device__ __forceinline__ void write_tokens(const TokenArgs& g, const T* row, i
 __device__ __forceinline__ void write_row(const TokenArgs& g, int64_t r, const RowSums& s, float log_sum) {
     const float h = g.entropy ? row_entropy(s) : 0.0f;
     if (g.entropy) g.entropy[r] = h;
-    if (g.stats) g.stats[r] = RowStats{s.max, log_sum, h, 0.0f};
+    if (g.stats) g.stats[r] = s.sure() ? RowStats{s.max, s.rest_below, h, s.below} : RowStats{s.max, log_sum, h, INFINITY};
 }
 
 __device__ __forceinline__ void write_top(const TokenArgs& g, int64_t r, int32_t k, uint64_t key, float max, float log_sum) {
@@ -389,13 +395,24 @@ __device__ __forceinline__ void top_of_part(TopShared<THREADS>& sh, const T* row
     keep_best(sh, top, false);
 }
 
-// What a workgroup finds out about the elements [lo, hi) of a row.
-struct PartSums {
-    float max, sum, rest, weighted;     // sum = 1 + rest, as far as fp32 tells
-};
+// f(element, its number) for every element of a thread.
+template <typename T, int N, int THREADS, typename F>
+__device__ __forceinline__ void each_element(const T* row, const Share<N, THREADS>& share, F&& f) {
+    const int32_t tid = threadIdx.x;
+    for (int32_t i = 0; i * THREADS + tid < share.vectors; ++i) {
+        float x[N];
+        load_elements<N>(x, row + share.at(i, tid));
+#pragma unroll
+        for (int q = 0; q < N; ++q) f(x[q], share.at(i, tid) + q);
+    }
+    if (tid < share.head()) f((float)row[share.lo + tid], share.lo + tid);
+    if (tid < share.tail()) f((float)row[share.full + tid], share.full + tid);
+}
+
+// What a workgroup finds out about the elements [lo, hi) of a row.  `tell`: M2 and R2 are of use to somebody.
 template <typename T, bool ENT, bool TOP, int THREADS, bool WIDE>
-__device__ __forceinline__ PartSums sums_of_part(const T* row, const Share<16 / sizeof(T), THREADS>& share, float* scratch, int32_t* owner,
-                                                 uint64_t* low, uint64_t* high) {
+__device__ __forceinline__ RowSums sums_of_part(const T* row, const Share<16 / sizeof(T), THREADS>& share, bool tell, float* scratch, int32_t* owner,
+                                                uint64_t* low, uint64_t* high) {
     constexpr int N = 16 / sizeof(T), U = 4;
     const int32_t tid = threadIdx.x, vectors = share.vectors;
     if (tid == 0) *owner = THREADS;
@@ -441,7 +458,7 @@ __device__ __forceinline__ PartSums sums_of_part(const T* row, const Share<16 / 
         run.take(x, share.full + tid);
     }
 
-    PartSums p;
+    RowSums p;
     p.max = block_max<THREADS>(run.max, scratch);
     const float to = fmaxf(p.max, -kTokFltMax);
     const float d = run.term(to), f = exp2_of(-d);
@@ -450,11 +467,11 @@ __device__ __forceinline__ PartSums sums_of_part(const T* row, const Share<16 / 
         t = ENT && f > 0.0f ? f * (run.t - d * s) : 0.0f;
         s *= f;
     }
-    p.sum = s;
+    float sum = s;                  // 1 + rest, as far as fp32 tells
     p.weighted = t;
-    block_sum2<THREADS>(p.sum, p.weighted, scratch + kScratch);
-    p.rest = p.sum == 0.0f ? 0.0f : p.sum - 1.0f;
-    if (p.sum > 0.0f && p.sum < 1.5f) {
+    block_sum2<THREADS>(sum, p.weighted, scratch + kScratch);
+    p.rest = sum == 0.0f ? 0.0f : sum - 1.0f;
+    if (sum > 0.0f && sum < 1.5f) {
         // One element holds most of the sum: `sum - 1` would keep little of the others.  Its thread's terms are taken again, without it.
         if (run.max == p.max) atomicMin(owner, tid);
         __syncthreads();
@@ -482,6 +499,17 @@ __device__ __forceinline__ PartSums sums_of_part(const T* row, const Share<16 / 
         p.rest = s;
         p.weighted = t;
         block_sum2<THREADS>(p.rest, p.weighted, scratch + 3 * kScratch);
+        if (tell && p.rest < kTinyRest) {
+            float below = -INFINITY, of_below = 0.0f, none = 0.0f;
+            each_element(row, share, [&](float x, int32_t) { below = fmaxf(below, x == p.max ? -INFINITY : x); });
+            below = block_max<THREADS>(below, scratch + 5 * kScratch);
+            if (below > -INFINITY) {
+                each_element(row, share, [&](float x, int32_t) { of_below += x == p.max ? 0.0f : exp2_of((x - below) * kTokLog2e); });
+                block_sum2<THREADS>(of_below, none, scratch + 6 * kScratch);
+                p.below = below;
+                p.rest_below = of_below;
+            }
+        }
     }
     if constexpr (TOP) {
         // the thread's largest element as a key lies between these two (the vector is known, the place in it is not)
@@ -499,10 +527,11 @@ __device__ __forceinline__ PartSums sums_of_part(const T* row, const Share<16 / 
 template <typename T, bool ENT, bool TOP, int THREADS>
 __global__ void __launch_bounds__(THREADS) token_row_kernel(TokenArgs g) {
     constexpr int N = 16 / sizeof(T);
-    __shared__ float scratch[5 * kScratch];
+    __shared__ float scratch[8 * kScratch];
     __shared__ int32_t owner;
     __shared__ std::conditional_t<TOP, TopShared<THREADS>, int> tops;
     const int32_t tid = threadIdx.x;
+    const bool tell = g.neg || g.stats;
     for (int64_t unit = blockIdx.x; unit < g.rows * g.parts; unit += gridDim.x) {
         const int64_t r = unit / g.parts;
         const int32_t part = (int32_t)(unit - r * g.parts);
@@ -512,24 +541,20 @@ __global__ void __launch_bounds__(THREADS) token_row_kernel(TokenArgs g) {
         Asked asked{-1, 0.0f};
         if (g.parts == 1) asked = asked_of<T>(g, row, r, tid);
         uint64_t low = 0, high = 0;
-        PartSums p = sums_of_part<T, ENT, TOP, THREADS, false>(row, share, scratch, &owner, &low, &high);
-        if (fabsf(p.max) > 0.5f * kFar && fabsf(p.max) < INFINITY) {
+        RowSums sums = sums_of_part<T, ENT, TOP, THREADS, false>(row, share, tell, scratch, &owner, &low, &high);
+        if (fabsf(sums.max) > 0.5f * kFar && fabsf(sums.max) < INFINITY) {
             __syncthreads();
-            p = sums_of_part<T, ENT, TOP, THREADS, true>(row, share, scratch, &owner, &low, &high);
+            sums = sums_of_part<T, ENT, TOP, THREADS, true>(row, share, tell, scratch, &owner, &low, &high);
         }
-        const RowSums sums{p.max, p.rest, p.weighted};
         if constexpr (TOP) top_of_part<T, N, THREADS>(tops, row, share, low, high, g.top);
         if (g.parts == 1) {
             const float log_sum = row_log_sum(sums);
             write_tokens<T>(g, row, r, tid, THREADS, asked, sums, log_sum);
             if (tid == 0) write_row(g, r, sums, log_sum);
             if constexpr (TOP)
-                if (tid < g.top) write_top(g, r, tid, tops.best[tid], p.max, log_sum);
+                if (tid < g.top) write_top(g, r, tid, tops.best[tid], sums.max, log_sum);
         } else {
-            if (tid == 0) {
-                float* to = g.partial + unit * 4;
-                to[0] = p.max; to[1] = p.rest; to[2] = p.weighted;
-            }
+            if (tid == 0) *reinterpret_cast<RowSums*>(g.partial + unit * kPartial) = sums;
             if constexpr (TOP)
                 if (tid < g.top) g.lists[unit * g.top + tid] = tops.best[tid];
         }
@@ -538,11 +563,12 @@ __global__ void __launch_bounds__(THREADS) token_row_kernel(TokenArgs g) {
 }
 
 constexpr int kMaxParts = 64;
+static_assert(sizeof(RowSums) <= kPartial * sizeof(float), "a row part leaves a RowSums");
 
 // Joins the parts of a row.
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kTokBlock) token_join_kernel(TokenArgs g) {
-    __shared__ float scratch[5 * kScratch];
+    __shared__ float scratch[6 * kScratch];
     __shared__ int32_t owner;
     __shared__ std::conditional_t<TOP, Best<kMaxParts * kMaxTop, kTokBlock>, int> tops;
     const int32_t tid = threadIdx.x, parts = g.parts;
@@ -556,26 +582,33 @@ __global__ void __launch_bounds__(kTokBlock) token_join_kernel(TokenArgs g) {
         for (int32_t p = tid; p < all; p += kTokBlock) tops.keys[p] = lists[p];
         if (tid == 0) tops.count = all;
     }
-    float m = -INFINITY, rest = 0.0f, weighted = 0.0f;
-    if (tid < parts) {
-        const float* p = g.partial + (r * parts + tid) * 4;
-        m = p[0]; rest = p[1]; weighted = p[2];
-    }
-    const bool none = m == -INFINITY && rest == 0.0f;
-    const float max = block_max<kTokBlock>(m, scratch);
-    if (tid < parts && m == max) atomicMin(&owner, tid);
+    RowSums mine{-INFINITY, 0.0f, 0.0f};
+    if (tid < parts) mine = *reinterpret_cast<const RowSums*>(g.partial + (r * parts + tid) * kPartial);
+    const bool none = row_empty(mine);
+    const float max = block_max<kTokBlock>(mine.max, scratch);
+    if (tid < parts && mine.max == max) atomicMin(&owner, tid);
     __syncthreads();
     // the part that holds the maximum keeps its R; the others bring their own maximum's term along
-    const float d = (fmaxf(max, -kTokFltMax) - fmaxf(m, -kTokFltMax)) * kTokLog2e, f = exp2_of(-d);
-    float s = rest, t = weighted;
+    const float d = (fmaxf(max, -kTokFltMax) - fmaxf(mine.max, -kTokFltMax)) * kTokLog2e, f = exp2_of(-d), whole = 1.0f + mine.rest;
+    float s = mine.rest, t = mine.weighted;
     if (tid != owner && tid < parts) {
-        const float whole = 1.0f + rest;
         s = none ? 0.0f : f * whole;
-        t = !none && f > 0.0f ? f * (weighted - d * whole) : 0.0f;
-        if (rest != rest) s = rest;
+        t = !none && f > 0.0f ? f * (mine.weighted - d * whole) : 0.0f;
+        if (mine.rest != mine.rest) s = mine.rest;
     }
     block_sum2<kTokBlock>(s, t, scratch + kScratch);
-    const RowSums sums{max, s, t};
+    RowSums sums{max, s, t};
+    if ((g.neg || g.stats) && s < kTinyRest && max > -INFINITY) {
+        // M2 and R2 likewise: the owner's part brings its own (its R is no larger), the others their maximum and sum
+        const float top = tid != owner ? mine.max : mine.sure() ? mine.below : -INFINITY;
+        const float below = block_max<kTokBlock>(top, scratch + 3 * kScratch);
+        if (below > -INFINITY) {
+            float of_below = top > -INFINITY ? exp2_of((top - below) * kTokLog2e) * (tid != owner ? whole : mine.rest_below) : 0.0f, zero = 0.0f;
+            block_sum2<kTokBlock>(of_below, zero, scratch + 4 * kScratch);
+            sums.below = below;
+            sums.rest_below = of_below;
+        }
+    }
     const float log_sum = row_log_sum(sums);
     write_tokens<T>(g, row, r, tid, kTokBlock, asked, sums, log_sum);
     if (tid == 0) write_row(g, r, sums, log_sum);
@@ -617,7 +650,20 @@ __global__ void __launch_bounds__(kTokBlock) token_short_kernel(TokenArgs g) {
         }
         rest = group_sum<G>(rest);
         if constexpr (ENT) weighted = group_sum<G>(weighted);
-        const RowSums sums{max, rest, weighted};
+        RowSums sums{max, rest, weighted};
+        if ((g.neg || g.stats) && rest < kTinyRest && max > -INFINITY) {
+            float below = -INFINITY, of_below = 0.0f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) below = fmaxf(below, lane + G * e == first ? -INFINITY : x[e]);
+            below = group_max<G>(below);
+#pragma unroll
+            for (int e = 0; e < E; ++e) of_below += lane + G * e == first ? 0.0f : exp2_of((x[e] - below) * kTokLog2e);
+            of_below = group_sum<G>(of_below);
+            if (below > -INFINITY) {
+                sums.below = below;
+                sums.rest_below = of_below;
+            }
+        }
         const float log_sum = row_log_sum(sums);
         write_tokens<T>(g, row, r, lane, G, asked, sums, log_sum);
         if (lane == 0) write_row(g, r, sums, log_sum);
@@ -640,15 +686,28 @@ __global__ void __launch_bounds__(kTokBlock) token_short_kernel(TokenArgs g) {
 
 // ---- gradient -----------------------------------------------------------------------------------------------------
 //   dx_j = sum_{k: t_k != j} p_j (n_k p_k / (1 - p_k) - g_k) + sum_{k: t_k = j} (g_k (1 - p_j) - n_k p_j) - h p_j (ln p_j + H)
-// with g, n, h the adjoints of logp, neg, H.  The two sums are kept apart: in a sure row n p / (1 - p) is large, and its share for the
-// token itself must not be the difference of two large numbers.
+// with g, n, h the adjoints of logp, neg, H.  The two sums are kept apart: where p is near 1 n p / (1 - p) is large, and its share for the
+// token itself must not be the difference of two large numbers.  In a sure row p_j / (1 - p) for the token of the maximum, the share of
+// element j in the others' sum, is q_j = e^(x_j - M2) / R2 (neither p_j nor 1 - p needs to be in fp32's range).
+struct BackRow {
+    float max, log_sum, entropy, below, rest_below;
+    explicit __device__ __forceinline__ BackRow(const RowStats& s)
+        : max(s.max), log_sum(s.sum), entropy(s.entropy), below(s.below), rest_below(s.sum) {
+        if (sure()) log_sum = expf(below - max) * rest_below;
+    }
+    __device__ __forceinline__ bool sure() const { return below < max; }
+    // nothing but -inf (a row of NaN, or of NaN and -inf, has a log_sum of NaN)
+    __device__ __forceinline__ bool empty() const { return max == -INFINITY && log_sum == 0.0f; }
+    __device__ __forceinline__ float share(float x) const { return x < max ? exp2_of((x - below) * kTokLog2e) / rest_below : 0.0f; }
+};
 struct TokenGrad {
     int32_t token;          // < 0: nothing (not asked, out of range, or no adjoint)
     float others, itself;   // n p / (1 - p) - g;  g (1 - p) - n p
 };
 
+// `sure` += n p of a sure row's token of the maximum, which goes to the other elements by their shares.
 template <typename T>
-__device__ __forceinline__ TokenGrad token_grad(const TokenArgs& g, const T* row, int64_t r, int32_t k, const RowStats& s) {
+__device__ __forceinline__ TokenGrad token_grad(const TokenArgs& g, const T* row, int64_t r, int32_t k, const BackRow& s, float& sure) {
     TokenGrad out{-1, 0.0f, 0.0f};
     const int64_t t = g.tokens[g.token_rows.at(r) + k * g.token_stride];
     if (t < 0) return out;
@@ -658,11 +717,15 @@ __device__ __forceinline__ TokenGrad token_grad(const TokenArgs& g, const T* row
         out.others = __int_as_float(0x7fc00000);
         return out;
     }
-    const float lp = row_logp((float)row[t], s.max, s.log_sum) + (s.log_sum - s.log_sum);       // (a NaN of the row reaches every token)
+    const float x = (float)row[t], lp = row_logp(x, s.max, s.log_sum) + (s.log_sum - s.log_sum);       // (a NaN of the row reaches every token)
     const float p = expf(lp), away = -expm1f(lp);
     out.token = (int32_t)t;
     float w = nk != 0.0f && away > 0.0f ? nk * p / away : 0.0f;
-    if (fabsf(w) > 1e38f) w = copysignf(1e38f, w);      // (1 - p at the end of the range: finite, as what it stands for is)
+    if (fabsf(w) > 1e38f) w = copysignf(1e38f, w);      // (an adjoint beyond 2^60: no infinity that meets a p_j of 0)
+    if (s.sure() && x == s.max) {
+        sure += nk * p;
+        w = 0.0f;
+    }
     out.others = w - gk;
     out.itself = gk * away - nk * p;
     if (lp != lp) out.others = out.itself = lp;
@@ -684,7 +747,7 @@ struct BulkGrad {
     }
     __device__ __forceinline__ float p(float x) const { return exp2_of(fmaf(x - max, kTokLog2e, -shift)); }
 };
-__device__ __forceinline__ BulkGrad bulk_grad(const RowStats& s, float others, float h) {
+__device__ __forceinline__ BulkGrad bulk_grad(const BackRow& s, float others, float h) {
     BulkGrad b;
     b.max = s.max;
     b.shift = s.log_sum * kTokLog2e;
@@ -700,7 +763,7 @@ template <typename T, int THREADS>
 __global__ void __launch_bounds__(THREADS) token_back_kernel(TokenArgs g) {
     constexpr int N = 16 / sizeof(T), U = 4;
     __shared__ TokenGrad grads[kMaxTokens];
-    __shared__ float scratch[2 * kScratch];
+    __shared__ float scratch[4 * kScratch];
     const int32_t tid = threadIdx.x, K = g.num_tokens;
     for (int64_t unit = blockIdx.x; unit < g.rows * g.parts; unit += gridDim.x) {
         const int64_t r = unit / g.parts;
@@ -714,20 +777,32 @@ __global__ void __launch_bounds__(THREADS) token_back_kernel(TokenArgs g) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (u * THREADS + tid < share.vectors) next[u] = stream_raw<N>(row + share.at(u, tid));
-        const RowStats s = g.stats[r];
-        float others = 0.0f, asked = 0.0f;
+        const BackRow s(g.stats[r]);
+        float others = 0.0f, asked = 0.0f, sure = 0.0f, none = 0.0f;
         for (int32_t k = tid; k < K; k += THREADS) {
-            const TokenGrad t = token_grad<T>(g, row, r, k, s);
+            const TokenGrad t = token_grad<T>(g, row, r, k, s, sure);
             grads[k] = t;
             others += t.others;
             asked += t.token >= 0 || t.others != t.others ? 1.0f : 0.0f;
         }
         block_sum2<THREADS>(others, asked, scratch);
+        if (s.sure()) block_sum2<THREADS>(sure, none, scratch + 2 * kScratch);
         const float h = g.dentropy ? g.dentropy[r] : 0.0f;
         // a row that nothing was asked of, or that allows nothing, has no gradient, whatever it holds
         const bool live = !s.empty() && (asked > 0.0f || h != 0.0f);
         const BulkGrad bulk = bulk_grad(s, others, h);
-        if (live) {
+        if (live && sure != 0.0f) {
+            for (int32_t i = 0; i * THREADS + tid < share.vectors; ++i) {
+                float x[N];
+                load_elements<N>(x, row + share.at(i, tid));
+#pragma unroll
+                for (int q = 0; q < N; ++q) x[q] = bulk.at(x[q]) + sure * s.share(x[q]);
+                stream_elements<N>(out + share.at(i, tid), x);
+            }
+            const int32_t at[2] = {share.lo + tid, share.full + tid};
+            if (tid < share.head()) out[at[0]] = (T)(bulk.at((float)row[at[0]]) + sure * s.share((float)row[at[0]]));
+            if (tid < share.tail()) out[at[1]] = (T)(bulk.at((float)row[at[1]]) + sure * s.share((float)row[at[1]]));
+        } else if (live) {
             for (int32_t i = 0; i * THREADS + tid < share.vectors; i += U) {
                 Raw<T, N> now[U];
 #pragma unroll
@@ -769,7 +844,8 @@ __global__ void __launch_bounds__(THREADS) token_back_kernel(TokenArgs g) {
                     }
                 }
                 const float x = (float)row[j];
-                if (first) out[j] = (T)(itself + (rest != 0.0f ? rest * bulk.p(x) : 0.0f) + bulk.entropy_at(x));
+                if (first)
+                    out[j] = (T)(itself + (rest != 0.0f ? rest * bulk.p(x) : 0.0f) + (sure != 0.0f ? sure * s.share(x) : 0.0f) + bulk.entropy_at(x));
             }
         }
         __syncthreads();            // grads and scratch are free again
@@ -783,10 +859,10 @@ __global__ void __launch_bounds__(kTokBlock) token_back_short_kernel(TokenArgs g
     for (int64_t r = ((int64_t)blockIdx.x * kTokBlock + threadIdx.x) / G; r < g.rows; r += (int64_t)gridDim.x * (kTokBlock / G)) {
         const T* row = static_cast<const T*>(g.logits) + g.logit_rows.at(r);
         T* out = static_cast<T*>(g.dlogits) + r * g.vocab;
-        const RowStats s = g.stats[r];
+        const BackRow s(g.stats[r]);
         const float h = g.dentropy ? g.dentropy[r] : 0.0f;
         const BulkGrad bulk = bulk_grad(s, 0.0f, h);
-        float p[E], y[E], asked = 0.0f;
+        float p[E], y[E], asked = 0.0f, sure = 0.0f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const bool in = lane + G * e < g.vocab && !s.empty();
@@ -796,7 +872,7 @@ __global__ void __launch_bounds__(kTokBlock) token_back_short_kernel(TokenArgs g
         }
         for (int32_t k0 = 0; k0 < g.num_tokens; k0 += G) {
             TokenGrad mine{-1, 0.0f, 0.0f};
-            if (k0 + lane < g.num_tokens) mine = token_grad<T>(g, row, r, k0 + lane, s);
+            if (k0 + lane < g.num_tokens) mine = token_grad<T>(g, row, r, k0 + lane, s, sure);
             const int32_t n = g.num_tokens - k0 < G ? g.num_tokens - k0 : G;
             for (int32_t o = 0; o < n; ++o) {
                 const int32_t token = __shfl(mine.token, o, G);
@@ -806,6 +882,12 @@ __global__ void __launch_bounds__(kTokBlock) token_back_short_kernel(TokenArgs g
 #pragma unroll
                 for (int e = 0; e < E; ++e) y[e] += lane + G * e == token ? itself : (others != 0.0f ? others * p[e] : 0.0f);
             }
+        }
+        if (s.sure()) {
+            sure = group_sum<G>(sure);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (sure != 0.0f && lane + G * e < g.vocab) y[e] += sure * s.share((float)row[lane + G * e]);
         }
         const bool live = !s.empty() && (asked > 0.0f || h != 0.0f);
 #pragma unroll
