@@ -9,6 +9,7 @@ from __future__ import annotations
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd.forward_ad import unpack_dual
 from torch.autograd.function import once_differentiable
 
 from . import binding as _b
@@ -29,6 +30,12 @@ def _check_tensor(t, name, dtypes=None):
         raise ValueError(name + " must be a CUDA tensor")
     if dtypes is not None and t.dtype not in dtypes:
         raise ValueError("%s must be %s" % (name, " or ".join(str(d).replace("torch.", "") for d in dtypes)))
+
+
+def _refuse_tangents(who, *tensors):
+    """The operators have no forward-mode derivative, and a kernel would drop a dual tensor's tangent without a word."""
+    if any(t is not None and unpack_dual(t).tangent is not None for t in tensors):
+        raise RuntimeError(who + " has no forward-mode derivative")
 
 
 def _ptr(t):
@@ -140,7 +147,8 @@ def token_logprobs(logits, tokens=None, *, complement=False, entropy=False, top=
     rounds to 1); with ``entropy`` the rows' entropies ``[...]``; with ``top`` = n the n most likely tokens, equal ones by their
     index, as ``top_logp[..., n]`` and ``top_tokens[..., n]``.  A logit of -inf is a token that is not allowed, a negative token
     asks for nothing (weight 1 for both literals, log 0; no gradient), a token >= V gives NaN.  ``logp``, ``neg`` and ``entropy``
-    are differentiable with respect to ``logits``; of the alternatives neither is (ask for them as ``tokens``).
+    are differentiable with respect to ``logits`` (backward only: tensors with tangents are refused); of the alternatives neither is
+    (ask for them as ``tokens``).
 
     The elements of a row should be next to each other and the rows reachable with two strides (as those of ``logits[:, :-1]``
     are); anything else is copied first.  At most 1024 tokens and 64 alternatives a row.
@@ -161,6 +169,7 @@ def token_logprobs(logits, tokens=None, *, complement=False, entropy=False, top=
     top = int(top)
     if logits.shape[-1] >= 1 << 31 or not 0 <= top <= min(_MOST_TOP, logits.shape[-1]):
         raise ValueError("top must be 0 .. min(V, %d), and V below 2^31" % _MOST_TOP)
+    _refuse_tangents("token_logprobs", logits)
     if torch.is_grad_enabled() and logits.requires_grad:
         return TokenLogprobs(*_TokenLogprobs.apply(logits, tokens, complement, entropy, top))
     return TokenLogprobs(*_tokens_forward(logits, tokens, complement, entropy, top, False)[:5])
@@ -259,8 +268,8 @@ def gated_scan(gates, inputs, initial=None, semiring=KLAY_REAL, offsets=None):
     one after the other: ``gates``, ``inputs`` are ``[N, C]``, sequence s is the rows ``offsets[s]`` to ``offsets[s + 1] - 1``, the
     states are ``[S, C]``; a sequence may be empty, and rows of none get states and gradients of 0.
 
-    Differentiable (``KLAY_REAL``, ``KLAY_LOG``) with respect to gates, inputs and initial, through both results.  The channels
-    should be next to each other; other layouts are copied first.
+    Differentiable (``KLAY_REAL``, ``KLAY_LOG``; backward only: tensors with tangents are refused) with respect to gates, inputs and
+    initial, through both results.  The channels should be next to each other; other layouts are copied first.
     """
     _check_recurrence(gates, inputs, semiring)
     if gates.dim() != (3 if offsets is None else 2):
@@ -275,6 +284,7 @@ def gated_scan(gates, inputs, initial=None, semiring=KLAY_REAL, offsets=None):
         if initial.shape != (sequences, gates.shape[-1]) or initial.device != gates.device:
             raise ValueError("initial must be [%d, %d] on the device of gates" % (sequences, gates.shape[-1]))
     semiring = int(semiring)
+    _refuse_tangents("gated_scan", gates, inputs, initial)
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (gates, inputs, initial)):
         if semiring == KLAY_MAXLOG:
             raise RuntimeError("the (max, +) semiring is not differentiated; evaluate it under torch.no_grad()")
@@ -298,6 +308,7 @@ def gated_step(gates, inputs, state, semiring=KLAY_REAL, out=None):
     ss, os = state.stride(), out.stride()
     if (channels > 1 and (ss[1] != 1 or os[1] != 1)) or (batch > 1 and (ss[0] < channels or os[0] < channels)):
         raise ValueError("state and out must have their channels next to each other and rows that do not overlap")
+    _refuse_tangents("gated_step", gates, inputs, state, out)
     if torch.is_grad_enabled() and (gates.requires_grad or inputs.requires_grad or state.requires_grad or out.requires_grad):
         raise RuntimeError("gated_step is not differentiated; call it under torch.no_grad(), or gated_scan")
     (gates, gs), (inputs, xs) = _channels_last(gates), _channels_last(inputs)
