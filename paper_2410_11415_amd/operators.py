@@ -177,12 +177,13 @@ def token_logprobs(logits, tokens=None, *, complement=False, entropy=False, top=
 
 # ---- gated recurrence ---------------------------------------------------------------------------------------------
 def _channels_last(t):
-    """(t, its strides), or those of a copy where its channels lie apart (or its time steps further than the kernels reach)"""
-    strides = t.stride()
-    if (strides[-1] != 1 and t.shape[-1] != 1) or strides[-2] > _MOST_CHANNELS:
+    """(t, its strides), or those of a copy where its channels lie apart (or its time steps further than the kernels reach).  The stride
+    of a single step is 0: whatever the tensor says, contiguous() would leave it as it is."""
+    shape, strides = t.shape, t.stride()
+    if (strides[-1] != 1 and shape[-1] != 1) or (strides[-2] > _MOST_CHANNELS and shape[-2] > 1):
         t = t.contiguous()
         strides = t.stride()
-    return t, strides
+    return t, strides if shape[-2] > 1 else strides[:-2] + (0, 1)
 
 
 def _scan_args(gates, inputs, initial, semiring, offsets, row_info):

@@ -47,3 +47,32 @@ def test_transformed_functions_are_refused(calls):
     with pytest.raises(RuntimeError, match="forward-mode"):
         torch.func.jvp(lambda x: operators.token_logprobs(x, None, entropy=True).entropy, (torch.ones(2, 5),), (torch.ones(2, 5),))
     assert not calls
+
+
+FAR = 1 << 26           # further than the kernels' 32-bit offsets of a time step reach
+
+
+@pytest.mark.parametrize("which", ["gates", "inputs"])
+def test_the_stride_of_a_single_step(calls, which):
+    """one step out of a long time-first tensor, and one packed row of a wide one: no copy, and no stride that the library refuses"""
+    far, near = torch.ones(12).as_strided((3, 1, 4), (4, FAR, 1)), torch.ones(3, 1, 4)
+    operators.gated_scan(*((far, near) if which == "gates" else (near, far)))
+    row, plain = torch.ones(4).as_strided((1, 4), (FAR, 1)), torch.ones(1, 4)
+    operators.gated_scan(*((row, plain) if which == "gates" else (plain, row)), offsets=torch.tensor([0, 1]))
+    operators.gated_step(*((row, plain) if which == "gates" else (plain, row)), torch.ones(1, 4))
+    dense, packed, step = calls
+    for args, given in ((dense, far), (packed, row)):
+        assert 0 <= args.gates_time_stride <= 1 << 25 and 0 <= args.inputs_time_stride <= 1 << 25
+        assert (args.gates if which == "gates" else args.inputs) == given.data_ptr()
+    assert dense.gates_batch_stride == dense.inputs_batch_stride == 4
+    assert step[5 if which == "gates" else 7] == row.data_ptr()
+
+
+def test_steps_too_far_apart_are_copied(calls):
+    """(the library's arguments are those of the copy, whose memory is gone by now)"""
+    base = torch.empty(0).set_(torch.UntypedStorage(4 * (FAR + 8)), 0, (2, 4), (FAR, 1))
+    base[0], base[1] = 1.0, 2.0
+    operators.gated_scan(base, torch.ones(2, 4), offsets=torch.tensor([0, 2]))
+    assert calls[0].gates != base.data_ptr() and calls[0].gates_time_stride == 4
+    operators.gated_scan(base[None], torch.ones(1, 2, 4))
+    assert calls[1].gates != base.data_ptr() and calls[1].gates_time_stride == 4
