@@ -47,19 +47,19 @@ constexpr int64_t kWaveRow = 16384;
 constexpr int64_t kManyRows = 2 * kComputeUnits;        // workgroups that keep the chip busy by themselves
 
 klay_status check_tokens(const klay_tokens_args* a, const char* who) {
-    const std::string name(who);
-    if (!a) return fail(KLAY_EINVAL, name + ": null argument");
-    if (!known_dtype(a->dtype)) return fail(KLAY_EINVAL, name + ": unknown dtype");
+    auto refused = [who](const std::string& why) { return fail(KLAY_EINVAL, who + (": " + why)); };
+    if (!a) return refused("null argument");
+    if (!known_dtype(a->dtype)) return refused("unknown dtype");
     if (a->vocab < 1 || a->num_tokens < 0 || a->num_tokens > klay::kMaxTokens)
-        return fail(KLAY_EINVAL, name + ": vocab must be >= 1 and num_tokens 0 .. " + std::to_string(klay::kMaxTokens));
+        return refused("vocab must be >= 1 and num_tokens 0 .. " + std::to_string(klay::kMaxTokens));
     if (a->top < 0 || a->top > klay::kMaxTop || a->top > a->vocab)
-        return fail(KLAY_EINVAL, name + ": top must be 0 .. min(vocab, " + std::to_string(klay::kMaxTop) + ")");
-    if (a->rows < 0 || a->rows > INT32_MAX) return fail(KLAY_EINVAL, name + ": rows must be 0 .. 2^31 - 1");
+        return refused("top must be 0 .. min(vocab, " + std::to_string(klay::kMaxTop) + ")");
+    if (a->rows < 0 || a->rows > INT32_MAX) return refused("rows must be 0 .. 2^31 - 1");
     if (a->rows == 0) return KLAY_OK;
-    if (!a->logits || (a->num_tokens > 0 && !a->tokens)) return fail(KLAY_EINVAL, name + ": null argument");
+    if (!a->logits || (a->num_tokens > 0 && !a->tokens)) return refused("null argument");
     if (a->logit_rows.inner < 1 || a->logit_rows.inner > INT32_MAX ||
         (a->num_tokens > 0 && (a->token_rows.inner < 1 || a->token_rows.inner > INT32_MAX)))
-        return fail(KLAY_EINVAL, name + ": the inner axis of rows must be 1 .. 2^31 - 1");
+        return refused("the inner axis of rows must be 1 .. 2^31 - 1");
     return KLAY_OK;
 }
 
@@ -169,21 +169,21 @@ struct ScanPlan {
 };
 
 klay_status check_scan(const klay_scan_args* a, bool inputs, const char* who) {
-    const std::string name(who);
-    if (!a) return fail(KLAY_EINVAL, name + ": null argument");
-    if (!known_dtype(a->dtype)) return fail(KLAY_EINVAL, name + ": unknown dtype");
-    if (a->semiring != KLAY_REAL && a->semiring != KLAY_LOG && a->semiring != KLAY_MAXLOG) return fail(KLAY_EINVAL, name + ": unknown semiring");
-    if (a->semiring != KLAY_REAL && a->dtype != KLAY_F32) return fail(KLAY_EINVAL, name + ": the log-domain semirings take KLAY_F32 only");
+    auto refused = [who](const std::string& why) { return fail(KLAY_EINVAL, who + (": " + why)); };
+    if (!a) return refused("null argument");
+    if (!known_dtype(a->dtype)) return refused("unknown dtype");
+    if (a->semiring != KLAY_REAL && a->semiring != KLAY_LOG && a->semiring != KLAY_MAXLOG) return refused("unknown semiring");
+    if (a->semiring != KLAY_REAL && a->dtype != KLAY_F32) return refused("the log-domain semirings take KLAY_F32 only");
     if (a->channels < 1 || a->channels > kMostChannels || a->batch < 0 || a->time < 0 || a->time > INT32_MAX || a->batch > INT32_MAX / 8)
-        return fail(KLAY_EINVAL, name + ": channels must be 1 .. 2^25, time 0 .. 2^31 - 1, batch 0 .. 2^28 - 1");
+        return refused("channels must be 1 .. 2^25, time 0 .. 2^31 - 1, batch 0 .. 2^28 - 1");
     if (a->gates_time_stride < 0 || a->gates_time_stride > kMostChannels || a->inputs_time_stride < 0 || a->inputs_time_stride > kMostChannels)
-        return fail(KLAY_EINVAL, name + ": the time strides must be 0 .. 2^25");
+        return refused("the time strides must be 0 .. 2^25");
     if (a->offsets) {
-        if (a->batch != 1) return fail(KLAY_EINVAL, name + ": packed sequences have batch = 1");
-        if (a->sequences < 0 || a->sequences > INT32_MAX / 8) return fail(KLAY_EINVAL, name + ": sequences must be 0 .. 2^28 - 1");
-        if (a->time > 0 && !a->row_info) return fail(KLAY_EINVAL, name + ": packed sequences need row_info");
+        if (a->batch != 1) return refused("packed sequences have batch = 1");
+        if (a->sequences < 0 || a->sequences > INT32_MAX / 8) return refused("sequences must be 0 .. 2^28 - 1");
+        if (a->time > 0 && !a->row_info) return refused("packed sequences need row_info");
     }
-    if (a->batch > 0 && a->time > 0 && (!a->gates || (inputs && !a->inputs))) return fail(KLAY_EINVAL, name + ": null argument");
+    if (a->batch > 0 && a->time > 0 && (!a->gates || (inputs && !a->inputs))) return refused("null argument");
     return KLAY_OK;
 }
 
@@ -330,7 +330,7 @@ size_t klay_tokens_workspace_bytes(const klay_tokens_args* a) {
 }
 
 klay_status klay_tokens_forward(const klay_tokens_args* a, float* logp, float* neg, float* entropy, float* stats, float* top_logp,
-                                int64_t* top_tokens, void* workspace, size_t workspace_bytes, void* stream) {
+                                int64_t* top_tokens, void* workspace, size_t workspace_bytes, void* stream) try {
     const klay_status st = check_tokens(a, "klay_tokens_forward");
     if (st != KLAY_OK || a->rows == 0) return st;
     if ((a->num_tokens > 0 && !logp) || (a->top > 0 && (!top_logp || !top_tokens)))
@@ -353,10 +353,12 @@ klay_status klay_tokens_forward(const klay_tokens_args* a, float* logp, float* n
     if (a->dtype == KLAY_F32) return run_tokens<klay::f32>(g, plan.threads, stream);
     if (a->dtype == KLAY_BF16) return run_tokens<klay::bf16>(g, plan.threads, stream);
     return run_tokens<klay::f16>(g, plan.threads, stream);
+} catch (const std::bad_alloc&) {
+    return fail(KLAY_ENOMEM, "klay_tokens_forward: out of host memory");
 }
 
 klay_status klay_tokens_backward(const klay_tokens_args* a, const float* stats, const float* dlogp, const float* dneg,
-                                 const float* dentropy, void* dlogits, void* stream) {
+                                 const float* dentropy, void* dlogits, void* stream) try {
     const klay_status st = check_tokens(a, "klay_tokens_backward");
     if (st != KLAY_OK || a->rows == 0) return st;
     if (!stats || !dlogits) return fail(KLAY_EINVAL, "klay_tokens_backward: null argument");
@@ -371,6 +373,8 @@ klay_status klay_tokens_backward(const klay_tokens_args* a, const float* stats, 
     if (a->dtype == KLAY_F32) return run_tokens_back<klay::f32>(g, plan.threads, stream);
     if (a->dtype == KLAY_BF16) return run_tokens_back<klay::bf16>(g, plan.threads, stream);
     return run_tokens_back<klay::f16>(g, plan.threads, stream);
+} catch (const std::bad_alloc&) {
+    return fail(KLAY_ENOMEM, "klay_tokens_backward: out of host memory");
 }
 
 size_t klay_scan_workspace_bytes(const klay_scan_args* a) {
@@ -378,7 +382,7 @@ size_t klay_scan_workspace_bytes(const klay_scan_args* a) {
     return (size_t)scan_words(scan_plan(a)) * sizeof(uint64_t);
 }
 
-klay_status klay_scan_forward(const klay_scan_args* a, void* states, float* final, void* workspace, size_t workspace_bytes, void* stream) {
+klay_status klay_scan_forward(const klay_scan_args* a, void* states, float* final, void* workspace, size_t workspace_bytes, void* stream) try {
     klay_status st = check_scan(a, true, "klay_scan_forward");
     if (st != KLAY_OK) return st;
     const int64_t sequences = a->offsets ? a->sequences : a->batch;
@@ -411,10 +415,12 @@ klay_status klay_scan_forward(const klay_scan_args* a, void* states, float* fina
     g.out = states;
     g.final = final;
     return run_scan(a, g, p, false, stream);
+} catch (const std::bad_alloc&) {
+    return fail(KLAY_ENOMEM, "klay_scan_forward: out of host memory");
 }
 
 klay_status klay_scan_backward(const klay_scan_args* a, const void* states, const void* dstates, const float* dfinal, void* dgates,
-                               void* dinputs, float* dinitial, void* workspace, size_t workspace_bytes, void* stream) {
+                               void* dinputs, float* dinitial, void* workspace, size_t workspace_bytes, void* stream) try {
     klay_status st = check_scan(a, a && a->semiring == KLAY_LOG, "klay_scan_backward");
     if (st != KLAY_OK) return st;
     if (a->semiring == KLAY_MAXLOG) return fail(KLAY_EINVAL, "klay_scan_backward: the (max, +) semiring is not differentiated");
@@ -444,11 +450,13 @@ klay_status klay_scan_backward(const klay_scan_args* a, const void* states, cons
     g.da = dgates; g.dx = dinputs;
     g.dinitial = dinitial;
     return run_scan(a, g, p, true, stream);
+} catch (const std::bad_alloc&) {
+    return fail(KLAY_ENOMEM, "klay_scan_backward: out of host memory");
 }
 
 klay_status klay_scan_step(int32_t dtype, int32_t semiring, int32_t device, int64_t rows, int32_t channels, const void* gates,
                            int64_t gates_stride, const void* inputs, int64_t inputs_stride, float* state, int64_t state_stride, void* out,
-                           int64_t out_stride, void* stream) {
+                           int64_t out_stride, void* stream) try {
     if (!known_dtype(dtype)) return fail(KLAY_EINVAL, "klay_scan_step: unknown dtype");
     if (semiring != KLAY_REAL && semiring != KLAY_LOG && semiring != KLAY_MAXLOG) return fail(KLAY_EINVAL, "klay_scan_step: unknown semiring");
     if (semiring != KLAY_REAL && dtype != KLAY_F32) return fail(KLAY_EINVAL, "klay_scan_step: the log-domain semirings take KLAY_F32 only");
@@ -465,6 +473,8 @@ klay_status klay_scan_step(int32_t dtype, int32_t semiring, int32_t device, int6
     if (dtype == KLAY_F32) return run_step<klay::SEMI_REAL, klay::f32>(g, wide, stream);
     if (dtype == KLAY_BF16) return run_step<klay::SEMI_REAL, klay::bf16>(g, wide, stream);
     return run_step<klay::SEMI_REAL, klay::f16>(g, wide, stream);
+} catch (const std::bad_alloc&) {
+    return fail(KLAY_ENOMEM, "klay_scan_step: out of host memory");
 }
 
 }  // extern "C"
