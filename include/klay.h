@@ -340,7 +340,8 @@ void klay_destroy(klay_circuit* c);
 /*
  * Operators between a network and a circuit's leaf weights.  They need no handle; every call enqueues kernels on `stream` of `device`
  * (of the calling thread's current device it makes no use, and leaves it as it was), allocates nothing and does not synchronise.
- * Two calls may overlap if they share no buffer that either writes.
+ * Two calls may overlap if they share no buffer that either writes.  An output must not overlap another one or an input (klay_scan_step's
+ * state excepted); that dlogits is the logits, final the initial states, dinitial dfinal, or dgates or dinputs the states is refused.
  */
 
 /* Types of the tensors that a network gives and takes: IEEE single, bfloat16, IEEE half.  All arithmetic is in single. */

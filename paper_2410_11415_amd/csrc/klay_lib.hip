@@ -362,6 +362,7 @@ klay_status klay_tokens_backward(const klay_tokens_args* a, const float* stats, 
     const klay_status st = check_tokens(a, "klay_tokens_backward");
     if (st != KLAY_OK || a->rows == 0) return st;
     if (!stats || !dlogits) return fail(KLAY_EINVAL, "klay_tokens_backward: null argument");
+    if (dlogits == a->logits) return fail(KLAY_EINVAL, "klay_tokens_backward: dlogits must not be the logits, which are read again");
     klay::TokenArgs g = token_args(a);
     const TokenPlan plan = a->vocab <= kShortRow ? TokenPlan() : backward_plan(a);
     g.parts = plan.parts; g.part = plan.part;
@@ -388,6 +389,7 @@ klay_status klay_scan_forward(const klay_scan_args* a, void* states, float* fina
     const int64_t sequences = a->offsets ? a->sequences : a->batch;
     const bool rows = a->batch > 0 && a->time > 0;
     if (rows && !states) return fail(KLAY_EINVAL, "klay_scan_forward: null argument");
+    if (final && final == a->initial) return fail(KLAY_EINVAL, "klay_scan_forward: final must not be initial, which is read again");
     ScanPlan p = rows ? scan_plan(a) : ScanPlan();
     st = scan_workspace(a, p, workspace, workspace_bytes, "klay_scan_forward");
     if (st != KLAY_OK) return st;
@@ -427,6 +429,8 @@ klay_status klay_scan_backward(const klay_scan_args* a, const void* states, cons
     const int64_t sequences = a->offsets ? a->sequences : a->batch;
     const bool rows = a->batch > 0 && a->time > 0;
     if (rows && !states) return fail(KLAY_EINVAL, "klay_scan_backward: null argument");
+    if ((dinitial && dinitial == dfinal) || (rows && (dgates == states || dinputs == states)))
+        return fail(KLAY_EINVAL, "klay_scan_backward: dinitial must not be dfinal, nor dgates or dinputs the states, which are read again");
     ScanPlan p = rows ? scan_plan(a) : ScanPlan();
     st = scan_workspace(a, p, workspace, workspace_bytes, "klay_scan_backward");
     if (st != KLAY_OK) return st;

@@ -1,5 +1,5 @@
 """Calls of the operators that reach the library with other arguments than were meant, or not at all, with no GPU: the library's calls are
-replaced by ones that take down their arguments."""
+replaced by ones that take down their arguments.  And outputs in the place of inputs that are read again, which the library refuses."""
 import pytest
 import torch
 import torch.autograd.forward_ad as fwd
@@ -76,3 +76,33 @@ def test_steps_too_far_apart_are_copied(calls):
     assert calls[0].gates != base.data_ptr() and calls[0].gates_time_stride == 4
     operators.gated_scan(base[None], torch.ones(1, 2, 4))
     assert calls[1].gates != base.data_ptr() and calls[1].gates_time_stride == 4
+
+
+# ---- one buffer for two arguments ---------------------------------------------------------------------------------
+P, Q, R = 4096, 8192, 12288         # pointers that no refused call looks behind
+
+
+def tokens_args():
+    rows = binding.klay_rows(4, 0, 10)
+    return binding.klay_tokens_args(0, 0, 10, 0, 0, 0, 4, P, rows, None, rows, 0)
+
+
+def scan_args(batch=2, time=5):
+    return binding.klay_scan_args(0, 0, 0, 3, batch, time, 0, P, P, 15, 3, 15, 3, None, None, Q)
+
+
+SHARED = {
+    "dlogits": lambda: binding.klay_tokens_backward(tokens_args(), Q, None, None, Q, P),
+    "final": lambda: binding.klay_scan_forward(scan_args(), R, Q, None, 0),
+    "final, no steps": lambda: binding.klay_scan_forward(scan_args(time=0), None, Q, None, 0),
+    "dinitial": lambda: binding.klay_scan_backward(scan_args(), R, None, Q, P, P, Q, None, 0),
+    "dgates": lambda: binding.klay_scan_backward(scan_args(), R, None, None, R, None, None, None, 0),
+    "dinputs": lambda: binding.klay_scan_backward(scan_args(), R, None, None, None, R, None, None, 0),
+}
+
+
+@pytest.mark.parametrize("which", sorted(SHARED))
+def test_outputs_in_the_place_of_inputs(which):
+    with pytest.raises(binding.KlayError, match="must not be") as e:
+        SHARED[which]()
+    assert e.value.status == binding.KLAY_EINVAL
