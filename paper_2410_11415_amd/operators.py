@@ -9,7 +9,7 @@ from __future__ import annotations
 from typing import NamedTuple, Optional
 
 import torch
-from torch.autograd.forward_ad import unpack_dual
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
 from . import binding as _b
@@ -33,8 +33,9 @@ def _check_tensor(t, name, dtypes=None):
 
 
 def _refuse_tangents(who, *tensors):
-    """The operators have no forward-mode derivative, and a kernel would drop a dual tensor's tangent without a word."""
-    if any(t is not None and unpack_dual(t).tangent is not None for t in tensors):
+    """The operators have no forward-mode derivative, and a kernel would drop a dual tensor's tangent without a word.  (Outside of a dual level,
+    where this torch tells, there is none: a look at every tensor costs the host a microsecond a call.)"""
+    if getattr(forward_ad, "_current_level", 0) >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
         raise RuntimeError(who + " has no forward-mode derivative")
 
 
@@ -177,13 +178,19 @@ def token_logprobs(logits, tokens=None, *, complement=False, entropy=False, top=
 
 # ---- gated recurrence ---------------------------------------------------------------------------------------------
 def _channels_last(t):
-    """(t, its strides), or those of a copy where its channels lie apart (or its time steps further than the kernels reach).  The stride
-    of a single step is 0: whatever the tensor says, contiguous() would leave it as it is."""
-    shape, strides = t.shape, t.stride()
-    if (strides[-1] != 1 and shape[-1] != 1) or (strides[-2] > _MOST_CHANNELS and shape[-2] > 1):
+    """(t, its strides), or those of a copy where its channels lie apart (or its time steps further than the kernels reach; the stride of a
+    single step, which contiguous() would leave as it is, is of no account)"""
+    strides = t.stride()
+    if strides[-1] != 1 and t.shape[-1] != 1:
         t = t.contiguous()
         strides = t.stride()
-    return t, strides if shape[-2] > 1 else strides[:-2] + (0, 1)
+    elif strides[-2] > _MOST_CHANNELS:
+        if t.shape[-2] > 1:
+            t = t.contiguous()
+            strides = t.stride()
+        else:
+            strides = strides[:-2] + (0, 1)
+    return t, strides
 
 
 def _scan_args(gates, inputs, initial, semiring, offsets, row_info):
