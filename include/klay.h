@@ -407,7 +407,8 @@ klay_status klay_tokens_backward(const klay_tokens_args* args, const float* stat
  *   states      device [batch, time, channels] of `dtype`, contiguous: h, each rounded once from fp32
  *   final       device fp32 [batch or sequences, channels]: the states behind the last steps (of an empty sequence: its initial one); or NULL
  *   workspace   device, 16-byte aligned, klay_scan_workspace_bytes(args) bytes (for either direction); NULL where that is 0
- * Sums are in single.  Products of many gates may leave its range where the states themselves do not (gates above 1 behind a state of 0).
+ * Sums are in single.  Products of many gates, which may leave its range where the states themselves do not (gates above 1 behind a state of
+ * 0), are held as mantissa and exponent then (REAL).
  * A state that is NaN or infinite (in the log domain: +inf) makes all behind it in its sequence and channel NaN or infinite.
  * Offsets that are none (descending, out of range) give undefined values, but no access outside the arrays.
  * Errors: KLAY_EINVAL, KLAY_ENOMEM (workspace too small), KLAY_EHIP.
@@ -428,7 +429,7 @@ klay_status klay_scan_forward(const klay_scan_args* args, void* states, float* f
 /*
  * klay_scan_backward -- derivative of a klay_scan_forward (REAL, LOG) with respect to gates, inputs and initial states.
  *   args        as for the forward call; REAL does not read inputs (may be NULL)
- *   states      as written by the forward call
+ *   states      as written by the forward call (16-bit types: dgates is made with the state before a step as it stands there, rounded)
  *   dstates     device [batch, time, channels] of `dtype`, contiguous, or NULL (no adjoint); dfinal fp32, or NULL
  *   dgates, dinputs   device [batch, time, channels] of `dtype`, contiguous; dinitial fp32; each may be NULL (not wanted)
  * A step whose value is log 0 passes nothing down.  Errors: as klay_scan_forward; MAXLOG is not differentiated (KLAY_EINVAL).

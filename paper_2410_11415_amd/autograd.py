@@ -66,7 +66,8 @@ class CircuitLayer(torch.nn.Module):
         """The circuit on the answers of a network: variable ``g * K + k`` is "position g answers ``tokens[..., g, k]``", its log
         weight (and with ``complement`` that of its negation; without, a negated literal weighs 1, for circuits that say by themselves
         that a position answers one thing) comes from ``logits[B, G, V]`` by :func:`token_logprobs`.  ``tokens``: int64 ``[G, K]`` or
-        ``[B, G, K]`` with G * K the circuit's variables; log-domain semirings only.  Gradients go to ``logits``.
+        ``[B, G, K]`` with G * K the circuit's variables; log-domain semirings only.  Gradients go to ``logits``.  Tokens must be below
+        V: the NaN that others get counts as impossible in the circuit's OR gates.
         """
         from .operators import token_logprobs
         if self.semiring not in (KLAY_LOG, KLAY_MAXLOG):

@@ -40,11 +40,16 @@ bool known_dtype(int32_t t) { return t == KLAY_F32 || t == KLAY_BF16 || t == KLA
 int dtype_bytes(int32_t t) { return t == KLAY_F32 ? 4 : 2; }
 
 // ---- tokens ---------------------------------------------------------------------------------------------------------
-constexpr int32_t kShortRow = 512, kShortestRow = 64;   // rows in the registers of a wave, of a quarter of one
+// Rows in the registers of a wave, of a quarter of one (us, forward and reverse: 65536 x 64 bf16 by quarters / whole waves 13.8 / 50.4, 11.8 / 35.8;
+// 65536 x 512 fp32 by a wave's registers / by a wave that goes through vectors 53.6 / 57.7, 94.6 / 102.5; 65536 x 257 bf16 58 / 58, 50 / 110; 65536 x 512
+// bf16 77.5 / 56.0, 83.4 / 91.9).
+constexpr int32_t kShortRow = 512, kShortestRow = 64;
 // Up to this many bytes a row is a single wave's where there are rows enough (us, four waves / one: 8192 x 8192 bf16 forward 38 / 30,
 // 16384 x 1000 bf16 45 / 19; 4096 x 32768 bf16 48 / 51, backward 112 / 150).
 constexpr int64_t kWaveRow = 16384;
-constexpr int64_t kManyRows = 2 * kComputeUnits;        // workgroups that keep the chip busy by themselves
+// Workgroups that keep the chip busy by themselves (us, forward, as few rows / as many: 256 x 32771 bf16 7.5 / 9.5, 511 rows 13.1 / 11.6, 768 rows 18.7 / 14.2;
+// 256 x 131072 16.6 / 16.6; 511 x 8191 7.3 / 7.8, 1024 rows 8.2 / 9.2, 2000 rows 13.4 / 11.7).
+constexpr int64_t kManyRows = 2 * kComputeUnits;
 
 klay_status check_tokens(const klay_tokens_args* a, const char* who) {
     auto refused = [who](const std::string& why) { return fail(KLAY_EINVAL, who + (": " + why)); };
@@ -81,7 +86,8 @@ TokenPlan in_parts(const klay_tokens_args* a, int threads, int64_t parts) {
 }
 
 // Many rows: a workgroup each.  Few: sixteen waves each, and several workgroups only where a row is so long that what they save is more
-// than the second launch that joins them costs (a workgroup takes in some 55 GB/s; the join is about 8 us).
+// than the second launch that joins them costs (a workgroup takes in some 55 GB/s; the join is about 8 us.  Whole / in parts, us: 1 x 200000 bf16
+// 15.2 / 13.1, 1 x 262144 18.5 / 14.4, 64 x 262144 19.6 / 15.7; 1 x 300000 20.6 / 13.1, 64 x 300000 21.8 / 15.7, 120 x 300000 22.1 / 25.1, 120 x 1000000 62 / 52).
 TokenPlan forward_plan(const klay_tokens_args* a) {
     const int64_t bytes = (int64_t)a->vocab * dtype_bytes(a->dtype);
     if (a->rows >= kManyRows) return in_parts(a, bytes <= kWaveRow ? 64 : 256, 1);

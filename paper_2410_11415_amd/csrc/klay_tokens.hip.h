@@ -3,7 +3,8 @@
 //   M = max x, d_j = x_j - M, S = sum e^d_j = 1 + R (R: all terms but the maximum's own), ln S = log1p(R)
 //   logp_k = d_{t_k} - ln S,  neg_k = ln(1 - p_{t_k}),  H = ln S - sum e^d_j d_j / S
 // R is kept apart from the 1 because everything that a sure network answers lives in it: logp of the likely token is -log1p(R) and its
-// neg ln R - log1p(R), both to fp32's relative accuracy, where S itself has rounded R away.  Below 2^-64 (the others more than 44 under the
+// neg ln R - log1p(R), both as exact, relative to themselves, as the others' exponents are (a few 2^-24 times their distance), where S itself has
+// rounded R away.  Below 2^-64 (the others more than 44 under the
 // maximum: a very sure network, or finite masks that leave one token) R = e^(M2 - M) R2 is held as M2, the largest of the others, and R2,
 // their sum relative to it, since terms below 2^-126 are lost relative to M (2^31 of them are 2^-31 of an R that is not held so).
 //
@@ -11,8 +12,8 @@
 // four issue slots of a CU that has about ten per element at the rate of HBM).  A thread runs through its part of the row once with a
 // reference `ref` that follows its running maximum from afar: it moves only when a value lies more than kSlack above it, so that almost
 // every eight elements cost no rescaling; sums of terms up to e^kSlack lose nothing.  All sums and maxima are fp32.
-// Measured with entropy, bf16 (reads alone reach 7.0 TB/s, a copy 6.1): 4096 x 131072 forward 168 us = 6.4 TB/s at 91% of the vector unit's issue
-// slots, backward 350 us = 6.1 TB/s; 4096 x 32771 forward 52 us = 5.1 TB/s; 1 x 131072 with eight alternatives 17 us, of which one workgroup
+// Measured with entropy, bf16 (reads alone reach 7.0 TB/s, a copy 6.1): 4096 x 131072 forward 165 us = 6.5 TB/s at 88% of the vector unit's issue
+// slots, backward 352 us = 6.1 TB/s; 4096 x 32771 forward 53 us = 5.1 TB/s; 1 x 131072 with eight alternatives 17.7 us, of which one workgroup
 // reads for five.
 #pragma once
 

@@ -276,6 +276,9 @@ def gated_scan(gates, inputs, initial=None, semiring=KLAY_REAL, offsets=None):
     one after the other: ``gates``, ``inputs`` are ``[N, C]``, sequence s is the rows ``offsets[s]`` to ``offsets[s + 1] - 1``, the
     states are ``[S, C]``; a sequence may be empty, and rows of none get states and gradients of 0.
 
+    With 16-bit types the gradient of a gate is made with the state before it as it was returned, rounded to those bits (its relative
+    error about half as much again: 2.3e-3 for 1.7e-3 in bfloat16); pass float32 where that matters.
+
     Differentiable (``KLAY_REAL``, ``KLAY_LOG``; backward only: tensors with tangents are refused) with respect to gates, inputs and
     initial, through both results.  The channels should be next to each other; other layouts are copied first.
     """
