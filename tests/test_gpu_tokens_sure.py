@@ -88,7 +88,7 @@ def rows_of(kind, rows, vocab, dtype, rng):
         x[:] = -np.inf
         x[at, best] = 3.0
     else:
-        x -= kind
+        x -= MIXED[at % len(MIXED), None] if kind == "mixed" else kind
         x[at, best] = rng.uniform(2, 4, size=rows)
     x = torch.from_numpy(x).to(getattr(torch, dtype))
     return x, x.double().numpy(), best
@@ -125,6 +125,7 @@ def check(kind, rows, vocab, dtype, complement=True, entropy=True, looked_at=Non
         ref.close(n(dx[r]), want["dx"], want["dx_tol"], dtype, what + "dlogits")
 
 
+MIXED = np.array([0.0, 60.0, 5.0, 15.0, 1e4, 1.0, 46.0, 95.0])
 KINDS = [15.0, 25.0, 40.0, 46.0, 80.0, 90.0, 110.0, 1e4, "lowest", "lone", "alone"]
 
 
@@ -152,6 +153,13 @@ def test_rows_of_several_workgroups(kind, dtype, vocab):
 @pytest.mark.parametrize("vocab", [50, 700, 9001])
 def test_many_rows(kind, vocab):
     check(kind, 600, vocab, "float32", looked_at=[0, 1, 299, 300, 598, 599])
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16"])
+@pytest.mark.parametrize("vocab", [10, 64, 300, 700, 5000])
+def test_sure_rows_beside_others(vocab, dtype):
+    """(four rows of up to 64 logits share a wave)"""
+    check("mixed", 40, vocab, dtype)
 
 
 def test_the_circuit_of_a_sure_answer():
