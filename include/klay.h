@@ -396,6 +396,86 @@ klay_status klay_tokens_backward(const klay_tokens_args* args, const float* stat
                                  const float* dentropy, void* dlogits, void* stream);
 
 /*
+ * klay_head_forward -- what klay_tokens_forward says of rows of logits, straight from the network's last layer: logit j of row i is
+ * hidden_i . weight_j + bias_j, made in pieces on the chip (fp32 sums, not rounded) and never written.
+ *   hidden      device [rows, width] of `dtype`, the elements of a row next to each other, rows placed by hidden_rows
+ *   weight      device [vocab, width] of `dtype`, the elements of a row next to each other, rows weight_stride elements apart (>= 0)
+ *   bias        device [vocab] fp32, or NULL.  -inf: a token that is not allowed, whatever its weights hold
+ *   tokens      device [rows, num_tokens] int64, placed by token_rows and token_stride: as for klay_tokens_forward
+ *   logp, neg, entropy   as for klay_tokens_forward
+ *   kept        device, 16-byte aligned, klay_list_kept_bytes(rows, num_tokens) bytes: what klay_head_backward needs of the rows; NULL: not kept
+ *   workspace   device, 16-byte aligned, klay_head_workspace_bytes(args, 0) bytes (for klay_head_backward: args, 1)
+ * Rows whose start, stride or length is no multiple of 16 bytes are copied into the workspace first.  A row whose hidden state, or any allowed
+ * token's weights, holds a NaN or an infinity may get NaN in every value.  (fp32: elements are taken apart into three bf16; below 3.38e38.)
+ * Errors: KLAY_EINVAL (sizes out of range: 1 <= vocab <= 2^31 - 4097, 1 <= width <= 2^20, 0 <= num_tokens <= 1024, 0 <= rows <= 2^20; null or
+ * unknown arguments), KLAY_ENOMEM (workspace too small), KLAY_EHIP.
+ */
+typedef struct klay_head_args {
+    int32_t dtype, device, width, vocab, num_tokens, reserved;
+    int64_t rows;
+    const void* hidden;
+    klay_rows hidden_rows;
+    const void* weight;
+    int64_t weight_stride;
+    const float* bias;
+    const int64_t* tokens;
+    klay_rows token_rows;
+    int64_t token_stride;
+} klay_head_args;
+size_t klay_list_kept_bytes(int64_t rows, int32_t num_tokens);
+size_t klay_head_workspace_bytes(const klay_head_args* args, int32_t backward);
+klay_status klay_head_forward(const klay_head_args* args, float* logp, float* neg, float* entropy, void* kept, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/*
+ * klay_head_backward -- derivative of a klay_head_forward, which has kept its rows; hidden, weight, bias must be as they were.
+ *   dlogp, dneg, dentropy   device, shaped as the outputs; each may be NULL (no adjoint)
+ *   dhidden     device [rows, width] contiguous, of `dtype`; dweight device [vocab, width] contiguous, of `dtype`; dbias device [vocab]
+ *               fp32; each may be NULL (not wanted); every entry is written (nothing where rows = 0)
+ * The adjoints of the logits are made again in pieces of the vocabulary and rounded to `dtype` on their way into the two products (fp16: under a
+ * power of two common to all); sums are fp32, and the same inputs give the same bits.  A row all of whose adjoints are exactly 0, or that
+ * allows nothing, has no gradient and gives none, whatever it holds.
+ */
+klay_status klay_head_backward(const klay_head_args* args, const void* kept, const float* dlogp, const float* dneg, const float* dentropy,
+                               void* dhidden, void* dweight, float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * klay_distill_forward -- divergence of rows of logits from what a teacher says of its likeliest tokens (args->tokens, a list a row):
+ *   p = softmax(x / temperature);  q = softmax(teacher / temperature) over the listed tokens
+ *   loss = sum_k q_k (ln q_k - ln p_{t_k})
+ *   rest: the teacher gives log probabilities, q_k = exp(teacher_k), and all tokens that are not listed are one more answer, q_r = 1 - sum q
+ *   (0 where that is negative, or no such token is allowed): + q_r (ln q_r - ln(1 - sum of p over the listed tokens))
+ *   args        logits and tokens as for klay_tokens_forward, top = 0, num_tokens >= 1.  A negative token lists nothing; a token >= vocab
+ *               gives NaN; of a token listed more than once the q add up in the gradient
+ *   teacher     logits: device fp32 [rows, num_tokens], placed by rows and stride (elements); 0.001 <= temperature <= 1000
+ *   loss        device [rows] fp32
+ *   kept        as for klay_head_forward, for klay_distill_backward
+ * A row that lists nothing has loss 0 and no gradient.  A listed token that is not allowed and that the teacher gives mass to: +inf.  A NaN or +inf,
+ * of a logit or of the teacher's, makes the loss of its row NaN.  No workspace.  Errors: as klay_tokens_forward.
+ */
+typedef struct klay_teacher {
+    const float* logits;
+    klay_rows rows;
+    int64_t stride;
+    float temperature;
+    int32_t rest;
+} klay_teacher;
+klay_status klay_distill_forward(const klay_tokens_args* args, const klay_teacher* teacher, float* loss, void* kept, void* stream);
+
+/*
+ * klay_distill_backward -- its derivative with respect to the logits (the teacher is not differentiated), which must be as they were.
+ *   dloss       device [rows] fp32;  dlogits device [rows, vocab] contiguous, of `dtype`; every entry is written, rounded once
+ */
+klay_status klay_distill_backward(const klay_tokens_args* args, const klay_teacher* teacher, const void* kept, const float* dloss,
+                                  void* dlogits, void* stream);
+
+/* The divergence straight from the network's last layer: logits, rows, workspace and gradients as for klay_head_forward and _backward. */
+klay_status klay_head_distill_forward(const klay_head_args* args, const klay_teacher* teacher, float* loss, void* kept, void* workspace,
+                                      size_t workspace_bytes, void* stream);
+klay_status klay_head_distill_backward(const klay_head_args* args, const klay_teacher* teacher, const void* kept, const float* dloss,
+                                       void* dhidden, void* dweight, float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * klay_scan_forward -- gated recurrence over sequences in a semiring (Section 4), the value of a chain of AND and OR gates of any length:
  *   h_t = a_t (x) h_{t-1} (+) x_t:  REAL: a h + x;  LOG: log(exp(a + h) + exp(x));  MAXLOG: max(a + h, x)
  *   gates, inputs   device [batch, time, channels] of `dtype` (KLAY_F32 in the log-domain semirings), channels next to each other,

@@ -70,13 +70,29 @@ class CircuitLayer(torch.nn.Module):
         V: the NaN that others get counts as impossible in the circuit's OR gates.
         """
         from .operators import token_logprobs
+        tokens = self._tokens_of(logits, tokens, "logits", "V")
+        return self._on(token_logprobs(logits, tokens, complement=complement))
+
+    def from_hidden(self, hidden, weight, tokens, bias=None, complement: bool = True):
+        """:meth:`from_logits` of the logits ``hidden @ weight.T + bias`` (``hidden[B, G, D]``, ``weight[V, D]``, ``bias[V]`` or None) by
+        :func:`head_logprobs`: the network's last layer and the circuit's leaf weights as one, without the logits.  Gradients go to
+        ``hidden``, ``weight`` and ``bias``."""
+        from .operators import head_logprobs
+        tokens = self._tokens_of(hidden, tokens, "hidden", "D")
+        return self._on(head_logprobs(hidden, weight, tokens, bias, complement=complement))
+
+    def _tokens_of(self, given, tokens, name, last):
+        """``tokens`` as [B, G, K], where they and ``given`` fit the circuit."""
         if self.semiring not in (KLAY_LOG, KLAY_MAXLOG):
-            raise ValueError("from_logits gives log weights: the layer's semiring must be KLAY_LOG or KLAY_MAXLOG")
-        if logits.dim() != 3 or tokens.dim() not in (2, 3) or tokens.shape[-2] != logits.shape[1]:
-            raise ValueError("logits must be [B, G, V] and tokens [G, K] or [B, G, K]")
-        batch, groups = logits.shape[:2]
+            raise ValueError("from_%s gives log weights: the layer's semiring must be KLAY_LOG or KLAY_MAXLOG" % name)
+        if given.dim() != 3 or tokens.dim() not in (2, 3) or tokens.shape[-2] != given.shape[1]:
+            raise ValueError("%s must be [B, G, %s] and tokens [G, K] or [B, G, K]" % (name, last))
+        batch, groups = given.shape[:2]
         if groups * tokens.shape[-1] != self.circuit.num_vars:
             raise ValueError("tokens must name %d variables, not %d x %d" % (self.circuit.num_vars, groups, tokens.shape[-1]))
-        r = token_logprobs(logits, tokens.expand(batch, -1, -1) if tokens.dim() == 2 else tokens, complement=complement)
-        weights = r.logp.reshape(batch, -1)
-        return self(weights, r.neg.reshape(batch, -1) if complement else torch.zeros_like(weights))
+        return tokens.expand(batch, -1, -1) if tokens.dim() == 2 else tokens
+
+    def _on(self, r):
+        """The circuit on the log weights of literals."""
+        weights = r.logp.reshape(r.logp.shape[0], -1)
+        return self(weights, torch.zeros_like(weights) if r.neg is None else r.neg.reshape(weights.shape))

@@ -29,7 +29,9 @@ EXPORTS = ("klay_build", "klay_build_ex", "klay_forward", "klay_backward", "klay
            "klay_set_profiling", "klay_get_profile", "klay_destroy", "klay_last_error", "klay_builder_create",
            "klay_builder_add", "klay_builder_finish", "klay_builder_destroy", "klay_forward_lits", "klay_backward_lits", "klay_root_positions", "klay_forward_f64",
            "klay_backward_f64", "klay_forward_static", "klay_persistent_layers", "klay_tokens_workspace_bytes", "klay_tokens_forward",
-           "klay_tokens_backward", "klay_scan_workspace_bytes", "klay_scan_forward", "klay_scan_backward", "klay_scan_step")
+           "klay_tokens_backward", "klay_scan_workspace_bytes", "klay_scan_forward", "klay_scan_backward", "klay_scan_step",
+           "klay_list_kept_bytes", "klay_head_workspace_bytes", "klay_head_forward", "klay_head_backward", "klay_distill_forward",
+           "klay_distill_backward", "klay_head_distill_forward", "klay_head_distill_backward")
 
 
 class KlayError(RuntimeError):
@@ -67,6 +69,18 @@ class klay_tokens_args(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int32), ("device", ctypes.c_int32), ("vocab", ctypes.c_int32), ("num_tokens", ctypes.c_int32),
                 ("top", ctypes.c_int32), ("reserved", ctypes.c_int32), ("rows", ctypes.c_int64), ("logits", ctypes.c_void_p),
                 ("logit_rows", klay_rows), ("tokens", ctypes.c_void_p), ("token_rows", klay_rows), ("token_stride", ctypes.c_int64)]
+
+
+class klay_head_args(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("device", ctypes.c_int32), ("width", ctypes.c_int32), ("vocab", ctypes.c_int32),
+                ("num_tokens", ctypes.c_int32), ("reserved", ctypes.c_int32), ("rows", ctypes.c_int64), ("hidden", ctypes.c_void_p),
+                ("hidden_rows", klay_rows), ("weight", ctypes.c_void_p), ("weight_stride", ctypes.c_int64), ("bias", ctypes.c_void_p),
+                ("tokens", ctypes.c_void_p), ("token_rows", klay_rows), ("token_stride", ctypes.c_int64)]
+
+
+class klay_teacher(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("rows", klay_rows), ("stride", ctypes.c_int64), ("temperature", ctypes.c_float),
+                ("rest", ctypes.c_int32)]
 
 
 class klay_scan_args(ctypes.Structure):
@@ -145,6 +159,23 @@ def load():
     lib.klay_tokens_forward.argtypes = [ctypes.POINTER(klay_tokens_args), vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.klay_tokens_backward.restype = ctypes.c_int
     lib.klay_tokens_backward.argtypes = [ctypes.POINTER(klay_tokens_args), vp, vp, vp, vp, vp, vp]
+    head, teacher, size = ctypes.POINTER(klay_head_args), ctypes.POINTER(klay_teacher), ctypes.c_size_t
+    lib.klay_list_kept_bytes.restype = size
+    lib.klay_list_kept_bytes.argtypes = [i64, i32]
+    lib.klay_head_workspace_bytes.restype = size
+    lib.klay_head_workspace_bytes.argtypes = [head, i32]
+    lib.klay_head_forward.restype = ctypes.c_int
+    lib.klay_head_forward.argtypes = [head, vp, vp, vp, vp, vp, size, vp]
+    lib.klay_head_backward.restype = ctypes.c_int
+    lib.klay_head_backward.argtypes = [head, vp, vp, vp, vp, vp, vp, vp, vp, size, vp]
+    lib.klay_distill_forward.restype = ctypes.c_int
+    lib.klay_distill_forward.argtypes = [ctypes.POINTER(klay_tokens_args), teacher, vp, vp, vp]
+    lib.klay_distill_backward.restype = ctypes.c_int
+    lib.klay_distill_backward.argtypes = [ctypes.POINTER(klay_tokens_args), teacher, vp, vp, vp, vp]
+    lib.klay_head_distill_forward.restype = ctypes.c_int
+    lib.klay_head_distill_forward.argtypes = [head, teacher, vp, vp, vp, size, vp]
+    lib.klay_head_distill_backward.restype = ctypes.c_int
+    lib.klay_head_distill_backward.argtypes = [head, teacher, vp, vp, vp, vp, vp, vp, size, vp]
     lib.klay_scan_workspace_bytes.restype = ctypes.c_size_t
     lib.klay_scan_workspace_bytes.argtypes = [ctypes.POINTER(klay_scan_args)]
     lib.klay_scan_forward.restype = ctypes.c_int
@@ -266,6 +297,41 @@ def klay_tokens_forward(args, logp_ptr, neg_ptr, entropy_ptr, stats_ptr, top_log
 
 def klay_tokens_backward(args, stats_ptr, dlogp_ptr, dneg_ptr, dentropy_ptr, dlogits_ptr, stream=0):
     _check(load().klay_tokens_backward(args, stats_ptr, dlogp_ptr, dneg_ptr, dentropy_ptr, dlogits_ptr, stream))
+
+
+def klay_list_kept_bytes(rows, num_tokens) -> int:
+    return load().klay_list_kept_bytes(rows, num_tokens)
+
+
+def klay_head_workspace_bytes(args, backward=False) -> int:
+    return load().klay_head_workspace_bytes(args, backward)
+
+
+def klay_head_forward(args, logp_ptr, neg_ptr, entropy_ptr, kept_ptr, workspace_ptr, workspace_bytes, stream=0):
+    _check(load().klay_head_forward(args, logp_ptr, neg_ptr, entropy_ptr, kept_ptr, workspace_ptr, workspace_bytes, stream))
+
+
+def klay_head_backward(args, kept_ptr, dlogp_ptr, dneg_ptr, dentropy_ptr, dhidden_ptr, dweight_ptr, dbias_ptr, workspace_ptr, workspace_bytes,
+                       stream=0):
+    _check(load().klay_head_backward(args, kept_ptr, dlogp_ptr, dneg_ptr, dentropy_ptr, dhidden_ptr, dweight_ptr, dbias_ptr, workspace_ptr,
+                                     workspace_bytes, stream))
+
+
+def klay_distill_forward(args, teacher, loss_ptr, kept_ptr, stream=0):
+    _check(load().klay_distill_forward(args, teacher, loss_ptr, kept_ptr, stream))
+
+
+def klay_distill_backward(args, teacher, kept_ptr, dloss_ptr, dlogits_ptr, stream=0):
+    _check(load().klay_distill_backward(args, teacher, kept_ptr, dloss_ptr, dlogits_ptr, stream))
+
+
+def klay_head_distill_forward(args, teacher, loss_ptr, kept_ptr, workspace_ptr, workspace_bytes, stream=0):
+    _check(load().klay_head_distill_forward(args, teacher, loss_ptr, kept_ptr, workspace_ptr, workspace_bytes, stream))
+
+
+def klay_head_distill_backward(args, teacher, kept_ptr, dloss_ptr, dhidden_ptr, dweight_ptr, dbias_ptr, workspace_ptr, workspace_bytes, stream=0):
+    _check(load().klay_head_distill_backward(args, teacher, kept_ptr, dloss_ptr, dhidden_ptr, dweight_ptr, dbias_ptr, workspace_ptr,
+                                             workspace_bytes, stream))
 
 
 def klay_scan_workspace_bytes(args) -> int:

@@ -4,12 +4,13 @@ from __future__ import annotations
 import os
 import shutil
 import subprocess
+import tempfile
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_DIR = os.path.join(_HERE, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "libklay.so")
-SOURCES = ["klay_lib.hip", "layerize.cpp"]
+SOURCES = ["klay_lib.hip", "klay_head.hip", "klay_head_f32.hip", "klay_head_bf16.hip", "klay_head_f16.hip", "layerize.cpp"]
 
 
 def hipcc() -> str:
@@ -23,13 +24,19 @@ def build(verbose: bool = False) -> str:
     """Compile unconditionally and return the library path."""
     os.makedirs(LIB_DIR, exist_ok=True)
     tmp = LIB_PATH + ".tmp.%d" % os.getpid()
-    cmd = [hipcc(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
-           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-           "-Wall", "-Wno-unused-command-line-argument",
-           "-o", tmp] + [os.path.join(CSRC, f) for f in SOURCES]
-    if verbose:
-        print(" ".join(cmd))
-    subprocess.check_call(cmd)
+    flags = [hipcc(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
+             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+             "-Wall", "-Wno-unused-command-line-argument"]
+    with tempfile.TemporaryDirectory(dir=LIB_DIR) as objects:
+        compiles = [flags + ["-c", "-o", os.path.join(objects, f + ".o"), os.path.join(CSRC, f)] for f in SOURCES]
+        link = [flags[0], "--offload-arch=gfx950", "-shared", "-o", tmp] + [c[c.index("-o") + 1] for c in compiles]
+        if verbose:
+            print("\n".join(" ".join(c) for c in compiles + [link]))
+        running = [subprocess.Popen(c) for c in compiles]
+        failed = [c for c, p in zip(compiles, running) if p.wait() != 0]
+        if failed:
+            raise subprocess.CalledProcessError(1, failed[0])
+        subprocess.check_call(link)
     os.replace(tmp, LIB_PATH)
     return LIB_PATH
 

@@ -1,0 +1,94 @@
+// The launches of one type of a head's elements.
+#pragma once
+
+#include "klay_entry.h"
+#include "klay_head.hip.h"
+
+#include <algorithm>
+
+namespace klay {
+
+template <typename T> using Tile32 = Tile<T, 32, 128, 1, 4, 3>;
+template <typename T> using Tile64 = Tile<T, 64, 128, 1, 4, 3>;
+template <typename T> using Tile128 = Tile<T, 128, 128, 2, 2, 2>;
+template <typename T> using Tile256 = Tile<T, 256, 256, 2, 4, 2>;
+
+template <typename Tile> Tiles tiles_of(int64_t rows, int64_t columns) {
+    return Tiles{(rows + Tile::kM - 1) / Tile::kM, (columns + Tile::kN - 1) / Tile::kN};
+}
+inline uint32_t grid_of(int64_t items, int64_t each, int64_t most) { return (uint32_t)std::max<int64_t>(1, std::min((items + each - 1) / each, most)); }
+
+template <typename Tile> klay_status run_forward(const HeadArgs& g, bool entropy, void* stream) {
+    const Tiles tiles = tiles_of<Tile>(g.rows, g.weight.rows);
+    const dim3 grid((uint32_t)(tiles.m * tiles.n)), block(Tile::kThreads);
+    if (entropy) KLAY_LAUNCH((head_forward_kernel<Tile, true>), grid, block, stream, g, tiles);
+    else KLAY_LAUNCH((head_forward_kernel<Tile, false>), grid, block, stream, g, tiles);
+    return KLAY_OK;
+}
+template <typename Tile> klay_status run_adjoint(const HeadArgs& g, void* stream) {
+    const Tiles tiles = tiles_of<Tile>(std::max<int64_t>(g.rows, g.g_across ? g.g_rows : 0), g.g_columns);
+    KLAY_LAUNCH((head_adjoint_kernel<Tile>), dim3((uint32_t)(tiles.m * tiles.n)), dim3(Tile::kThreads), stream, g, tiles);
+    return KLAY_OK;
+}
+template <typename Tile> klay_status run_products(const ProductArgs& g, void* stream) {
+    int64_t blocks[2] = {0, 0};
+    for (int i = 0; i < g.jobs; ++i) {
+        const Tiles tiles = tiles_of<Tile>(g.job[i].rows, g.job[i].columns);
+        blocks[i] = tiles.m * tiles.n * g.job[i].splits;
+    }
+    if (blocks[0] + blocks[1] > 0)
+        KLAY_LAUNCH((head_product_kernel<Tile>), dim3((uint32_t)(blocks[0] + blocks[1])), dim3(Tile::kThreads), stream, g, blocks[0]);
+    return KLAY_OK;
+}
+
+template <typename T> klay_status HeadLaunch<T>::forward(HeadTile tile, const HeadArgs& g, bool entropy, void* stream) {
+    switch (tile) {
+        case TILE_32: return run_forward<Tile32<T>>(g, entropy, stream);
+        case TILE_64: return run_forward<Tile64<T>>(g, entropy, stream);
+        case TILE_128: return run_forward<Tile128<T>>(g, entropy, stream);
+        default: return run_forward<Tile256<T>>(g, entropy, stream);
+    }
+}
+template <typename T> klay_status HeadLaunch<T>::adjoint(HeadTile tile, const HeadArgs& g, void* stream) {
+    switch (tile) {
+        case TILE_32: return run_adjoint<Tile32<T>>(g, stream);
+        case TILE_64: return run_adjoint<Tile64<T>>(g, stream);
+        case TILE_128: return run_adjoint<Tile128<T>>(g, stream);
+        default: return run_adjoint<Tile256<T>>(g, stream);
+    }
+}
+template <typename T> klay_status HeadLaunch<T>::products(HeadTile tile, const ProductArgs& g, void* stream) {
+    switch (tile) {
+        case TILE_32: return run_products<Tile32<T>>(g, stream);
+        case TILE_64: return run_products<Tile64<T>>(g, stream);
+        case TILE_128: return run_products<Tile128<T>>(g, stream);
+        default: return run_products<Tile256<T>>(g, stream);
+    }
+}
+template <typename T> klay_status HeadLaunch<T>::sums(const SumsArgs& g, void* stream) {
+    int64_t most = 0;
+    for (int i = 0; i < g.sums; ++i) most = std::max<int64_t>(most, g.sum[i].count);
+    if (most > 0) KLAY_LAUNCH((head_sums_kernel<T>), dim3(grid_of(most, 256, 8192)), dim3(256), stream, g);
+    return KLAY_OK;
+}
+template <typename T> klay_status HeadLaunch<T>::pack(const PackArgs& g, bool across, void* stream) {
+    if (g.count < 1 || g.columns < 1) return KLAY_OK;
+    if (across) KLAY_LAUNCH((head_pack_across_kernel<T>), dim3(grid_of((g.padded + 63) / 64 * ((g.columns + 63) / 64), 1, 8192)), dim3(256), stream, g);
+    else KLAY_LAUNCH((head_pack_kernel<T>), dim3(grid_of(g.count * (g.padded * (int64_t)sizeof(T) / 16), 256, 8192)), dim3(256), stream, g);
+    return KLAY_OK;
+}
+
+}  // namespace klay
+
+// Kernels are instantiated by name: the compiler leaves out the host side of some that are only launched.
+#define KLAY_HEAD_TILE(TILE)                                                                   \
+    template __global__ void klay::head_forward_kernel<TILE, true>(klay::HeadArgs, klay::Tiles);  \
+    template __global__ void klay::head_forward_kernel<TILE, false>(klay::HeadArgs, klay::Tiles); \
+    template __global__ void klay::head_adjoint_kernel<TILE>(klay::HeadArgs, klay::Tiles);        \
+    template __global__ void klay::head_product_kernel<TILE>(klay::ProductArgs, int64_t);
+#define KLAY_HEAD(T)                          \
+    KLAY_HEAD_TILE(klay::Tile32<klay::T>)     \
+    KLAY_HEAD_TILE(klay::Tile64<klay::T>)     \
+    KLAY_HEAD_TILE(klay::Tile128<klay::T>)    \
+    KLAY_HEAD_TILE(klay::Tile256<klay::T>)    \
+    template struct klay::HeadLaunch<klay::T>;

@@ -1,43 +1,22 @@
 // The library's device code: the circuit evaluator (klay_api.hip) and the operators that need no handle, whose entry points are here.
-// One translation unit, so that all entry points report through the same thread-local message.
+// The entry points elsewhere (klay_head.hip) report through the message that is kept here.
 #include "klay_api.hip"
 
+#include "klay_entry.h"
 #include "klay_scan.hip.h"
 #include "klay_tokens.hip.h"
 
-#include <initializer_list>
+klay_status klay::report(klay_status status, const std::string& message) { return fail(status, message); }
 
 namespace {
 
-// Makes `device` current for a call, and the earlier one again afterwards.
-struct OnDevice {
-    int before = -1;
-    bool changed = false;
-    hipError_t status;
-    explicit OnDevice(int device) {
-        status = hipGetDevice(&before);
-        if (status == hipSuccess && before != device) {
-            status = hipSetDevice(device);
-            changed = status == hipSuccess;
-        }
-    }
-    ~OnDevice() {
-        if (changed) (void)hipSetDevice(before);
-    }
-};
+using klay::OnDevice;
+using klay::aligned_to;
+using klay::dtype_bytes;
+using klay::kComputeUnits;
+using klay::known_dtype;
 
-// Launch errors come as the launch's own status; what an earlier call has left is none of ours.
-#define KLAY_LAUNCH(kernel, grid, block, stream, ...)                                                    \
-    do {                                                                                                 \
-        (void)hipGetLastError();                                                                         \
-        hipLaunchKernelGGL(kernel, grid, block, 0, static_cast<hipStream_t>(stream), __VA_ARGS__);       \
-        KLAY_HIP(hipGetLastError());                                                                     \
-    } while (0)
-
-constexpr int kComputeUnits = 256;
 constexpr int32_t kMostChannels = 1 << 25;      // and the most elements from one time step to the next: a wave's rows lie within 32-bit offsets
-bool known_dtype(int32_t t) { return t == KLAY_F32 || t == KLAY_BF16 || t == KLAY_F16; }
-int dtype_bytes(int32_t t) { return t == KLAY_F32 ? 4 : 2; }
 
 // ---- tokens ---------------------------------------------------------------------------------------------------------
 // Rows in the registers of a wave, of a quarter of one (us, forward and reverse: 65536 x 64 bf16 by quarters / whole waves 13.8 / 50.4, 11.8 / 35.8;
@@ -191,13 +170,6 @@ klay_status check_scan(const klay_scan_args* a, bool inputs, const char* who) {
     }
     if (a->batch > 0 && a->time > 0 && (!a->gates || (inputs && !a->inputs))) return refused("null argument");
     return KLAY_OK;
-}
-
-// All of them multiples of `bytes`?
-bool aligned_to(size_t bytes, std::initializer_list<const void*> all) {
-    uintptr_t bits = 0;
-    for (const void* p : all) bits |= reinterpret_cast<uintptr_t>(p);
-    return bits % bytes == 0;
 }
 
 // Waves as many as the time steps give work to, eight at most (sixteen: within 5% either way, and the log semiring's reverse sweep runs out of

@@ -1,7 +1,9 @@
 """The operators between a network and a circuit's leaf weights, as differentiable PyTorch functions: log probabilities of given
-tokens (:func:`token_logprobs`) and gated recurrences over sequences in the library's semirings (:func:`gated_scan`, and
-:func:`gated_step` for one step).  Marshalling only, on torch's current stream of the tensors' device: the kernels are those of
-``klay_tokens_*`` and ``klay_scan_*`` (include/klay.h, which says what they compute and refuse).  Results and workspaces are torch
+tokens (:func:`token_logprobs`; :func:`head_logprobs` straight from the hidden states before the network's last layer), divergences from
+what a teacher says of its likeliest tokens (:func:`token_distill`, :func:`head_distill`) and gated recurrences over sequences in the
+library's semirings (:func:`gated_scan`, and :func:`gated_step` for one step).  Marshalling only, on torch's current stream of the tensors'
+device: the kernels are those of ``klay_tokens_*``, ``klay_head_*``, ``klay_distill_*`` and ``klay_scan_*`` (include/klay.h, which says what
+they compute and refuse).  Results and workspaces are torch
 tensors, so calls may be captured into a graph and made on several streams at once.
 """
 from __future__ import annotations
@@ -174,6 +176,256 @@ def token_logprobs(logits, tokens=None, *, complement=False, entropy=False, top=
     if torch.is_grad_enabled() and logits.requires_grad:
         return TokenLogprobs(*_TokenLogprobs.apply(logits, tokens, complement, entropy, top))
     return TokenLogprobs(*_tokens_forward(logits, tokens, complement, entropy, top, False)[:5])
+
+
+# ---- the network's last layer and its losses as one ---------------------------------------------------------------
+class HeadLogprobs(NamedTuple):
+    """What :func:`head_logprobs` returns; None for what was not asked."""
+    logp: Optional[torch.Tensor]
+    neg: Optional[torch.Tensor]
+    entropy: Optional[torch.Tensor]
+
+
+def _head_args(hidden, weight, bias, tokens):
+    width, vocab = hidden.shape[-1], weight.shape[0]
+    if hidden.stride(-1) != 1 and width != 1:
+        hidden = hidden.contiguous()
+    if weight.stride(-1) != 1 and width != 1:
+        weight = weight.contiguous()
+    if bias is not None:
+        bias = bias.contiguous()
+    hidden, hidden_rows = _rows_of(hidden)
+    k = stride = pointer = 0
+    token_rows = hidden_rows
+    if tokens is not None:
+        tokens, token_rows = _rows_of(tokens)
+        k, stride, pointer = tokens.shape[-1], tokens.stride(-1), tokens.data_ptr()
+    args = _b.klay_head_args(_DTYPES[hidden.dtype], hidden.get_device(), width, vocab, k, 0, hidden.numel() // width, hidden.data_ptr(),
+                             hidden_rows, weight.data_ptr(), weight.stride(0), _ptr(bias), pointer, token_rows, stride)
+    return args, (hidden, weight, bias, tokens)
+
+
+def _teacher_args(teacher, temperature, rest):
+    teacher, rows = _rows_of(teacher)
+    return _b.klay_teacher(teacher.data_ptr(), rows, teacher.stride(-1), temperature, rest), teacher
+
+
+def _kept(like, args):
+    return like.new_empty((_b.klay_list_kept_bytes(args.rows, args.num_tokens),), dtype=torch.uint8)
+
+
+def _workspace(like, args, backward):
+    size = _b.klay_head_workspace_bytes(args, backward)
+    return (like.new_empty((size,), dtype=torch.uint8) if size else None), size
+
+
+def _head_forward(hidden, weight, bias, tokens, complement, entropy, keep):
+    args, alive = _head_args(hidden, weight, bias, tokens)
+    lead, new, k = tuple(hidden.shape[:-1]), hidden.new_empty, args.num_tokens
+    logp = None if tokens is None else new(lead + (k,), dtype=torch.float32)
+    neg = new(lead + (k,), dtype=torch.float32) if complement else None
+    h = new(lead, dtype=torch.float32) if entropy else None
+    kept = _kept(hidden, args) if keep else None
+    work, size = _workspace(hidden, args, False)
+    _b.klay_head_forward(args, _ptr(logp), _ptr(neg), _ptr(h), _ptr(kept), _ptr(work), size, _stream(args.device))
+    return logp, neg, h, kept, args, alive
+
+
+def _head_gradients(ctx, hidden, weight, bias):
+    """Where the gradients of a head's inputs go; of no rows they are zeros."""
+    make = torch.empty if hidden.numel() else torch.zeros
+    return [make(t.shape, dtype=t.dtype, device=t.device) if need and t is not None else None
+            for t, need in zip((hidden, weight, bias), ctx.needs_input_grad)]
+
+
+class _HeadLogprobs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, hidden, weight, bias, tokens, complement, entropy):
+        *out, kept, ctx.args, used = _head_forward(hidden, weight, bias, tokens, complement, entropy, True)
+        ctx.places = _places(*used)
+        ctx.save_for_backward(*used, kept)
+        ctx.set_materialize_grads(False)
+        return tuple(out)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dlogp, dneg, dentropy):
+        hidden, weight, bias, tokens, kept = ctx.saved_tensors
+        dlogp, dneg, dentropy = (None if t is None else t.contiguous() for t in (dlogp, dneg, dentropy))
+        args = ctx.args
+        if ctx.places != _places(hidden, weight, bias, tokens):                   # what was saved has been put elsewhere
+            args, (hidden, weight, bias, tokens) = _head_args(hidden, weight, bias, tokens)
+        grads = _head_gradients(ctx, hidden, weight, bias)
+        work, size = _workspace(hidden, args, True)
+        _b.klay_head_backward(args, kept.data_ptr(), _ptr(dlogp), _ptr(dneg), _ptr(dentropy), *map(_ptr, grads), _ptr(work), size,
+                              _stream(args.device))
+        return (*grads, None, None, None)
+
+
+def _check_head(hidden, weight, bias, tokens):
+    _check_tensor(hidden, "hidden", _DTYPES)
+    _check_tensor(weight, "weight", (hidden.dtype,))
+    if hidden.dim() < 1 or weight.dim() != 2 or hidden.shape[-1] != weight.shape[1]:
+        raise ValueError("hidden must be [..., D] and weight [V, D]")
+    if not 1 <= weight.shape[1] <= 1 << 20 or not 1 <= weight.shape[0] < (1 << 31) - 4096:
+        raise ValueError("weight must have 1 .. 2^20 columns and 1 .. 2^31 - 4097 rows")
+    if hidden.numel() // hidden.shape[-1] > 1 << 20:
+        raise ValueError("hidden must have at most 2^20 rows; split the call")
+    if bias is not None:
+        _check_tensor(bias, "bias", (torch.float32,))
+        if bias.shape != weight.shape[:1]:
+            raise ValueError("bias must be [V] = [%d]" % weight.shape[0])
+    if any(t is not None and t.device != hidden.device for t in (weight, bias)):
+        raise ValueError("weight and bias must be on the device of hidden")
+    if tokens is not None:
+        _check_tokens(tokens, hidden, "hidden")
+
+
+def _check_tokens(tokens, of, name):
+    _check_tensor(tokens, "tokens", (torch.int64,))
+    if tokens.device != of.device:
+        raise ValueError("tokens must be on the device of " + name)
+    if tokens.dim() != of.dim() or tokens.shape[:-1] != of.shape[:-1]:
+        raise ValueError("tokens must be [..., K] with the leading axes of %s, %s" % (name, tuple(of.shape[:-1])))
+    if tokens.shape[-1] > _MOST_TOKENS:
+        raise ValueError("tokens must be at most %d a row" % _MOST_TOKENS)
+
+
+def head_logprobs(hidden, weight, tokens=None, bias=None, *, complement=False, entropy=False) -> HeadLogprobs:
+    """:func:`token_logprobs` of the logits ``hidden @ weight.T + bias``, which are never in memory: ``hidden[..., D]``, ``weight[V, D]``
+    (both float32, bfloat16 or float16), ``bias[V]`` float32 or None, ``tokens[..., K]`` int64.  The logits are made in pieces on the chip,
+    in float32, forward and once more backward, so that a call needs memory for a few thousand columns of them at a time.
+
+    ``logp[..., K]``, with ``complement`` ``neg[..., K]``, with ``entropy`` the entropies ``[...]``, all float32 and differentiable with
+    respect to ``hidden``, ``weight`` and ``bias`` (backward only: tensors with tangents are refused).  A bias of -inf is a token that is
+    not allowed; a negative token asks for nothing, a token >= V gives NaN.  The gradients have the types of their inputs.  With 16-bit types the
+    logits' adjoints are rounded to those bits before they meet the weights and the hidden states (float16: scaled into its range first).
+
+    Rows should start at multiples of 16 bytes, with D a multiple of 16 bytes; others are copied first.  At most 2^20 rows, 1024 tokens
+    a row.
+    """
+    _check_head(hidden, weight, bias, tokens)
+    if tokens is None and complement:
+        raise ValueError("complement needs tokens")
+    _refuse_tangents("head_logprobs", hidden, weight, bias)
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (hidden, weight, bias)):
+        return HeadLogprobs(*_HeadLogprobs.apply(hidden, weight, bias, tokens, complement, entropy))
+    return HeadLogprobs(*_head_forward(hidden, weight, bias, tokens, complement, entropy, False)[:3])
+
+
+# ---- divergence from a teacher's list -------------------------------------------------------------------------------
+def _check_teacher(tokens, teacher, temperature, of, name):
+    if tokens is None or tokens.shape[-1] < 1:
+        raise ValueError("tokens must be [..., K] with K >= 1")
+    _check_tensor(teacher, "teacher", (torch.float32,))
+    if teacher.shape != tokens.shape or teacher.device != of.device:
+        raise ValueError("teacher must have the shape of tokens, on the device of " + name)
+    if not 1e-3 <= temperature <= 1e3:
+        raise ValueError("temperature must be 0.001 .. 1000")
+    if teacher.requires_grad and torch.is_grad_enabled():
+        raise ValueError("the teacher is not differentiated: detach it")
+
+
+def _distill_forward(logits, tokens, teacher, temperature, rest, keep):
+    args, alive = _token_args(logits, tokens, 0)
+    told, teacher = _teacher_args(teacher, temperature, rest)
+    loss = logits.new_empty(tuple(logits.shape[:-1]), dtype=torch.float32)
+    kept = _kept(logits, args) if keep else None
+    _b.klay_distill_forward(args, told, _ptr(loss), _ptr(kept), _stream(args.device))
+    return loss, kept, args, told, alive + (teacher,)
+
+
+class _TokenDistill(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, tokens, teacher, temperature, rest):
+        loss, kept, ctx.args, ctx.told, used = _distill_forward(logits, tokens, teacher, temperature, rest, True)
+        ctx.places = _places(*used)
+        ctx.save_for_backward(*used, kept)
+        return loss
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dloss):
+        logits, tokens, teacher, kept = ctx.saved_tensors
+        args, told = ctx.args, ctx.told
+        if ctx.places != _places(logits, tokens, teacher):                        # what was saved has been put elsewhere
+            args, (logits, tokens) = _token_args(logits, tokens, 0)
+            told, teacher = _teacher_args(teacher, told.temperature, told.rest)
+        dloss = dloss.contiguous()
+        dlogits = logits.new_empty(logits.shape)
+        _b.klay_distill_backward(args, told, kept.data_ptr(), dloss.data_ptr(), dlogits.data_ptr(), _stream(args.device))
+        return dlogits, None, None, None, None
+
+
+def token_distill(logits, tokens, teacher, *, temperature=1.0, rest=False):
+    """Divergence of a student's ``logits[..., V]`` (float32, bfloat16 or float16) from what a teacher says of its likeliest tokens,
+    ``tokens[..., K]`` (int64) and ``teacher[..., K]`` (float32; those of :func:`token_logprobs` with ``top``): per row, float32,
+
+        loss = sum_k q_k (ln q_k - ln p_{t_k}),  p = softmax(logits / temperature),  q = softmax(teacher / temperature) over the list.
+
+    With ``rest`` ``teacher`` holds log probabilities, q_k = exp(teacher_k), and all tokens that are not listed are one more answer with what
+    the list leaves, q_r = 1 - sum q (0 where no such token is allowed): the loss gets + q_r (ln q_r - ln p_r).
+
+    A negative token lists nothing (lists of different lengths), a row that lists nothing has loss 0; a token >= V gives NaN.  A logit of -inf is a
+    token that is not allowed.  Differentiable with respect to ``logits`` (backward only: tensors with tangents are refused); the teacher is a
+    constant.  Times temperature^2 where gradients of several temperatures are to be of one size: left to the caller.  Layouts as for
+    :func:`token_logprobs`; temperatures of 0.001 .. 1000.
+    """
+    _check_tensor(logits, "logits", _DTYPES)
+    if logits.dim() < 1 or not 1 <= logits.shape[-1] < 1 << 31:
+        raise ValueError("logits must be [..., V] with 1 <= V < 2^31")
+    _check_tokens(tokens, logits, "logits")
+    temperature, rest = float(temperature), bool(rest)
+    _check_teacher(tokens, teacher, temperature, logits, "logits")
+    _refuse_tangents("token_distill", logits, teacher)
+    if torch.is_grad_enabled() and logits.requires_grad:
+        return _TokenDistill.apply(logits, tokens, teacher, temperature, rest)
+    return _distill_forward(logits, tokens, teacher, temperature, rest, False)[0]
+
+
+def _head_distill_forward(hidden, weight, bias, tokens, teacher, temperature, rest, keep):
+    args, alive = _head_args(hidden, weight, bias, tokens)
+    told, teacher = _teacher_args(teacher, temperature, rest)
+    loss = hidden.new_empty(tuple(hidden.shape[:-1]), dtype=torch.float32)
+    kept = _kept(hidden, args) if keep else None
+    work, size = _workspace(hidden, args, False)
+    _b.klay_head_distill_forward(args, told, _ptr(loss), _ptr(kept), _ptr(work), size, _stream(args.device))
+    return loss, kept, args, told, alive + (teacher,)
+
+
+class _HeadDistill(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, hidden, weight, bias, tokens, teacher, temperature, rest):
+        loss, kept, ctx.args, ctx.told, used = _head_distill_forward(hidden, weight, bias, tokens, teacher, temperature, rest, True)
+        ctx.places = _places(*used)
+        ctx.save_for_backward(*used, kept)
+        return loss
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dloss):
+        hidden, weight, bias, tokens, teacher, kept = ctx.saved_tensors
+        args, told = ctx.args, ctx.told
+        if ctx.places != _places(hidden, weight, bias, tokens, teacher):          # what was saved has been put elsewhere
+            args, (hidden, weight, bias, tokens) = _head_args(hidden, weight, bias, tokens)
+            told, teacher = _teacher_args(teacher, told.temperature, told.rest)
+        dloss = dloss.contiguous()
+        grads = _head_gradients(ctx, hidden, weight, bias)
+        work, size = _workspace(hidden, args, True)
+        _b.klay_head_distill_backward(args, told, kept.data_ptr(), dloss.data_ptr(), *map(_ptr, grads), _ptr(work), size, _stream(args.device))
+        return (*grads, None, None, None, None)
+
+
+def head_distill(hidden, weight, tokens, teacher, bias=None, *, temperature=1.0, rest=False):
+    """:func:`token_distill` of the logits ``hidden @ weight.T + bias``, which are never in memory (arguments, gradients and limits as for
+    :func:`head_logprobs`)."""
+    _check_head(hidden, weight, bias, tokens)
+    temperature, rest = float(temperature), bool(rest)
+    _check_teacher(tokens, teacher, temperature, hidden, "hidden")
+    _refuse_tangents("head_distill", hidden, weight, bias, teacher)
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (hidden, weight, bias)):
+        return _HeadDistill.apply(hidden, weight, bias, tokens, teacher, temperature, rest)
+    return _head_distill_forward(hidden, weight, bias, tokens, teacher, temperature, rest, False)[0]
 
 
 # ---- gated recurrence ---------------------------------------------------------------------------------------------
