@@ -457,8 +457,8 @@ typedef struct klay_teacher {
     const float* logits;
     klay_rows rows;
     int64_t stride;
-    float temperature;
-    int32_t rest;
+    double temperature;
+    int32_t rest, reserved;
 } klay_teacher;
 klay_status klay_distill_forward(const klay_tokens_args* args, const klay_teacher* teacher, float* loss, void* kept, void* stream);
 

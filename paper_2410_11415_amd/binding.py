@@ -79,8 +79,8 @@ class klay_head_args(ctypes.Structure):
 
 
 class klay_teacher(ctypes.Structure):
-    _fields_ = [("logits", ctypes.c_void_p), ("rows", klay_rows), ("stride", ctypes.c_int64), ("temperature", ctypes.c_float),
-                ("rest", ctypes.c_int32)]
+    _fields_ = [("logits", ctypes.c_void_p), ("rows", klay_rows), ("stride", ctypes.c_int64), ("temperature", ctypes.c_double),
+                ("rest", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class klay_scan_args(ctypes.Structure):

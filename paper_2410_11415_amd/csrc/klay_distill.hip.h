@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(THREADS) distill_back_kernel(DistillArgs g) {
         const Share<N, THREADS> share(out + lo, lo, hi);
         const TeachStats st = reinterpret_cast<const TeachStats*>(g.teach.stats)[r];
         const float d = g.dloss[r] * (float)g.teach.inverse_temperature;
-        const bool live = d != 0.0f;
+        const bool live = d != 0.0f && st.live;
         const float A = live ? d * st.others : 0.0f, off = st.ref_log * kTokLog2e;
         auto at = [&](float x) { return A * exp2_of(fmaf(x - st.ref, g.scale, -off)); };
         if (A != 0.0f) {

@@ -53,7 +53,7 @@ klay_status check_head(const klay_head_args* a, const char* who) {
 klay_status check_teacher(const klay_teacher* t, int64_t rows, int32_t num_tokens, const char* who) {
     auto refused = [who](const std::string& why) { return report(KLAY_EINVAL, who + (": " + why)); };
     if (!t) return refused("null argument");
-    if (!(t->temperature >= 1e-3f && t->temperature <= 1e3f)) return refused("temperature must be 0.001 .. 1000");
+    if (!(t->temperature >= 1e-3 && t->temperature <= 1e3)) return refused("temperature must be 0.001 .. 1000");
     if (rows == 0) return KLAY_OK;
     if (num_tokens < 1) return refused("a teacher lists at least one token");
     if (!t->logits) return refused("null argument");
@@ -190,11 +190,11 @@ klay::TeachArgs teach_args(const klay_teacher* t) {
     g.teacher = t->logits;
     g.teacher_rows = map_of(t->rows);
     g.teacher_stride = t->stride;
-    g.inverse_temperature = 1.0 / (double)t->temperature;
+    g.inverse_temperature = 1.0 / t->temperature;
     g.rest = t->rest != 0;
     return g;
 }
-float scale_of(const klay_teacher* t) { return t ? (float)(1.4426950408889634 / (double)t->temperature) : klay::kTokLog2e; }
+float scale_of(const klay_teacher* t) { return t ? (float)(1.4426950408889634 / t->temperature) : klay::kTokLog2e; }
 void* in(void* workspace, size_t at) { return static_cast<char*>(workspace) + at; }
 #define KLAY_DO(call)                          \
     do {                                       \
@@ -307,7 +307,7 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
     ad.slots = kept.slots;
     ad.values = kept.values;
     ad.dlogp = dlogp; ad.dneg = dneg; ad.dentropy = dentropy; ad.dloss = dloss;
-    ad.inverse_temperature = teacher ? 1.0f / teacher->temperature : 1.0f;
+    ad.inverse_temperature = teacher ? (float)(1.0 / teacher->temperature) : 1.0f;
     ad.rows = a->rows;
     ad.num_tokens = a->num_tokens;
     ad.coefs = static_cast<float4*>(in(workspace, p.coefs));
@@ -328,7 +328,7 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
     };
     if (dweight) {
         klay::PackArgs c = across(a->hidden, a->hidden_rows, a->rows, p.g_rows, p.h_across);
-        c.coefs = reinterpret_cast<const float*>(ad.coefs);
+        c.coefs = ad.coefs;
         KLAY_DO(klay::HeadLaunch<T>::pack(c, true, stream));
     }
     const bool whole = p.piece >= a->vocab;             // one piece

@@ -26,7 +26,7 @@ struct HeadArgs {
     float* values;                          // [rows, num_tokens]: the listed tokens' logits
     float4* partial;                        // [rows, tiles of tokens]: max, rest, weighted
     // backward
-    const float4* coefs;                    // [rows]: ref, ln S log2 e, A, B ln 2
+    const float4* coefs;                    // [rows]: ref (+inf: the row has no gradient), ln S log2 e, A, B ln 2
     const float* entries;                   // [rows, num_tokens]
     const uint32_t* largest;                // bits of the largest adjoint (fp16), or null
     void *g, *g_across;                     // [rows, g_columns], [g_columns, g_rows]
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(Tile::kThreads) head_adjoint_kernel(HeadArgs g
     const int64_t m0 = tm * BM, n0 = tn * BN;
     Tile t;
     if (g.num_tokens) marks.make(g, m0, g.first + (int32_t)n0, threadIdx.x, Tile::kThreads);
-    for (int row = threadIdx.x; row < BM; row += Tile::kThreads) coefs[row] = m0 + row < g.rows ? g.coefs[m0 + row] : make_float4(0, 0, 0, 0);
+    for (int row = threadIdx.x; row < BM; row += Tile::kThreads) coefs[row] = m0 + row < g.rows ? g.coefs[m0 + row] : make_float4(INFINITY, 0, 0, 0);
     t.run(g.hidden, g.weight, m0, n0, 0, g.stages, sh);
     const float up = adjoint_scale(g.largest);
     float bias[TN], sum[TN] = {};
@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(Tile::kThreads) head_adjoint_kernel(HeadArgs g
             for (int e = 0; e < 4; ++e) {
                 const int row = t.row(i) + 8 * q + e;
                 const float4 c = coefs[row];
-                const bool live = c.z != 0.0f || c.w != 0.0f;
+                const bool live = c.x < INFINITY;
 #pragma unroll
                 for (int j = 0; j < TN; ++j) {
                     const float x = bias[j] == -INFINITY ? -INFINITY : t.acc[i][j][4 * q + e] + bias[j];

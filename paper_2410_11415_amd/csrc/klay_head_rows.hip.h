@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(256) head_logprobs_adjoint_kernel(AdjointArgs 
     bad = wave_max(bad);
     if (asked == 0.0f || st.empty) {
         for (int32_t u = lane; u < K; u += 64) entries[u] = 0.0f;
-        if (lane == 0) g.coefs[r] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (lane == 0) g.coefs[r] = make_float4(INFINITY, 0.0f, 0.0f, 0.0f);
         return;
     }
     auto adjoints = [&](int32_t u, double& gu, double& nu) {
@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(256) head_logprobs_adjoint_kernel(AdjointArgs 
         most = fmaxf(most, fabsf(entry));
     }
     note_largest(g.largest, most);
-    if (lane == 0) g.coefs[r] = make_float4(st.ref, st.ref_log * kTokLog2e, (float)A, (float)B * kTokLn2);
+    if (lane == 0) g.coefs[r] = make_float4(nan ? 0.0f : st.ref, st.ref_log * kTokLog2e, (float)A, (float)B * kTokLn2);
 }
 
 __global__ void __launch_bounds__(256) head_distill_adjoint_kernel(AdjointArgs g) {
@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(256) head_distill_adjoint_kernel(AdjointArgs g
     const int32_t lane = threadIdx.x & 63, K = g.num_tokens;
     const TeachStats st = reinterpret_cast<const TeachStats*>(g.stats)[r];
     const float d = g.dloss[r] * g.inverse_temperature;
-    const bool live = d != 0.0f;
+    const bool live = d != 0.0f && st.live;
     const float A = live ? d * st.others : 0.0f;
     float most = fabsf(A);
     for (int32_t u = lane; u < K; u += 64) {
@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(256) head_distill_adjoint_kernel(AdjointArgs g
         most = fmaxf(most, fabsf(entry));
     }
     note_largest(g.largest, most);
-    if (lane == 0) g.coefs[r] = make_float4(st.ref, st.ref_log * kTokLog2e, A, 0.0f);
+    if (lane == 0) g.coefs[r] = make_float4(!live ? INFINITY : A == A ? st.ref : 0.0f, st.ref_log * kTokLog2e, A, 0.0f);
 }
 
 }  // namespace klay

@@ -184,7 +184,9 @@ struct TeachArgs {
     float* moved;                           // [rows, num_tokens]: of a sorted token its entry of the gradient, p - q; or null
 };
 struct TeachStats {
-    float ref, ref_log, others, unused[5];  // others: (1 - P) - q_r, which the tokens that are not listed have by their shares of 1 - P
+    float ref, ref_log, others;             // others: (1 - P) - q_r, which the tokens that are not listed have by their shares of 1 - P
+    int32_t live;                           // 0: nothing is listed, or nothing allowed: no gradient
+    float unused[4];
 };
 static_assert(sizeof(TeachStats) == kRowFloats * sizeof(float), "what a row keeps");
 
@@ -263,7 +265,8 @@ __device__ __forceinline__ void finish_distill(const TeachArgs& t, int64_t r, in
         TeachStats st = {};
         st.ref = others ? o.max : 0.0f;
         st.ref_log = (float)log_o;
-        st.others = !teaches || empty ? 0.0f : nan ? NAN : (float)(o_mass / s - q_rest);
+        st.live = teaches && !empty;
+        st.others = !st.live ? 0.0f : nan ? NAN : (float)(o_mass / s - q_rest);
         reinterpret_cast<TeachStats*>(t.stats)[r] = st;
     }
 }

@@ -186,13 +186,11 @@ struct PackArgs {
     void* to;
     int64_t stride;                         // of the copy, elements
     int64_t padded;                         // elements of a row of the copy; zeros behind what is taken
-    const float* coefs;                     // of row r four floats: a row whose last two are 0 is zeros; null: none is
-    const float* bias;                      // a row whose entry is -inf is zeros; null: none is
+    const float4* coefs;                    // a row whose x is +inf has no gradient and is zeros; null: none is
+    const float* bias;                      // of a row whose entry is -inf only what is finite is taken; null: all is
 };
 __device__ __forceinline__ int64_t packed_row(const PackArgs& g, int64_t r) { return r / g.inner * g.outer + r % g.inner * g.inner_stride; }
-__device__ __forceinline__ bool packed_live(const PackArgs& g, int64_t r) {
-    return (!g.coefs || g.coefs[4 * r + 2] != 0.0f || g.coefs[4 * r + 3] != 0.0f) && !(g.bias && g.bias[r] == -INFINITY);
-}
+__device__ __forceinline__ bool packed_live(const PackArgs& g, int64_t r) { return !g.coefs || g.coefs[r].x < INFINITY; }
 
 // Rows as they are: a thread takes 16 bytes of the copy.
 template <typename T>
@@ -221,7 +219,10 @@ __device__ __forceinline__ void pack_across(const PackArgs& g, int64_t block, in
         for (int e = threadIdx.x; e < 64 * 64; e += 256) {
             const int r = e >> 6, c = e & 63;
             T x = (T)0.0f;
-            if (r0 + r < g.count && c0 + c < g.columns && packed_live(g, r0 + r)) x = (static_cast<const T*>(g.from) + packed_row(g, r0 + r))[c0 + c];
+            if (r0 + r < g.count && c0 + c < g.columns && packed_live(g, r0 + r)) {
+                x = (static_cast<const T*>(g.from) + packed_row(g, r0 + r))[c0 + c];
+                if (g.bias && g.bias[r0 + r] == -INFINITY && !(fabsf((float)x) < INFINITY)) x = (T)0.0f;
+            }
             square[r][c] = x;
         }
         __syncthreads();

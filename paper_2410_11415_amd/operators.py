@@ -207,7 +207,7 @@ def _head_args(hidden, weight, bias, tokens):
 
 def _teacher_args(teacher, temperature, rest):
     teacher, rows = _rows_of(teacher)
-    return _b.klay_teacher(teacher.data_ptr(), rows, teacher.stride(-1), temperature, rest), teacher
+    return _b.klay_teacher(teacher.data_ptr(), rows, teacher.stride(-1), temperature, rest, 0), teacher
 
 
 def _kept(like, args):
