@@ -128,7 +128,7 @@ struct HeadPlan {
     size_t hidden = 0, weight = 0, partial = 0, kept = 0, coefs = 0, entries = 0, largest = 0, g = 0, g_across = 0, w_across = 0, h_across = 0,
            dh_sums = 0, dw_sums = 0, db_sums = 0, bytes = 0;
 };
-int64_t stages_of(int64_t elements, const Sizes& s) { return tiles(elements * s.bytes, klay::kStageBytes); }
+int64_t stages_of(int64_t elements, const Sizes& s) { return tiles(elements * s.bytes, klay::kMostStageBytes); }
 
 HeadPlan head_plan(const klay_head_args* a, bool back) {
     const Sizes s(a->dtype);
@@ -219,6 +219,7 @@ template <typename T> struct Head {
         g.inner = std::max<int64_t>(rows.inner, 1);
         g.count = count;
         g.columns = a->width;
+        g.wide = reinterpret_cast<uintptr_t>(from) % 16 == 0 && g.outer % s.lot == 0 && g.inner_stride % s.lot == 0;
         return g;
     }
     klay_rows weight_rows() const { return klay_rows{INT64_MAX, 0, a->weight_stride}; }
@@ -251,7 +252,6 @@ template <typename T> struct Head {
         g.bias = a->bias;
         g.vocab = a->vocab;
         g.rows = a->rows;
-        g.stages = (int32_t)stages_of(p.padded, s);
         g.num_tokens = a->num_tokens;
         g.sorted = kept.sorted;
         return g;
@@ -322,7 +322,8 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
     KLAY_DO(operands());
     const auto across = [&](const void* from, const klay_rows& rows, int64_t count, int64_t padded, size_t to) {
         klay::PackArgs c = copy(from, rows, count);
-        c.stride = c.padded = padded;
+        c.padded = padded;
+        c.stride = padded;
         c.to = in(workspace, to);
         return c;
     };
@@ -348,6 +349,8 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
         g.g_across = dweight ? in(workspace, p.g_across) : nullptr;
         g.g_columns = columns;
         g.g_rows = p.g_rows;
+        g.g_stride = columns;
+        g.g_across_stride = p.g_rows;
         g.bias_partial = dbias ? static_cast<float*>(in(workspace, p.db_sums)) : nullptr;
         KLAY_DO(klay::HeadLaunch<T>::adjoint(p.tile, g, stream));
         klay::ProductJob jobs[2];
@@ -359,10 +362,9 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
             KLAY_DO(klay::HeadLaunch<T>::pack(c, true, stream));
             klay::ProductJob& j = jobs[n];
             job_tile[n++] = p.dh.tile;
-            j.a = klay::Operand{g.g, columns * s.bytes, a->rows, (int32_t)(columns / s.lot)};
-            j.b = klay::Operand{c.to, columns * s.bytes, a->width, (int32_t)(columns / s.lot)};
-            j.stages = (int32_t)stages_of(columns, s);
-            j.splits = std::min(p.dh.splits, j.stages);
+            j.a = klay::Operand{g.g, g.g_stride * s.bytes, a->rows, (int32_t)(columns / s.lot)};
+            j.b = klay::Operand{c.to, c.stride * s.bytes, a->width, (int32_t)(columns / s.lot)};
+            j.splits = (int32_t)std::min<int64_t>(p.dh.splits, stages_of(columns, s));
             j.rows = a->rows;
             j.columns = a->width;
             j.out = whole && j.splits == 1 ? dhidden : nullptr;
@@ -374,9 +376,8 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
         if (dweight) {
             klay::ProductJob& j = jobs[n];
             job_tile[n++] = p.dw.tile;
-            j.a = klay::Operand{g.g_across, p.g_rows * s.bytes, count, (int32_t)(p.g_rows / s.lot)};
-            j.b = klay::Operand{in(workspace, p.h_across), p.g_rows * s.bytes, a->width, (int32_t)(p.g_rows / s.lot)};
-            j.stages = (int32_t)stages_of(p.g_rows, s);
+            j.a = klay::Operand{g.g_across, g.g_across_stride * s.bytes, count, (int32_t)(p.g_rows / s.lot)};
+            j.b = klay::Operand{in(workspace, p.h_across), g.g_across_stride * s.bytes, a->width, (int32_t)(p.g_rows / s.lot)};
             j.splits = p.dw.splits;
             j.rows = count;
             j.columns = a->width;

@@ -19,7 +19,7 @@ struct HeadArgs {
     const float* bias;                      // of these tokens, or null
     int32_t first, vocab;                   // the first of these tokens; how many tokens there are in all
     int64_t rows;
-    int32_t stages, num_tokens;
+    int32_t num_tokens;
     const int32_t* sorted;                  // [rows, num_tokens]
     float scale;                            // log2 e / T
     // forward
@@ -29,15 +29,15 @@ struct HeadArgs {
     const float4* coefs;                    // [rows]: ref (+inf: the row has no gradient), ln S log2 e, A, B ln 2
     const float* entries;                   // [rows, num_tokens]
     const uint32_t* largest;                // bits of the largest adjoint (fp16), or null
-    void *g, *g_across;                     // [rows, g_columns], [g_columns, g_rows]
-    int64_t g_columns, g_rows;
+    void *g, *g_across;                     // [rows, g_columns], [g_columns, g_rows], their rows so many elements apart
+    int64_t g_columns, g_rows, g_stride, g_across_stride;
     float* bias_partial;                    // [tiles of rows, g_columns], or null
 };
 
 // One product of a launch: `splits` runs over its stages, each into fp32 sums of its own or, if it is the only one of all pieces, into `out`.
 struct ProductJob {
     Operand a, b;
-    int32_t stages, splits;
+    int32_t splits;
     int64_t rows, columns;
     void* out;                              // [rows, columns], or null
     float* sums;                            // [splits, rows, columns]
@@ -103,17 +103,22 @@ __device__ __forceinline__ float half_sum(float x) {
 
 // ---- forward ---------------------------------------------------------------------------------------------------------
 template <typename Tile, bool ENT>
-__global__ void __launch_bounds__(Tile::kThreads) head_forward_kernel(HeadArgs g, Tiles tiles) {
+__global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_forward_kernel(HeadArgs g, Tiles tiles) {
     constexpr int BM = Tile::kM, BN = Tile::kN, TM = Tile::TM, TN = Tile::TN, WN = Tile::kWavesN;
-    __shared__ typename Tile::Shared sh[Tile::kStages];
-    __shared__ Marks<BM, BN> marks;
-    __shared__ float parts[WN][3][BM];
+    // (one object: of several the compiler would wait for all loads into one before every read of it)
+    __shared__ struct {
+        typename Tile::Shared stage[Tile::kStages];
+        Marks<BM, BN> marks;
+        float parts[WN][3][BM];
+    } sh;
+    auto &marks = sh.marks;
+    auto &parts = sh.parts;
     int64_t tm, tn;
     tiles.at(blockIdx.x, tm, tn);
     const int64_t m0 = tm * BM, n0 = tn * BN;
     Tile t;
     if (g.num_tokens) marks.make(g, m0, g.first + (int32_t)n0, threadIdx.x, Tile::kThreads);
-    t.run(g.hidden, g.weight, m0, n0, 0, g.stages, sh);           // (its barriers are behind the marks, too)
+    t.run(g.hidden, g.weight, m0, n0, 0, Tile::stages(g.hidden), sh.stage);           // (its barriers are behind the marks, too)
     float bias[TN];
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
@@ -187,20 +192,25 @@ __global__ void __launch_bounds__(Tile::kThreads) head_forward_kernel(HeadArgs g
 
 // ---- backward --------------------------------------------------------------------------------------------------------
 template <typename Tile>
-__global__ void __launch_bounds__(Tile::kThreads) head_adjoint_kernel(HeadArgs g, Tiles tiles) {
+__global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_adjoint_kernel(HeadArgs g, Tiles tiles) {
     typedef typename Tile::Element T;
     constexpr int BM = Tile::kM, BN = Tile::kN, TM = Tile::TM, TN = Tile::TN, WM = Tile::kWavesM;
-    __shared__ typename Tile::Shared sh[Tile::kStages];
-    __shared__ Marks<BM, BN> marks;
-    __shared__ float4 coefs[BM];
-    __shared__ float sums[WM][BN];
+    __shared__ struct {
+        typename Tile::Shared stage[Tile::kStages];
+        Marks<BM, BN> marks;
+        float4 coefs[BM];
+        float sums[WM][BN];
+    } sh;
+    auto &marks = sh.marks;
+    auto &coefs = sh.coefs;
+    auto &sums = sh.sums;
     int64_t tm, tn;
     tiles.at(blockIdx.x, tm, tn);
     const int64_t m0 = tm * BM, n0 = tn * BN;
     Tile t;
     if (g.num_tokens) marks.make(g, m0, g.first + (int32_t)n0, threadIdx.x, Tile::kThreads);
     for (int row = threadIdx.x; row < BM; row += Tile::kThreads) coefs[row] = m0 + row < g.rows ? g.coefs[m0 + row] : make_float4(INFINITY, 0, 0, 0);
-    t.run(g.hidden, g.weight, m0, n0, 0, g.stages, sh);
+    t.run(g.hidden, g.weight, m0, n0, 0, Tile::stages(g.hidden), sh.stage);
     const float up = adjoint_scale(g.largest);
     float bias[TN], sum[TN] = {};
 #pragma unroll
@@ -240,9 +250,9 @@ __global__ void __launch_bounds__(Tile::kThreads) head_adjoint_kernel(HeadArgs g
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     scaled[e] = d[j][e] * up;
-                    if (out && r + e < g.rows) out[(r + e) * g.g_columns + c] = (T)scaled[e];
+                    if (out && r + e < g.rows) out[(r + e) * g.g_stride + c] = (T)scaled[e];
                 }
-                if (across && r < g.g_rows) store_elements<4>(across + c * g.g_rows + r, scaled);      // (g_rows is a multiple of 8)
+                if (across && r < g.g_rows) store_elements<4>(across + c * g.g_across_stride + r, scaled);      // (g_rows is a multiple of 8)
             }
         }
     }
@@ -263,7 +273,7 @@ __global__ void __launch_bounds__(Tile::kThreads) head_adjoint_kernel(HeadArgs g
 }
 
 template <typename Tile>
-__global__ void __launch_bounds__(Tile::kThreads) head_product_kernel(ProductArgs g, int64_t first_job) {
+__global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_product_kernel(ProductArgs g, int64_t first_job) {
     typedef typename Tile::Element T;
     __shared__ typename Tile::Shared sh[Tile::kStages];
     const int which = blockIdx.x >= first_job;
@@ -275,7 +285,8 @@ __global__ void __launch_bounds__(Tile::kThreads) head_product_kernel(ProductArg
     int64_t tm, tn;
     tiles.at(id - split * all, tm, tn);
     const int64_t m0 = tm * Tile::kM, n0 = tn * Tile::kN;
-    const int32_t from = (int32_t)((int64_t)job.stages * split / job.splits), to = (int32_t)((int64_t)job.stages * (split + 1) / job.splits);
+    const int64_t stages = Tile::stages(job.a);
+    const int32_t from = (int32_t)(stages * split / job.splits), to = (int32_t)(stages * (split + 1) / job.splits);
     Tile t;
     t.run(job.a, job.b, m0, n0, from, to, sh);
     const float down = 1.0f / adjoint_scale(g.largest);

@@ -8,10 +8,10 @@
 
 namespace klay {
 
-template <typename T> using Tile32 = Tile<T, 32, 128, 1, 4, 3>;
-template <typename T> using Tile64 = Tile<T, 64, 128, 1, 4, 3>;
-template <typename T> using Tile128 = Tile<T, 128, 128, 2, 2, 2>;
-template <typename T> using Tile256 = Tile<T, 256, 256, 2, 4, 2>;
+template <typename T> using Tile32 = Tile<T, 32, 128, 1, 4, 3, 128>;
+template <typename T> using Tile64 = Tile<T, 64, 128, 1, 4, 3, 128>;
+template <typename T> using Tile128 = Tile<T, 128, 128, 2, 2, 2, 128>;
+template <typename T> using Tile256 = Tile<T, 256, 256, 2, 4, 2, 128>;
 
 template <typename Tile> Tiles tiles_of(int64_t rows, int64_t columns) {
     return Tiles{(rows + Tile::kM - 1) / Tile::kM, (columns + Tile::kN - 1) / Tile::kN};

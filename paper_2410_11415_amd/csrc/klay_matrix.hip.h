@@ -14,8 +14,8 @@ template <typename T> using Eight = typename Pieces<T, 8>::Vec;
 __device__ __forceinline__ Acc mma(Eight<bf16> a, Eight<bf16> b, Acc c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ Acc mma(Eight<f16> a, Eight<f16> b, Acc c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
-constexpr int kStageBytes = 128;            // a row's share of a stage: 64 k's of 16 bits, 32 of 32
-constexpr int kStagePieces = kStageBytes / 16;
+// A stage of k: SB bytes of each row, 64 or 128 (32 or 64 k's of 16 bits, half as many of 32).
+constexpr int kMostStageBytes = 128;
 constexpr uint32_t kMostStride = 1u << 23;  // bytes from row to row: 256 rows lie within 31 bits
 
 // One side of a product.
@@ -26,70 +26,84 @@ struct Operand {
     int32_t pieces;                         // 16-byte pieces of a row; what lies behind them reads as zeros
 };
 
-// The 16-byte pieces of a stage's row lie permuted by bits 1 .. 3 of the row, so that the rows of a fragment come from all banks.
-__device__ __forceinline__ int place_of(int row, int piece) { return piece ^ ((row >> 1) & 7); }
+// The 16-byte pieces of a stage's row lie permuted by the row's place among sixteen, so that the rows of a fragment come from all banks.
+template <int SB> __device__ __forceinline__ int place_of(int row, int piece) { return piece ^ (SB == 128 ? (row >> 1) & 7 : (row >> 2) & 3); }
 
-// A wave's part of the loads of ROWS rows by WAVES waves: 1 KB, eight rows, an instruction, straight into shared memory.
-template <int ROWS, int WAVES> struct Stage {
-    static constexpr int kLoads = ROWS / 8 / WAVES;
-    static_assert(ROWS % (8 * WAVES) == 0 && (WAVES % 2 == 0 || kLoads == 1), "whole loads, one permutation a lane");
+// A wave's part of the loads of one side's ROWS rows by WAVES waves: 1 KB an instruction, straight into shared memory.  HALF > 0: they come in two halves,
+// of which the first has the first HALF of every 2 HALF rows.
+template <int ROWS, int HALF, int WAVES, int SB> struct Stage {
+    static constexpr int kHalves = HALF > 0 ? 2 : 1, kRows = 1024 / SB, kPieces = SB / 16, kLoads = ROWS / kHalves / kRows / WAVES;
+    static_assert(ROWS % (kHalves * kRows * WAVES) == 0 && HALF % kRows == 0 && (WAVES * kRows) % 16 == 0, "whole loads, one permutation a lane");
     Stretch from;
-    uint32_t offset[kLoads];
+    uint32_t offset[kHalves][kLoads];
     int32_t piece, pieces;
+    static __device__ __forceinline__ int first_row(int half, int i, int wave) {
+        const int r = (i * WAVES + wave) * kRows;
+        if constexpr (HALF == 0) return r;
+        else return r / HALF * 2 * HALF + half * HALF + r % HALF;
+    }
     __device__ __forceinline__ void init(const Operand& s, int64_t row0, int wave, int lane) {
         from = stretch_at(static_cast<const char*>(s.p) + row0 * s.stride);
         pieces = s.pieces;
-        piece = place_of(wave * 8 + (lane >> 3), lane & 7);
+        piece = place_of<SB>(first_row(0, 0, wave) + lane / kPieces, lane % kPieces);
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int r = (i * WAVES + wave) * 8 + (lane >> 3);
-            offset[i] = row0 + r < s.rows ? (uint32_t)r * (uint32_t)s.stride + (uint32_t)piece * 16u : kNoLane;
-        }
+        for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int r = first_row(h, i, wave) + lane / kPieces;
+                offset[h][i] = row0 + r < s.rows ? (uint32_t)r * (uint32_t)s.stride + (uint32_t)piece * 16u : kNoLane;
+            }
     }
-    // stage `at` of k; behind the last piece: zeros
-    __device__ __forceinline__ void load(int at, char* lds, int wave) const {
-        const bool in = at * kStagePieces + piece < pieces;
+    // a half, or all, of stage `at` of k; behind the last piece: zeros
+    __device__ __forceinline__ void load(int half, int at, char* lds, int wave) const {
+        const bool in = at * kPieces + piece < pieces;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(lds + (i * WAVES + wave) * 1024), 16,
-                                                     in ? offset[i] : kNoLane, at * kStageBytes, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(lds + first_row(half, i, wave) * SB), 16,
+                                                     in ? offset[half][i] : kNoLane, at * SB, 0, 0);
     }
 };
 
 // The eight k's of a lane's row that a matrix instruction takes, `half` 0 or 1 of sixteen.
 template <typename T> struct Fragment {
-    static constexpr int kSixteens = 4;     // of a stage
     Eight<T> x;
-    __device__ __forceinline__ void load(const char* lds, int row, int s, int half) {
-        x = *reinterpret_cast<const Eight<T>*>(lds + row * kStageBytes + place_of(row, 2 * s + half) * 16);
+    template <int SB> __device__ __forceinline__ void load(const char* lds, int row, int s, int half) {
+        x = *reinterpret_cast<const Eight<T>*>(lds + row * SB + place_of<SB>(row, 2 * s + half) * 16);
     }
 };
 template <> struct Fragment<f32> {
-    static constexpr int kSixteens = 2;
+    typedef float Four __attribute__((ext_vector_type(4)));
+    typedef float Floats __attribute__((ext_vector_type(8)));
+    Four x[2];
     Eight<bf16> hi, mid, lo;
-    __device__ __forceinline__ void load(const char* lds, int row, int s, int half) {
-        typedef float Four __attribute__((ext_vector_type(4)));
-        typedef float Floats __attribute__((ext_vector_type(8)));
-        const Four a = *reinterpret_cast<const Four*>(lds + row * kStageBytes + place_of(row, 4 * s + 2 * half) * 16);
-        const Four b = *reinterpret_cast<const Four*>(lds + row * kStageBytes + place_of(row, 4 * s + 2 * half + 1) * 16);
-        Floats x = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-        hi = __builtin_convertvector(x, Eight<bf16>);
-        x -= __builtin_convertvector(hi, Floats);
-        mid = __builtin_convertvector(x, Eight<bf16>);
-        x -= __builtin_convertvector(mid, Floats);
-        lo = __builtin_convertvector(x, Eight<bf16>);
+    template <int SB> __device__ __forceinline__ void load(const char* lds, int row, int s, int half) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) x[p] = *reinterpret_cast<const Four*>(lds + row * SB + place_of<SB>(row, 4 * s + 2 * half + p) * 16);
+    }
+    __device__ __forceinline__ void take_apart() {
+        Floats y = __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
+        hi = __builtin_convertvector(y, Eight<bf16>);
+        y -= __builtin_convertvector(hi, Floats);
+        mid = __builtin_convertvector(y, Eight<bf16>);
+        y -= __builtin_convertvector(mid, Floats);
+        lo = __builtin_convertvector(y, Eight<bf16>);
     }
 };
 
-// A tile of BM x BN by WM x WN waves, S stages of k in shared memory; wave (wm, wn) has TM x TN blocks of 32 x 32 in registers.  Lane l of a block holds
+// A tile of BM x BN by WM x WN waves, S stages of SB bytes of k in shared memory; wave (wm, wn) has TM x TN blocks of 32 x 32 in registers.  Lane l of a block holds
 // column l % 32 and of it the rows 8 q + 4 (l / 32) + e as element 4 q + e.
-template <typename T, int BM, int BN, int WM, int WN, int S> struct Tile {
-    static constexpr int kM = BM, kN = BN, kWavesM = WM, kWavesN = WN, kWaves = WM * WN, kThreads = 64 * kWaves, kStages = S;
+template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile {
+    static constexpr int kM = BM, kN = BN, kWavesM = WM, kWavesN = WN, kWaves = WM * WN, kThreads = 64 * kWaves, kStages = S, kStageBytes = SB;
     static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
+    static constexpr int kParts = SB / (16 * sizeof(T));        // sixteen k's each
+    static constexpr bool kQuarters = !std::is_same_v<T, f32> && TM % 2 == 0 && TN % 2 == 0 && S == 2;      // (fp32: no registers for that many fragments)
+    typedef Stage<BM, kQuarters ? TM * 16 : 0, kWaves, SB> LoadsA;
+    typedef Stage<BN, kQuarters ? TN * 16 : 0, kWaves, SB> LoadsB;
     typedef T Element;
     struct Shared {                         // one stage
-        char a[BM * kStageBytes], b[BN * kStageBytes];
+        char a[BM * SB], b[BN * SB];
     };
+    static __device__ __forceinline__ int stages(const Operand& o) { return (o.pieces * 16 + SB - 1) / SB; }
     Acc acc[TM][TN];
     int wave, lane, wm, wn;
     __device__ __forceinline__ Tile() {
@@ -102,63 +116,168 @@ template <typename T, int BM, int BN, int WM, int WN, int S> struct Tile {
     __device__ __forceinline__ int row(int i) const { return (wm * TM + i) * 32 + 4 * (lane >> 5); }
     __device__ __forceinline__ int column(int j) const { return (wn * TN + j) * 32 + (lane & 31); }
 
-    __device__ __forceinline__ void step(const char* a, const char* b) {
+    // What a matrix instruction of each block takes: sixteen k's.
+    struct Fragments {
+        Fragment<T> a[TM], b[TN];
+    };
+    __device__ __forceinline__ void fetch(Fragments& f, const Shared& sh, int s) const {
         const int r = lane & 31, half = lane >> 5;
 #pragma unroll
-        for (int s = 0; s < Fragment<T>::kSixteens; ++s) {
-            Fragment<T> fa[TM], fb[TN];
+        for (int j = 0; j < TN; ++j) f.b[j].template load<SB>(sh.b, (wn * TN + j) * 32 + r, s, half);
 #pragma unroll
-            for (int i = 0; i < TM; ++i) fa[i].load(a, (wm * TM + i) * 32 + r, s, half);
+        for (int i = 0; i < TM; ++i) f.a[i].template load<SB>(sh.a, (wm * TM + i) * 32 + r, s, half);
+    }
+    __device__ __forceinline__ void multiply(Fragments& f) {
+        auto all = [&](auto&& one) {
 #pragma unroll
-            for (int j = 0; j < TN; ++j) fb[j].load(b, (wn * TN + j) * 32 + r, s, half);
-            auto all = [&](auto&& one) {
+            for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int i = 0; i < TM; ++i)
+                for (int j = 0; j < TN; ++j) acc[i][j] = one(f.a[i], f.b[j], acc[i][j]);
+        };
+        typedef Fragment<T> F;
+        if constexpr (std::is_same_v<T, f32>) {              // smallest first
 #pragma unroll
-                    for (int j = 0; j < TN; ++j) acc[i][j] = one(fa[i], fb[j], acc[i][j]);
-            };
-            typedef Fragment<T> F;
-            if constexpr (std::is_same_v<T, f32>) {          // smallest first
-                all([](const F& x, const F& y, Acc c) { return mma(x.lo, y.hi, c); });
-                all([](const F& x, const F& y, Acc c) { return mma(x.hi, y.lo, c); });
-                all([](const F& x, const F& y, Acc c) { return mma(x.mid, y.mid, c); });
-                all([](const F& x, const F& y, Acc c) { return mma(x.mid, y.hi, c); });
-                all([](const F& x, const F& y, Acc c) { return mma(x.hi, y.mid, c); });
-                all([](const F& x, const F& y, Acc c) { return mma(x.hi, y.hi, c); });
-            } else {
-                all([](const F& x, const F& y, Acc c) { return mma(x.x, y.x, c); });
-            }
+            for (int i = 0; i < TM; ++i) f.a[i].take_apart();
+#pragma unroll
+            for (int j = 0; j < TN; ++j) f.b[j].take_apart();
+            all([](const F& x, const F& y, Acc c) { return mma(x.lo, y.hi, c); });
+            all([](const F& x, const F& y, Acc c) { return mma(x.hi, y.lo, c); });
+            all([](const F& x, const F& y, Acc c) { return mma(x.mid, y.mid, c); });
+            all([](const F& x, const F& y, Acc c) { return mma(x.mid, y.hi, c); });
+            all([](const F& x, const F& y, Acc c) { return mma(x.hi, y.mid, c); });
+            all([](const F& x, const F& y, Acc c) { return mma(x.hi, y.hi, c); });
+        } else {
+            all([](const F& x, const F& y, Acc c) { return mma(x.x, y.x, c); });
         }
     }
-    // Stages from .. to - 1 of rows m0 .. of a and n0 .. of b.  Stage s + S - 1 is asked for while stage s is worked on, in the place of stage s - 1, which
-    // all waves have left at the barrier between the two.  (Stages behind the last one read zeros, so that always as many loads are on their way.)
-    // Ends with a barrier: shared memory is free again.
+    // Stages from .. to - 1 (one at least) of rows m0 .. of a and n0 .. of b.  Ends with a barrier: shared memory is free again.
     __device__ __forceinline__ void run(const Operand& oa, const Operand& ob, int64_t m0, int64_t n0, int from, int to, Shared (&sh)[S]) {
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j) acc[i][j] = Acc{};
-        Stage<BM, kWaves> la;
-        Stage<BN, kWaves> lb;
+        LoadsA la;
+        LoadsB lb;
         la.init(oa, m0, wave, lane);
         lb.init(ob, n0, wave, lane);
-        constexpr int kInFlight = (S - 2) * (Stage<BM, kWaves>::kLoads + Stage<BN, kWaves>::kLoads);
+        if constexpr (kQuarters) run_quarters(la, lb, from, to, sh);
+        else run_stages(la, lb, from, to, sh);
+        arrived<0>();
+    }
+
+    // All but the `left` youngest of this wave's loads have come, and its reads of shared memory; then those of all waves.
+    template <int LEFT> static __device__ __forceinline__ void arrived() {
+#ifdef __HIP_DEVICE_COMPILE__
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+#endif
+    }
+
+    // A stage at a time: stage s + S is asked for when all waves have left stage s.  (Stages behind the last one read zeros, so that always as many
+    // loads are on their way.)
+    __device__ __forceinline__ void run_stages(const LoadsA& la, const LoadsB& lb, int from, int to, Shared (&sh)[S]) {
+        constexpr int kLoads = LoadsA::kLoads + LoadsB::kLoads;
 #pragma unroll
-        for (int s = 0; s < S - 1; ++s) {
-            la.load(from + s, sh[s].a, wave);
-            lb.load(from + s, sh[s].b, wave);
+        for (int s = 0; s < S; ++s) {
+            la.load(0, from + s, sh[s].a, wave);
+            lb.load(0, from + s, sh[s].b, wave);
         }
+        arrived<(S - 1) * kLoads>();
         for (int kt = from; kt < to; kt += S) {
 #pragma unroll
             for (int s = 0; s < S; ++s) {
-                if (kt + s >= to) break;
-                asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kInFlight) : "memory");
-                la.load(kt + s + S - 1, sh[(s + S - 1) % S].a, wave);
-                lb.load(kt + s + S - 1, sh[(s + S - 1) % S].b, wave);
-                step(sh[s].a, sh[s].b);
+                Fragments f;
+#pragma unroll
+                for (int part = 0; part < kParts; ++part) {
+                    fetch(f, sh[s], part);
+                    if (part == kParts - 1 && kt + s + 1 < to) {
+                        arrived<(S - 2) * kLoads>();
+                        la.load(0, kt + s + S, sh[s].a, wave);
+                        lb.load(0, kt + s + S, sh[s].b, wave);
+                    }
+                    multiply(f);
+                }
+                if (kt + s + 1 >= to) break;
             }
         }
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+
+    // A stage in four phases, a quarter of the blocks each: A0 B0, A0 B1, A1 B0, A1 B1, of halves of the wave's rows and columns.  A phase's fragments are in
+    // registers when it begins; while its matrix instructions run, the half that a later phase needs is read: B1, A1, the next stage's A0, its B0.  A half that
+    // all waves have read (the barrier behind each phase) is filled again at once, for the stage after next: seven phases before it is read, so that six
+    // halves are on their way at every barrier and the loads never pause.  (Loading whole stages, one ahead: 3790 us for the loop of 4096 x 131072 x 4096.)
+    static constexpr int HA = TM / 2 > 0 ? TM / 2 : 1, HB = TN / 2 > 0 ? TN / 2 : 1;
+    struct HalfA { Fragment<T> x[HA][kParts]; };
+    struct HalfB { Fragment<T> x[HB][kParts]; };
+    __device__ __forceinline__ void fetch(HalfA& f, const Shared& sh, int half) const {
+#pragma unroll
+        for (int i = 0; i < HA; ++i)
+#pragma unroll
+            for (int s = 0; s < kParts; ++s) f.x[i][s].template load<SB>(sh.a, (wm * TM + half * HA + i) * 32 + (lane & 31), s, lane >> 5);
+    }
+    __device__ __forceinline__ void fetch(HalfB& f, const Shared& sh, int half) const {
+#pragma unroll
+        for (int j = 0; j < HB; ++j)
+#pragma unroll
+            for (int s = 0; s < kParts; ++s) f.x[j][s].template load<SB>(sh.b, (wn * TN + half * HB + j) * 32 + (lane & 31), s, lane >> 5);
+    }
+    template <int FROM, int TO> __device__ __forceinline__ void multiply(const HalfA& a, const HalfB& b, int ha, int hb) {
+#pragma unroll
+        for (int s = FROM; s < TO; ++s)
+#pragma unroll
+            for (int i = 0; i < HA; ++i)
+#pragma unroll
+                for (int j = 0; j < HB; ++j) acc[ha * HA + i][hb * HB + j] = mma(a.x[i][s].x, b.x[j][s].x, acc[ha * HA + i][hb * HB + j]);
+    }
+    // One phase; `others` asks for the half that is free now and reads the one that is needed later.
+    template <typename F> __device__ __forceinline__ void phase(const HalfA& a, const HalfB& b, int ha, int hb, F&& others) {
+        multiply<0, 1>(a, b, ha, hb);                     // (the matrix cores have work at once)
+        __builtin_amdgcn_sched_barrier(0);
+        others();
+        __builtin_amdgcn_sched_barrier(0);
+        multiply<1, kParts>(a, b, ha, hb);
+        __builtin_amdgcn_sched_barrier(0);
+        arrived<3 * (LoadsA::kLoads + LoadsB::kLoads)>();
+    }
+    __device__ __forceinline__ void run_quarters(const LoadsA& la, const LoadsB& lb, int from, int to, Shared (&sh)[S]) {
+        constexpr int kLoads = LoadsA::kLoads + LoadsB::kLoads;
+        HalfA a0, a1;
+        HalfB b0, b1;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            la.load(0, from + s, sh[s].a, wave);
+            lb.load(0, from + s, sh[s].b, wave);
+            lb.load(1, from + s, sh[s].b, wave);
+            la.load(1, from + s, sh[s].a, wave);
+        }
+        arrived<3 * kLoads>();
+        fetch(a0, sh[0], 0);
+        fetch(b0, sh[0], 0);
+        arrived<3 * kLoads>();
+        la.load(0, from + 2, sh[0].a, wave);
+        arrived<3 * kLoads>();
+        for (int kt = from; kt < to; kt += 2) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                Shared &now = sh[s], &next = sh[s ^ 1];
+                phase(a0, b0, 0, 0, [&] {
+                    lb.load(0, kt + s + 2, now.b, wave);
+                    fetch(b1, now, 1);
+                });
+                phase(a0, b1, 0, 1, [&] {
+                    lb.load(1, kt + s + 2, now.b, wave);
+                    fetch(a1, now, 1);
+                });
+                phase(a1, b0, 1, 0, [&] {
+                    la.load(1, kt + s + 2, now.a, wave);
+                    fetch(a0, next, 0);
+                });
+                phase(a1, b1, 1, 1, [&] {
+                    la.load(0, kt + s + 3, next.a, wave);
+                    fetch(b0, next, 0);
+                });
+                if (kt + s + 1 >= to) break;
+            }
+        }
     }
 };
 
@@ -187,6 +306,7 @@ struct PackArgs {
     int64_t stride;                         // of the copy, elements
     int64_t padded;                         // elements of a row of the copy; zeros behind what is taken
     const float4* coefs;                    // a row whose x is +inf has no gradient and is zeros; null: none is
+    int32_t wide;                           // rows start at multiples of 16 bytes
     const float* bias;                      // of a row whose entry is -inf only what is finite is taken; null: all is
 };
 __device__ __forceinline__ int64_t packed_row(const PackArgs& g, int64_t r) { return r / g.inner * g.outer + r % g.inner * g.inner_stride; }
@@ -208,31 +328,46 @@ __device__ __forceinline__ void pack_rows(const PackArgs& g, int64_t block, int6
     }
 }
 
-// Rows and columns exchanged: copy[c][r], `padded` (a multiple of 16 bytes) next to each other, by squares of 64 x 64.
+// Rows and columns exchanged: copy[c][r], `padded` (a multiple of 16 bytes) next to each other, by squares of 64 x 64; 16 bytes a thread both ways where
+// the rows lie so (`wide`).
 template <typename T>
 __device__ __forceinline__ void pack_across(const PackArgs& g, int64_t block, int64_t blocks) {
     constexpr int N = 16 / sizeof(T);
-    __shared__ T square[64][65];
+    typedef typename Pieces<T, N>::Vec Vec;
+    __shared__ T square[64][64 + 4 / sizeof(T)];
     const int64_t across = (g.columns + 63) / 64, all = (g.padded + 63) / 64 * across;
     for (int64_t i = block; i < all; i += blocks) {
         const int64_t r0 = i / across * 64, c0 = (i % across) * 64;
-        for (int e = threadIdx.x; e < 64 * 64; e += 256) {
-            const int r = e >> 6, c = e & 63;
-            T x = (T)0.0f;
-            if (r0 + r < g.count && c0 + c < g.columns && packed_live(g, r0 + r)) {
-                x = (static_cast<const T*>(g.from) + packed_row(g, r0 + r))[c0 + c];
-                if (g.bias && g.bias[r0 + r] == -INFINITY && !(fabsf((float)x) < INFINITY)) x = (T)0.0f;
+#pragma unroll
+        for (int step = 0; step < 64 * 64 / N / 256; ++step) {
+            const int e = step * 256 + threadIdx.x, r = e / (64 / N), c = e % (64 / N) * N;
+            Vec x = {};
+            if (r0 + r < g.count && packed_live(g, r0 + r)) {
+                const T* row = static_cast<const T*>(g.from) + packed_row(g, r0 + r) + c0 + c;
+                if (g.wide && c0 + c + N <= g.columns) {
+                    x = *reinterpret_cast<const Vec*>(row);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < N; ++q)
+                        if (c0 + c + q < g.columns) x[q] = row[q];
+                }
+                if (g.bias && g.bias[r0 + r] == -INFINITY) {
+#pragma unroll
+                    for (int q = 0; q < N; ++q) x[q] = fabsf((float)x[q]) < INFINITY ? x[q] : (T)0.0f;
+                }
             }
-            square[r][c] = x;
+#pragma unroll
+            for (int q = 0; q < N; ++q) square[r][c + q] = x[q];
         }
         __syncthreads();
-        for (int e = threadIdx.x; e < 64 * 64 / N; e += 256) {
-            const int c = e / (64 / N), r = e % (64 / N) * N;
+#pragma unroll
+        for (int step = 0; step < 64 * 64 / N / 256; ++step) {
+            const int e = step * 256 + threadIdx.x, c = e / (64 / N), r = e % (64 / N) * N;
             if (c0 + c >= g.columns || r0 + r >= g.padded) continue;
-            typename Pieces<T, N>::Vec out;
+            Vec out;
 #pragma unroll
             for (int q = 0; q < N; ++q) out[q] = square[r + q][c];
-            *reinterpret_cast<typename Pieces<T, N>::Vec*>(static_cast<T*>(g.to) + (c0 + c) * g.stride + r0 + r) = out;
+            *reinterpret_cast<Vec*>(static_cast<T*>(g.to) + (c0 + c) * g.stride + r0 + r) = out;
         }
         __syncthreads();
     }
