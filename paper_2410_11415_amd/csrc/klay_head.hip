@@ -105,7 +105,7 @@ struct ProductPlan {
 };
 ProductPlan product_plan(int64_t rows, int64_t columns, int64_t stages) {
     ProductPlan p;
-    const auto count = [&](klay::HeadTile t) { return tiles(rows, klay::kTileSizes[t].m) * tiles(columns, klay::kTileSizes[t].n); };
+    const auto count = [&](klay::HeadTile t) { return tiles(rows, klay::kTileSizes[t].rows) * tiles(columns, klay::kTileSizes[t].columns); };
     p.tile = rows <= 32 ? klay::TILE_32 : rows <= 64 ? klay::TILE_64 : rows > 128 && columns > 128 && count(klay::TILE_256) >= 192 ? klay::TILE_256 : klay::TILE_128;
     const int64_t want = p.tile == klay::TILE_256 ? klay::kComputeUnits : 2 * klay::kComputeUnits;
     p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({want / count(p.tile), stages / 4, 32}));
@@ -149,7 +149,7 @@ HeadPlan head_plan(const klay_head_args* a, bool back) {
     if (!back) {
         p.row_block = std::min(a->rows, kRowBlock);
         p.tile = logits_tile(p.row_block, a->vocab);
-        p.tiles_n = tiles(a->vocab, klay::kTileSizes[p.tile].n);
+        p.tiles_n = tiles(a->vocab, klay::kTileSizes[p.tile].columns);
         p.partial = take(p.row_block * p.tiles_n * sizeof(float4));
         p.kept = take(kept_bytes(a->rows, a->num_tokens));
     } else {
@@ -169,7 +169,7 @@ HeadPlan head_plan(const klay_head_args* a, bool back) {
         p.dw = product_plan(std::min<int64_t>(p.piece, a->vocab), a->width, stages_of(p.g_rows, s));
         p.dh_sums = take(p.dh.splits * a->rows * a->width * 4);
         p.dw_sums = take(p.dw.splits == 1 ? 0 : p.dw.splits * columns * a->width * 4);
-        p.db_sums = take(tiles(p.g_rows, klay::kTileSizes[p.tile].m) * columns * 4);
+        p.db_sums = take(tiles(p.g_rows, klay::kTileSizes[p.tile].rows) * columns * 4);
     }
     p.bytes = at;
     return p;
@@ -388,7 +388,7 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
             if (!j.out) sums.sum[sums.sums++] = klay::SumArgs{j.sums, count * a->width, count * a->width, j.splits, 1, out};
         }
         if (dbias)
-            sums.sum[sums.sums++] = klay::SumArgs{g.bias_partial, count, columns, (int32_t)tiles(std::max(a->rows, dweight ? p.g_rows : 0), klay::kTileSizes[p.tile].m), 0, dbias + first};
+            sums.sum[sums.sums++] = klay::SumArgs{g.bias_partial, count, columns, (int32_t)tiles(std::max(a->rows, dweight ? p.g_rows : 0), klay::kTileSizes[p.tile].rows), 0, dbias + first};
         for (int i = 0; i < n;) {
             klay::ProductArgs pr{};
             pr.largest = ad.largest;

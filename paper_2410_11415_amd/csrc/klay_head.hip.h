@@ -58,17 +58,17 @@ __device__ __forceinline__ float adjoint_scale(const uint32_t* largest) {
     return exp2_of((float)(k > 100 ? 100 : k));
 }
 
-// The tokens of a row that fall into a tile: `first` their first place in the row's sorted list, a bit for each column.
-template <int BM, int BN> struct Marks {
-    static constexpr int kWords = BN / 32;
-    uint32_t bits[BM][kWords];
-    int32_t first[BM];
-    __device__ __forceinline__ void make(const HeadArgs& g, int64_t m0, int32_t token0, int32_t thread, int32_t threads) {
-        for (int i = thread; i < BM; i += threads) {
+// The tokens of a row that fall into a tile of ROWS rows and COLUMNS tokens: `first` their first place in the row's sorted list, a bit for each column.
+template <int ROWS, int COLUMNS> struct Marks {
+    static constexpr int kWords = COLUMNS / 32;
+    uint32_t bits[ROWS][kWords];
+    int32_t first[ROWS];
+    __device__ __forceinline__ void make(const HeadArgs& g, int64_t row0, int32_t token0, int32_t thread, int32_t threads) {
+        for (int i = thread; i < ROWS; i += threads) {
 #pragma unroll
             for (int w = 0; w < kWords; ++w) bits[i][w] = 0;
-            if (m0 + i >= g.rows) continue;
-            const int32_t* list = g.sorted + (m0 + i) * g.num_tokens;
+            if (row0 + i >= g.rows) continue;
+            const int32_t* list = g.sorted + (row0 + i) * g.num_tokens;
             int32_t lo = 0, hi = g.num_tokens;
             while (lo < hi) {
                 const int32_t mid = (lo + hi) >> 1;
@@ -78,7 +78,7 @@ template <int BM, int BN> struct Marks {
             first[i] = lo;
             for (; lo < g.num_tokens; ++lo) {
                 const uint32_t c = (uint32_t)list[lo] - (uint32_t)token0;
-                if (c >= (uint32_t)BN) break;
+                if (c >= (uint32_t)COLUMNS) break;
                 bits[i][c >> 5] |= 1u << (c & 31);
             }
         }
@@ -89,185 +89,221 @@ template <int BM, int BN> struct Marks {
         return p;
     }
 };
-
-// Over the 32 lanes of a half; all of them get the result.
-__device__ __forceinline__ float other_row(float x) { return __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(x), 0x401f)); }     // lane ^ 16
-__device__ __forceinline__ float half_max(float x) {
-    x = group_max<16>(x);
-    return fmaxf(x, other_row(x));
+// f(i, e, place) for a lane's marked columns of its row of block j: element e of its i-th block, and the token's place in the row's list.
+template <typename Tile, typename M, typename F>
+__device__ __forceinline__ void each_mark(const Tile& t, const M& marks, int j, F&& f) {
+#pragma unroll
+    for (int i = 0; i < Tile::TM; ++i) {
+        const int word = t.wm * Tile::TM + i;
+        const uint32_t mine = marks.bits[t.row(j)][word] >> (4 * (t.lane >> 5));
+        if (__ballot((mine & 0x0f0f0f0fu) != 0) == 0) continue;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            if (mine >> (8 * (e >> 2) + (e & 3)) & 1u) f(i, e, marks.place(t.row(j), word, 8 * (e >> 2) + (e & 3) + 4 * (t.lane >> 5)));
+    }
 }
-__device__ __forceinline__ float half_sum(float x) {
-    x = group_sum<16>(x);
-    return x + other_row(x);
+// The bias of a lane's columns, -inf where there are none: `some` is whether it changes anything.
+template <typename Tile>
+__device__ __forceinline__ bool some_bias(const HeadArgs& g, int64_t column0) { return g.bias != nullptr || column0 + Tile::kM > g.weight.rows; }
+template <typename Tile>
+__device__ __forceinline__ void add_bias(Tile& t, const HeadArgs& g, int64_t column0) {
+#pragma unroll
+    for (int i = 0; i < Tile::TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int64_t c = column0 + t.column(i) + 8 * (e >> 2) + (e & 3);
+            const float b = c < g.weight.rows ? (g.bias ? g.bias[c] : 0.0f) : -INFINITY;
+#pragma unroll
+            for (int j = 0; j < Tile::TN; ++j) t.acc[i][j][e] = b == -INFINITY ? -INFINITY : t.acc[i][j][e] + b;
+        }
 }
 
 // ---- forward ---------------------------------------------------------------------------------------------------------
+// What a lane finds out about its columns of its row of block j, and the other half of the wave about the others': y = x scale - shift with shift = max scale
+// rounded by itself is one multiply-add; what that rounding puts into all terms, 2^d, comes out again at the end.  WIDE takes the difference first, for
+// maxima so far from 0 that the product would leave the range of fp32 (a row of nothing but the type's lowest value, for one).
+struct Part {
+    float max, rest, weighted;
+};
+template <bool ENT, bool WIDE, typename Tile>
+__device__ __forceinline__ Part part_of(const Tile& t, int j, float max, float scale) {
+    const float to = WIDE ? fmaxf(max, -kTokFltMax) : max == -INFINITY ? 0.0f : max, shift = to * scale;
+    auto term = [&](float x) { return WIDE ? (x - to) * scale : fmaf(x, scale, -shift); };
+    float s = 0.0f, u = 0.0f;
+#pragma unroll
+    for (int i = 0; i < Tile::TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float y = term(t.acc[i][j][e]), p = exp2_of(y);
+            s += p;
+            if constexpr (ENT) u = fmaf(p, fmaxf(y, -200.0f), u);
+        }
+    s += __shfl_xor(s, 32);
+    if constexpr (ENT) u += __shfl_xor(u, 32);
+    if constexpr (!WIDE) {
+        const float d = fmaf(to, scale, -shift), f = exp2_of(-d);
+        u = f * (u - d * s);
+        s *= f;
+    }
+    float rest = s == 0.0f ? 0.0f : s - 1.0f;
+    if (s > 0.0f && s < 1.5f) {                                  // one holds most of the sum: the others by themselves
+        rest = 0.0f;
+#pragma unroll
+        for (int i = 0; i < Tile::TM; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) rest += t.acc[i][j][e] == max ? 0.0f : exp2_of((t.acc[i][j][e] - to) * scale);
+    }
+    const float other = __shfl_xor(rest, 32);                    // (both halves have the same s)
+    if (s > 0.0f && s < 1.5f) rest += other;
+    return Part{max, rest, u};
+}
+// The part with the larger maximum keeps its rest; the other brings its maximum's own term along.
+__device__ __forceinline__ Part joined(const Part& a, const Part& b, float scale) {
+    const bool up = b.max > a.max;
+    const Part big = up ? b : a, small = up ? a : b;
+    const bool none = small.max == -INFINITY && small.rest == 0.0f;
+    const float d = (fmaxf(small.max, -kTokFltMax) - fmaxf(big.max, -kTokFltMax)) * scale, f = none ? 0.0f : exp2_of(d), whole = 1.0f + small.rest;
+    return Part{big.max, big.rest + (none ? 0.0f : f * whole), big.weighted + (f > 0.0f ? f * (small.weighted + d * whole) : 0.0f)};
+}
+
 template <typename Tile, bool ENT>
 __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_forward_kernel(HeadArgs g, Tiles tiles) {
-    constexpr int BM = Tile::kM, BN = Tile::kN, TM = Tile::TM, TN = Tile::TN, WN = Tile::kWavesN;
+    constexpr int ROWS = Tile::kN, COLUMNS = Tile::kM, TM = Tile::TM, TN = Tile::TN, PARTS = Tile::kWavesM;
     // (one object: of several the compiler would wait for all loads into one before every read of it)
     __shared__ struct {
         typename Tile::Shared stage[Tile::kStages];
-        Marks<BM, BN> marks;
-        float parts[WN][3][BM];
+        Marks<ROWS, COLUMNS> marks;
+        Part parts[PARTS][ROWS];
     } sh;
-    auto &marks = sh.marks;
-    auto &parts = sh.parts;
-    int64_t tm, tn;
-    tiles.at(blockIdx.x, tm, tn);
-    const int64_t m0 = tm * BM, n0 = tn * BN;
+    int64_t tr, tc;
+    tiles.at(blockIdx.x, tr, tc);
+    const int64_t row0 = tr * ROWS, column0 = tc * COLUMNS;
     Tile t;
-    if (g.num_tokens) marks.make(g, m0, g.first + (int32_t)n0, threadIdx.x, Tile::kThreads);
-    t.run(g.hidden, g.weight, m0, n0, 0, Tile::stages(g.hidden), sh.stage);           // (its barriers are behind the marks, too)
-    float bias[TN];
+    if (g.num_tokens) sh.marks.make(g, row0, g.first + (int32_t)column0, threadIdx.x, Tile::kThreads);
+    t.run(g.weight, g.hidden, column0, row0, 0, Tile::stages(g.hidden), sh.stage);           // (its barriers are behind the marks, too)
+    if (some_bias<Tile>(g, column0)) add_bias(t, g, column0);
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-        const int64_t c = n0 + t.column(j);
-        bias[j] = c < g.weight.rows ? (g.bias ? g.bias[c] : 0.0f) : -INFINITY;
-    }
+        if (g.num_tokens)
+            each_mark(t, sh.marks, j, [&](int i, int e, int32_t place) {
+                g.values[(row0 + t.row(j)) * g.num_tokens + place] = t.acc[i][j][e];
+                t.acc[i][j][e] = -INFINITY;
+            });
+        float max = t.acc[0][j][0];
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int row = t.row(i) + (e >> 2) * 8 + (e & 3);
-            float x[TN], max = -INFINITY;
-#pragma unroll
-            for (int j = 0; j < TN; ++j) x[j] = bias[j] == -INFINITY ? -INFINITY : t.acc[i][j][e] + bias[j];
-            if (g.num_tokens) {
-#pragma unroll
-                for (int j = 0; j < TN; ++j) {
-                    const int word = t.wn * TN + j, bit = t.lane & 31;
-                    if (marks.bits[row][word] >> bit & 1u) {
-                        g.values[(m0 + row) * g.num_tokens + marks.place(row, word, bit)] = x[j];
-                        x[j] = -INFINITY;
-                    }
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < TN; ++j) max = fmaxf(max, x[j]);
-            max = half_max(max);
-            const float to = fmaxf(max, -kTokFltMax);
-            float s = 0.0f, u = 0.0f;
-#pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                const float y = (x[j] - to) * g.scale, p = exp2_of(y);
-                s += p;
-                if constexpr (ENT) u = fmaf(p, fmaxf(y, -200.0f), u);
-            }
-            s = half_sum(s);
-            if constexpr (ENT) u = half_sum(u);
-            float rest = s == 0.0f ? 0.0f : s - 1.0f;
-            if (s > 0.0f && s < 1.5f) {                           // one holds most of the sum: the others by themselves
-                rest = 0.0f;
-#pragma unroll
-                for (int j = 0; j < TN; ++j) rest += x[j] == max ? 0.0f : exp2_of((x[j] - to) * g.scale);
-                rest = half_sum(rest);
-            }
-            if ((t.lane & 31) == 0) {
-                parts[t.wn][0][row] = max;
-                parts[t.wn][1][row] = rest;
-                parts[t.wn][2][row] = u;
-            }
+            for (int e = 0; e < 16; ++e) max = fmaxf(max, t.acc[i][j][e]);
+        max = fmaxf(max, __shfl_xor(max, 32));
+        Part part = part_of<ENT, false>(t, j, max, g.scale);
+        const bool far = fabsf(max) < INFINITY && fabsf(max) * g.scale > 1e37f;
+        if (__ballot(far)) {
+            const Part wide = part_of<ENT, true>(t, j, max, g.scale);
+            if (far) part = wide;                                 // (a row's bits do not depend on its neighbours)
         }
+        if (t.lane < 32) sh.parts[t.wm][t.row(j)] = part;
     }
     __syncthreads();
-    for (int row = threadIdx.x; row < BM; row += Tile::kThreads) {
-        if (m0 + row >= g.rows) break;
-        float max = parts[0][0][row], rest = parts[0][1][row], u = parts[0][2][row];
+    for (int row = threadIdx.x; row < ROWS; row += Tile::kThreads) {
+        if (row0 + row >= g.rows) break;
+        Part part = sh.parts[0][row];
 #pragma unroll
-        for (int w = 1; w < WN; ++w) {
-            // the part with the larger maximum keeps its rest; the other brings its maximum's own term along
-            const float m = parts[w][0][row], r = parts[w][1][row], v = parts[w][2][row];
-            const bool up = m > max;
-            const float big = up ? m : max, small = up ? max : m, r_big = up ? r : rest, r_small = up ? rest : r, u_small = up ? u : v;
-            const bool none = small == -INFINITY && r_small == 0.0f;
-            const float d = (fmaxf(small, -kTokFltMax) - fmaxf(big, -kTokFltMax)) * g.scale, f = none ? 0.0f : exp2_of(d), whole = 1.0f + r_small;
-            rest = r_big + (none ? 0.0f : f * whole);
-            u = (up ? v : u) + (f > 0.0f ? f * (u_small + d * whole) : 0.0f);
-            max = big;
-        }
-        g.partial[(m0 + row) * tiles.n + tn] = make_float4(max, rest, u, 0.0f);
+        for (int w = 1; w < PARTS; ++w) part = joined(part, sh.parts[w][row], g.scale);
+        g.partial[(row0 + row) * tiles.n + tc] = make_float4(part.max, part.rest, part.weighted, 0.0f);
     }
+}
+
+// Over the 32 lanes of a half of the wave; all of them get the result.
+__device__ __forceinline__ float half_sum(float x) {
+    x = group_sum<16>(x);
+    return x + __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(x), 0x401f));       // (lane ^ 16)
 }
 
 // ---- backward --------------------------------------------------------------------------------------------------------
 template <typename Tile>
 __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_adjoint_kernel(HeadArgs g, Tiles tiles) {
     typedef typename Tile::Element T;
-    constexpr int BM = Tile::kM, BN = Tile::kN, TM = Tile::TM, TN = Tile::TN, WM = Tile::kWavesM;
+    constexpr int ROWS = Tile::kN, COLUMNS = Tile::kM, TM = Tile::TM, TN = Tile::TN, WN = Tile::kWavesN;
     __shared__ struct {
         typename Tile::Shared stage[Tile::kStages];
-        Marks<BM, BN> marks;
-        float4 coefs[BM];
-        float sums[WM][BN];
+        Marks<ROWS, COLUMNS> marks;
+        float sums[WN][COLUMNS];
     } sh;
-    auto &marks = sh.marks;
-    auto &coefs = sh.coefs;
-    auto &sums = sh.sums;
-    int64_t tm, tn;
-    tiles.at(blockIdx.x, tm, tn);
-    const int64_t m0 = tm * BM, n0 = tn * BN;
+    int64_t tr, tc;
+    tiles.at(blockIdx.x, tr, tc);
+    const int64_t row0 = tr * ROWS, column0 = tc * COLUMNS;
     Tile t;
-    if (g.num_tokens) marks.make(g, m0, g.first + (int32_t)n0, threadIdx.x, Tile::kThreads);
-    for (int row = threadIdx.x; row < BM; row += Tile::kThreads) coefs[row] = m0 + row < g.rows ? g.coefs[m0 + row] : make_float4(INFINITY, 0, 0, 0);
-    t.run(g.hidden, g.weight, m0, n0, 0, Tile::stages(g.hidden), sh.stage);
+    if (g.num_tokens) sh.marks.make(g, row0, g.first + (int32_t)column0, threadIdx.x, Tile::kThreads);
+    t.run(g.weight, g.hidden, column0, row0, 0, Tile::stages(g.hidden), sh.stage);
+    if (some_bias<Tile>(g, column0)) add_bias(t, g, column0);
+    const bool last = column0 + COLUMNS > g.weight.rows;
     const float up = adjoint_scale(g.largest);
-    float bias[TN], sum[TN] = {};
+    // where the tile lies in the two arrays: a lane's own offset, and one that is the same for all lanes
+    const Stretch out = stretch_at(g.g ? static_cast<T*>(g.g) + row0 * g.g_columns + column0 : nullptr);
+    const Stretch across = stretch_at(g.g_across ? static_cast<T*>(g.g_across) + column0 * g.g_rows + row0 : nullptr);
+    const uint32_t wide = (uint32_t)(g.g_columns * sizeof(T)), high = (uint32_t)(g.g_rows * sizeof(T)), lower = 4 * (t.lane >> 5);
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-        const int64_t c = n0 + t.column(j);
-        bias[j] = c < g.weight.rows ? (g.bias ? g.bias[c] : 0.0f) : -INFINITY;
-    }
-    T *out = static_cast<T*>(g.g), *across = static_cast<T*>(g.g_across);
+        const int64_t r = row0 + t.row(j);
+        const float4 c = r < g.rows ? g.coefs[r] : make_float4(INFINITY, 0.0f, 0.0f, 0.0f);
+        const bool live = c.x < INFINITY;
+        const uint32_t at_out = g.g && r < g.rows ? t.row(j) * wide + lower * (uint32_t)sizeof(T) : kNoLane;
+        const uint32_t at_across = g.g_across && r < g.g_rows ? t.row(j) * (uint32_t)sizeof(T) + lower * high : kNoLane;
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
+        for (int i = 0; i < TM; ++i) {
+            const uint32_t block = (t.wm * TM + i) * 32;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            float d[TN][4];
+            for (int e = 0; e < 16; ++e) {
+                const float y = fmaf(t.acc[i][j][e] - c.x, g.scale, -c.y);
+                t.acc[i][j][e] = live ? exp2_of(y) * fmaf(c.w, fmaxf(y, -200.0f), c.z) : 0.0f;
+            }
+            if (g.num_tokens) {
+                const uint32_t mine = sh.marks.bits[t.row(j)][block / 32] >> lower;
+                if (__ballot((mine & 0x0f0f0f0fu) != 0)) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int row = t.row(i) + 8 * q + e;
-                const float4 c = coefs[row];
-                const bool live = c.x < INFINITY;
-#pragma unroll
-                for (int j = 0; j < TN; ++j) {
-                    const float x = bias[j] == -INFINITY ? -INFINITY : t.acc[i][j][4 * q + e] + bias[j];
-                    const float y = fmaf(x - c.x, g.scale, -c.y);
-                    d[j][e] = live ? exp2_of(y) * fmaf(c.w, fmaxf(y, -200.0f), c.z) : 0.0f;
-                    if (n0 + t.column(j) >= g.weight.rows) d[j][e] = 0.0f;
-                    if (g.num_tokens) {
-                        const int word = t.wn * TN + j, bit = t.lane & 31;
-                        if (marks.bits[row][word] >> bit & 1u) d[j][e] = g.entries[(m0 + row) * g.num_tokens + marks.place(row, word, bit)];
+                    for (int e = 0; e < 16; ++e) {
+                        const int bit = 8 * (e >> 2) + (e & 3);
+                        if (mine >> bit & 1u) t.acc[i][j][e] = g.entries[r * g.num_tokens + sh.marks.place(t.row(j), block / 32, bit + lower)];
                     }
-                    sum[j] += d[j][e];
                 }
             }
+            if (last) {                                           // (columns of no token: nothing, whatever the row holds)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                const int64_t c = n0 + t.column(j), r = m0 + t.row(i) + 8 * q;
-                if (c >= g.g_columns) continue;
-                float scaled[4];
+                for (int e = 0; e < 16; ++e)
+                    if (column0 + t.column(i) + 8 * (e >> 2) + (e & 3) >= g.weight.rows) t.acc[i][j][e] = 0.0f;
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (column0 + block + 8 * q >= g.g_columns) break;      // (a multiple of 8, as g_rows)
+                float d[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) d[e] = t.acc[i][j][4 * q + e] * up;
+                store_row<4, T>(out, at_out, (block + 8 * q) * (uint32_t)sizeof(T), d);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    scaled[e] = d[j][e] * up;
-                    if (out && r + e < g.rows) out[(r + e) * g.g_stride + c] = (T)scaled[e];
+                    const float one[1] = {d[e]};
+                    store_row<1, T>(across, at_across, (block + 8 * q + e) * high, one);
                 }
-                if (across && r < g.g_rows) store_elements<4>(across + c * g.g_across_stride + r, scaled);      // (g_rows is a multiple of 8)
             }
         }
     }
     if (g.bias_partial) {
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            sum[j] += __shfl_xor(sum[j], 32);
-            if (t.lane < 32) sums[t.wm][t.column(j)] = sum[j];
-        }
-        __syncthreads();
-        for (int c = threadIdx.x; c < BN; c += Tile::kThreads) {
-            float s = sums[0][c];
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int w = 1; w < WM; ++w) s += sums[w][c];
-            if (n0 + c < g.g_columns) g.bias_partial[tm * g.g_columns + n0 + c] = s;
+            for (int e = 0; e < 16; ++e) {
+                float sum = t.acc[i][0][e];
+#pragma unroll
+                for (int j = 1; j < TN; ++j) sum += t.acc[i][j][e];
+                sum = half_sum(sum);
+                if ((t.lane & 31) == 0) sh.sums[t.wn][t.column(i) + 8 * (e >> 2) + (e & 3)] = sum;
+            }
+        __syncthreads();
+        for (int c = threadIdx.x; c < COLUMNS; c += Tile::kThreads) {
+            float s = sh.sums[0][c];
+#pragma unroll
+            for (int w = 1; w < WN; ++w) s += sh.sums[w][c];
+            if (column0 + c < g.g_columns) g.bias_partial[tr * g.g_columns + column0 + c] = s;
         }
     }
 }
@@ -279,36 +315,55 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_pro
     const int which = blockIdx.x >= first_job;
     const ProductJob& job = g.job[which];
     int64_t id = blockIdx.x - (which ? first_job : 0);
-    const Tiles tiles{(job.rows + Tile::kM - 1) / Tile::kM, (job.columns + Tile::kN - 1) / Tile::kN};
+    const Tiles tiles{(job.rows + Tile::kN - 1) / Tile::kN, (job.columns + Tile::kM - 1) / Tile::kM};
     const int64_t all = tiles.m * tiles.n;
     const int32_t split = (int32_t)(id / all);
-    int64_t tm, tn;
-    tiles.at(id - split * all, tm, tn);
-    const int64_t m0 = tm * Tile::kM, n0 = tn * Tile::kN;
+    int64_t tr, tc;
+    tiles.at(id - split * all, tr, tc);
+    const int64_t row0 = tr * Tile::kN, column0 = tc * Tile::kM;
     const int64_t stages = Tile::stages(job.a);
     const int32_t from = (int32_t)(stages * split / job.splits), to = (int32_t)(stages * (split + 1) / job.splits);
     Tile t;
-    t.run(job.a, job.b, m0, n0, from, to, sh);
+    t.run(job.b, job.a, column0, row0, from, to, sh);
     const float down = 1.0f / adjoint_scale(g.largest);
+    const bool fours = job.columns % 4 == 0;
 #pragma unroll
-    for (int i = 0; i < Tile::TM; ++i)
+    for (int j = 0; j < Tile::TN; ++j) {
+        const int64_t r = row0 + t.row(j);
+        if (r >= job.rows) continue;
 #pragma unroll
-        for (int j = 0; j < Tile::TN; ++j) {
-            const int64_t c = n0 + t.column(j);
-            if (c >= job.columns) continue;
+        for (int i = 0; i < Tile::TM; ++i)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int64_t r = m0 + t.row(i) + (e >> 2) * 8 + (e & 3);
-                if (r >= job.rows) continue;
-                const float x = t.acc[i][j][e] * down;
-                if (job.out) {
-                    static_cast<T*>(job.out)[r * job.columns + c] = (T)x;
+            for (int q = 0; q < 4; ++q) {
+                const int64_t c = column0 + t.column(i) + 8 * q;
+                float x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = t.acc[i][j][4 * q + e] * down;
+                if (c >= job.columns) continue;
+                float* s = job.out ? nullptr : job.sums + ((int64_t)split * job.rows + r) * job.columns + c;
+                T* out = job.out ? static_cast<T*>(job.out) + r * job.columns + c : nullptr;
+                if (fours) {
+                    if (out) {
+                        store_elements<4>(out, x);
+                    } else {
+                        if (job.add) {
+                            float before[4];
+                            load_elements<4>(before, s);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) x[e] += before[e];
+                        }
+                        store_elements<4>(s, x);
+                    }
                 } else {
-                    float* s = job.sums + ((int64_t)split * job.rows + r) * job.columns + c;
-                    *s = job.add ? *s + x : x;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (c + e >= job.columns) break;
+                        if (out) out[e] = (T)x[e];
+                        else s[e] = job.add ? s[e] + x[e] : x[e];
+                    }
                 }
             }
-        }
+    }
 }
 
 // out[i] = sum over parts of from[part][i], in their order
@@ -341,7 +396,7 @@ template <typename T> __global__ void __launch_bounds__(256) head_pack_across_ke
 // ---- launches of a type, each type in a translation unit of its own -------------------------------------------------
 enum HeadTile : int { TILE_32, TILE_64, TILE_128, TILE_256 };
 struct TileSize {
-    int m, n;
+    int rows, columns;
 };
 constexpr TileSize kTileSizes[] = {{32, 128}, {64, 128}, {128, 128}, {256, 256}};
 

@@ -8,13 +8,13 @@
 
 namespace klay {
 
-template <typename T> using Tile32 = Tile<T, 32, 128, 1, 4, 3, 128>;
-template <typename T> using Tile64 = Tile<T, 64, 128, 1, 4, 3, 128>;
+template <typename T> using Tile32 = Tile<T, 128, 32, 4, 1, 3, 128>;
+template <typename T> using Tile64 = Tile<T, 128, 64, 4, 1, 3, 128>;
 template <typename T> using Tile128 = Tile<T, 128, 128, 2, 2, 2, 128>;
 template <typename T> using Tile256 = Tile<T, 256, 256, 2, 4, 2, 128>;
 
 template <typename Tile> Tiles tiles_of(int64_t rows, int64_t columns) {
-    return Tiles{(rows + Tile::kM - 1) / Tile::kM, (columns + Tile::kN - 1) / Tile::kN};
+    return Tiles{(rows + Tile::kN - 1) / Tile::kN, (columns + Tile::kM - 1) / Tile::kM};
 }
 inline uint32_t grid_of(int64_t items, int64_t each, int64_t most) { return (uint32_t)std::max<int64_t>(1, std::min((items + each - 1) / each, most)); }
 

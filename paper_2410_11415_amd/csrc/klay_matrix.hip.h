@@ -1,4 +1,4 @@
-// Products of matrices for the head of a network: C[m, n] = sum_k A[m, k] B[n, k], both operands with k next to each other, sums in fp32 by
+// Products of matrices for the head of a network: C[n, m] = sum_k A[m, k] B[n, k], both operands with k next to each other, sums in fp32 by
 // v_mfma_f32_32x32x16.  fp32 elements are three bf16 each on their way into the registers (a float's 24 bits are three times eight: hi + mid +
 // lo = x exactly between 2^-110 and 3.38e38), and of the nine products the six that reach fp32's precision are made; the dropped ones are below 2^-25
 // of hi x hi.
@@ -90,8 +90,9 @@ template <> struct Fragment<f32> {
     }
 };
 
-// A tile of BM x BN by WM x WN waves, S stages of SB bytes of k in shared memory; wave (wm, wn) has TM x TN blocks of 32 x 32 in registers.  Lane l of a block holds
-// column l % 32 and of it the rows 8 q + 4 (l / 32) + e as element 4 q + e.
+// A tile of BM columns x BN rows of the result by WM x WN waves, S stages of SB bytes of k in shared memory; wave (wm, wn) has TM x TN blocks of 32 x 32 in
+// registers.  Lane l of a block holds row l % 32 of the result and of it the columns 8 q + 4 (l / 32) + e as element 4 q + e, so that what is summed or
+// looked for along a row stays within a lane but for the other half of the wave.
 template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile {
     static constexpr int kM = BM, kN = BN, kWavesM = WM, kWavesN = WN, kWaves = WM * WN, kThreads = 64 * kWaves, kStages = S, kStageBytes = SB;
     static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
@@ -112,9 +113,9 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
         wm = wave / WN;
         wn = wave % WN;
     }
-    // of the tile: a lane's first row of block row i (the others: + 8 q + e), its column of block column j
-    __device__ __forceinline__ int row(int i) const { return (wm * TM + i) * 32 + 4 * (lane >> 5); }
-    __device__ __forceinline__ int column(int j) const { return (wn * TN + j) * 32 + (lane & 31); }
+    // of the tile: a lane's first column of the i-th blocks (the others: + 8 q + e), its row of the j-th
+    __device__ __forceinline__ int column(int i) const { return (wm * TM + i) * 32 + 4 * (lane >> 5); }
+    __device__ __forceinline__ int row(int j) const { return (wn * TN + j) * 32 + (lane & 31); }
 
     // What a matrix instruction of each block takes: sixteen k's.
     struct Fragments {
