@@ -449,9 +449,9 @@ klay_status klay_head_backward(const klay_head_args* args, const void* kept, con
  *               gives NaN; of a token listed more than once the q add up in the gradient
  *   teacher     logits: device fp32 [rows, num_tokens], placed by rows and stride (elements); 0.001 <= temperature <= 1000
  *   loss        device [rows] fp32
- *   kept        as for klay_head_forward, for klay_distill_backward
+ *   kept        as for klay_head_forward, for klay_distill_backward, and the call's own workspace: required
  * A row that lists nothing has loss 0 and no gradient.  A listed token that is not allowed and that the teacher gives mass to: +inf.  A NaN or +inf,
- * of a logit or of the teacher's, makes the loss of its row NaN.  No workspace.  Errors: as klay_tokens_forward.
+ * of a logit or of the teacher's, makes the loss of its row NaN.  Errors: as klay_tokens_forward.
  */
 typedef struct klay_teacher {
     const float* logits;

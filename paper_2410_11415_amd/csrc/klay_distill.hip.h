@@ -10,7 +10,8 @@ namespace klay {
 struct DistillArgs {
     const void* logits;
     RowMap logit_rows;
-    ListArgs list;                          // its sorted, slots: where they are kept, or null
+    ListArgs list;                          // its sorted, slots: where they are kept
+    float* sums;                            // [rows, kRowFloats]: of a row what the run over it leaves
     float scale;                            // log2 e / T
     TeachArgs teach;                        // moved: as sorted
     // backward
@@ -36,20 +37,38 @@ struct MassRun {
     }
 };
 
-constexpr int kChunk = 32;                  // vectors of a thread whose bits are held at a time
+constexpr int kChunk = 64;                  // vectors of a thread whose bits are held at a time
 
-template <typename T, int THREADS>
-__global__ void __launch_bounds__(THREADS) distill_row_kernel(DistillArgs g) {
+// Few rows: a workgroup of sixteen waves each, whose first one puts the row together (FINISH).  Many: four waves each, which leave a row's sums, and a wave a
+// row afterwards, since the 64-bit arithmetic takes twice the registers of the run over the row (4096 x 131072 bf16 in one / in two: 334 / @@ us).
+template <typename T, int THREADS, bool FINISH>
+__global__ void __launch_bounds__(THREADS, FINISH ? 4 : 6) distill_row_kernel(DistillArgs g) {
     constexpr int N = 16 / sizeof(T), U = 4;
     __shared__ int32_t mark[kMaxListed], sorted[kMaxListed], slots[kMaxListed];
     __shared__ float listed[kMaxListed];
-    __shared__ uint32_t skip[THREADS];
+    __shared__ uint64_t skip[THREADS];
     __shared__ float scratch[6 * kScratch];
     const int32_t tid = threadIdx.x, K = g.list.num_tokens, vocab = g.list.vocab;
     for (int64_t r = blockIdx.x; r < g.list.rows; r += gridDim.x) {
         const T* row = static_cast<const T*>(g.logits) + g.logit_rows.at(r);
-        make_list(g.list, r, true, tid, THREADS, mark, sorted, slots);
-        for (int32_t u = tid; u < K; u += THREADS) listed[u] = sorted[u] < kNoToken ? (float)row[sorted[u]] : 0.0f;
+        if (K <= 64) {
+            if (tid < 64) {
+                bool first;
+                const int32_t token = tid < K ? token_of(g.list, r, tid) : kNothing, slot = slot_in_wave(token, K, first);
+                if (tid < K) {
+                    slots[tid] = slot;
+                    sorted[tid] = kNoToken;
+                    if (first) {
+                        sorted[slot] = token;
+                        listed[slot] = (float)row[token];
+                    }
+                }
+            }
+            __syncthreads();
+        } else {
+            make_list(g.list, r, true, tid, THREADS, mark, sorted, slots);
+            for (int32_t u = tid; u < K; u += THREADS) listed[u] = sorted[u] < kNoToken ? (float)row[sorted[u]] : 0.0f;
+        }
         const Share<N, THREADS> share(row, 0, vocab);
         MassRun run;
         auto single = [&](int32_t j) {
@@ -66,36 +85,48 @@ __global__ void __launch_bounds__(THREADS) distill_row_kernel(DistillArgs g) {
         if (tid < share.head()) single(share.lo + tid);
         if (tid < share.tail()) single(share.full + tid);
         for (int32_t c0 = 0; c0 * THREADS < share.vectors; c0 += kChunk) {
+            const int32_t left = share.vectors - c0 * THREADS - tid, rounds = left <= 0 ? 0 : (left + THREADS - 1) / THREADS;
+            const int32_t count = rounds < kChunk ? rounds : kChunk;
+            Raw<T, N> next[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (u < count) next[u] = stream_raw<N>(row + share.at(c0 + u, tid));
             skip[tid] = 0;
             __syncthreads();
             for (int32_t u = tid; u < K; u += THREADS) {
                 const int32_t j = sorted[u];
                 if (j == kNoToken || !share.in_vector(j)) continue;
                 const int32_t v = (j - share.begin) / N - c0 * THREADS;
-                if (v >= 0 && v < kChunk * THREADS) atomicOr(&skip[v % THREADS], 1u << (v / THREADS));
+                if (v >= 0 && v < kChunk * THREADS)
+                    atomicOr(reinterpret_cast<unsigned long long*>(&skip[v % THREADS]), 1ull << (v / THREADS));
             }
             __syncthreads();
-            const uint32_t out = skip[tid];
-            const int32_t left = share.vectors - c0 * THREADS - tid, count = left <= 0 ? 0 : (left + THREADS - 1) / THREADS < kChunk ? (left + THREADS - 1) / THREADS : kChunk;
-            Raw<T, N> next[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (u < count) next[u] = stream_raw<N>(row + share.at(c0 + u, tid));
-            for (int32_t i = 0; i < count; i += U) {
+            const uint64_t out = skip[tid];
+            int32_t i = 0;
+            // whole steps of U vectors, the next step's on their way meanwhile
+            for (; i + U <= count; i += U) {
                 Raw<T, N> now[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) now[u] = next[u];
 #pragma unroll
                 for (int u = 0; u < U; ++u)
                     if (i + U + u < count) next[u] = stream_raw<N>(row + share.at(c0 + i + U + u, tid));
+                const uint32_t skipped = (uint32_t)(out >> i) & ((1u << U) - 1u);
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    if (i + u >= count || (out >> (i + u) & 1u)) continue;
                     float x[N];
 #pragma unroll
                     for (int q = 0; q < N; ++q) x[q] = piece<N, T>(now[u], q);
-                    run.take(x, g.scale);
+                    if (!(skipped >> u & 1u)) run.take(x, g.scale);
                 }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (i + u >= count || (out >> (i + u) & 1ull)) continue;
+                float x[N];
+#pragma unroll
+                for (int q = 0; q < N; ++q) x[q] = piece<N, T>(next[u], q);
+                run.take(x, g.scale);
             }
             __syncthreads();                // the bits are read
         }
@@ -106,11 +137,13 @@ __global__ void __launch_bounds__(THREADS) distill_row_kernel(DistillArgs g) {
             const int32_t v = (j - share.begin) / N;
             if (u > 0 && share.in_vector(sorted[u - 1]) && (sorted[u - 1] - share.begin) / N == v) continue;
             int32_t at = u;
+            float x[N];
+            load_elements<N>(x, row + share.begin + v * N);
+#pragma unroll
             for (int q = 0; q < N; ++q) {
-                const int32_t e = share.begin + v * N + q;
-                if (at < K && sorted[at] == e) { ++at; continue; }
-                const float x[1] = {(float)row[e]};
-                run.take(x, g.scale);
+                if (at < K && sorted[at] == share.begin + v * N + q) { ++at; continue; }
+                const float one[1] = {x[q]};
+                run.take(one, g.scale);
             }
         }
         Others o;
@@ -120,20 +153,38 @@ __global__ void __launch_bounds__(THREADS) distill_row_kernel(DistillArgs g) {
         if (s > 0.0f) s *= exp2_of((run.ref - to) * g.scale);
         block_sum2<THREADS>(s, none, scratch + kScratch);
         o.sum = s;
-        if (tid < 64) finish_distill(g.teach, r, K, sorted, slots, listed, o);
-        if (g.list.sorted)
-            for (int32_t u = tid; u < K; u += THREADS) g.list.sorted[r * K + u] = sorted[u];
+        if constexpr (FINISH) {
+            if (tid < 64) finish_distill(g.teach, r, K, sorted, slots, listed, o);
+        } else {
+            if (tid == 0) {
+                g.sums[r * kRowFloats] = o.max;
+                g.sums[r * kRowFloats + 1] = s;
+            }
+            for (int32_t u = tid; u < K; u += THREADS) {
+                g.list.slots[r * K + u] = slots[u];
+                g.teach.moved[r * K + u] = listed[u];
+            }
+        }
+        for (int32_t u = tid; u < K; u += THREADS) g.list.sorted[r * K + u] = sorted[u];
         __syncthreads();                    // shared memory is free again
     }
 }
+__global__ void __launch_bounds__(256) distill_finish_kernel(DistillArgs g) {
+    const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), at = r * g.list.num_tokens;
+    if (r >= g.list.rows) return;
+    Others o;
+    o.max = g.sums[r * kRowFloats];
+    o.sum = g.sums[r * kRowFloats + 1];
+    finish_distill(g.teach, r, g.list.num_tokens, g.list.sorted + at, g.list.slots + at, g.teach.moved + at, o);
+}
 
-// Rows of at most 512: a wave each, the logits in its registers.
+// Rows of at most 512: a wave each, the logits in its registers; lists of at most LISTED.
 constexpr int kShortDistill = 512;
-template <typename T>
+template <typename T, int LISTED>
 __global__ void __launch_bounds__(256) distill_short_kernel(DistillArgs g) {
     constexpr int E = kShortDistill / 64;
-    __shared__ int32_t mark[4][kMaxListed], sorted[4][kMaxListed], slots[4][kMaxListed];
-    __shared__ float listed[4][kMaxListed];
+    __shared__ int32_t mark[4][LISTED], sorted[4][LISTED], slots[4][LISTED];
+    __shared__ float listed[4][LISTED];
     __shared__ uint32_t bits[4][kShortDistill / 32];
     const int w = threadIdx.x >> 6;
     const int32_t lane = threadIdx.x & 63, K = g.list.num_tokens;
@@ -144,7 +195,19 @@ __global__ void __launch_bounds__(256) distill_short_kernel(DistillArgs g) {
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] = there && lane + 64 * e < g.list.vocab ? (float)row[lane + 64 * e] : -INFINITY;
     if (lane < kShortDistill / 32) bits[w][lane] = 0;
-    make_list(g.list, r, there, lane, 64, mark[w], sorted[w], slots[w]);
+    if constexpr (LISTED <= 64) {
+        bool first;
+        const int32_t token = there && lane < K ? token_of(g.list, r, lane) : kNothing, slot = slot_in_wave(token, K, first);
+        if (lane < K) {
+            slots[w][lane] = slot;
+            sorted[w][lane] = kNoToken;
+        }
+        __syncthreads();
+        if (first) sorted[w][slot] = token;
+        __syncthreads();
+    } else {
+        make_list(g.list, r, there, lane, 64, mark[w], sorted[w], slots[w]);
+    }
     for (int32_t u = lane; u < K; u += 64) {
         const int32_t j = sorted[w][u];
         if (j == kNoToken) continue;
@@ -167,8 +230,7 @@ __global__ void __launch_bounds__(256) distill_short_kernel(DistillArgs g) {
     for (int e = 0; e < E; ++e) s += exp2_of((x[e] - to) * g.scale);
     o.sum = group_sum<64>(s);
     finish_distill(g.teach, r, K, sorted[w], slots[w], listed[w], o);
-    if (g.list.sorted)
-        for (int32_t u = lane; u < K; u += 64) g.list.sorted[r * K + u] = sorted[w][u];
+    for (int32_t u = lane; u < K; u += 64) g.list.sorted[r * K + u] = sorted[w][u];
 }
 
 // dx_j = A s_j, then the listed tokens' entries.  A workgroup a row part.

@@ -93,22 +93,28 @@ bool direct(const void* p, const klay_rows& rows, int64_t count, int64_t width, 
     return rows.inner >= count && rows.inner_stride >= 0 && rows.inner_stride % s.lot == 0 && rows.inner_stride * s.bytes <= klay::kMostStride;
 }
 
+// The largest tile of which there are three for four CUs; the smaller ones only where there are rows for more than one.
 klay::HeadTile logits_tile(int64_t rows, int64_t columns) {
-    if (rows <= 32) return klay::TILE_32;
-    if (rows <= 64) return klay::TILE_64;
-    return rows > 128 && tiles(rows, 256) * tiles(columns, 256) >= 192 ? klay::TILE_256 : klay::TILE_128;
+    const auto count = [&](klay::HeadTile t) { return tiles(rows, klay::kTileSizes[t].rows) * tiles(columns, klay::kTileSizes[t].columns); };
+    for (klay::HeadTile t : {klay::TILE_256, klay::TILE_128, klay::TILE_64})
+        if (rows > klay::kTileSizes[t].rows / 2 && count(t) >= 192) return t;
+    return rows > 32 && count(klay::TILE_32) > 4 * klay::kComputeUnits ? klay::TILE_64 : klay::TILE_32;
 }
 
 struct ProductPlan {
     klay::HeadTile tile;
     int32_t splits;
 };
+// The largest tile of which there are as many as CUs, its stages shared out where need be, at least eight each.
 ProductPlan product_plan(int64_t rows, int64_t columns, int64_t stages) {
     ProductPlan p;
     const auto count = [&](klay::HeadTile t) { return tiles(rows, klay::kTileSizes[t].rows) * tiles(columns, klay::kTileSizes[t].columns); };
-    p.tile = rows <= 32 ? klay::TILE_32 : rows <= 64 ? klay::TILE_64 : rows > 128 && columns > 128 && count(klay::TILE_256) >= 192 ? klay::TILE_256 : klay::TILE_128;
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(stages / 8, 32));
+    if (rows <= 32) p.tile = klay::TILE_32;
+    else if (rows <= 64) p.tile = klay::TILE_64;
+    else p.tile = rows > 128 && columns > 128 && count(klay::TILE_256) * std::min<int64_t>(most, 8) >= 192 ? klay::TILE_256 : klay::TILE_128;
     const int64_t want = p.tile == klay::TILE_256 ? klay::kComputeUnits : 2 * klay::kComputeUnits;
-    p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({want / count(p.tile), stages / 4, 32}));
+    p.splits = (int32_t)std::max<int64_t>(1, std::min(want / count(p.tile), most));
     return p;
 }
 
@@ -122,7 +128,7 @@ struct HeadPlan {
     int64_t row_block = 0, tiles_n = 0;
     klay::HeadTile tile = klay::TILE_32;
     // backward
-    int64_t piece = 0, g_rows = 0;
+    int64_t piece = 0, g_rows = 0, wide = 0;       // wide: width up to a multiple of 4, as the products' sums are stored
     ProductPlan dh{}, dw{};
     // bytes from the start of the workspace
     size_t hidden = 0, weight = 0, partial = 0, kept = 0, coefs = 0, entries = 0, largest = 0, g = 0, g_across = 0, w_across = 0, h_across = 0,
@@ -167,8 +173,9 @@ HeadPlan head_plan(const klay_head_args* a, bool back) {
         p.h_across = take(a->width * p.g_rows * s.bytes);
         p.dh = product_plan(a->rows, a->width, stages_of(columns, s));
         p.dw = product_plan(std::min<int64_t>(p.piece, a->vocab), a->width, stages_of(p.g_rows, s));
-        p.dh_sums = take(p.dh.splits * a->rows * a->width * 4);
-        p.dw_sums = take(p.dw.splits == 1 ? 0 : p.dw.splits * columns * a->width * 4);
+        p.wide = up(a->width, 4);
+        p.dh_sums = take(p.dh.splits * a->rows * p.wide * 4);
+        p.dw_sums = take(p.dw.splits == 1 && p.wide == a->width ? 0 : p.dw.splits * columns * p.wide * 4);
         p.db_sums = take(tiles(p.g_rows, klay::kTileSizes[p.tile].rows) * columns * 4);
     }
     p.bytes = at;
@@ -367,11 +374,12 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
             j.splits = (int32_t)std::min<int64_t>(p.dh.splits, stages_of(columns, s));
             j.rows = a->rows;
             j.columns = a->width;
-            j.out = whole && j.splits == 1 ? dhidden : nullptr;
+            j.wide = p.wide;
+            j.out = whole && j.splits == 1 && p.wide == a->width ? dhidden : nullptr;
             j.sums = static_cast<float*>(in(workspace, p.dh_sums));
             j.add = first > 0;
             if (first + p.piece >= a->vocab && !j.out)
-                sums.sum[sums.sums++] = klay::SumArgs{j.sums, a->rows * a->width, a->rows * a->width, whole ? j.splits : p.dh.splits, 1, dhidden};
+                sums.sum[sums.sums++] = klay::SumArgs{j.sums, a->rows, a->width, p.wide, a->rows * p.wide, whole ? j.splits : p.dh.splits, 1, dhidden};
         }
         if (dweight) {
             klay::ProductJob& j = jobs[n];
@@ -381,14 +389,15 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
             j.splits = p.dw.splits;
             j.rows = count;
             j.columns = a->width;
+            j.wide = p.wide;
             void* out = static_cast<char*>(dweight) + first * a->width * s.bytes;
-            j.out = j.splits == 1 ? out : nullptr;
+            j.out = j.splits == 1 && p.wide == a->width ? out : nullptr;
             j.sums = static_cast<float*>(in(workspace, p.dw_sums));
             j.add = 0;
-            if (!j.out) sums.sum[sums.sums++] = klay::SumArgs{j.sums, count * a->width, count * a->width, j.splits, 1, out};
+            if (!j.out) sums.sum[sums.sums++] = klay::SumArgs{j.sums, count, a->width, p.wide, count * p.wide, j.splits, 1, out};
         }
         if (dbias)
-            sums.sum[sums.sums++] = klay::SumArgs{g.bias_partial, count, columns, (int32_t)tiles(std::max(a->rows, dweight ? p.g_rows : 0), klay::kTileSizes[p.tile].rows), 0, dbias + first};
+            sums.sum[sums.sums++] = klay::SumArgs{g.bias_partial, 1, count, count, columns, (int32_t)tiles(std::max(a->rows, dweight ? p.g_rows : 0), klay::kTileSizes[p.tile].rows), 0, dbias + first};
         for (int i = 0; i < n;) {
             klay::ProductArgs pr{};
             pr.largest = ad.largest;
@@ -449,10 +458,16 @@ klay::DistillArgs distill_args(const klay_tokens_args* a, const klay_teacher* t)
     return g;
 }
 template <typename T> klay_status run_distill(const klay::DistillArgs& g, void* stream) {
-    const dim3 grid(capped_grid(g.list.rows));
-    if (g.list.vocab <= klay::kShortDistill) KLAY_LAUNCH((klay::distill_short_kernel<T>), dim3((uint32_t)tiles(g.list.rows, 4)), dim3(256), stream, g);
-    else if (g.list.rows >= kManyRows) KLAY_LAUNCH((klay::distill_row_kernel<T, 256>), grid, dim3(256), stream, g);
-    else KLAY_LAUNCH((klay::distill_row_kernel<T, 1024>), grid, dim3(1024), stream, g);
+    const dim3 grid(capped_grid(g.list.rows)), waves((uint32_t)tiles(g.list.rows, 4));
+    if (g.list.vocab <= klay::kShortDistill) {
+        if (g.list.num_tokens <= 64) KLAY_LAUNCH((klay::distill_short_kernel<T, 64>), waves, dim3(256), stream, g);
+        else KLAY_LAUNCH((klay::distill_short_kernel<T, klay::kMaxListed>), waves, dim3(256), stream, g);
+    } else if (g.list.rows >= kManyRows) {
+        KLAY_LAUNCH((klay::distill_row_kernel<T, 256, false>), grid, dim3(256), stream, g);
+        KLAY_LAUNCH(klay::distill_finish_kernel, waves, dim3(256), stream, g);
+    } else {
+        KLAY_LAUNCH((klay::distill_row_kernel<T, 1024, true>), grid, dim3(1024), stream, g);
+    }
     return KLAY_OK;
 }
 template <typename T> klay_status run_distill_back(klay::DistillArgs g, void* stream) {
@@ -527,16 +542,15 @@ klay_status klay_head_distill_backward(const klay_head_args* a, const klay_teach
 klay_status klay_distill_forward(const klay_tokens_args* a, const klay_teacher* teacher, float* loss, void* kept, void* stream) try {
     KLAY_DO(check_distill(a, teacher, "klay_distill_forward"));
     if (a->rows == 0) return KLAY_OK;
-    if (!loss) return report(KLAY_EINVAL, "klay_distill_forward: null argument");
+    if (!loss || !kept) return report(KLAY_EINVAL, "klay_distill_forward: null argument");
     if (reinterpret_cast<uintptr_t>(kept) % 16) return report(KLAY_EINVAL, "klay_distill_forward: kept must be 16-byte aligned");
     klay::DistillArgs g = distill_args(a, teacher);
     g.teach.loss = loss;
-    if (kept) {
-        const Kept k = kept_at(kept, a->rows, a->num_tokens);
-        g.teach.stats = k.stats;
-        g.teach.moved = k.values;
-        g.list.sorted = k.sorted;
-    }
+    const Kept k = kept_at(kept, a->rows, a->num_tokens);
+    g.teach.stats = g.sums = k.stats;
+    g.teach.moved = k.values;
+    g.list.sorted = k.sorted;
+    g.list.slots = k.slots;
     klay::OnDevice on(a->device);
     if (on.status != hipSuccess) return report(KLAY_EHIP, std::string("klay_distill_forward: ") + hipGetErrorString(on.status));
     if (a->dtype == KLAY_F32) return run_distill<klay::f32>(g, stream);

@@ -38,9 +38,9 @@ struct HeadArgs {
 struct ProductJob {
     Operand a, b;
     int32_t splits;
-    int64_t rows, columns;
-    void* out;                              // [rows, columns], or null
-    float* sums;                            // [splits, rows, columns]
+    int64_t rows, columns, wide;            // wide: columns, up to a multiple of 4
+    void* out;                              // [rows, wide], or null
+    float* sums;                            // [splits, rows, wide]
     int32_t add;                            // to what is there
 };
 struct ProductArgs {
@@ -63,20 +63,38 @@ template <int ROWS, int COLUMNS> struct Marks {
     static constexpr int kWords = COLUMNS / 32;
     uint32_t bits[ROWS][kWords];
     int32_t first[ROWS];
+    // Short lists entry by entry, all loads at once; long ones row by row, from where a search finds the tile's first.  (Every thread comes here: barriers.)
     __device__ __forceinline__ void make(const HeadArgs& g, int64_t row0, int32_t token0, int32_t thread, int32_t threads) {
+        const int32_t K = g.num_tokens;
         for (int i = thread; i < ROWS; i += threads) {
 #pragma unroll
             for (int w = 0; w < kWords; ++w) bits[i][w] = 0;
-            if (row0 + i >= g.rows) continue;
-            const int32_t* list = g.sorted + (row0 + i) * g.num_tokens;
-            int32_t lo = 0, hi = g.num_tokens;
+            first[i] = INT32_MAX;
+        }
+        __syncthreads();
+        const int32_t rows = g.rows - row0 < ROWS ? (int32_t)(g.rows - row0) : ROWS;
+        const int32_t* lists = g.sorted + row0 * K;
+        if (K <= 8) {
+#pragma unroll 4
+            for (int32_t n = thread; n < rows * K; n += threads) {
+                const uint32_t c = (uint32_t)lists[n] - (uint32_t)token0;
+                if (c >= (uint32_t)COLUMNS) continue;
+                const int32_t i = n / K;
+                atomicOr(&bits[i][c >> 5], 1u << (c & 31));
+                atomicMin(&first[i], n - i * K);
+            }
+            return;
+        }
+        for (int i = thread; i < rows; i += threads) {
+            const int32_t* list = lists + (int64_t)i * K;
+            int32_t lo = 0, hi = K;
             while (lo < hi) {
                 const int32_t mid = (lo + hi) >> 1;
                 if (list[mid] < token0) lo = mid + 1;
                 else hi = mid;
             }
             first[i] = lo;
-            for (; lo < g.num_tokens; ++lo) {
+            for (; lo < K; ++lo) {
                 const uint32_t c = (uint32_t)list[lo] - (uint32_t)token0;
                 if (c >= (uint32_t)COLUMNS) break;
                 bits[i][c >> 5] |= 1u << (c & 31);
@@ -179,8 +197,9 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_for
     tiles.at(blockIdx.x, tr, tc);
     const int64_t row0 = tr * ROWS, column0 = tc * COLUMNS;
     Tile t;
-    if (g.num_tokens) sh.marks.make(g, row0, g.first + (int32_t)column0, threadIdx.x, Tile::kThreads);
-    t.run(g.weight, g.hidden, column0, row0, 0, Tile::stages(g.hidden), sh.stage);           // (its barriers are behind the marks, too)
+    t.run(g.weight, g.hidden, column0, row0, 0, Tile::stages(g.hidden), sh.stage, [&] {
+        if (g.num_tokens) sh.marks.make(g, row0, g.first + (int32_t)column0, threadIdx.x, Tile::kThreads);
+    });
     if (some_bias<Tile>(g, column0)) add_bias(t, g, column0);
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
@@ -233,8 +252,9 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_adj
     tiles.at(blockIdx.x, tr, tc);
     const int64_t row0 = tr * ROWS, column0 = tc * COLUMNS;
     Tile t;
-    if (g.num_tokens) sh.marks.make(g, row0, g.first + (int32_t)column0, threadIdx.x, Tile::kThreads);
-    t.run(g.weight, g.hidden, column0, row0, 0, Tile::stages(g.hidden), sh.stage);
+    t.run(g.weight, g.hidden, column0, row0, 0, Tile::stages(g.hidden), sh.stage, [&] {
+        if (g.num_tokens) sh.marks.make(g, row0, g.first + (int32_t)column0, threadIdx.x, Tile::kThreads);
+    });
     if (some_bias<Tile>(g, column0)) add_bias(t, g, column0);
     const bool last = column0 + COLUMNS > g.weight.rows;
     const float up = adjoint_scale(g.largest);
@@ -324,9 +344,8 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_pro
     const int64_t stages = Tile::stages(job.a);
     const int32_t from = (int32_t)(stages * split / job.splits), to = (int32_t)(stages * (split + 1) / job.splits);
     Tile t;
-    t.run(job.b, job.a, column0, row0, from, to, sh);
+    t.run(job.b, job.a, column0, row0, from, to, sh, [] {});
     const float down = 1.0f / adjoint_scale(g.largest);
-    const bool fours = job.columns % 4 == 0;
 #pragma unroll
     for (int j = 0; j < Tile::TN; ++j) {
         const int64_t r = row0 + t.row(j);
@@ -336,40 +355,30 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_pro
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int64_t c = column0 + t.column(i) + 8 * q;
+                if (c >= job.wide) continue;                      // (a multiple of 4)
                 float x[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[e] = t.acc[i][j][4 * q + e] * down;
-                if (c >= job.columns) continue;
-                float* s = job.out ? nullptr : job.sums + ((int64_t)split * job.rows + r) * job.columns + c;
-                T* out = job.out ? static_cast<T*>(job.out) + r * job.columns + c : nullptr;
-                if (fours) {
-                    if (out) {
-                        store_elements<4>(out, x);
-                    } else {
-                        if (job.add) {
-                            float before[4];
-                            load_elements<4>(before, s);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) x[e] += before[e];
-                        }
-                        store_elements<4>(s, x);
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (c + e >= job.columns) break;
-                        if (out) out[e] = (T)x[e];
-                        else s[e] = job.add ? s[e] + x[e] : x[e];
-                    }
+                if (job.out) {
+                    store_elements<4>(static_cast<T*>(job.out) + r * job.wide + c, x);
+                    continue;
                 }
+                float* s = job.sums + ((int64_t)split * job.rows + r) * job.wide + c;
+                if (job.add) {
+                    float before[4];
+                    load_elements<4>(before, s);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] += before[e];
+                }
+                store_elements<4>(s, x);
             }
     }
 }
 
-// out[i] = sum over parts of from[part][i], in their order
+// out[row][column] = sum over parts of from[part][row][column], in their order; rows of `from` are `wide` apart
 struct SumArgs {
     const float* from;
-    int64_t count, apart;
+    int64_t rows, columns, wide, apart;
     int32_t parts, typed;                   // typed: out is of the operands' type, otherwise fp32
     void* out;
 };
@@ -381,9 +390,21 @@ template <typename T>
 __global__ void __launch_bounds__(256) head_sums_kernel(SumsArgs g) {
     for (int s = 0; s < g.sums; ++s) {
         const SumArgs& a = g.sum[s];
-        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.count; i += (int64_t)gridDim.x * 256) {
-            float x = a.from[i];
-            for (int32_t p = 1; p < a.parts; ++p) x += a.from[p * a.apart + i];
+        const int64_t all = a.rows * a.columns;
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+            int64_t at = i;
+            if (a.wide != a.columns) {
+                const int64_t r = i / a.columns;
+                at = r * a.wide + (i - r * a.columns);
+            }
+            float x = a.from[at];
+            for (int32_t p = 1; p < a.parts; p += 8) {
+                float y[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) y[q] = p + q < a.parts ? a.from[(p + q) * a.apart + at] : 0.0f;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) x += y[q];
+            }
             if (a.typed) static_cast<T*>(a.out)[i] = (T)x;
             else static_cast<float*>(a.out)[i] = x;
         }

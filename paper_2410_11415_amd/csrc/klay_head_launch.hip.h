@@ -67,7 +67,7 @@ template <typename T> klay_status HeadLaunch<T>::products(HeadTile tile, const P
 }
 template <typename T> klay_status HeadLaunch<T>::sums(const SumsArgs& g, void* stream) {
     int64_t most = 0;
-    for (int i = 0; i < g.sums; ++i) most = std::max<int64_t>(most, g.sum[i].count);
+    for (int i = 0; i < g.sums; ++i) most = std::max<int64_t>(most, g.sum[i].rows * g.sum[i].columns);
     if (most > 0) KLAY_LAUNCH((head_sums_kernel<T>), dim3(grid_of(most, 256, 8192)), dim3(256), stream, g);
     return KLAY_OK;
 }

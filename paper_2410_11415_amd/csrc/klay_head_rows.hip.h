@@ -5,35 +5,26 @@
 
 namespace klay {
 
-// The tiles' sums of a row, by a wave.  `scale` = log2 e / T.
+// The tiles' sums of a row, by a wave: a lane's tiles one after the other, four loads on their way, then the lanes pair by pair.  `scale` = log2 e / T.
 __device__ __forceinline__ Others join_tiles(const float4* partial, int64_t tiles, float scale) {
     const int32_t lane = threadIdx.x & 63;
-    float max = -INFINITY;
-    for (int64_t i = lane; i < tiles; i += 64) max = fmaxf(max, partial[i].x);
-    const float mine_max = max;
-    max = wave_max(max);
-    Others o;
-    o.max = max;
-    const float to = fmaxf(max, -kTokFltMax);
-    double sum = 0.0, rest = 0.0, weighted = 0.0;
-    int32_t owner = 1 << 30;
-    if (mine_max == max)
-        for (int64_t i = lane; i < tiles; i += 64)
-            if (partial[i].x == max) { owner = (int32_t)i; break; }
-    owner = wave_min(owner);
-    for (int64_t i = lane; i < tiles; i += 64) {
-        const float4 p = partial[i];
-        if (p.x == -INFINITY && p.y == 0.0f) continue;
-        const float y = (fmaxf(p.x, -kTokFltMax) - to) * scale, f = exp2_of(y);
-        const double whole = 1.0 + (double)p.y;
-        sum += f * whole;
-        rest += i == owner ? (double)p.y : f * whole;
-        if (f > 0.0f) weighted += f * ((double)p.z + y * whole);
-        if (p.y != p.y) sum = rest = p.y;
+    Part mine{-INFINITY, 0.0f, 0.0f};
+    for (int64_t i = lane; i < tiles; i += 256) {
+        float4 p[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) p[u] = i + 64 * u < tiles ? partial[i + 64 * u] : make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) mine = joined(mine, Part{p[u].x, p[u].y, p[u].z}, scale);
     }
-    o.sum = wave_sum(sum);
-    o.rest = wave_sum(rest);
-    o.weighted = wave_sum(weighted) * 0.693147180559945309;      // (the tiles' are in powers of two)
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1)
+        mine = joined(mine, Part{__shfl_xor(mine.max, d), __shfl_xor(mine.rest, d), __shfl_xor(mine.weighted, d)}, scale);
+    Others o;
+    o.max = lane_of(mine.max, 0);                                // (lanes that joined equal maxima in another order may differ in the last bit)
+    const double rest = lane_of(mine.rest, 0);
+    o.sum = o.max == -INFINITY && rest == 0.0 ? 0.0 : 1.0 + rest;
+    o.rest = rest;
+    o.weighted = lane_of(mine.weighted, 0) * 0.693147180559945309;       // (the tiles' are in powers of two)
     return o;
 }
 
@@ -63,6 +54,19 @@ __global__ void __launch_bounds__(256) head_lists_kernel(ListArgs g) {
     __shared__ int32_t mark[4][kMaxListed], sorted[4][kMaxListed], slots[4][kMaxListed];
     const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int64_t r = (int64_t)blockIdx.x * 4 + w;
+    if (g.num_tokens <= 64) {
+        if (r >= g.rows) return;
+        const int64_t at = r * g.num_tokens;
+        bool first;
+        const int32_t token = lane < g.num_tokens ? token_of(g, r, lane) : kNothing, slot = slot_in_wave(token, g.num_tokens, first);
+        const int32_t many = __popcll(__ballot(first));
+        if (lane < g.num_tokens) {
+            g.slots[at + lane] = slot;
+            if (first) g.sorted[at + slot] = token;
+            if (lane >= many) g.sorted[at + lane] = kNoToken;
+        }
+        return;
+    }
     make_list(g, r, r < g.rows, lane, 64, mark[w], sorted[w], slots[w]);
     if (r >= g.rows) return;
     for (int32_t k = lane; k < g.num_tokens; k += 64) {
@@ -117,8 +121,19 @@ __global__ void __launch_bounds__(256) head_logprobs_adjoint_kernel(AdjointArgs 
         if (lane == 0) g.coefs[r] = make_float4(INFINITY, 0.0f, 0.0f, 0.0f);
         return;
     }
+    // the entries of a token added up; of at most 64 entries from the lanes that hold them (all lanes ask together)
+    const int32_t slot0 = lane < K ? slots[lane] : kNothing;
+    const float g0 = dlogp && lane < K ? dlogp[lane] : 0.0f, n0 = dneg && lane < K ? dneg[lane] : 0.0f;
     auto adjoints = [&](int32_t u, double& gu, double& nu) {
         gu = nu = 0.0;
+        if (K <= 64) {
+            for (int32_t k = 0; k < K; ++k) {
+                const bool this_one = __builtin_amdgcn_readlane(slot0, k) == u;
+                gu += this_one ? lane_of(g0, k) : 0.0f;
+                nu += this_one ? lane_of(n0, k) : 0.0f;
+            }
+            return;
+        }
         for (int32_t k = 0; k < K; ++k) {
             if (slots[k] != u) continue;
             if (dlogp) gu += dlogp[k];
@@ -131,11 +146,13 @@ __global__ void __launch_bounds__(256) head_logprobs_adjoint_kernel(AdjointArgs 
         return (u != st.owner && nu != 0.0 && away > 0.0 ? nu * exp(lp) / away : 0.0) - gu;
     };
     const double away = st.owner >= 0 ? (double)st.away : 1.0;
-    double all = 0.0, sure = 0.0;
-    for (int32_t u = lane; u < K; u += 64) {
-        if (sorted[u] == kNoToken) continue;
+    double all = 0.0, sure = 0.0, gu0 = 0.0, nu0 = 0.0;           // gu0, nu0: those of token `lane`
+    for (int32_t u0 = 0; u0 < K; u0 += 64) {
+        const int32_t u = u0 + lane;
         double gu, nu;
         adjoints(u, gu, nu);
+        if (u0 == 0) { gu0 = gu; nu0 = nu; }
+        if (u >= K || sorted[u] == kNoToken) continue;
         all += weight(u, gu, nu);
         if (u == st.owner) sure = nu * exp(logp(u));
     }
@@ -147,8 +164,8 @@ __global__ void __launch_bounds__(256) head_logprobs_adjoint_kernel(AdjointArgs 
     for (int32_t u = lane; u < K; u += 64) {
         float entry = 0.0f;
         if (sorted[u] < kNoToken) {
-            double gu, nu;
-            adjoints(u, gu, nu);
+            double gu = gu0, nu = nu0;
+            if (u >= 64) adjoints(u, gu, nu);
             const double lp = logp(u), p = exp(lp), others = all - weight(u, gu, nu);
             double d = (u == st.owner ? gu * away : gu * -expm1(lp)) - nu * p + p * others;
             if (u != st.owner && sure != 0.0) d += sure * exp(((double)x[u] - st.ref) - st.ref_log);

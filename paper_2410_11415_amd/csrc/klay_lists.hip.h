@@ -56,17 +56,30 @@ __device__ __forceinline__ void make_list(const ListArgs& g, int64_t r, bool the
     }
     __syncthreads();
 }
+// Of at most 64 entries, by a wave whose lanes hold them (`token`: kNothing behind the last): lane k gets the slot of entry k, and whether it is its
+// token's first mention.
+__device__ __forceinline__ int32_t slot_in_wave(int32_t token, int32_t K, bool& first) {
+    const int32_t lane = threadIdx.x & 63;
+    bool again = token < 0;
+    for (int32_t o = 0; o < K; ++o) again |= o < lane && __builtin_amdgcn_readlane(token, o) == token;
+    first = !again;
+    const int32_t mark = again ? kNoToken : token;
+    int32_t place = 0;
+    for (int32_t o = 0; o < K; ++o) place += __builtin_amdgcn_readlane(mark, o) < token;
+    return token < 0 ? token : place;
+}
 
 // ---- sums over a wave ---------------------------------------------------------------------------------------------
-__device__ __forceinline__ double wave_sum(double x) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
-    return x;
+__device__ __forceinline__ double lane_of(double x, int lane) {
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(x), lane), __builtin_amdgcn_readlane(__double2loint(x), lane));
 }
-__device__ __forceinline__ double wave_max(double x) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) x = fmax(x, __shfl_xor(x, d));
-    return x;
+__device__ __forceinline__ float lane_of(float x, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane)); }
+template <int CONTROL> __device__ __forceinline__ double with_lane_sum(double x) {
+    return x + __hiloint2double(from_lane<CONTROL>(0, __double2hiint(x)), from_lane<CONTROL>(0, __double2loint(x)));
+}
+__device__ __forceinline__ double wave_sum(double x) {
+    x = with_lane_sum<LANES_MIRROR>(with_lane_sum<LANES_HALF_MIRROR>(with_lane_sum<LANES_XOR2>(with_lane_sum<LANES_XOR1>(x))));
+    return lane_of(with_lane_sum<LANES_NEXT_HALF>(with_lane_sum<LANES_NEXT_ROW>(x)), 63);
 }
 __device__ __forceinline__ float wave_max(float x) { return group_max<64>(x); }
 __device__ __forceinline__ int32_t wave_min(int32_t x) {
@@ -197,18 +210,18 @@ __device__ __forceinline__ void finish_distill(const TeachArgs& t, int64_t r, in
     const float* teacher = t.teacher + t.teacher_rows.at(t.first + r);
     const double inv = t.inverse_temperature;
     float most = -INFINITY;
-    double z_most = -INFINITY, any = 0.0, bad = 0.0;
+    float z_top = -INFINITY, any = 0.0f, bad = 0.0f;
     for (int32_t k = lane; k < K; k += 64) {
         if (sorted[k] < kNoToken) most = fmaxf(most, x[k]);
         if (slots[k] == kNothing) continue;
-        if (slots[k] == kOutside) bad = 1.0;
-        const double z = teacher[k * t.teacher_stride];
-        if (z != z || z == INFINITY) bad = 1.0;
-        z_most = fmax(z_most, z);
-        any = 1.0;
+        if (slots[k] == kOutside) bad = 1.0f;
+        const float z = teacher[k * t.teacher_stride];
+        if (z != z || z == INFINITY) bad = 1.0f;
+        z_top = fmaxf(z_top, z);
+        any = 1.0f;
     }
     most = wave_max(most);
-    z_most = wave_max(z_most);
+    const double z_most = wave_max(z_top);
     any = wave_max(any);
     bad = wave_max(bad);
     const float M = fmaxf(most, o.max);
@@ -223,12 +236,12 @@ __device__ __forceinline__ void finish_distill(const TeachArgs& t, int64_t r, in
     const double o_mass = o.sum * exp((o_at - at) * inv);
     s = wave_sum(s) + o_mass;
     zs = wave_sum(zs);
-    const bool teaches = any > 0.0 && (t.rest || z_most > -INFINITY || bad > 0.0);
+    const bool teaches = any > 0.0f && (t.rest || z_most > -INFINITY || bad > 0.0f);
     const double log_s = log(s), log_z = t.rest ? 0.0 : log(zs);
     const bool others = o.max > -INFINITY;
     const double q_rest = t.rest && others ? fmax(0.0, 1.0 - zs) : 0.0;
-    const bool empty = M == -INFINITY && s == 0.0, nan = bad > 0.0 || M == INFINITY || s != s;
-    double loss = 0.0;
+    const bool empty = M == -INFINITY && s == 0.0, nan = bad > 0.0f || M == INFINITY || s != s;
+    double loss = 0.0, q0 = 0.0;                              // q0: of entry `lane`
     for (int32_t k = lane; k < K; k += 64) {
         const int32_t u = slots[k];
         if (u < 0) continue;
@@ -236,22 +249,25 @@ __device__ __forceinline__ void finish_distill(const TeachArgs& t, int64_t r, in
         const double lq = t.rest ? z : (z - z_most) * inv - log_z, q = z > -INFINITY ? exp(lq) : 0.0;
         const double lp = x[u] > -INFINITY || x[u] != x[u] ? ((double)x[u] - at) * inv - log_s : -INFINITY;
         if (q > 0.0) loss += q * (lq - lp);
+        if (k == lane) q0 = q;
     }
     if (t.moved) {
         for (int32_t u0 = 0; u0 < K; u0 += 64) {             // (all lanes together: every x of these 64 is read before one is written)
             const int32_t u = u0 + lane;
-            float moved = 0.0f;
-            if (u < K && sorted[u] < kNoToken && !empty && teaches) {
-                const double lp = x[u] > -INFINITY ? ((double)x[u] - at) * inv - log_s : -INFINITY;
-                double taken = 0.0;
+            const bool there = u < K && sorted[u] < kNoToken && !empty && teaches;
+            double taken = 0.0;
+            if (K <= 64) {
+                const int32_t slot = lane < K ? slots[lane] : kNothing;
+                for (int32_t k = 0; k < K; ++k) taken += __builtin_amdgcn_readlane(slot, k) == u ? lane_of(q0, k) : 0.0;
+            } else if (there) {
                 for (int32_t k = 0; k < K; ++k) {
                     if (slots[k] != u) continue;
                     const double z = teacher[k * t.teacher_stride];
                     if (z > -INFINITY) taken += t.rest ? exp(z) : exp((z - z_most) * inv - log_z);
                 }
-                moved = nan ? NAN : (float)(exp(lp) - taken);
             }
-            if (u < K) t.moved[r * K + u] = moved;
+            const double lp = there && x[u] > -INFINITY ? ((double)x[u] - at) * inv - log_s : -INFINITY;
+            if (u < K) t.moved[r * K + u] = !there ? 0.0f : nan ? NAN : (float)(exp(lp) - taken);
         }
     }
     loss = wave_sum(loss);

@@ -151,8 +151,10 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
             all([](const F& x, const F& y, Acc c) { return mma(x.x, y.x, c); });
         }
     }
-    // Stages from .. to - 1 (one at least) of rows m0 .. of a and n0 .. of b.  Ends with a barrier: shared memory is free again.
-    __device__ __forceinline__ void run(const Operand& oa, const Operand& ob, int64_t m0, int64_t n0, int from, int to, Shared (&sh)[S]) {
+    // Stages from .. to - 1 (one at least) of rows m0 .. of a and n0 .. of b.  `meanwhile` is done while the first loads are on their way.  Ends with a barrier: shared
+    // memory is free again.
+    template <typename F> __device__ __forceinline__ void run(const Operand& oa, const Operand& ob, int64_t m0, int64_t n0, int from, int to, Shared (&sh)[S],
+                                                              F&& meanwhile) {
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -161,8 +163,8 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
         LoadsB lb;
         la.init(oa, m0, wave, lane);
         lb.init(ob, n0, wave, lane);
-        if constexpr (kQuarters) run_quarters(la, lb, from, to, sh);
-        else run_stages(la, lb, from, to, sh);
+        if constexpr (kQuarters) run_quarters(la, lb, from, to, sh, meanwhile);
+        else run_stages(la, lb, from, to, sh, meanwhile);
         arrived<0>();
     }
 
@@ -175,13 +177,14 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
 
     // A stage at a time: stage s + S is asked for when all waves have left stage s.  (Stages behind the last one read zeros, so that always as many
     // loads are on their way.)
-    __device__ __forceinline__ void run_stages(const LoadsA& la, const LoadsB& lb, int from, int to, Shared (&sh)[S]) {
+    template <typename F> __device__ __forceinline__ void run_stages(const LoadsA& la, const LoadsB& lb, int from, int to, Shared (&sh)[S], F&& meanwhile) {
         constexpr int kLoads = LoadsA::kLoads + LoadsB::kLoads;
 #pragma unroll
         for (int s = 0; s < S; ++s) {
             la.load(0, from + s, sh[s].a, wave);
             lb.load(0, from + s, sh[s].b, wave);
         }
+        meanwhile();
         arrived<(S - 1) * kLoads>();
         for (int kt = from; kt < to; kt += S) {
 #pragma unroll
@@ -239,7 +242,7 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
         __builtin_amdgcn_sched_barrier(0);
         arrived<3 * (LoadsA::kLoads + LoadsB::kLoads)>();
     }
-    __device__ __forceinline__ void run_quarters(const LoadsA& la, const LoadsB& lb, int from, int to, Shared (&sh)[S]) {
+    template <typename F> __device__ __forceinline__ void run_quarters(const LoadsA& la, const LoadsB& lb, int from, int to, Shared (&sh)[S], F&& meanwhile) {
         constexpr int kLoads = LoadsA::kLoads + LoadsB::kLoads;
         HalfA a0, a1;
         HalfB b0, b1;
@@ -250,6 +253,7 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
             lb.load(1, from + s, sh[s].b, wave);
             la.load(1, from + s, sh[s].a, wave);
         }
+        meanwhile();
         arrived<3 * kLoads>();
         fetch(a0, sh[0], 0);
         fetch(b0, sh[0], 0);

@@ -326,19 +326,18 @@ def _check_teacher(tokens, teacher, temperature, of, name):
         raise ValueError("the teacher is not differentiated: detach it")
 
 
-def _distill_forward(logits, tokens, teacher, temperature, rest, keep):
+def _distill_forward(logits, tokens, teacher, temperature, rest):
     args, alive = _token_args(logits, tokens, 0)
     told, teacher = _teacher_args(teacher, temperature, rest)
-    loss = logits.new_empty(tuple(logits.shape[:-1]), dtype=torch.float32)
-    kept = _kept(logits, args) if keep else None
-    _b.klay_distill_forward(args, told, _ptr(loss), _ptr(kept), _stream(args.device))
+    loss, kept = logits.new_empty(tuple(logits.shape[:-1]), dtype=torch.float32), _kept(logits, args)
+    _b.klay_distill_forward(args, told, loss.data_ptr(), kept.data_ptr(), _stream(args.device))
     return loss, kept, args, told, alive + (teacher,)
 
 
 class _TokenDistill(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, tokens, teacher, temperature, rest):
-        loss, kept, ctx.args, ctx.told, used = _distill_forward(logits, tokens, teacher, temperature, rest, True)
+        loss, kept, ctx.args, ctx.told, used = _distill_forward(logits, tokens, teacher, temperature, rest)
         ctx.places = _places(*used)
         ctx.save_for_backward(*used, kept)
         return loss
@@ -380,7 +379,7 @@ def token_distill(logits, tokens, teacher, *, temperature=1.0, rest=False):
     _refuse_tangents("token_distill", logits, teacher)
     if torch.is_grad_enabled() and logits.requires_grad:
         return _TokenDistill.apply(logits, tokens, teacher, temperature, rest)
-    return _distill_forward(logits, tokens, teacher, temperature, rest, False)[0]
+    return _distill_forward(logits, tokens, teacher, temperature, rest)[0]
 
 
 def _head_distill_forward(hidden, weight, bias, tokens, teacher, temperature, rest, keep):
