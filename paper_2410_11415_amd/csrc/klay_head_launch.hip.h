@@ -10,8 +10,17 @@ namespace klay {
 
 template <typename T> using Tile32 = Tile<T, 128, 32, 4, 1, 3, 128>;
 template <typename T> using Tile64 = Tile<T, 128, 64, 4, 1, 3, 128>;
-template <typename T> using Tile128 = Tile<T, 128, 128, 2, 2, 2, 128>;
-template <typename T> using Tile256 = Tile<T, 256, 256, 2, 4, 2, 128>;
+template <typename T> struct Large {
+    typedef Tile<T, 128, 128, 2, 2, 2, 128> Tile128;
+    typedef Tile<T, 256, 256, 2, 4, 2, 128> Tile256;
+};
+// fp32: six products a pair of elements, so that a quarter of the k's are as long a stage
+template <> struct Large<f32> {
+    typedef Tile<f32, 128, 128, 2, 2, 2, 64> Tile128;
+    typedef Tile<f32, 256, 256, 2, 4, 2, 64> Tile256;
+};
+template <typename T> using Tile128 = typename Large<T>::Tile128;
+template <typename T> using Tile256 = typename Large<T>::Tile256;
 
 template <typename Tile> Tiles tiles_of(int64_t rows, int64_t columns) {
     return Tiles{(rows + Tile::kN - 1) / Tile::kN, (columns + Tile::kM - 1) / Tile::kM};

@@ -1,7 +1,7 @@
 // Products of matrices for the head of a network: C[n, m] = sum_k A[m, k] B[n, k], both operands with k next to each other, sums in fp32 by
 // v_mfma_f32_32x32x16.  fp32 elements are three bf16 each on their way into the registers (a float's 24 bits are three times eight: hi + mid +
-// lo = x exactly between 2^-110 and 3.38e38), and of the nine products the six that reach fp32's precision are made; the dropped ones are below 2^-25
-// of hi x hi.
+// lo = x exactly above 2^-110), and of the nine products the six that reach fp32's precision are made; the dropped ones are below 2^-21 of hi x hi
+// each, 2^-24 on average.
 #pragma once
 
 #include "klay_typed.hip.h"
@@ -80,15 +80,42 @@ template <> struct Fragment<f32> {
 #pragma unroll
         for (int p = 0; p < 2; ++p) x[p] = *reinterpret_cast<const Four*>(lds + row * SB + place_of<SB>(row, 4 * s + 2 * half + p) * 16);
     }
+    // Cut, not rounded: masks, subtractions and moves of bytes only, five and a half a number (conversions are slower: 760 us for 4096 x 1024 x 16384, @@).
     __device__ __forceinline__ void take_apart() {
-        Floats y = __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
-        hi = __builtin_convertvector(y, Eight<bf16>);
-        y -= __builtin_convertvector(hi, Floats);
-        mid = __builtin_convertvector(y, Eight<bf16>);
-        y -= __builtin_convertvector(mid, Floats);
-        lo = __builtin_convertvector(y, Eight<bf16>);
+        typedef uint32_t Words __attribute__((ext_vector_type(4)));
+        Words w[3];
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            float a = x[e / 4][e % 4], b = x[e / 4][e % 4 + 1];
+#pragma unroll
+            for (int p = 0; p < 3; ++p) {
+                const uint32_t u = __float_as_uint(a), v = __float_as_uint(b);
+                w[p][e / 2] = __builtin_amdgcn_perm(v, u, 0x07060302);          // the upper halves of both
+                if (p == 2) break;
+                a -= __uint_as_float(u & 0xffff0000u);
+                b -= __uint_as_float(v & 0xffff0000u);
+            }
+        }
+        hi = __builtin_bit_cast(Eight<bf16>, w[0]);
+        mid = __builtin_bit_cast(Eight<bf16>, w[1]);
+        lo = __builtin_bit_cast(Eight<bf16>, w[2]);
     }
 };
+
+// The products of a pair of fragments, by `all`, which makes one of them for all pairs; fp32: the smallest ones first.
+template <typename T, typename All> __device__ __forceinline__ void products(All&& all) {
+    typedef Fragment<T> F;
+    if constexpr (std::is_same_v<T, f32>) {
+        all([](const F& x, const F& y, Acc c) { return mma(x.lo, y.hi, c); });
+        all([](const F& x, const F& y, Acc c) { return mma(x.hi, y.lo, c); });
+        all([](const F& x, const F& y, Acc c) { return mma(x.mid, y.mid, c); });
+        all([](const F& x, const F& y, Acc c) { return mma(x.mid, y.hi, c); });
+        all([](const F& x, const F& y, Acc c) { return mma(x.hi, y.mid, c); });
+        all([](const F& x, const F& y, Acc c) { return mma(x.hi, y.hi, c); });
+    } else {
+        all([](const F& x, const F& y, Acc c) { return mma(x.x, y.x, c); });
+    }
+}
 
 // A tile of BM columns x BN rows of the result by WM x WN waves, S stages of SB bytes of k in shared memory; wave (wm, wn) has TM x TN blocks of 32 x 32 in
 // registers.  Lane l of a block holds row l % 32 of the result and of it the columns 8 q + 4 (l / 32) + e as element 4 q + e, so that what is summed or
@@ -97,7 +124,7 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
     static constexpr int kM = BM, kN = BN, kWavesM = WM, kWavesN = WN, kWaves = WM * WN, kThreads = 64 * kWaves, kStages = S, kStageBytes = SB;
     static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
     static constexpr int kParts = SB / (16 * sizeof(T));        // sixteen k's each
-    static constexpr bool kQuarters = !std::is_same_v<T, f32> && TM % 2 == 0 && TN % 2 == 0 && S == 2;      // (fp32: no registers for that many fragments)
+    static constexpr bool kQuarters = TM % 2 == 0 && TN % 2 == 0 && S == 2;
     typedef Stage<BM, kQuarters ? TM * 16 : 0, kWaves, SB> LoadsA;
     typedef Stage<BN, kQuarters ? TN * 16 : 0, kWaves, SB> LoadsB;
     typedef T Element;
@@ -135,21 +162,13 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
 #pragma unroll
                 for (int j = 0; j < TN; ++j) acc[i][j] = one(f.a[i], f.b[j], acc[i][j]);
         };
-        typedef Fragment<T> F;
-        if constexpr (std::is_same_v<T, f32>) {              // smallest first
+        if constexpr (std::is_same_v<T, f32>) {
 #pragma unroll
             for (int i = 0; i < TM; ++i) f.a[i].take_apart();
 #pragma unroll
             for (int j = 0; j < TN; ++j) f.b[j].take_apart();
-            all([](const F& x, const F& y, Acc c) { return mma(x.lo, y.hi, c); });
-            all([](const F& x, const F& y, Acc c) { return mma(x.hi, y.lo, c); });
-            all([](const F& x, const F& y, Acc c) { return mma(x.mid, y.mid, c); });
-            all([](const F& x, const F& y, Acc c) { return mma(x.mid, y.hi, c); });
-            all([](const F& x, const F& y, Acc c) { return mma(x.hi, y.mid, c); });
-            all([](const F& x, const F& y, Acc c) { return mma(x.hi, y.hi, c); });
-        } else {
-            all([](const F& x, const F& y, Acc c) { return mma(x.x, y.x, c); });
         }
+        products<T>(all);
     }
     // Stages from .. to - 1 (one at least) of rows m0 .. of a and n0 .. of b.  `meanwhile` is done while the first loads are on their way.  Ends with a barrier: shared
     // memory is free again.
@@ -224,21 +243,45 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
 #pragma unroll
             for (int s = 0; s < kParts; ++s) f.x[j][s].template load<SB>(sh.b, (wn * TN + half * HB + j) * 32 + (lane & 31), s, lane >> 5);
     }
+    template <typename Half> static __device__ __forceinline__ void take_apart(Half& f) {
+        if constexpr (std::is_same_v<T, f32>)
+            for (auto& row : f.x)
+                for (auto& x : row) x.take_apart();
+    }
     template <int FROM, int TO> __device__ __forceinline__ void multiply(const HalfA& a, const HalfB& b, int ha, int hb) {
 #pragma unroll
-        for (int s = FROM; s < TO; ++s)
+        for (int s = FROM; s < TO; ++s) {
+            auto all = [&](auto&& one) {
 #pragma unroll
-            for (int i = 0; i < HA; ++i)
+                for (int i = 0; i < HA; ++i)
 #pragma unroll
-                for (int j = 0; j < HB; ++j) acc[ha * HA + i][hb * HB + j] = mma(a.x[i][s].x, b.x[j][s].x, acc[ha * HA + i][hb * HB + j]);
+                    for (int j = 0; j < HB; ++j) acc[ha * HA + i][hb * HB + j] = one(a.x[i][s], b.x[j][s], acc[ha * HA + i][hb * HB + j]);
+            };
+            products<T>(all);
+        }
     }
-    // One phase; `others` asks for the half that is free now and reads the one that is needed later.
-    template <typename F> __device__ __forceinline__ void phase(const HalfA& a, const HalfB& b, int ha, int hb, F&& others) {
-        multiply<0, 1>(a, b, ha, hb);                     // (the matrix cores have work at once)
-        __builtin_amdgcn_sched_barrier(0);
-        others();
-        __builtin_amdgcn_sched_barrier(0);
-        multiply<1, kParts>(a, b, ha, hb);
+    // One phase; `others` asks for the half that is free now and reads `next`, the one that is needed later.  fp32: which is taken apart between the matrix
+    // instructions, at most kApart vector instructions behind each, while they run.
+    static constexpr int kApart = 8;
+    template <typename Half, typename F>
+    __device__ __forceinline__ void phase(const HalfA& a, const HalfB& b, int ha, int hb, Half& next, F&& others) {
+        if constexpr (std::is_same_v<T, f32>) {
+            others();
+            __builtin_amdgcn_sched_barrier(0);
+            multiply<0, kParts>(a, b, ha, hb);
+            take_apart(next);
+#pragma unroll
+            for (int m = 0; m < 6 * HA * HB * kParts; ++m) {
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x2, kApart, 0);
+            }
+        } else {
+            multiply<0, 1>(a, b, ha, hb);                 // (the matrix cores have work at once)
+            __builtin_amdgcn_sched_barrier(0);
+            others();
+            __builtin_amdgcn_sched_barrier(0);
+            multiply<1, kParts>(a, b, ha, hb);
+        }
         __builtin_amdgcn_sched_barrier(0);
         arrived<3 * (LoadsA::kLoads + LoadsB::kLoads)>();
     }
@@ -258,25 +301,27 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
         fetch(a0, sh[0], 0);
         fetch(b0, sh[0], 0);
         arrived<3 * kLoads>();
+        take_apart(a0);
+        take_apart(b0);
         la.load(0, from + 2, sh[0].a, wave);
         arrived<3 * kLoads>();
         for (int kt = from; kt < to; kt += 2) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 Shared &now = sh[s], &next = sh[s ^ 1];
-                phase(a0, b0, 0, 0, [&] {
+                phase(a0, b0, 0, 0, b1, [&] {
                     lb.load(0, kt + s + 2, now.b, wave);
                     fetch(b1, now, 1);
                 });
-                phase(a0, b1, 0, 1, [&] {
+                phase(a0, b1, 0, 1, a1, [&] {
                     lb.load(1, kt + s + 2, now.b, wave);
                     fetch(a1, now, 1);
                 });
-                phase(a1, b0, 1, 0, [&] {
+                phase(a1, b0, 1, 0, a0, [&] {
                     la.load(1, kt + s + 2, now.a, wave);
                     fetch(a0, next, 0);
                 });
-                phase(a1, b1, 1, 1, [&] {
+                phase(a1, b1, 1, 1, b0, [&] {
                     la.load(0, kt + s + 3, next.a, wave);
                     fetch(b0, next, 0);
                 });
