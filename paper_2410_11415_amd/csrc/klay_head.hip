@@ -106,21 +106,22 @@ struct ProductPlan {
     int32_t splits;
 };
 // The largest tile of which there are as many as CUs, its stages shared out where need be, at least eight each.
-ProductPlan product_plan(int64_t rows, int64_t columns, int64_t stages) {
-    ProductPlan p;
-    const auto count = [&](klay::HeadTile t) { return tiles(rows, klay::kTileSizes[t].rows) * tiles(columns, klay::kTileSizes[t].columns); };
-    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(stages / 8, 32));
-    if (rows <= 32) p.tile = klay::TILE_32;
-    else if (rows <= 64) p.tile = klay::TILE_64;
-    else p.tile = rows > 128 && columns > 128 && count(klay::TILE_256) * std::min<int64_t>(most, 8) >= 192 ? klay::TILE_256 : klay::TILE_128;
-    const int64_t want = p.tile == klay::TILE_256 ? klay::kComputeUnits : 2 * klay::kComputeUnits;
-    p.splits = (int32_t)std::max<int64_t>(1, std::min(want / count(p.tile), most));
-    return p;
+klay::HeadTile product_tile(int64_t rows, int64_t columns, int64_t stages) {
+    if (rows <= 32) return klay::TILE_32;
+    if (rows <= 64) return klay::TILE_64;
+    const int64_t large = tiles(rows, klay::kTileSizes[klay::TILE_256].rows) * tiles(columns, klay::kTileSizes[klay::TILE_256].columns);
+    return rows > 128 && columns > 128 && large * std::min<int64_t>(stages / 8, 8) >= 192 ? klay::TILE_256 : klay::TILE_128;
+}
+ProductPlan product_plan(klay::HeadTile tile, int64_t rows, int64_t columns, int64_t stages) {
+    const int64_t count = tiles(rows, klay::kTileSizes[tile].rows) * tiles(columns, klay::kTileSizes[tile].columns);
+    const int64_t want = tile == klay::TILE_256 ? klay::kComputeUnits : 2 * klay::kComputeUnits;
+    return ProductPlan{tile, (int32_t)std::max<int64_t>(1, std::min<int64_t>({want / count, stages / 8, 32}))};
 }
 
 constexpr int64_t kRowBlock = 16384;        // rows whose tiles' sums are held at a time
 constexpr int64_t kPieceElements = 1 << 25; // adjoints of logits that are held at a time, about
 constexpr int64_t kMostPiece = 1 << 20;
+constexpr int64_t kSmallProduct = 1ll << 30;    // up to here (rows x width x tokens) the two products are one launch, whatever tiles they would take alone
 
 struct HeadPlan {
     bool copy_hidden = false, copy_weight = false;
@@ -171,8 +172,11 @@ HeadPlan head_plan(const klay_head_args* a, bool back) {
         p.g_across = take(columns * p.g_rows * s.bytes);
         p.w_across = take(a->width * columns * s.bytes);
         p.h_across = take(a->width * p.g_rows * s.bytes);
-        p.dh = product_plan(a->rows, a->width, stages_of(columns, s));
-        p.dw = product_plan(std::min<int64_t>(p.piece, a->vocab), a->width, stages_of(p.g_rows, s));
+        const int64_t dw_rows = std::min<int64_t>(p.piece, a->vocab), dh_stages = stages_of(columns, s), dw_stages = stages_of(p.g_rows, s);
+        klay::HeadTile dh = product_tile(a->rows, a->width, dh_stages), dw = product_tile(dw_rows, a->width, dw_stages);
+        if (a->rows * a->width * dw_rows < kSmallProduct) dh = dw = std::min(dh, dw);
+        p.dh = product_plan(dh, a->rows, a->width, dh_stages);
+        p.dw = product_plan(dw, dw_rows, a->width, dw_stages);
         p.wide = up(a->width, 4);
         p.dh_sums = take(p.dh.splits * a->rows * p.wide * 4);
         p.dw_sums = take(p.dw.splits == 1 && p.wide == a->width ? 0 : p.dw.splits * columns * p.wide * 4);
@@ -231,26 +235,32 @@ template <typename T> struct Head {
     }
     klay_rows weight_rows() const { return klay_rows{INT64_MAX, 0, a->weight_stride}; }
     // the operands as the products take them
-    klay_status operands() {
+    klay::PacksArgs packs{};
+    klay::PackArgs& pack(const void* from, const klay_rows& rows, int64_t count, bool across, int64_t padded, size_t to) {
+        klay::PackArgs& c = packs.copy[packs.copies];
+        packs.across[packs.copies++] = across;
+        c = copy(from, rows, count);
+        c.stride = c.padded = padded;
+        c.to = in(workspace, to);
+        return c;
+    }
+    klay_status run_packs() {
+        const klay_status st = klay::HeadLaunch<T>::pack(packs, stream);
+        packs = klay::PacksArgs{};
+        return st;
+    }
+    // the operands as the products take them, their copies among `packs`
+    void operands() {
         hidden = klay::Operand{a->hidden, a->rows == 1 ? 0 : a->hidden_rows.inner_stride * s.bytes, a->rows, (int32_t)(p.padded / s.lot)};
         weight = klay::Operand{a->weight, a->vocab == 1 ? 0 : a->weight_stride * s.bytes, a->vocab, (int32_t)(p.padded / s.lot)};
-        klay::PackArgs c = copy(a->hidden, a->hidden_rows, a->rows);
-        c.stride = c.padded = p.padded;
         if (p.copy_hidden) {
-            c.to = in(workspace, p.hidden);
-            KLAY_DO(klay::HeadLaunch<T>::pack(c, false, stream));
-            hidden.p = c.to;
+            hidden.p = pack(a->hidden, a->hidden_rows, a->rows, false, p.padded, p.hidden).to;
             hidden.stride = p.padded * s.bytes;
         }
         if (p.copy_weight) {
-            c = copy(a->weight, weight_rows(), a->vocab);
-            c.stride = c.padded = p.padded;
-            c.to = in(workspace, p.weight);
-            KLAY_DO(klay::HeadLaunch<T>::pack(c, false, stream));
-            weight.p = c.to;
+            weight.p = pack(a->weight, weight_rows(), a->vocab, false, p.padded, p.weight).to;
             weight.stride = p.padded * s.bytes;
         }
-        return KLAY_OK;
     }
     klay::HeadArgs args(const Kept& kept) const {
         klay::HeadArgs g{};
@@ -268,8 +278,9 @@ template <typename T> struct Head {
         klay::ListArgs lists = list_args(a->tokens, a->token_rows, a->token_stride, a->rows, a->num_tokens, a->vocab);
         lists.sorted = kept.sorted;
         lists.slots = kept.slots;
-        if (a->num_tokens > 0) KLAY_LAUNCH(klay::head_lists_kernel, dim3((uint32_t)tiles(a->rows, 4)), dim3(256), stream, lists);
-        KLAY_DO(operands());
+        if (a->num_tokens > 1) KLAY_LAUNCH(klay::head_lists_kernel, dim3((uint32_t)tiles(a->rows, 4)), dim3(256), stream, lists);
+        operands();
+        KLAY_DO(run_packs());
         const float scale = scale_of(teacher);
         for (int64_t r0 = 0; r0 < a->rows; r0 += p.row_block) {
             const int64_t rows = std::min(p.row_block, a->rows - r0), at = r0 * a->num_tokens;
@@ -277,11 +288,13 @@ template <typename T> struct Head {
             g.hidden.p = static_cast<const char*>(g.hidden.p) + r0 * g.hidden.stride;
             g.hidden.rows = g.rows = rows;
             g.scale = scale;
-            g.sorted += at;
+            g.sorted = a->num_tokens > 1 ? g.sorted + at : nullptr;
+            g.list = lists;
+            g.list_row = r0;
             g.values = kept.values + at;
             g.partial = static_cast<float4*>(in(workspace, p.partial));
             KLAY_DO(klay::HeadLaunch<T>::forward(p.tile, g, !teacher && (entropy || stats), stream));
-            const klay::FinishArgs f{g.partial, p.tiles_n, rows, a->num_tokens, scale, g.sorted, kept.slots + at, g.values};
+            const klay::FinishArgs f{g.partial, p.tiles_n, rows, a->num_tokens, scale, kept.sorted + at, kept.slots + at, g.values, lists, r0};
             const dim3 grid((uint32_t)tiles(rows, 4));
             if (teacher) {
                 klay::TeachArgs t = teach_args(teacher);
@@ -303,8 +316,6 @@ template <typename T> struct Head {
                          void* dhidden, void* dweight, float* dbias);
 };
 
-__global__ void clear_kernel(uint32_t* p) { *p = 0; }
-
 template <typename T>
 klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, const float* dlogp, const float* dneg, const float* dentropy,
                               const float* dloss, void* dhidden, void* dweight, float* dbias) {
@@ -319,26 +330,20 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
     ad.num_tokens = a->num_tokens;
     ad.coefs = static_cast<float4*>(in(workspace, p.coefs));
     ad.entries = static_cast<float*>(in(workspace, p.entries));
-    if (a->dtype == KLAY_F16) {
-        ad.largest = static_cast<uint32_t*>(in(workspace, p.largest));
-        KLAY_LAUNCH(clear_kernel, dim3(1), dim3(1), stream, ad.largest);
-    }
+    operands();
+    if (a->dtype == KLAY_F16) ad.largest = packs.clear = static_cast<uint32_t*>(in(workspace, p.largest));
+    // A row without a gradient gives none, whatever it holds: its adjoints are zeros, so that only what is not finite has to go.  (In a row that has one
+    // the logits, and with them the adjoints, are NaN then.)
+    if (dweight) pack(a->hidden, a->hidden_rows, a->rows, true, p.g_rows, p.h_across).finite = 1;
+    const auto weights_across = [&](int64_t first, int64_t count) {
+        klay::PackArgs& c = pack(static_cast<const char*>(a->weight) + first * a->weight_stride * s.bytes, weight_rows(), count, true, up(count, 8), p.w_across);
+        c.bias = a->bias ? a->bias + first : nullptr;
+    };
+    if (dhidden) weights_across(0, std::min<int64_t>(p.piece, a->vocab));
+    KLAY_DO(run_packs());
     const dim3 row_grid((uint32_t)tiles(a->rows, 4));
     if (teacher) KLAY_LAUNCH(klay::head_distill_adjoint_kernel, row_grid, dim3(256), stream, ad);
     else KLAY_LAUNCH(klay::head_logprobs_adjoint_kernel, row_grid, dim3(256), stream, ad);
-    KLAY_DO(operands());
-    const auto across = [&](const void* from, const klay_rows& rows, int64_t count, int64_t padded, size_t to) {
-        klay::PackArgs c = copy(from, rows, count);
-        c.padded = padded;
-        c.stride = padded;
-        c.to = in(workspace, to);
-        return c;
-    };
-    if (dweight) {
-        klay::PackArgs c = across(a->hidden, a->hidden_rows, a->rows, p.g_rows, p.h_across);
-        c.coefs = ad.coefs;
-        KLAY_DO(klay::HeadLaunch<T>::pack(c, true, stream));
-    }
     const bool whole = p.piece >= a->vocab;             // one piece
     klay::SumsArgs sums{};
     for (int64_t first = 0; first < a->vocab; first += p.piece) {
@@ -356,21 +361,20 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
         g.g_across = dweight ? in(workspace, p.g_across) : nullptr;
         g.g_columns = columns;
         g.g_rows = p.g_rows;
-        g.g_stride = columns;
-        g.g_across_stride = p.g_rows;
         g.bias_partial = dbias ? static_cast<float*>(in(workspace, p.db_sums)) : nullptr;
         KLAY_DO(klay::HeadLaunch<T>::adjoint(p.tile, g, stream));
         klay::ProductJob jobs[2];
         klay::HeadTile job_tile[2];
         int n = 0;
         if (dhidden) {
-            klay::PackArgs c = across(static_cast<const char*>(a->weight) + first * a->weight_stride * s.bytes, weight_rows(), count, columns, p.w_across);
-            c.bias = g.bias;
-            KLAY_DO(klay::HeadLaunch<T>::pack(c, true, stream));
+            if (first > 0) {
+                weights_across(first, count);
+                KLAY_DO(run_packs());
+            }
             klay::ProductJob& j = jobs[n];
             job_tile[n++] = p.dh.tile;
-            j.a = klay::Operand{g.g, g.g_stride * s.bytes, a->rows, (int32_t)(columns / s.lot)};
-            j.b = klay::Operand{c.to, c.stride * s.bytes, a->width, (int32_t)(columns / s.lot)};
+            j.a = klay::Operand{g.g, columns * s.bytes, a->rows, (int32_t)(columns / s.lot)};
+            j.b = klay::Operand{in(workspace, p.w_across), columns * s.bytes, a->width, (int32_t)(columns / s.lot)};
             j.splits = (int32_t)std::min<int64_t>(p.dh.splits, stages_of(columns, s));
             j.rows = a->rows;
             j.columns = a->width;
@@ -384,8 +388,8 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
         if (dweight) {
             klay::ProductJob& j = jobs[n];
             job_tile[n++] = p.dw.tile;
-            j.a = klay::Operand{g.g_across, g.g_across_stride * s.bytes, count, (int32_t)(p.g_rows / s.lot)};
-            j.b = klay::Operand{in(workspace, p.h_across), g.g_across_stride * s.bytes, a->width, (int32_t)(p.g_rows / s.lot)};
+            j.a = klay::Operand{g.g_across, p.g_rows * s.bytes, count, (int32_t)(p.g_rows / s.lot)};
+            j.b = klay::Operand{in(workspace, p.h_across), p.g_rows * s.bytes, a->width, (int32_t)(p.g_rows / s.lot)};
             j.splits = p.dw.splits;
             j.rows = count;
             j.columns = a->width;

@@ -20,7 +20,9 @@ struct HeadArgs {
     int32_t first, vocab;                   // the first of these tokens; how many tokens there are in all
     int64_t rows;
     int32_t num_tokens;
-    const int32_t* sorted;                  // [rows, num_tokens]
+    const int32_t* sorted;                  // [rows, num_tokens]; null (num_tokens = 1): `list` as it was given, from its row list_row on
+    ListArgs list;
+    int64_t list_row;
     float scale;                            // log2 e / T
     // forward
     float* values;                          // [rows, num_tokens]: the listed tokens' logits
@@ -29,8 +31,8 @@ struct HeadArgs {
     const float4* coefs;                    // [rows]: ref (+inf: the row has no gradient), ln S log2 e, A, B ln 2
     const float* entries;                   // [rows, num_tokens]
     const uint32_t* largest;                // bits of the largest adjoint (fp16), or null
-    void *g, *g_across;                     // [rows, g_columns], [g_columns, g_rows], their rows so many elements apart
-    int64_t g_columns, g_rows, g_stride, g_across_stride;
+    void *g, *g_across;                     // [rows, g_columns], [g_columns, g_rows], contiguous
+    int64_t g_columns, g_rows;
     float* bias_partial;                    // [tiles of rows, g_columns], or null
 };
 
@@ -77,7 +79,7 @@ template <int ROWS, int COLUMNS> struct Marks {
         if (K <= 8) {
 #pragma unroll 4
             for (int32_t n = thread; n < rows * K; n += threads) {
-                const uint32_t c = (uint32_t)lists[n] - (uint32_t)token0;
+                const uint32_t c = (uint32_t)(g.sorted ? lists[n] : token_of(g.list, g.list_row + row0 + n, 0)) - (uint32_t)token0;
                 if (c >= (uint32_t)COLUMNS) continue;
                 const int32_t i = n / K;
                 atomicOr(&bits[i][c >> 5], 1u << (c & 31));
@@ -411,8 +413,26 @@ __global__ void __launch_bounds__(256) head_sums_kernel(SumsArgs g) {
     }
 }
 
-template <typename T> __global__ void __launch_bounds__(256) head_pack_kernel(PackArgs g) { pack_rows<T>(g, blockIdx.x, gridDim.x); }
-template <typename T> __global__ void __launch_bounds__(256) head_pack_across_kernel(PackArgs g) { pack_across<T>(g, blockIdx.x, gridDim.x); }
+// Copies of a launch: workgroups until[i - 1] .. until[i] - 1 make copy i.
+struct PacksArgs {
+    PackArgs copy[4];
+    int32_t across[4];
+    uint32_t until[4];
+    int32_t copies;
+    uint32_t* clear;                        // a word that is made 0, or null
+};
+template <typename T> __global__ void __launch_bounds__(256) head_pack_kernel(PacksArgs g) {
+    if (g.clear && blockIdx.x == 0 && threadIdx.x == 0) *g.clear = 0;
+    uint32_t first = 0;
+    for (int i = 0; i < g.copies; ++i) {
+        if (blockIdx.x < g.until[i]) {
+            if (g.across[i]) pack_across<T>(g.copy[i], blockIdx.x - first, g.until[i] - first);
+            else pack_rows<T>(g.copy[i], blockIdx.x - first, g.until[i] - first);
+            return;
+        }
+        first = g.until[i];
+    }
+}
 
 // ---- launches of a type, each type in a translation unit of its own -------------------------------------------------
 enum HeadTile : int { TILE_32, TILE_64, TILE_128, TILE_256 };
@@ -426,7 +446,7 @@ template <typename T> struct HeadLaunch {
     static klay_status adjoint(HeadTile tile, const HeadArgs& g, void* stream);
     static klay_status products(HeadTile tile, const ProductArgs& g, void* stream);
     static klay_status sums(const SumsArgs& g, void* stream);
-    static klay_status pack(const PackArgs& g, bool across, void* stream);
+    static klay_status pack(PacksArgs& g, void* stream);      // (copies, across, copy, clear given)
 };
 
 }  // namespace klay

@@ -80,10 +80,14 @@ template <typename T> klay_status HeadLaunch<T>::sums(const SumsArgs& g, void* s
     if (most > 0) KLAY_LAUNCH((head_sums_kernel<T>), dim3(grid_of(most, 256, 8192)), dim3(256), stream, g);
     return KLAY_OK;
 }
-template <typename T> klay_status HeadLaunch<T>::pack(const PackArgs& g, bool across, void* stream) {
-    if (g.count < 1 || g.columns < 1) return KLAY_OK;
-    if (across) KLAY_LAUNCH((head_pack_across_kernel<T>), dim3(grid_of((g.padded + 63) / 64 * ((g.columns + 63) / 64), 1, 8192)), dim3(256), stream, g);
-    else KLAY_LAUNCH((head_pack_kernel<T>), dim3(grid_of(g.count * (g.padded * (int64_t)sizeof(T) / 16), 256, 8192)), dim3(256), stream, g);
+template <typename T> klay_status HeadLaunch<T>::pack(PacksArgs& g, void* stream) {
+    uint32_t blocks = 0;
+    for (int i = 0; i < g.copies; ++i) {
+        const PackArgs& c = g.copy[i];
+        blocks += g.across[i] ? grid_of((c.padded + 63) / 64 * ((c.columns + 63) / 64), 1, 8192) : grid_of(c.count * (c.padded * (int64_t)sizeof(T) / 16), 256, 8192);
+        g.until[i] = blocks;
+    }
+    if (blocks > 0 || g.clear) KLAY_LAUNCH((head_pack_kernel<T>), dim3(std::max<uint32_t>(blocks, 1)), dim3(256), stream, g);
     return KLAY_OK;
 }
 

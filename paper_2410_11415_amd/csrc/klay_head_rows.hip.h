@@ -33,20 +33,46 @@ struct FinishArgs {
     int64_t tiles, rows;
     int32_t num_tokens;
     float scale;
-    const int32_t *sorted, *slots;
+    int32_t *sorted, *slots;
     const float* values;
+    ListArgs list;                          // num_tokens = 1: no list has been made; it is the token, of row list_row + r, and is written here
+    int64_t list_row;
 };
+// A row's one token as its list.
+struct One {
+    int32_t sorted, slot;
+};
+__device__ __forceinline__ bool list_of_one(const FinishArgs& g, int64_t r, One* one) {
+    if (g.num_tokens != 1) return false;
+    if ((threadIdx.x & 63) == 0) {
+        const int32_t t = token_of(g.list, g.list_row + r, 0);
+        *one = One{t >= 0 ? t : kNoToken, t >= 0 ? 0 : t};
+        g.sorted[r] = one->sorted;
+        g.slots[r] = one->slot;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    return true;
+}
 __global__ void __launch_bounds__(256) head_logprobs_finish_kernel(FinishArgs g, RowOut out) {
     const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (r >= g.rows) return;
+    __shared__ One one[4];
+    One* mine = one + (threadIdx.x >> 6);
     const int64_t at = r * g.num_tokens;
-    finish_logprobs(out, r, g.num_tokens, g.sorted + at, g.slots + at, g.values + at, join_tiles(g.partial + r * g.tiles, g.tiles, g.scale));
+    const bool single = list_of_one(g, r, mine);
+    finish_logprobs(out, r, g.num_tokens, single ? &mine->sorted : g.sorted + at, single ? &mine->slot : g.slots + at, g.values + at,
+                    join_tiles(g.partial + r * g.tiles, g.tiles, g.scale));
 }
 __global__ void __launch_bounds__(256) head_distill_finish_kernel(FinishArgs g, TeachArgs t) {
     const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (r >= g.rows) return;
+    __shared__ One one[4];
+    One* mine = one + (threadIdx.x >> 6);
     const int64_t at = r * g.num_tokens;
-    finish_distill(t, r, g.num_tokens, g.sorted + at, g.slots + at, g.values + at, join_tiles(g.partial + r * g.tiles, g.tiles, g.scale));
+    const bool single = list_of_one(g, r, mine);
+    finish_distill(t, r, g.num_tokens, single ? &mine->sorted : g.sorted + at, single ? &mine->slot : g.slots + at, g.values + at,
+                   join_tiles(g.partial + r * g.tiles, g.tiles, g.scale));
 }
 
 // The lists of rows: a wave a row.

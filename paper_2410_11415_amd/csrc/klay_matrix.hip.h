@@ -355,12 +355,11 @@ struct PackArgs {
     void* to;
     int64_t stride;                         // of the copy, elements
     int64_t padded;                         // elements of a row of the copy; zeros behind what is taken
-    const float4* coefs;                    // a row whose x is +inf has no gradient and is zeros; null: none is
     int32_t wide;                           // rows start at multiples of 16 bytes
-    const float* bias;                      // of a row whose entry is -inf only what is finite is taken; null: all is
+    int32_t finite;                         // 1: only what is finite is taken, zeros for the rest
+    const float* bias;                      // of a row whose entry is -inf likewise; null: of none
 };
 __device__ __forceinline__ int64_t packed_row(const PackArgs& g, int64_t r) { return r / g.inner * g.outer + r % g.inner * g.inner_stride; }
-__device__ __forceinline__ bool packed_live(const PackArgs& g, int64_t r) { return !g.coefs || g.coefs[r].x < INFINITY; }
 
 // Rows as they are: a thread takes 16 bytes of the copy.
 template <typename T>
@@ -392,7 +391,7 @@ __device__ __forceinline__ void pack_across(const PackArgs& g, int64_t block, in
         for (int step = 0; step < 64 * 64 / N / 256; ++step) {
             const int e = step * 256 + threadIdx.x, r = e / (64 / N), c = e % (64 / N) * N;
             Vec x = {};
-            if (r0 + r < g.count && packed_live(g, r0 + r)) {
+            if (r0 + r < g.count) {
                 const T* row = static_cast<const T*>(g.from) + packed_row(g, r0 + r) + c0 + c;
                 if (g.wide && c0 + c + N <= g.columns) {
                     x = *reinterpret_cast<const Vec*>(row);
@@ -401,7 +400,7 @@ __device__ __forceinline__ void pack_across(const PackArgs& g, int64_t block, in
                     for (int q = 0; q < N; ++q)
                         if (c0 + c + q < g.columns) x[q] = row[q];
                 }
-                if (g.bias && g.bias[r0 + r] == -INFINITY) {
+                if (g.finite || (g.bias && g.bias[r0 + r] == -INFINITY)) {
 #pragma unroll
                     for (int q = 0; q < N; ++q) x[q] = fabsf((float)x[q]) < INFINITY ? x[q] : (T)0.0f;
                 }

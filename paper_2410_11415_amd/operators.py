@@ -211,7 +211,8 @@ def _teacher_args(teacher, temperature, rest):
 
 
 def _kept(like, args):
-    return like.new_empty((_b.klay_list_kept_bytes(args.rows, args.num_tokens),), dtype=torch.uint8)
+    """klay_list_kept_bytes of memory"""
+    return like.new_empty((args.rows * (8 + 3 * args.num_tokens),), dtype=torch.float32)
 
 
 def _workspace(like, args, backward):
@@ -233,8 +234,8 @@ def _head_forward(hidden, weight, bias, tokens, complement, entropy, keep):
 
 def _head_gradients(ctx, hidden, weight, bias):
     """Where the gradients of a head's inputs go; of no rows they are zeros."""
-    make = torch.empty if hidden.numel() else torch.zeros
-    return [make(t.shape, dtype=t.dtype, device=t.device) if need and t is not None else None
+    rows = hidden.numel() > 0
+    return [None if t is None or not need else t.new_empty(t.shape) if rows else t.new_zeros(t.shape)
             for t, need in zip((hidden, weight, bias), ctx.needs_input_grad)]
 
 
