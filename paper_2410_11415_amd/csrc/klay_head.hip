@@ -90,7 +90,7 @@ struct Sizes {
 bool direct(const void* p, const klay_rows& rows, int64_t count, int64_t width, const Sizes& s) {
     if (reinterpret_cast<uintptr_t>(p) % 16 || width % s.lot) return false;
     if (count == 1) return true;
-    return rows.inner >= count && rows.inner_stride >= 0 && rows.inner_stride % s.lot == 0 && rows.inner_stride * s.bytes <= klay::kMostStride;
+    return rows.inner >= count && rows.inner_stride >= width && rows.inner_stride % s.lot == 0 && rows.inner_stride * s.bytes <= klay::kMostStride;
 }
 
 // The largest tile of which there are three for four CUs; the smaller ones only where there are rows for more than one.
@@ -169,9 +169,14 @@ HeadPlan head_plan(const klay_head_args* a, bool back) {
         p.entries = take(asked * 4);
         p.largest = take(4);
         p.g = take(a->rows * columns * s.bytes);
-        p.g_across = take(columns * p.g_rows * s.bytes);
-        p.w_across = take(a->width * columns * s.bytes);
-        p.h_across = take(a->width * p.g_rows * s.bytes);
+        if (s.bytes == 2) {
+            p.h_across = take(a->rows * p.padded * s.bytes);
+            if (a->bias) p.w_across = take(columns * p.padded * s.bytes);
+        } else {
+            p.g_across = take(columns * p.g_rows * s.bytes);
+            p.w_across = take(a->width * columns * s.bytes);
+            p.h_across = take(a->width * p.g_rows * s.bytes);
+        }
         const int64_t dw_rows = std::min<int64_t>(p.piece, a->vocab), dh_stages = stages_of(columns, s), dw_stages = stages_of(p.g_rows, s);
         klay::HeadTile dh = product_tile(a->rows, a->width, dh_stages), dw = product_tile(dw_rows, a->width, dw_stages);
         if (a->rows * a->width * dw_rows < kSmallProduct) dh = dw = std::min(dh, dw);
@@ -251,8 +256,8 @@ template <typename T> struct Head {
     }
     // the operands as the products take them, their copies among `packs`
     void operands() {
-        hidden = klay::Operand{a->hidden, a->rows == 1 ? 0 : a->hidden_rows.inner_stride * s.bytes, a->rows, (int32_t)(p.padded / s.lot)};
-        weight = klay::Operand{a->weight, a->vocab == 1 ? 0 : a->weight_stride * s.bytes, a->vocab, (int32_t)(p.padded / s.lot)};
+        hidden = klay::Operand{a->hidden, (a->rows == 1 ? p.padded : a->hidden_rows.inner_stride) * s.bytes, a->rows, (int32_t)(p.padded / s.lot)};
+        weight = klay::Operand{a->weight, (a->vocab == 1 ? p.padded : a->weight_stride) * s.bytes, a->vocab, (int32_t)(p.padded / s.lot)};
         if (p.copy_hidden) {
             hidden.p = pack(a->hidden, a->hidden_rows, a->rows, false, p.padded, p.hidden).to;
             hidden.stride = p.padded * s.bytes;
@@ -334,9 +339,14 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
     if (a->dtype == KLAY_F16) ad.largest = packs.clear = static_cast<uint32_t*>(in(workspace, p.largest));
     // A row without a gradient gives none, whatever it holds: its adjoints are zeros, so that only what is not finite has to go.  (In a row that has one
     // the logits, and with them the adjoints, are NaN then.)
-    if (dweight) pack(a->hidden, a->hidden_rows, a->rows, true, p.g_rows, p.h_across).finite = 1;
+    // 16-bit operands are read across by the products themselves.
+    constexpr bool wide_type = sizeof(T) == 4;
+    if (dweight) pack(a->hidden, a->hidden_rows, a->rows, wide_type, wide_type ? p.g_rows : p.padded, p.h_across).finite = 1;
+    const bool copy_piece = wide_type || a->bias;
     const auto weights_across = [&](int64_t first, int64_t count) {
-        klay::PackArgs& c = pack(static_cast<const char*>(a->weight) + first * a->weight_stride * s.bytes, weight_rows(), count, true, up(count, 8), p.w_across);
+        if (!copy_piece) return;
+        klay::PackArgs& c = pack(static_cast<const char*>(a->weight) + first * a->weight_stride * s.bytes, weight_rows(), count, wide_type,
+                                 wide_type ? up(count, 8) : p.padded, p.w_across);
         c.bias = a->bias ? a->bias + first : nullptr;
     };
     if (dhidden) weights_across(0, std::min<int64_t>(p.piece, a->vocab));
@@ -357,13 +367,13 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
         g.coefs = ad.coefs;
         g.entries = ad.entries;
         g.largest = ad.largest;
-        g.g = dhidden ? in(workspace, p.g) : nullptr;
-        g.g_across = dweight ? in(workspace, p.g_across) : nullptr;
+        g.g = dhidden || (dweight && !wide_type) ? in(workspace, p.g) : nullptr;
+        g.g_across = dweight && wide_type ? in(workspace, p.g_across) : nullptr;
         g.g_columns = columns;
         g.g_rows = p.g_rows;
         g.bias_partial = dbias ? static_cast<float*>(in(workspace, p.db_sums)) : nullptr;
         KLAY_DO(klay::HeadLaunch<T>::adjoint(p.tile, g, stream));
-        klay::ProductJob jobs[2];
+        klay::ProductJob jobs[2] = {};
         klay::HeadTile job_tile[2];
         int n = 0;
         if (dhidden) {
@@ -374,7 +384,9 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
             klay::ProductJob& j = jobs[n];
             job_tile[n++] = p.dh.tile;
             j.a = klay::Operand{g.g, columns * s.bytes, a->rows, (int32_t)(columns / s.lot)};
-            j.b = klay::Operand{in(workspace, p.w_across), columns * s.bytes, a->width, (int32_t)(columns / s.lot)};
+            if (wide_type) j.b = klay::Operand{in(workspace, p.w_across), columns * s.bytes, a->width, (int32_t)(columns / s.lot)};
+            else if (copy_piece) j.b = klay::Operand{in(workspace, p.w_across), p.padded * s.bytes, p.padded, (int32_t)count};
+            else j.b = klay::Operand{g.weight.p, g.weight.stride, p.padded, (int32_t)count};
             j.splits = (int32_t)std::min<int64_t>(p.dh.splits, stages_of(columns, s));
             j.rows = a->rows;
             j.columns = a->width;
@@ -388,8 +400,14 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
         if (dweight) {
             klay::ProductJob& j = jobs[n];
             job_tile[n++] = p.dw.tile;
-            j.a = klay::Operand{g.g_across, p.g_rows * s.bytes, count, (int32_t)(p.g_rows / s.lot)};
-            j.b = klay::Operand{in(workspace, p.h_across), p.g_rows * s.bytes, a->width, (int32_t)(p.g_rows / s.lot)};
+            if (wide_type) {
+                j.a = klay::Operand{g.g_across, p.g_rows * s.bytes, count, (int32_t)(p.g_rows / s.lot)};
+                j.b = klay::Operand{in(workspace, p.h_across), p.g_rows * s.bytes, a->width, (int32_t)(p.g_rows / s.lot)};
+            } else {
+                j.a_across = 1;
+                j.a = klay::Operand{g.g, columns * s.bytes, columns, (int32_t)a->rows};
+                j.b = klay::Operand{in(workspace, p.h_across), p.padded * s.bytes, p.padded, (int32_t)a->rows};
+            }
             j.splits = p.dw.splits;
             j.rows = count;
             j.columns = a->width;
@@ -401,7 +419,7 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
             if (!j.out) sums.sum[sums.sums++] = klay::SumArgs{j.sums, count, a->width, p.wide, count * p.wide, j.splits, 1, out};
         }
         if (dbias)
-            sums.sum[sums.sums++] = klay::SumArgs{g.bias_partial, 1, count, count, columns, (int32_t)tiles(std::max(a->rows, dweight ? p.g_rows : 0), klay::kTileSizes[p.tile].rows), 0, dbias + first};
+            sums.sum[sums.sums++] = klay::SumArgs{g.bias_partial, 1, count, count, columns, (int32_t)tiles(std::max(a->rows, g.g_across ? p.g_rows : 0), klay::kTileSizes[p.tile].rows), 0, dbias + first};
         for (int i = 0; i < n;) {
             klay::ProductArgs pr{};
             pr.largest = ad.largest;

@@ -31,15 +31,15 @@ struct HeadArgs {
     const float4* coefs;                    // [rows]: ref (+inf: the row has no gradient), ln S log2 e, A, B ln 2
     const float* entries;                   // [rows, num_tokens]
     const uint32_t* largest;                // bits of the largest adjoint (fp16), or null
-    void *g, *g_across;                     // [rows, g_columns], [g_columns, g_rows], contiguous
+    void *g, *g_across;                     // [rows, g_columns]; fp32: and [g_columns, g_rows]; contiguous
     int64_t g_columns, g_rows;
     float* bias_partial;                    // [tiles of rows, g_columns], or null
 };
 
 // One product of a launch: `splits` runs over its stages, each into fp32 sums of its own or, if it is the only one of all pieces, into `out`.
 struct ProductJob {
-    Operand a, b;
-    int32_t splits;
+    Operand a, b;                           // 16-bit: b lies across, a where a_across
+    int32_t a_across, splits;
     int64_t rows, columns, wide;            // wide: columns, up to a multiple of 4
     void* out;                              // [rows, wide], or null
     float* sums;                            // [splits, rows, wide]
@@ -114,7 +114,7 @@ template <typename Tile, typename M, typename F>
 __device__ __forceinline__ void each_mark(const Tile& t, const M& marks, int j, F&& f) {
 #pragma unroll
     for (int i = 0; i < Tile::TM; ++i) {
-        const int word = t.wm * Tile::TM + i;
+        const int word = t.columns_from(i) / 32;
         const uint32_t mine = marks.bits[t.row(j)][word] >> (4 * (t.lane >> 5));
         if (__ballot((mine & 0x0f0f0f0fu) != 0) == 0) continue;
 #pragma unroll
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_for
     tiles.at(blockIdx.x, tr, tc);
     const int64_t row0 = tr * ROWS, column0 = tc * COLUMNS;
     Tile t;
-    t.run(g.weight, g.hidden, column0, row0, 0, Tile::stages(g.hidden), sh.stage, [&] {
+    t.template run<false, false>(g.weight, g.hidden, column0, row0, 0, Tile::stages(g.hidden), sh.stage, [&] {
         if (g.num_tokens) sh.marks.make(g, row0, g.first + (int32_t)column0, threadIdx.x, Tile::kThreads);
     });
     if (some_bias<Tile>(g, column0)) add_bias(t, g, column0);
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_adj
     tiles.at(blockIdx.x, tr, tc);
     const int64_t row0 = tr * ROWS, column0 = tc * COLUMNS;
     Tile t;
-    t.run(g.weight, g.hidden, column0, row0, 0, Tile::stages(g.hidden), sh.stage, [&] {
+    t.template run<false, false>(g.weight, g.hidden, column0, row0, 0, Tile::stages(g.hidden), sh.stage, [&] {
         if (g.num_tokens) sh.marks.make(g, row0, g.first + (int32_t)column0, threadIdx.x, Tile::kThreads);
     });
     if (some_bias<Tile>(g, column0)) add_bias(t, g, column0);
@@ -273,7 +273,7 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_adj
         const uint32_t at_across = g.g_across && r < g.g_rows ? t.row(j) * (uint32_t)sizeof(T) + lower * high : kNoLane;
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
-            const uint32_t block = (t.wm * TM + i) * 32;
+            const uint32_t block = t.columns_from(i);
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const float y = fmaf(t.acc[i][j][e] - c.x, g.scale, -c.y);
@@ -301,6 +301,7 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_adj
 #pragma unroll
                 for (int e = 0; e < 4; ++e) d[e] = t.acc[i][j][4 * q + e] * up;
                 store_row<4, T>(out, at_out, (block + 8 * q) * (uint32_t)sizeof(T), d);
+                if constexpr (sizeof(T) == 2) continue;          // (the products read it across)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float one[1] = {d[e]};
@@ -343,10 +344,15 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_pro
     int64_t tr, tc;
     tiles.at(id - split * all, tr, tc);
     const int64_t row0 = tr * Tile::kN, column0 = tc * Tile::kM;
-    const int64_t stages = Tile::stages(job.a);
+    const int64_t stages = job.a_across ? Tile::stages_across(job.a) : Tile::stages(job.a);
     const int32_t from = (int32_t)(stages * split / job.splits), to = (int32_t)(stages * (split + 1) / job.splits);
     Tile t;
-    t.run(job.b, job.a, column0, row0, from, to, sh, [] {});
+    if constexpr (sizeof(T) == 2) {
+        if (job.a_across) t.template run<true, true>(job.b, job.a, column0, row0, from, to, sh, [] {});
+        else t.template run<true, false>(job.b, job.a, column0, row0, from, to, sh, [] {});
+    } else {
+        t.template run<false, false>(job.b, job.a, column0, row0, from, to, sh, [] {});
+    }
     const float down = 1.0f / adjoint_scale(g.largest);
 #pragma unroll
     for (int j = 0; j < Tile::TN; ++j) {

@@ -1,4 +1,4 @@
-// Products of matrices for the head of a network: C[n, m] = sum_k A[m, k] B[n, k], both operands with k next to each other, sums in fp32 by
+// Products of matrices for the head of a network: C[n, m] = sum_k A[m, k] B[n, k], sums in fp32 by
 // v_mfma_f32_32x32x16.  fp32 elements are three bf16 each on their way into the registers (a float's 24 bits are three times eight: hi + mid +
 // lo = x exactly above 2^-110), and of the nine products the six that reach fp32's precision are made; the dropped ones are below 2^-21 of hi x hi
 // each, 2^-24 on average.
@@ -18,67 +18,124 @@ __device__ __forceinline__ Acc mma(Eight<f16> a, Eight<f16> b, Acc c) { return _
 constexpr int kMostStageBytes = 128;
 constexpr uint32_t kMostStride = 1u << 23;  // bytes from row to row: 256 rows lie within 31 bits
 
-// One side of a product.
+// One side of a product: rows with k next to each other; or, of 16-bit elements, `across`: rows of k with the side's own rows next to each other.
 struct Operand {
     const void* p;                          // 16-byte aligned
-    int64_t stride;                         // bytes from row to row, a multiple of 16, at most kMostStride
-    int64_t rows;
-    int32_t pieces;                         // 16-byte pieces of a row; what lies behind them reads as zeros
+    int64_t stride;                         // bytes from row to row (across: from k to k), a multiple of 16, as long as a row at least, at most kMostStride
+    int64_t rows;                           // (across: a multiple of 8)
+    int32_t pieces;                         // 16-byte pieces of a row; what lies behind them reads as zeros.  Across: the number of k's
 };
 
 // The 16-byte pieces of a stage's row lie permuted by the row's place among sixteen, so that the rows of a fragment come from all banks.
 template <int SB> __device__ __forceinline__ int place_of(int row, int piece) { return piece ^ (SB == 128 ? (row >> 1) & 7 : (row >> 2) & 3); }
 
-// A wave's part of the loads of one side's ROWS rows by WAVES waves: 1 KB an instruction, straight into shared memory.  HALF > 0: they come in two halves,
-// of which the first has the first HALF of every 2 HALF rows.
-template <int ROWS, int HALF, int WAVES, int SB> struct Stage {
-    static constexpr int kHalves = HALF > 0 ? 2 : 1, kRows = 1024 / SB, kPieces = SB / 16, kLoads = ROWS / kHalves / kRows / WAVES;
-    static_assert(ROWS % (kHalves * kRows * WAVES) == 0 && HALF % kRows == 0 && (WAVES * kRows) % 16 == 0, "whole loads, one permutation a lane");
+// `bytes` of memory from p on, which buffer loads do not read beyond (zeros instead).
+__device__ __forceinline__ Stretch stretch_of(const void* p, int64_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)(uint32_t)(bytes < (int64_t)kStretchBytes ? bytes : kStretchBytes), 0x00020000);
+}
+
+// x, about which the compiler knows nothing more: what is added to it is added where it is used, and not kept in registers of its own all the loop long.
+__device__ __forceinline__ uint32_t fresh(uint32_t x) {
+#ifdef __HIP_DEVICE_COMPILE__
+    asm volatile("" : "+v"(x));
+#endif
+    return x;
+}
+
+// A wave's part of the loads of one side's ROWS rows by WAVES waves, in HALVES halves: 1 KB an instruction, straight into shared memory.
+template <int ROWS, int HALVES, int WAVES, int SB> struct Stage {
+    static constexpr int kRows = 1024 / SB, kPieces = SB / 16, kLoads = ROWS / HALVES / kRows / WAVES;
+    static_assert(ROWS % (HALVES * kRows * WAVES) == 0 && (WAVES * kRows) % 16 == 0, "whole loads, one permutation a lane");
     Stretch from;
-    uint32_t offset[kHalves][kLoads];
+    uint32_t stride, offset;                // of the first load; the others' rows are whole strides on
     int32_t piece, pieces;
-    static __device__ __forceinline__ int first_row(int half, int i, int wave) {
-        const int r = (i * WAVES + wave) * kRows;
-        if constexpr (HALF == 0) return r;
-        else return r / HALF * 2 * HALF + half * HALF + r % HALF;
-    }
+    static __device__ __forceinline__ int first_row(int half, int i, int wave) { return half * (ROWS / HALVES) + (i * WAVES + wave) * kRows; }
     __device__ __forceinline__ void init(const Operand& s, int64_t row0, int wave, int lane) {
-        from = stretch_at(static_cast<const char*>(s.p) + row0 * s.stride);
+        const int64_t left = s.rows - row0;
+        from = stretch_of(static_cast<const char*>(s.p) + row0 * s.stride, (left < ROWS ? left : ROWS) * s.stride);
         pieces = s.pieces;
+        stride = (uint32_t)s.stride;
         piece = place_of<SB>(first_row(0, 0, wave) + lane / kPieces, lane % kPieces);
-#pragma unroll
-        for (int h = 0; h < kHalves; ++h)
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const int r = first_row(h, i, wave) + lane / kPieces;
-                offset[h][i] = row0 + r < s.rows ? (uint32_t)r * (uint32_t)s.stride + (uint32_t)piece * 16u : kNoLane;
-            }
+        offset = (uint32_t)(first_row(0, 0, wave) + lane / kPieces) * stride + (uint32_t)piece * 16u;
     }
     // a half, or all, of stage `at` of k; behind the last piece: zeros
     __device__ __forceinline__ void load(int half, int at, char* lds, int wave) const {
+        const uint32_t here = fresh(offset);
         const bool in = at * kPieces + piece < pieces;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(lds + first_row(half, i, wave) * SB), 16,
-                                                     in ? offset[half][i] : kNoLane, at * SB, 0, 0);
+                                                     in ? here + (first_row(half, i, 0) * stride + at * SB) : kNoLane, 0, 0, 0);
+    }
+};
+// Likewise of an operand that lies across: 64 k's of 64 of its rows (128 bytes) after the other.  Every other pair of k's has its 64-byte halves exchanged, so that the
+// four k's of a transposing read come from all banks.  (Of rows behind the last one comes what lies there, for results that nobody stores.)
+template <int ROWS, int HALVES, int WAVES> struct StageAcross {
+    static constexpr int kAll = ROWS < 64 ? 64 : ROWS, kLoads = kAll / HALVES / 8 / WAVES;
+    static_assert(kAll % (HALVES * 64) == 0 && kAll % (HALVES * 8 * WAVES) == 0, "whole loads");
+    const char* from;
+    int64_t bytes;                          // from there to the operand's end
+    uint32_t stride, offset;
+    static __device__ __forceinline__ int first(int half, int i, int wave) { return half * (kAll / HALVES) + (i * WAVES + wave) * 8; }
+    __device__ __forceinline__ void init(const Operand& s, int64_t row0, int wave, int lane) {
+        from = static_cast<const char*>(s.p) + row0 * 2;
+        stride = (uint32_t)s.stride;
+        bytes = (s.pieces - 1) * s.stride + (s.rows - row0) * 2;
+        const int k = lane >> 3;
+        offset = (uint32_t)k * stride + (uint32_t)((lane & 7) ^ (((k >> 1) & 1) << 2)) * 16u;
+    }
+    __device__ __forceinline__ void load(int half, int at, char* lds, int wave) const {
+        const int64_t gone = at * 64 * (int64_t)stride;
+        const Stretch stage = stretch_of(from + gone, gone < bytes ? bytes - gone : 0);
+        const uint32_t here = fresh(offset);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int place = first(half, i, wave);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(stage, (__attribute__((address_space(3))) void*)(lds + place * 128), 16,
+                                                     here + ((uint32_t)(place & 63) * stride + (uint32_t)(place & ~63) * 2u), 0, 0, 0);
+        }
     }
 };
 
-// The eight k's of a lane's row that a matrix instruction takes, `half` 0 or 1 of sixteen.
+// A transposing read: lane i of sixteen gets the i-th elements of four rows of sixteen that the lanes point to, a quarter of a row each.  (Of a pointer that nothing else
+// is said to reach: otherwise the compiler waits for all loads into shared memory before it.)
+typedef short FourShorts __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) FourShorts SharedFour;
+__device__ __forceinline__ FourShorts read_across(SharedFour* __restrict__ p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16(p); }
+
+// The eight k's of a lane's row that a matrix instruction takes.  `at`: where the lane's row (of the first block) starts in a stage's side, its first piece
+// (lane_place); `on`: bytes from the first block to this one.
 template <typename T> struct Fragment {
     Eight<T> x;
-    template <int SB> __device__ __forceinline__ void load(const char* lds, int row, int s, int half) {
-        x = *reinterpret_cast<const Eight<T>*>(lds + row * SB + place_of<SB>(row, 2 * s + half) * 16);
+    template <int SB> __device__ __forceinline__ void load(const char* lds, uint32_t at, int on, int s) {
+        x = *reinterpret_cast<const Eight<T>*>(lds + (at ^ (uint32_t)(32 * s)) + on);
+    }
+    // Of an operand that lies across (lane_place_across), `second` of a pair of blocks.
+    __device__ __forceinline__ void load_across(const char* lds, uint32_t at, int on, int second, int s) {
+        typedef short Shorts __attribute__((ext_vector_type(8)));
+        FourShorts part[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+            part[t] = read_across((SharedFour*)(lds + (at ^ (uint32_t)(64 * second)) + on + s * 2048 + t * 512));
+        x = __builtin_bit_cast(Eight<T>, (Shorts)__builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
+template <typename T, int SB> __device__ __forceinline__ uint32_t lane_place(int lane) {
+    const int row = lane & 31, half = lane >> 5;
+    return row * SB + place_of<SB>(row, sizeof(T) == 4 ? 2 * half : half) * 16;
+}
+__device__ __forceinline__ uint32_t lane_place_across(int lane) {
+    const int in = lane & 15, group = lane >> 4;
+    return (8 * (group >> 1) + (in >> 2)) * 128 + ((in >> 3) & 1) * 64 + (group & 1) * 32 + (in & 3) * 8;
+}
 template <> struct Fragment<f32> {
     typedef float Four __attribute__((ext_vector_type(4)));
     typedef float Floats __attribute__((ext_vector_type(8)));
     Four x[2];
     Eight<bf16> hi, mid, lo;
-    template <int SB> __device__ __forceinline__ void load(const char* lds, int row, int s, int half) {
+    template <int SB> __device__ __forceinline__ void load(const char* lds, uint32_t at, int on, int s) {
 #pragma unroll
-        for (int p = 0; p < 2; ++p) x[p] = *reinterpret_cast<const Four*>(lds + row * SB + place_of<SB>(row, 4 * s + 2 * half + p) * 16);
+        for (int p = 0; p < 2; ++p) x[p] = *reinterpret_cast<const Four*>(lds + (at ^ (uint32_t)(64 * s + 16 * p)) + on);
     }
     // Cut, not rounded: masks, subtractions and moves of bytes only, five and a half a number (conversions are slower: 760 us for 4096 x 1024 x 16384, @@).
     __device__ __forceinline__ void take_apart() {
@@ -125,35 +182,52 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
     static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
     static constexpr int kParts = SB / (16 * sizeof(T));        // sixteen k's each
     static constexpr bool kQuarters = TM % 2 == 0 && TN % 2 == 0 && S == 2;
-    typedef Stage<BM, kQuarters ? TM * 16 : 0, kWaves, SB> LoadsA;
-    typedef Stage<BN, kQuarters ? TN * 16 : 0, kWaves, SB> LoadsB;
+    static constexpr int kHalves = kQuarters ? 2 : 1, HA = TM / kHalves, HB = TN / kHalves;      // of the tile's columns and rows; blocks of a wave in each
+    template <bool ACROSS> using LoadsA = std::conditional_t<ACROSS, StageAcross<BM, kHalves, kWaves>, Stage<BM, kHalves, kWaves, SB>>;
+    template <bool ACROSS> using LoadsB = std::conditional_t<ACROSS, StageAcross<BN, kHalves, kWaves>, Stage<BN, kHalves, kWaves, SB>>;
     typedef T Element;
     struct Shared {                         // one stage
-        char a[BM * SB], b[BN * SB];
+        char a[BM * SB], b[(sizeof(T) == 2 && BN < 64 ? 64 : BN) * SB];
     };
     static __device__ __forceinline__ int stages(const Operand& o) { return (o.pieces * 16 + SB - 1) / SB; }
+    static __device__ __forceinline__ int stages_across(const Operand& o) { return (o.pieces + 63) / 64; }
     Acc acc[TM][TN];
     int wave, lane, wm, wn;
+    uint32_t lane_along, lane_across;
     __device__ __forceinline__ Tile() {
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         lane = threadIdx.x & 63;
         wm = wave / WN;
         wn = wave % WN;
+        lane_along = lane_place<T, SB>(lane);
+        lane_across = lane_place_across(lane);
     }
     // of the tile: a lane's first column of the i-th blocks (the others: + 8 q + e), its row of the j-th
-    __device__ __forceinline__ int column(int i) const { return (wm * TM + i) * 32 + 4 * (lane >> 5); }
-    __device__ __forceinline__ int row(int j) const { return (wn * TN + j) * 32 + (lane & 31); }
+    __device__ __forceinline__ int column(int i) const { return columns_from(i) + 4 * (lane >> 5); }
+    __device__ __forceinline__ int row(int j) const { return rows_from(j) + (lane & 31); }
+    // where a wave's i-th blocks of columns, its j-th of rows start
+    __device__ __forceinline__ int columns_from(int i) const { return i / HA * (BM / kHalves) + (wm * HA + i % HA) * 32; }
+    __device__ __forceinline__ int rows_from(int j) const { return j / HB * (BN / kHalves) + (wn * HB + j % HB) * 32; }
 
     // What a matrix instruction of each block takes: sixteen k's.
     struct Fragments {
         Fragment<T> a[TM], b[TN];
     };
-    __device__ __forceinline__ void fetch(Fragments& f, const Shared& sh, int s) const {
-        const int r = lane & 31, half = lane >> 5;
+    // `at`: the lane's place in the wave's first block; the block is `blocks` 32 rows on, of a wave whose blocks start at `wave0`
+    template <bool ACROSS> __device__ __forceinline__ void fetch(Fragment<T>& f, const char* lds, uint32_t at, int blocks, int s) const {
+        if constexpr (ACROSS) f.load_across(lds, at, blocks / 2 * 8192, blocks & 1, s);
+        else f.template load<SB>(lds, at, blocks * 32 * SB, s);
+    }
+    template <bool ACROSS> __device__ __forceinline__ uint32_t place(int wave0) const {
+        if constexpr (ACROSS) return fresh(lane_across ^ (wave0 & 32) * 2u) + (wave0 >> 6) * 8192u;
+        else return fresh(lane_along) + wave0 * SB;
+    }
+    template <bool AA, bool BA> __device__ __forceinline__ void fetch(Fragments& f, const Shared& sh, int s) const {
+        const uint32_t a = place<AA>(columns_from(0)), b = place<BA>(rows_from(0));
 #pragma unroll
-        for (int j = 0; j < TN; ++j) f.b[j].template load<SB>(sh.b, (wn * TN + j) * 32 + r, s, half);
+        for (int j = 0; j < TN; ++j) fetch<BA>(f.b[j], sh.b, b, j, s);
 #pragma unroll
-        for (int i = 0; i < TM; ++i) f.a[i].template load<SB>(sh.a, (wm * TM + i) * 32 + r, s, half);
+        for (int i = 0; i < TM; ++i) fetch<AA>(f.a[i], sh.a, a, i, s);
     }
     __device__ __forceinline__ void multiply(Fragments& f) {
         auto all = [&](auto&& one) {
@@ -170,20 +244,20 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
         }
         products<T>(all);
     }
-    // Stages from .. to - 1 (one at least) of rows m0 .. of a and n0 .. of b.  `meanwhile` is done while the first loads are on their way.  Ends with a barrier: shared
-    // memory is free again.
-    template <typename F> __device__ __forceinline__ void run(const Operand& oa, const Operand& ob, int64_t m0, int64_t n0, int from, int to, Shared (&sh)[S],
+    // Stages from .. to - 1 (one at least) of rows m0 .. of a and n0 .. of b (AA, BA: which of them lie across).  `meanwhile` is done while the first loads are on
+    // their way.  Ends with a barrier: shared memory is free again.
+    template <bool AA, bool BA, typename F> __device__ __forceinline__ void run(const Operand& oa, const Operand& ob, int64_t m0, int64_t n0, int from, int to, Shared (&sh)[S],
                                                               F&& meanwhile) {
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j) acc[i][j] = Acc{};
-        LoadsA la;
-        LoadsB lb;
+        LoadsA<AA> la;
+        LoadsB<BA> lb;
         la.init(oa, m0, wave, lane);
         lb.init(ob, n0, wave, lane);
-        if constexpr (kQuarters) run_quarters(la, lb, from, to, sh, meanwhile);
-        else run_stages(la, lb, from, to, sh, meanwhile);
+        if constexpr (kQuarters) run_quarters<AA, BA>(la, lb, from, to, sh, meanwhile);
+        else run_stages<AA, BA>(la, lb, from, to, sh, meanwhile);
         arrived<0>();
     }
 
@@ -196,8 +270,9 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
 
     // A stage at a time: stage s + S is asked for when all waves have left stage s.  (Stages behind the last one read zeros, so that always as many
     // loads are on their way.)
-    template <typename F> __device__ __forceinline__ void run_stages(const LoadsA& la, const LoadsB& lb, int from, int to, Shared (&sh)[S], F&& meanwhile) {
-        constexpr int kLoads = LoadsA::kLoads + LoadsB::kLoads;
+    template <bool AA, bool BA, typename F>
+    __device__ __forceinline__ void run_stages(const LoadsA<AA>& la, const LoadsB<BA>& lb, int from, int to, Shared (&sh)[S], F&& meanwhile) {
+        constexpr int kLoads = LoadsA<AA>::kLoads + LoadsB<BA>::kLoads;
 #pragma unroll
         for (int s = 0; s < S; ++s) {
             la.load(0, from + s, sh[s].a, wave);
@@ -211,7 +286,7 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
                 Fragments f;
 #pragma unroll
                 for (int part = 0; part < kParts; ++part) {
-                    fetch(f, sh[s], part);
+                    fetch<AA, BA>(f, sh[s], part);
                     if (part == kParts - 1 && kt + s + 1 < to) {
                         arrived<(S - 2) * kLoads>();
                         la.load(0, kt + s + S, sh[s].a, wave);
@@ -228,20 +303,21 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
     // registers when it begins; while its matrix instructions run, the half that a later phase needs is read: B1, A1, the next stage's A0, its B0.  A half that
     // all waves have read (the barrier behind each phase) is filled again at once, for the stage after next: seven phases before it is read, so that six
     // halves are on their way at every barrier and the loads never pause.  (Loading whole stages, one ahead: 3790 us for the loop of 4096 x 131072 x 4096.)
-    static constexpr int HA = TM / 2 > 0 ? TM / 2 : 1, HB = TN / 2 > 0 ? TN / 2 : 1;
     struct HalfA { Fragment<T> x[HA][kParts]; };
     struct HalfB { Fragment<T> x[HB][kParts]; };
-    __device__ __forceinline__ void fetch(HalfA& f, const Shared& sh, int half) const {
+    template <bool ACROSS> __device__ __forceinline__ void fetch(HalfA& f, const Shared& sh, int half) const {
+        const uint32_t at = place<ACROSS>(wm * HA * 32);
 #pragma unroll
         for (int i = 0; i < HA; ++i)
 #pragma unroll
-            for (int s = 0; s < kParts; ++s) f.x[i][s].template load<SB>(sh.a, (wm * TM + half * HA + i) * 32 + (lane & 31), s, lane >> 5);
+            for (int s = 0; s < kParts; ++s) fetch<ACROSS>(f.x[i][s], sh.a, at, half * (BM / 64) + i, s);
     }
-    __device__ __forceinline__ void fetch(HalfB& f, const Shared& sh, int half) const {
+    template <bool ACROSS> __device__ __forceinline__ void fetch(HalfB& f, const Shared& sh, int half) const {
+        const uint32_t at = place<ACROSS>(wn * HB * 32);
 #pragma unroll
         for (int j = 0; j < HB; ++j)
 #pragma unroll
-            for (int s = 0; s < kParts; ++s) f.x[j][s].template load<SB>(sh.b, (wn * TN + half * HB + j) * 32 + (lane & 31), s, lane >> 5);
+            for (int s = 0; s < kParts; ++s) fetch<ACROSS>(f.x[j][s], sh.b, at, half * (BN / 64) + j, s);
     }
     template <typename Half> static __device__ __forceinline__ void take_apart(Half& f) {
         if constexpr (std::is_same_v<T, f32>)
@@ -263,7 +339,7 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
     // One phase; `others` asks for the half that is free now and reads `next`, the one that is needed later.  fp32: which is taken apart between the matrix
     // instructions, at most kApart vector instructions behind each, while they run.
     static constexpr int kApart = 8;
-    template <typename Half, typename F>
+    template <int LEFT, typename Half, typename F>
     __device__ __forceinline__ void phase(const HalfA& a, const HalfB& b, int ha, int hb, Half& next, F&& others) {
         if constexpr (std::is_same_v<T, f32>) {
             others();
@@ -283,10 +359,11 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
             multiply<1, kParts>(a, b, ha, hb);
         }
         __builtin_amdgcn_sched_barrier(0);
-        arrived<3 * (LoadsA::kLoads + LoadsB::kLoads)>();
+        arrived<LEFT>();
     }
-    template <typename F> __device__ __forceinline__ void run_quarters(const LoadsA& la, const LoadsB& lb, int from, int to, Shared (&sh)[S], F&& meanwhile) {
-        constexpr int kLoads = LoadsA::kLoads + LoadsB::kLoads;
+    template <bool AA, bool BA, typename F>
+    __device__ __forceinline__ void run_quarters(const LoadsA<AA>& la, const LoadsB<BA>& lb, int from, int to, Shared (&sh)[S], F&& meanwhile) {
+        constexpr int kLeft = 3 * (LoadsA<AA>::kLoads + LoadsB<BA>::kLoads);
         HalfA a0, a1;
         HalfB b0, b1;
 #pragma unroll
@@ -297,33 +374,33 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
             la.load(1, from + s, sh[s].a, wave);
         }
         meanwhile();
-        arrived<3 * kLoads>();
-        fetch(a0, sh[0], 0);
-        fetch(b0, sh[0], 0);
-        arrived<3 * kLoads>();
+        arrived<kLeft>();
+        fetch<AA>(a0, sh[0], 0);
+        fetch<BA>(b0, sh[0], 0);
+        arrived<kLeft>();
         take_apart(a0);
         take_apart(b0);
         la.load(0, from + 2, sh[0].a, wave);
-        arrived<3 * kLoads>();
+        arrived<kLeft>();
         for (int kt = from; kt < to; kt += 2) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 Shared &now = sh[s], &next = sh[s ^ 1];
-                phase(a0, b0, 0, 0, b1, [&] {
+                phase<kLeft>(a0, b0, 0, 0, b1, [&] {
                     lb.load(0, kt + s + 2, now.b, wave);
-                    fetch(b1, now, 1);
+                    fetch<BA>(b1, now, 1);
                 });
-                phase(a0, b1, 0, 1, a1, [&] {
+                phase<kLeft>(a0, b1, 0, 1, a1, [&] {
                     lb.load(1, kt + s + 2, now.b, wave);
-                    fetch(a1, now, 1);
+                    fetch<AA>(a1, now, 1);
                 });
-                phase(a1, b0, 1, 0, a0, [&] {
+                phase<kLeft>(a1, b0, 1, 0, a0, [&] {
                     la.load(1, kt + s + 2, now.a, wave);
-                    fetch(a0, next, 0);
+                    fetch<AA>(a0, next, 0);
                 });
-                phase(a1, b1, 1, 1, b0, [&] {
+                phase<kLeft>(a1, b1, 1, 1, b0, [&] {
                     la.load(0, kt + s + 3, next.a, wave);
-                    fetch(b0, next, 0);
+                    fetch<BA>(b0, next, 0);
                 });
                 if (kt + s + 1 >= to) break;
             }
@@ -373,6 +450,10 @@ __device__ __forceinline__ void pack_rows(const PackArgs& g, int64_t block, int6
 #pragma unroll
         for (int e = 0; e < N; ++e)
             if (c + e < g.columns) out[e] = row[c + e];
+        if (g.finite || (g.bias && g.bias[r] == -INFINITY)) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) out[e] = fabsf((float)out[e]) < INFINITY ? out[e] : (T)0.0f;
+        }
         *reinterpret_cast<typename Pieces<T, N>::Vec*>(static_cast<T*>(g.to) + r * g.stride + c) = out;
     }
 }
