@@ -86,11 +86,11 @@ struct Sizes {
     explicit Sizes(int32_t dtype) : bytes(klay::dtype_bytes(dtype)), lot(16 / bytes) {}
 };
 
-// Rows that the products can read where they are: 16-byte pieces, one stride.
+// Rows that the products can read where they are: one stride, starts at multiples of 4 bytes.
 bool direct(const void* p, const klay_rows& rows, int64_t count, int64_t width, const Sizes& s) {
-    if (reinterpret_cast<uintptr_t>(p) % 16 || width % s.lot) return false;
-    if (count == 1) return true;
-    return rows.inner >= count && rows.inner_stride >= width && rows.inner_stride % s.lot == 0 && rows.inner_stride * s.bytes <= klay::kMostStride;
+    if (reinterpret_cast<uintptr_t>(p) % 4) return false;
+    if (count == 1) return width * s.bytes % 4 == 0;
+    return rows.inner >= count && rows.inner_stride >= width && rows.inner_stride * s.bytes % 4 == 0 && rows.inner_stride * s.bytes <= klay::kMostStride;
 }
 
 // The largest tile of which there are three for four CUs; the smaller ones only where there are rows for more than one.
@@ -129,10 +129,10 @@ struct HeadPlan {
     int64_t row_block = 0, tiles_n = 0;
     klay::HeadTile tile = klay::TILE_32;
     // backward
-    int64_t piece = 0, g_rows = 0, wide = 0;       // wide: width up to a multiple of 4, as the products' sums are stored
+    int64_t piece = 0;
     ProductPlan dh{}, dw{};
     // bytes from the start of the workspace
-    size_t hidden = 0, weight = 0, partial = 0, kept = 0, coefs = 0, entries = 0, largest = 0, g = 0, g_across = 0, w_across = 0, h_across = 0,
+    size_t hidden = 0, weight = 0, partial = 0, kept = 0, coefs = 0, entries = 0, largest = 0, g = 0, clean_hidden = 0, clean_weight = 0,
            dh_sums = 0, dw_sums = 0, db_sums = 0, bytes = 0;
 };
 int64_t stages_of(int64_t elements, const Sizes& s) { return tiles(elements * s.bytes, klay::kMostStageBytes); }
@@ -162,30 +162,22 @@ HeadPlan head_plan(const klay_head_args* a, bool back) {
     } else {
         const int64_t all = up(a->vocab, 256);
         p.piece = std::min({all, kMostPiece, std::max<int64_t>(256, kPieceElements / up(a->rows, 256) / 256 * 256)});
-        p.g_rows = up(a->rows, 8);
         const int64_t columns = up(std::min<int64_t>(p.piece, a->vocab), 8);
         p.tile = logits_tile(a->rows, columns);
         p.coefs = take(a->rows * sizeof(float4));
         p.entries = take(asked * 4);
         p.largest = take(4);
         p.g = take(a->rows * columns * s.bytes);
-        if (s.bytes == 2) {
-            p.h_across = take(a->rows * p.padded * s.bytes);
-            if (a->bias) p.w_across = take(columns * p.padded * s.bytes);
-        } else {
-            p.g_across = take(columns * p.g_rows * s.bytes);
-            p.w_across = take(a->width * columns * s.bytes);
-            p.h_across = take(a->width * p.g_rows * s.bytes);
-        }
-        const int64_t dw_rows = std::min<int64_t>(p.piece, a->vocab), dh_stages = stages_of(columns, s), dw_stages = stages_of(p.g_rows, s);
+        p.clean_hidden = take(a->rows * p.padded * s.bytes);
+        if (a->bias) p.clean_weight = take(columns * p.padded * s.bytes);
+        const int64_t dw_rows = std::min<int64_t>(p.piece, a->vocab), dh_stages = stages_of(columns, s), dw_stages = stages_of(a->rows, s);
         klay::HeadTile dh = product_tile(a->rows, a->width, dh_stages), dw = product_tile(dw_rows, a->width, dw_stages);
         if (a->rows * a->width * dw_rows < kSmallProduct) dh = dw = std::min(dh, dw);
         p.dh = product_plan(dh, a->rows, a->width, dh_stages);
         p.dw = product_plan(dw, dw_rows, a->width, dw_stages);
-        p.wide = up(a->width, 4);
-        p.dh_sums = take(p.dh.splits * a->rows * p.wide * 4);
-        p.dw_sums = take(p.dw.splits == 1 && p.wide == a->width ? 0 : p.dw.splits * columns * p.wide * 4);
-        p.db_sums = take(tiles(p.g_rows, klay::kTileSizes[p.tile].rows) * columns * 4);
+        p.dh_sums = take(p.dh.splits * a->rows * a->width * 4);
+        p.dw_sums = take(p.dw.splits == 1 ? 0 : p.dw.splits * columns * a->width * 4);
+        p.db_sums = take(tiles(a->rows, klay::kTileSizes[p.tile].rows) * columns * 4);
     }
     p.bytes = at;
     return p;
@@ -235,17 +227,15 @@ template <typename T> struct Head {
         g.inner = std::max<int64_t>(rows.inner, 1);
         g.count = count;
         g.columns = a->width;
-        g.wide = reinterpret_cast<uintptr_t>(from) % 16 == 0 && g.outer % s.lot == 0 && g.inner_stride % s.lot == 0;
         return g;
     }
     klay_rows weight_rows() const { return klay_rows{INT64_MAX, 0, a->weight_stride}; }
     // the operands as the products take them
     klay::PacksArgs packs{};
-    klay::PackArgs& pack(const void* from, const klay_rows& rows, int64_t count, bool across, int64_t padded, size_t to) {
-        klay::PackArgs& c = packs.copy[packs.copies];
-        packs.across[packs.copies++] = across;
+    klay::PackArgs& pack(const void* from, const klay_rows& rows, int64_t count, size_t to) {
+        klay::PackArgs& c = packs.copy[packs.copies++];
         c = copy(from, rows, count);
-        c.stride = c.padded = padded;
+        c.stride = c.padded = p.padded;
         c.to = in(workspace, to);
         return c;
     }
@@ -254,16 +244,21 @@ template <typename T> struct Head {
         packs = klay::PacksArgs{};
         return st;
     }
-    // the operands as the products take them, their copies among `packs`
+    // The operands as the products take them, their copies among `packs`.  (Where only one is copied, the other's rows have no zeros behind
+    // their ends: both are read as if they had none.)
+    int32_t tail = 0;
     void operands() {
-        hidden = klay::Operand{a->hidden, (a->rows == 1 ? p.padded : a->hidden_rows.inner_stride) * s.bytes, a->rows, (int32_t)(p.padded / s.lot)};
-        weight = klay::Operand{a->weight, (a->vocab == 1 ? p.padded : a->weight_stride) * s.bytes, a->vocab, (int32_t)(p.padded / s.lot)};
+        const bool padded = p.copy_hidden && p.copy_weight;
+        const int32_t pieces = (int32_t)(padded ? p.padded / s.lot : a->width / s.lot);
+        tail = padded ? 0 : (int32_t)(a->width % s.lot);
+        hidden = klay::Operand{a->hidden, (a->rows == 1 ? a->width : a->hidden_rows.inner_stride) * s.bytes, a->rows, pieces};
+        weight = klay::Operand{a->weight, (a->vocab == 1 ? a->width : a->weight_stride) * s.bytes, a->vocab, pieces};
         if (p.copy_hidden) {
-            hidden.p = pack(a->hidden, a->hidden_rows, a->rows, false, p.padded, p.hidden).to;
+            hidden.p = pack(a->hidden, a->hidden_rows, a->rows, p.hidden).to;
             hidden.stride = p.padded * s.bytes;
         }
         if (p.copy_weight) {
-            weight.p = pack(a->weight, weight_rows(), a->vocab, false, p.padded, p.weight).to;
+            weight.p = pack(a->weight, weight_rows(), a->vocab, p.weight).to;
             weight.stride = p.padded * s.bytes;
         }
     }
@@ -273,6 +268,7 @@ template <typename T> struct Head {
         g.weight = weight;
         g.bias = a->bias;
         g.vocab = a->vocab;
+        g.tail = tail;
         g.rows = a->rows;
         g.num_tokens = a->num_tokens;
         g.sorted = kept.sorted;
@@ -339,17 +335,11 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
     if (a->dtype == KLAY_F16) ad.largest = packs.clear = static_cast<uint32_t*>(in(workspace, p.largest));
     // A row without a gradient gives none, whatever it holds: its adjoints are zeros, so that only what is not finite has to go.  (In a row that has one
     // the logits, and with them the adjoints, are NaN then.)
-    // 16-bit operands are read across by the products themselves.
-    constexpr bool wide_type = sizeof(T) == 4;
-    if (dweight) pack(a->hidden, a->hidden_rows, a->rows, wide_type, wide_type ? p.g_rows : p.padded, p.h_across).finite = 1;
-    const bool copy_piece = wide_type || a->bias;
-    const auto weights_across = [&](int64_t first, int64_t count) {
-        if (!copy_piece) return;
-        klay::PackArgs& c = pack(static_cast<const char*>(a->weight) + first * a->weight_stride * s.bytes, weight_rows(), count, wide_type,
-                                 wide_type ? up(count, 8) : p.padded, p.w_across);
-        c.bias = a->bias ? a->bias + first : nullptr;
+    if (dweight) pack(a->hidden, a->hidden_rows, a->rows, p.clean_hidden).finite = 1;
+    const auto clean_weights = [&](int64_t first, int64_t count) {
+        if (a->bias) pack(static_cast<const char*>(a->weight) + first * a->weight_stride * s.bytes, weight_rows(), count, p.clean_weight).bias = a->bias + first;
     };
-    if (dhidden) weights_across(0, std::min<int64_t>(p.piece, a->vocab));
+    if (dhidden) clean_weights(0, std::min<int64_t>(p.piece, a->vocab));
     KLAY_DO(run_packs());
     const dim3 row_grid((uint32_t)tiles(a->rows, 4));
     if (teacher) KLAY_LAUNCH(klay::head_distill_adjoint_kernel, row_grid, dim3(256), stream, ad);
@@ -367,10 +357,8 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
         g.coefs = ad.coefs;
         g.entries = ad.entries;
         g.largest = ad.largest;
-        g.g = dhidden || (dweight && !wide_type) ? in(workspace, p.g) : nullptr;
-        g.g_across = dweight && wide_type ? in(workspace, p.g_across) : nullptr;
+        g.g = dhidden || dweight ? in(workspace, p.g) : nullptr;
         g.g_columns = columns;
-        g.g_rows = p.g_rows;
         g.bias_partial = dbias ? static_cast<float*>(in(workspace, p.db_sums)) : nullptr;
         KLAY_DO(klay::HeadLaunch<T>::adjoint(p.tile, g, stream));
         klay::ProductJob jobs[2] = {};
@@ -378,48 +366,40 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
         int n = 0;
         if (dhidden) {
             if (first > 0) {
-                weights_across(first, count);
+                clean_weights(first, count);
                 KLAY_DO(run_packs());
             }
             klay::ProductJob& j = jobs[n];
             job_tile[n++] = p.dh.tile;
             j.a = klay::Operand{g.g, columns * s.bytes, a->rows, (int32_t)(columns / s.lot)};
-            if (wide_type) j.b = klay::Operand{in(workspace, p.w_across), columns * s.bytes, a->width, (int32_t)(columns / s.lot)};
-            else if (copy_piece) j.b = klay::Operand{in(workspace, p.w_across), p.padded * s.bytes, p.padded, (int32_t)count};
-            else j.b = klay::Operand{g.weight.p, g.weight.stride, p.padded, (int32_t)count};
+            j.b = a->bias ? klay::Operand{in(workspace, p.clean_weight), p.padded * s.bytes, a->width, (int32_t)count}
+                          : klay::Operand{g.weight.p, g.weight.stride, a->width, (int32_t)count};
             j.splits = (int32_t)std::min<int64_t>(p.dh.splits, stages_of(columns, s));
             j.rows = a->rows;
             j.columns = a->width;
-            j.wide = p.wide;
-            j.out = whole && j.splits == 1 && p.wide == a->width ? dhidden : nullptr;
+            j.out = whole && j.splits == 1 ? dhidden : nullptr;
             j.sums = static_cast<float*>(in(workspace, p.dh_sums));
             j.add = first > 0;
-            if (first + p.piece >= a->vocab && !j.out)
-                sums.sum[sums.sums++] = klay::SumArgs{j.sums, a->rows, a->width, p.wide, a->rows * p.wide, whole ? j.splits : p.dh.splits, 1, dhidden};
+            const int64_t all = a->rows * a->width;
+            if (first + p.piece >= a->vocab && !j.out) sums.sum[sums.sums++] = klay::SumArgs{j.sums, all, all, whole ? j.splits : p.dh.splits, 1, dhidden};
         }
         if (dweight) {
             klay::ProductJob& j = jobs[n];
             job_tile[n++] = p.dw.tile;
-            if (wide_type) {
-                j.a = klay::Operand{g.g_across, p.g_rows * s.bytes, count, (int32_t)(p.g_rows / s.lot)};
-                j.b = klay::Operand{in(workspace, p.h_across), p.g_rows * s.bytes, a->width, (int32_t)(p.g_rows / s.lot)};
-            } else {
-                j.a_across = 1;
-                j.a = klay::Operand{g.g, columns * s.bytes, columns, (int32_t)a->rows};
-                j.b = klay::Operand{in(workspace, p.h_across), p.padded * s.bytes, p.padded, (int32_t)a->rows};
-            }
+            j.a_across = 1;
+            j.a = klay::Operand{g.g, columns * s.bytes, columns, (int32_t)a->rows};
+            j.b = klay::Operand{in(workspace, p.clean_hidden), p.padded * s.bytes, a->width, (int32_t)a->rows};
             j.splits = p.dw.splits;
             j.rows = count;
             j.columns = a->width;
-            j.wide = p.wide;
             void* out = static_cast<char*>(dweight) + first * a->width * s.bytes;
-            j.out = j.splits == 1 && p.wide == a->width ? out : nullptr;
+            j.out = j.splits == 1 ? out : nullptr;
             j.sums = static_cast<float*>(in(workspace, p.dw_sums));
             j.add = 0;
-            if (!j.out) sums.sum[sums.sums++] = klay::SumArgs{j.sums, count, a->width, p.wide, count * p.wide, j.splits, 1, out};
+            if (!j.out) sums.sum[sums.sums++] = klay::SumArgs{j.sums, count * a->width, count * a->width, j.splits, 1, out};
         }
         if (dbias)
-            sums.sum[sums.sums++] = klay::SumArgs{g.bias_partial, 1, count, count, columns, (int32_t)tiles(std::max(a->rows, g.g_across ? p.g_rows : 0), klay::kTileSizes[p.tile].rows), 0, dbias + first};
+            sums.sum[sums.sums++] = klay::SumArgs{g.bias_partial, count, columns, (int32_t)tiles(a->rows, klay::kTileSizes[p.tile].rows), 0, dbias + first};
         for (int i = 0; i < n;) {
             klay::ProductArgs pr{};
             pr.largest = ad.largest;

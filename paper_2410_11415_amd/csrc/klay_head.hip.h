@@ -3,7 +3,8 @@
 // and the logits of those that are; a wave a row joins them.  Backward, the tiles are made again, a piece of the vocabulary at a time, and turned
 // into the adjoint of the logits, which in all of these losses has the form
 //   G_ij = s_ij (A_i + B_i ln s_ij),  s_ij = e^((x_ij - ref_i) / T - ln S_i),
-// with an entry of its own for a listed token; then dH = G W, dW = G^T H, db = sum_i G_i.  G is rounded to the type of the operands (bf16: 2^-8 of an entry,
+// with an entry of its own for a listed token; then dH = G W, dW = G^T H, db = sum_i G_i, W, H and G^T read across from memory
+// that holds their rows.  G is rounded to the type of the operands (bf16: 2^-8 of an entry,
 // independent from entry to entry, as large as the rounding of the result; fp16: under a power of two taken from the largest entry, so that small
 // adjoints stay in its range; fp32: the three parts of all operands).  Sums over tokens and rows are in fp32, in an order that the sizes alone decide.
 #pragma once
@@ -19,6 +20,7 @@ struct HeadArgs {
     const float* bias;                      // of these tokens, or null
     int32_t first, vocab;                   // the first of these tokens; how many tokens there are in all
     int64_t rows;
+    int32_t tail;                           // elements of a row behind its last whole piece of 16 bytes
     int32_t num_tokens;
     const int32_t* sorted;                  // [rows, num_tokens]; null (num_tokens = 1): `list` as it was given, from its row list_row on
     ListArgs list;
@@ -31,18 +33,18 @@ struct HeadArgs {
     const float4* coefs;                    // [rows]: ref (+inf: the row has no gradient), ln S log2 e, A, B ln 2
     const float* entries;                   // [rows, num_tokens]
     const uint32_t* largest;                // bits of the largest adjoint (fp16), or null
-    void *g, *g_across;                     // [rows, g_columns]; fp32: and [g_columns, g_rows]; contiguous
-    int64_t g_columns, g_rows;
+    void* g;                                // [rows, g_columns], or null
+    int64_t g_columns;                      // a multiple of 8
     float* bias_partial;                    // [tiles of rows, g_columns], or null
 };
 
 // One product of a launch: `splits` runs over its stages, each into fp32 sums of its own or, if it is the only one of all pieces, into `out`.
 struct ProductJob {
-    Operand a, b;                           // 16-bit: b lies across, a where a_across
+    Operand a, b;                           // b lies across, a where a_across
     int32_t a_across, splits;
-    int64_t rows, columns, wide;            // wide: columns, up to a multiple of 4
-    void* out;                              // [rows, wide], or null
-    float* sums;                            // [splits, rows, wide]
+    int64_t rows, columns;
+    void* out;                              // [rows, columns], or null
+    float* sums;                            // [splits, rows, columns]
     int32_t add;                            // to what is there
 };
 struct ProductArgs {
@@ -138,6 +140,34 @@ __device__ __forceinline__ void add_bias(Tile& t, const HeadArgs& g, int64_t col
         }
 }
 
+// What the elements behind the last whole pieces add to the logits: through shared memory (`at`: 32 bytes a row and column), in fp32.
+template <typename Tile>
+__device__ __forceinline__ void add_tail(Tile& t, const HeadArgs& g, int64_t row0, int64_t column0, char* at) {
+    typedef typename Tile::Element T;
+    constexpr int ROWS = Tile::kN, COLUMNS = Tile::kM, MOST = 8;
+    float(*h)[MOST] = reinterpret_cast<float(*)[MOST]>(at), (*w)[MOST] = h + ROWS;
+    for (int i = threadIdx.x; i < (ROWS + COLUMNS) * MOST; i += Tile::kThreads) {
+        const int r = i / MOST, d = i % MOST;
+        const Operand& o = r < ROWS ? g.hidden : g.weight;
+        const int64_t row = r < ROWS ? row0 + r : column0 + r - ROWS;
+        h[r][d] = d < g.tail && row < o.rows ? (float)reinterpret_cast<const T*>(static_cast<const char*>(o.p) + row * o.stride + (int64_t)o.pieces * 16)[d] : 0.0f;
+    }
+    __syncthreads();
+    for (int d = 0; d < g.tail; ++d) {
+        float x[Tile::TN];
+#pragma unroll
+        for (int j = 0; j < Tile::TN; ++j) x[j] = h[t.row(j)][d];
+#pragma unroll
+        for (int i = 0; i < Tile::TM; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const float y = w[t.column(i) + 8 * (e >> 2) + (e & 3)][d];
+#pragma unroll
+                for (int j = 0; j < Tile::TN; ++j) t.acc[i][j][e] = fmaf(x[j], y, t.acc[i][j][e]);
+            }
+    }
+}
+
 // ---- forward ---------------------------------------------------------------------------------------------------------
 // What a lane finds out about its columns of its row of block j, and the other half of the wave about the others': y = x scale - shift with shift = max scale
 // rounded by itself is one multiply-add; what that rounding puts into all terms, 2^d, comes out again at the end.  WIDE takes the difference first, for
@@ -202,6 +232,7 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_for
     t.template run<false, false>(g.weight, g.hidden, column0, row0, 0, Tile::stages(g.hidden), sh.stage, [&] {
         if (g.num_tokens) sh.marks.make(g, row0, g.first + (int32_t)column0, threadIdx.x, Tile::kThreads);
     });
+    if (g.tail) add_tail(t, g, row0, column0, reinterpret_cast<char*>(sh.stage));
     if (some_bias<Tile>(g, column0)) add_bias(t, g, column0);
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
@@ -257,20 +288,19 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_adj
     t.template run<false, false>(g.weight, g.hidden, column0, row0, 0, Tile::stages(g.hidden), sh.stage, [&] {
         if (g.num_tokens) sh.marks.make(g, row0, g.first + (int32_t)column0, threadIdx.x, Tile::kThreads);
     });
+    if (g.tail) add_tail(t, g, row0, column0, reinterpret_cast<char*>(sh.stage));
     if (some_bias<Tile>(g, column0)) add_bias(t, g, column0);
     const bool last = column0 + COLUMNS > g.weight.rows;
     const float up = adjoint_scale(g.largest);
-    // where the tile lies in the two arrays: a lane's own offset, and one that is the same for all lanes
+    // where the tile lies: a lane's own offset, and one that is the same for all lanes
     const Stretch out = stretch_at(g.g ? static_cast<T*>(g.g) + row0 * g.g_columns + column0 : nullptr);
-    const Stretch across = stretch_at(g.g_across ? static_cast<T*>(g.g_across) + column0 * g.g_rows + row0 : nullptr);
-    const uint32_t wide = (uint32_t)(g.g_columns * sizeof(T)), high = (uint32_t)(g.g_rows * sizeof(T)), lower = 4 * (t.lane >> 5);
+    const uint32_t wide = (uint32_t)(g.g_columns * sizeof(T)), lower = 4 * (t.lane >> 5);
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
         const int64_t r = row0 + t.row(j);
         const float4 c = r < g.rows ? g.coefs[r] : make_float4(INFINITY, 0.0f, 0.0f, 0.0f);
         const bool live = c.x < INFINITY;
         const uint32_t at_out = g.g && r < g.rows ? t.row(j) * wide + lower * (uint32_t)sizeof(T) : kNoLane;
-        const uint32_t at_across = g.g_across && r < g.g_rows ? t.row(j) * (uint32_t)sizeof(T) + lower * high : kNoLane;
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             const uint32_t block = t.columns_from(i);
@@ -296,17 +326,11 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_adj
             }
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                if (column0 + block + 8 * q >= g.g_columns) break;      // (a multiple of 8, as g_rows)
+                if (column0 + block + 8 * q >= g.g_columns) break;      // (a multiple of 8)
                 float d[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) d[e] = t.acc[i][j][4 * q + e] * up;
                 store_row<4, T>(out, at_out, (block + 8 * q) * (uint32_t)sizeof(T), d);
-                if constexpr (sizeof(T) == 2) continue;          // (the products read it across)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float one[1] = {d[e]};
-                    store_row<1, T>(across, at_across, (block + 8 * q + e) * high, one);
-                }
             }
         }
     }
@@ -347,12 +371,8 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_pro
     const int64_t stages = job.a_across ? Tile::stages_across(job.a) : Tile::stages(job.a);
     const int32_t from = (int32_t)(stages * split / job.splits), to = (int32_t)(stages * (split + 1) / job.splits);
     Tile t;
-    if constexpr (sizeof(T) == 2) {
-        if (job.a_across) t.template run<true, true>(job.b, job.a, column0, row0, from, to, sh, [] {});
-        else t.template run<true, false>(job.b, job.a, column0, row0, from, to, sh, [] {});
-    } else {
-        t.template run<false, false>(job.b, job.a, column0, row0, from, to, sh, [] {});
-    }
+    if (job.a_across) t.template run<true, true>(job.b, job.a, column0, row0, from, to, sh, [] {});
+    else t.template run<true, false>(job.b, job.a, column0, row0, from, to, sh, [] {});
     const float down = 1.0f / adjoint_scale(g.largest);
 #pragma unroll
     for (int j = 0; j < Tile::TN; ++j) {
@@ -363,30 +383,44 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_pro
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int64_t c = column0 + t.column(i) + 8 * q;
-                if (c >= job.wide) continue;                      // (a multiple of 4)
+                if (c >= job.columns) continue;
+                const bool four = c + 4 <= job.columns;
                 float x[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[e] = t.acc[i][j][4 * q + e] * down;
                 if (job.out) {
-                    store_elements<4>(static_cast<T*>(job.out) + r * job.wide + c, x);
+                    T* out = static_cast<T*>(job.out) + r * job.columns + c;
+                    if (four) {
+                        store_elements<4>(out, x);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 3; ++e)
+                            if (c + e < job.columns) out[e] = (T)x[e];
+                    }
                     continue;
                 }
-                float* s = job.sums + ((int64_t)split * job.rows + r) * job.wide + c;
-                if (job.add) {
-                    float before[4];
-                    load_elements<4>(before, s);
+                float* s = job.sums + ((int64_t)split * job.rows + r) * job.columns + c;
+                if (four) {
+                    if (job.add) {
+                        float before[4];
+                        load_elements<4>(before, s);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] += before[e];
+                        for (int e = 0; e < 4; ++e) x[e] += before[e];
+                    }
+                    store_elements<4>(s, x);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 3; ++e)
+                        if (c + e < job.columns) s[e] = job.add ? s[e] + x[e] : x[e];
                 }
-                store_elements<4>(s, x);
             }
     }
 }
 
-// out[row][column] = sum over parts of from[part][row][column], in their order; rows of `from` are `wide` apart
+// out[i] = sum over parts of from[part][i], in their order
 struct SumArgs {
     const float* from;
-    int64_t rows, columns, wide, apart;
+    int64_t count, apart;
     int32_t parts, typed;                   // typed: out is of the operands' type, otherwise fp32
     void* out;
 };
@@ -398,18 +432,12 @@ template <typename T>
 __global__ void __launch_bounds__(256) head_sums_kernel(SumsArgs g) {
     for (int s = 0; s < g.sums; ++s) {
         const SumArgs& a = g.sum[s];
-        const int64_t all = a.rows * a.columns;
-        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-            int64_t at = i;
-            if (a.wide != a.columns) {
-                const int64_t r = i / a.columns;
-                at = r * a.wide + (i - r * a.columns);
-            }
-            float x = a.from[at];
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.count; i += (int64_t)gridDim.x * 256) {
+            float x = a.from[i];
             for (int32_t p = 1; p < a.parts; p += 8) {
                 float y[8];
 #pragma unroll
-                for (int q = 0; q < 8; ++q) y[q] = p + q < a.parts ? a.from[(p + q) * a.apart + at] : 0.0f;
+                for (int q = 0; q < 8; ++q) y[q] = p + q < a.parts ? a.from[(p + q) * a.apart + i] : 0.0f;
 #pragma unroll
                 for (int q = 0; q < 8; ++q) x += y[q];
             }
@@ -422,7 +450,6 @@ __global__ void __launch_bounds__(256) head_sums_kernel(SumsArgs g) {
 // Copies of a launch: workgroups until[i - 1] .. until[i] - 1 make copy i.
 struct PacksArgs {
     PackArgs copy[4];
-    int32_t across[4];
     uint32_t until[4];
     int32_t copies;
     uint32_t* clear;                        // a word that is made 0, or null
@@ -432,8 +459,7 @@ template <typename T> __global__ void __launch_bounds__(256) head_pack_kernel(Pa
     uint32_t first = 0;
     for (int i = 0; i < g.copies; ++i) {
         if (blockIdx.x < g.until[i]) {
-            if (g.across[i]) pack_across<T>(g.copy[i], blockIdx.x - first, g.until[i] - first);
-            else pack_rows<T>(g.copy[i], blockIdx.x - first, g.until[i] - first);
+            pack_rows<T>(g.copy[i], blockIdx.x - first, g.until[i] - first);
             return;
         }
         first = g.until[i];
@@ -452,7 +478,7 @@ template <typename T> struct HeadLaunch {
     static klay_status adjoint(HeadTile tile, const HeadArgs& g, void* stream);
     static klay_status products(HeadTile tile, const ProductArgs& g, void* stream);
     static klay_status sums(const SumsArgs& g, void* stream);
-    static klay_status pack(PacksArgs& g, void* stream);      // (copies, across, copy, clear given)
+    static klay_status pack(PacksArgs& g, void* stream);      // (copies, copy, clear given)
 };
 
 }  // namespace klay

@@ -35,7 +35,7 @@ template <typename Tile> klay_status run_forward(const HeadArgs& g, bool entropy
     return KLAY_OK;
 }
 template <typename Tile> klay_status run_adjoint(const HeadArgs& g, void* stream) {
-    const Tiles tiles = tiles_of<Tile>(std::max<int64_t>(g.rows, g.g_across ? g.g_rows : 0), g.g_columns);
+    const Tiles tiles = tiles_of<Tile>(g.rows, g.g_columns);
     KLAY_LAUNCH((head_adjoint_kernel<Tile>), dim3((uint32_t)(tiles.m * tiles.n)), dim3(Tile::kThreads), stream, g, tiles);
     return KLAY_OK;
 }
@@ -76,7 +76,7 @@ template <typename T> klay_status HeadLaunch<T>::products(HeadTile tile, const P
 }
 template <typename T> klay_status HeadLaunch<T>::sums(const SumsArgs& g, void* stream) {
     int64_t most = 0;
-    for (int i = 0; i < g.sums; ++i) most = std::max<int64_t>(most, g.sum[i].rows * g.sum[i].columns);
+    for (int i = 0; i < g.sums; ++i) most = std::max<int64_t>(most, g.sum[i].count);
     if (most > 0) KLAY_LAUNCH((head_sums_kernel<T>), dim3(grid_of(most, 256, 8192)), dim3(256), stream, g);
     return KLAY_OK;
 }
@@ -84,7 +84,7 @@ template <typename T> klay_status HeadLaunch<T>::pack(PacksArgs& g, void* stream
     uint32_t blocks = 0;
     for (int i = 0; i < g.copies; ++i) {
         const PackArgs& c = g.copy[i];
-        blocks += g.across[i] ? grid_of((c.padded + 63) / 64 * ((c.columns + 63) / 64), 1, 8192) : grid_of(c.count * (c.padded * (int64_t)sizeof(T) / 16), 256, 8192);
+        blocks += grid_of(c.count * (c.padded * (int64_t)sizeof(T) / 16), 256, 8192);
         g.until[i] = blocks;
     }
     if (blocks > 0 || g.clear) KLAY_LAUNCH((head_pack_kernel<T>), dim3(std::max<uint32_t>(blocks, 1)), dim3(256), stream, g);

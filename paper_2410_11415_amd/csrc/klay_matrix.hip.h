@@ -18,12 +18,13 @@ __device__ __forceinline__ Acc mma(Eight<f16> a, Eight<f16> b, Acc c) { return _
 constexpr int kMostStageBytes = 128;
 constexpr uint32_t kMostStride = 1u << 23;  // bytes from row to row: 256 rows lie within 31 bits
 
-// One side of a product: rows with k next to each other; or, of 16-bit elements, `across`: rows of k with the side's own rows next to each other.
+// One side of a product: rows with k next to each other; or, `across`, rows of k with the side's own rows next to each other.  Rows start at multiples of 4
+// bytes, and no byte behind the last one's end is read.
 struct Operand {
-    const void* p;                          // 16-byte aligned
-    int64_t stride;                         // bytes from row to row (across: from k to k), a multiple of 16, as long as a row at least, at most kMostStride
-    int64_t rows;                           // (across: a multiple of 8)
-    int32_t pieces;                         // 16-byte pieces of a row; what lies behind them reads as zeros.  Across: the number of k's
+    const void* p;
+    int64_t stride;                         // bytes from row to row (across: from k to k), a multiple of 4, as long as a row at least, at most kMostStride
+    int64_t rows;
+    int32_t pieces;                         // whole pieces of 16 bytes of a row; what lies behind them reads as zeros.  Across: the number of k's
 };
 
 // The 16-byte pieces of a stage's row lie permuted by the row's place among sixteen, so that the rows of a fragment come from all banks.
@@ -68,11 +69,13 @@ template <int ROWS, int HALVES, int WAVES, int SB> struct Stage {
                                                      in ? here + (first_row(half, i, 0) * stride + at * SB) : kNoLane, 0, 0, 0);
     }
 };
-// Likewise of an operand that lies across: 64 k's of 64 of its rows (128 bytes) after the other.  Every other pair of k's has its 64-byte halves exchanged, so that the
-// four k's of a transposing read come from all banks.  (Of rows behind the last one comes what lies there, for results that nobody stores.)
-template <int ROWS, int HALVES, int WAVES> struct StageAcross {
+// Likewise of an operand that lies across.  (Of rows behind the last one comes what lies there, for results that nobody stores.)
+template <int ROWS, int HALVES, int WAVES, int SB, int BYTES> struct StageAcross;
+// 16 bits: 64 k's of 64 of its rows (128 bytes) after the other.  Every other pair of k's has its 64-byte halves exchanged, so that the four k's of a transposing
+// read come from all banks.
+template <int ROWS, int HALVES, int WAVES, int SB> struct StageAcross<ROWS, HALVES, WAVES, SB, 2> {
     static constexpr int kAll = ROWS < 64 ? 64 : ROWS, kLoads = kAll / HALVES / 8 / WAVES;
-    static_assert(kAll % (HALVES * 64) == 0 && kAll % (HALVES * 8 * WAVES) == 0, "whole loads");
+    static_assert(SB == 128 && kAll % (HALVES * 64) == 0 && kAll % (HALVES * 8 * WAVES) == 0, "whole loads");
     const char* from;
     int64_t bytes;                          // from there to the operand's end
     uint32_t stride, offset;
@@ -80,7 +83,7 @@ template <int ROWS, int HALVES, int WAVES> struct StageAcross {
     __device__ __forceinline__ void init(const Operand& s, int64_t row0, int wave, int lane) {
         from = static_cast<const char*>(s.p) + row0 * 2;
         stride = (uint32_t)s.stride;
-        bytes = (s.pieces - 1) * s.stride + (s.rows - row0) * 2;
+        bytes = ((s.pieces - 1) * s.stride + (s.rows - row0) * 2 + 3) & ~(int64_t)3;     // (loads are in or out of range by four bytes)
         const int k = lane >> 3;
         offset = (uint32_t)k * stride + (uint32_t)((lane & 7) ^ (((k >> 1) & 1) << 2)) * 16u;
     }
@@ -94,6 +97,29 @@ template <int ROWS, int HALVES, int WAVES> struct StageAcross {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(stage, (__attribute__((address_space(3))) void*)(lds + place * 128), 16,
                                                      here + ((uint32_t)(place & 63) * stride + (uint32_t)(place & ~63) * 2u), 0, 0, 0);
         }
+    }
+};
+// 32 bits: the k's of a stage one after the other, a half's rows each.
+template <int ROWS, int HALVES, int WAVES, int SB> struct StageAcross<ROWS, HALVES, WAVES, SB, 4> {
+    static constexpr int kKs = SB / 4, kLong = ROWS / HALVES * 4, kEach = 1024 / kLong, kLoads = kKs / kEach / WAVES;
+    static_assert(kLong <= 1024 && kKs % (kEach * WAVES) == 0, "whole loads");
+    const char* from;
+    int64_t bytes;
+    uint32_t stride, offset;
+    __device__ __forceinline__ void init(const Operand& s, int64_t row0, int wave, int lane) {
+        from = static_cast<const char*>(s.p) + row0 * 4;
+        stride = (uint32_t)s.stride;
+        bytes = (s.pieces - 1) * s.stride + (s.rows - row0) * 4;
+        offset = (uint32_t)(wave * kEach + lane / (kLong / 16)) * stride + (uint32_t)(lane % (kLong / 16)) * 16u;
+    }
+    __device__ __forceinline__ void load(int half, int at, char* lds, int wave) const {
+        const int64_t gone = at * kKs * (int64_t)stride;
+        const Stretch stage = stretch_of(from + gone, gone < bytes ? bytes - gone : 0);
+        const uint32_t here = fresh(offset);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(stage, (__attribute__((address_space(3))) void*)(lds + half * kKs * kLong + (i * WAVES + wave) * 1024), 16,
+                                                     here + ((uint32_t)(i * WAVES * kEach) * stride + (uint32_t)(half * kLong)), 0, 0, 0);
     }
 };
 
@@ -110,8 +136,9 @@ template <typename T> struct Fragment {
     template <int SB> __device__ __forceinline__ void load(const char* lds, uint32_t at, int on, int s) {
         x = *reinterpret_cast<const Eight<T>*>(lds + (at ^ (uint32_t)(32 * s)) + on);
     }
-    // Of an operand that lies across (lane_place_across), `second` of a pair of blocks.
-    __device__ __forceinline__ void load_across(const char* lds, uint32_t at, int on, int second, int s) {
+    // Of an operand that lies across, `block` 32 rows on.
+    template <int LONG, int KS> __device__ __forceinline__ void load_across(const char* lds, uint32_t at, int half, int block, int s) {
+        const int blocks = half * (LONG / 64) + block, second = blocks & 1, on = blocks / 2 * 8192;      // (LONG: bytes of a k of a half)
         typedef short Shorts __attribute__((ext_vector_type(8)));
         FourShorts part[2];
 #pragma unroll
@@ -124,9 +151,12 @@ template <typename T, int SB> __device__ __forceinline__ uint32_t lane_place(int
     const int row = lane & 31, half = lane >> 5;
     return row * SB + place_of<SB>(row, sizeof(T) == 4 ? 2 * half : half) * 16;
 }
-__device__ __forceinline__ uint32_t lane_place_across(int lane) {
+// ... of an operand that lies across, LONG bytes of a k of a half of the tile, from row `wave0` of it on
+template <typename T, int LONG> __device__ __forceinline__ uint32_t lane_place_across(int lane, int wave0) {
+    if constexpr (sizeof(T) == 4) return (8 * (lane >> 5)) * LONG + (wave0 + (lane & 31)) * 4;
     const int in = lane & 15, group = lane >> 4;
-    return (8 * (group >> 1) + (in >> 2)) * 128 + ((in >> 3) & 1) * 64 + (group & 1) * 32 + (in & 3) * 8;
+    const uint32_t at = (8 * (group >> 1) + (in >> 2)) * 128 + ((in >> 3) & 1) * 64 + (group & 1) * 32 + (in & 3) * 8;
+    return (at ^ (wave0 & 32) * 2u) + (wave0 >> 6) * 8192u;
 }
 template <> struct Fragment<f32> {
     typedef float Four __attribute__((ext_vector_type(4)));
@@ -136,6 +166,10 @@ template <> struct Fragment<f32> {
     template <int SB> __device__ __forceinline__ void load(const char* lds, uint32_t at, int on, int s) {
 #pragma unroll
         for (int p = 0; p < 2; ++p) x[p] = *reinterpret_cast<const Four*>(lds + (at ^ (uint32_t)(64 * s + 16 * p)) + on);
+    }
+    template <int LONG, int KS> __device__ __forceinline__ void load_across(const char* lds, uint32_t at, int half, int block, int s) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e / 4][e % 4] = *reinterpret_cast<const float*>(lds + at + half * KS * LONG + (16 * s + e) * LONG + block * 128);
     }
     // Cut, not rounded: masks, subtractions and moves of bytes only, five and a half a number (conversions are slower: 760 us for 4096 x 1024 x 16384, @@).
     __device__ __forceinline__ void take_apart() {
@@ -183,24 +217,23 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
     static constexpr int kParts = SB / (16 * sizeof(T));        // sixteen k's each
     static constexpr bool kQuarters = TM % 2 == 0 && TN % 2 == 0 && S == 2;
     static constexpr int kHalves = kQuarters ? 2 : 1, HA = TM / kHalves, HB = TN / kHalves;      // of the tile's columns and rows; blocks of a wave in each
-    template <bool ACROSS> using LoadsA = std::conditional_t<ACROSS, StageAcross<BM, kHalves, kWaves>, Stage<BM, kHalves, kWaves, SB>>;
-    template <bool ACROSS> using LoadsB = std::conditional_t<ACROSS, StageAcross<BN, kHalves, kWaves>, Stage<BN, kHalves, kWaves, SB>>;
+    template <bool ACROSS> using LoadsA = std::conditional_t<ACROSS, StageAcross<BM, kHalves, kWaves, SB, sizeof(T)>, Stage<BM, kHalves, kWaves, SB>>;
+    template <bool ACROSS> using LoadsB = std::conditional_t<ACROSS, StageAcross<BN, kHalves, kWaves, SB, sizeof(T)>, Stage<BN, kHalves, kWaves, SB>>;
     typedef T Element;
     struct Shared {                         // one stage
         char a[BM * SB], b[(sizeof(T) == 2 && BN < 64 ? 64 : BN) * SB];
     };
-    static __device__ __forceinline__ int stages(const Operand& o) { return (o.pieces * 16 + SB - 1) / SB; }
-    static __device__ __forceinline__ int stages_across(const Operand& o) { return (o.pieces + 63) / 64; }
+    static __device__ __forceinline__ int stages(const Operand& o) { return o.pieces > 0 ? (o.pieces * 16 + SB - 1) / SB : 1; }
+    static __device__ __forceinline__ int stages_across(const Operand& o) { return (o.pieces + SB / (int)sizeof(T) - 1) / (SB / (int)sizeof(T)); }
     Acc acc[TM][TN];
     int wave, lane, wm, wn;
-    uint32_t lane_along, lane_across;
+    uint32_t lane_along;
     __device__ __forceinline__ Tile() {
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         lane = threadIdx.x & 63;
         wm = wave / WN;
         wn = wave % WN;
         lane_along = lane_place<T, SB>(lane);
-        lane_across = lane_place_across(lane);
     }
     // of the tile: a lane's first column of the i-th blocks (the others: + 8 q + e), its row of the j-th
     __device__ __forceinline__ int column(int i) const { return columns_from(i) + 4 * (lane >> 5); }
@@ -213,21 +246,21 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
     struct Fragments {
         Fragment<T> a[TM], b[TN];
     };
-    // `at`: the lane's place in the wave's first block; the block is `blocks` 32 rows on, of a wave whose blocks start at `wave0`
-    template <bool ACROSS> __device__ __forceinline__ void fetch(Fragment<T>& f, const char* lds, uint32_t at, int blocks, int s) const {
-        if constexpr (ACROSS) f.load_across(lds, at, blocks / 2 * 8192, blocks & 1, s);
-        else f.template load<SB>(lds, at, blocks * 32 * SB, s);
+    // The fragment of block `block` of a half of a side of ROWS rows; `at`: the lane's place in the wave's first block.
+    template <bool ACROSS, int ROWS> __device__ __forceinline__ void fetch(Fragment<T>& f, const char* lds, uint32_t at, int half, int block, int s) const {
+        if constexpr (ACROSS) f.template load_across<ROWS / kHalves * (int)sizeof(T), SB / (int)sizeof(T)>(lds, at, half, block, s);
+        else f.template load<SB>(lds, at, (half * (ROWS / kHalves) + block * 32) * SB, s);
     }
-    template <bool ACROSS> __device__ __forceinline__ uint32_t place(int wave0) const {
-        if constexpr (ACROSS) return fresh(lane_across ^ (wave0 & 32) * 2u) + (wave0 >> 6) * 8192u;
+    template <bool ACROSS, int ROWS> __device__ __forceinline__ uint32_t place(int wave0) const {
+        if constexpr (ACROSS) return lane_place_across<T, ROWS / kHalves * (int)sizeof(T)>(lane, wave0);
         else return fresh(lane_along) + wave0 * SB;
     }
     template <bool AA, bool BA> __device__ __forceinline__ void fetch(Fragments& f, const Shared& sh, int s) const {
-        const uint32_t a = place<AA>(columns_from(0)), b = place<BA>(rows_from(0));
+        const uint32_t a = place<AA, BM>(wm * HA * 32), b = place<BA, BN>(wn * HB * 32);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) fetch<BA>(f.b[j], sh.b, b, j, s);
+        for (int j = 0; j < TN; ++j) fetch<BA, BN>(f.b[j], sh.b, b, 0, j, s);
 #pragma unroll
-        for (int i = 0; i < TM; ++i) fetch<AA>(f.a[i], sh.a, a, i, s);
+        for (int i = 0; i < TM; ++i) fetch<AA, BM>(f.a[i], sh.a, a, 0, i, s);
     }
     __device__ __forceinline__ void multiply(Fragments& f) {
         auto all = [&](auto&& one) {
@@ -306,18 +339,18 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
     struct HalfA { Fragment<T> x[HA][kParts]; };
     struct HalfB { Fragment<T> x[HB][kParts]; };
     template <bool ACROSS> __device__ __forceinline__ void fetch(HalfA& f, const Shared& sh, int half) const {
-        const uint32_t at = place<ACROSS>(wm * HA * 32);
+        const uint32_t at = place<ACROSS, BM>(wm * HA * 32);
 #pragma unroll
         for (int i = 0; i < HA; ++i)
 #pragma unroll
-            for (int s = 0; s < kParts; ++s) fetch<ACROSS>(f.x[i][s], sh.a, at, half * (BM / 64) + i, s);
+            for (int s = 0; s < kParts; ++s) fetch<ACROSS, BM>(f.x[i][s], sh.a, at, half, i, s);
     }
     template <bool ACROSS> __device__ __forceinline__ void fetch(HalfB& f, const Shared& sh, int half) const {
-        const uint32_t at = place<ACROSS>(wn * HB * 32);
+        const uint32_t at = place<ACROSS, BN>(wn * HB * 32);
 #pragma unroll
         for (int j = 0; j < HB; ++j)
 #pragma unroll
-            for (int s = 0; s < kParts; ++s) fetch<ACROSS>(f.x[j][s], sh.b, at, half * (BN / 64) + j, s);
+            for (int s = 0; s < kParts; ++s) fetch<ACROSS, BN>(f.x[j][s], sh.b, at, half, j, s);
     }
     template <typename Half> static __device__ __forceinline__ void take_apart(Half& f) {
         if constexpr (std::is_same_v<T, f32>)
@@ -432,7 +465,6 @@ struct PackArgs {
     void* to;
     int64_t stride;                         // of the copy, elements
     int64_t padded;                         // elements of a row of the copy; zeros behind what is taken
-    int32_t wide;                           // rows start at multiples of 16 bytes
     int32_t finite;                         // 1: only what is finite is taken, zeros for the rest
     const float* bias;                      // of a row whose entry is -inf likewise; null: of none
 };
@@ -455,51 +487,6 @@ __device__ __forceinline__ void pack_rows(const PackArgs& g, int64_t block, int6
             for (int e = 0; e < N; ++e) out[e] = fabsf((float)out[e]) < INFINITY ? out[e] : (T)0.0f;
         }
         *reinterpret_cast<typename Pieces<T, N>::Vec*>(static_cast<T*>(g.to) + r * g.stride + c) = out;
-    }
-}
-
-// Rows and columns exchanged: copy[c][r], `padded` (a multiple of 16 bytes) next to each other, by squares of 64 x 64; 16 bytes a thread both ways where
-// the rows lie so (`wide`).
-template <typename T>
-__device__ __forceinline__ void pack_across(const PackArgs& g, int64_t block, int64_t blocks) {
-    constexpr int N = 16 / sizeof(T);
-    typedef typename Pieces<T, N>::Vec Vec;
-    __shared__ T square[64][64 + 4 / sizeof(T)];
-    const int64_t across = (g.columns + 63) / 64, all = (g.padded + 63) / 64 * across;
-    for (int64_t i = block; i < all; i += blocks) {
-        const int64_t r0 = i / across * 64, c0 = (i % across) * 64;
-#pragma unroll
-        for (int step = 0; step < 64 * 64 / N / 256; ++step) {
-            const int e = step * 256 + threadIdx.x, r = e / (64 / N), c = e % (64 / N) * N;
-            Vec x = {};
-            if (r0 + r < g.count) {
-                const T* row = static_cast<const T*>(g.from) + packed_row(g, r0 + r) + c0 + c;
-                if (g.wide && c0 + c + N <= g.columns) {
-                    x = *reinterpret_cast<const Vec*>(row);
-                } else {
-#pragma unroll
-                    for (int q = 0; q < N; ++q)
-                        if (c0 + c + q < g.columns) x[q] = row[q];
-                }
-                if (g.finite || (g.bias && g.bias[r0 + r] == -INFINITY)) {
-#pragma unroll
-                    for (int q = 0; q < N; ++q) x[q] = fabsf((float)x[q]) < INFINITY ? x[q] : (T)0.0f;
-                }
-            }
-#pragma unroll
-            for (int q = 0; q < N; ++q) square[r][c + q] = x[q];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int step = 0; step < 64 * 64 / N / 256; ++step) {
-            const int e = step * 256 + threadIdx.x, c = e / (64 / N), r = e % (64 / N) * N;
-            if (c0 + c >= g.columns || r0 + r >= g.padded) continue;
-            Vec out;
-#pragma unroll
-            for (int q = 0; q < N; ++q) out[q] = square[r + q][c];
-            *reinterpret_cast<Vec*>(static_cast<T*>(g.to) + (c0 + c) * g.stride + r0 + r) = out;
-        }
-        __syncthreads();
     }
 }
 

@@ -302,8 +302,8 @@ def head_logprobs(hidden, weight, tokens=None, bias=None, *, complement=False, e
     not allowed; a negative token asks for nothing, a token >= V gives NaN.  The gradients have the types of their inputs.  With 16-bit types the
     logits' adjoints are rounded to those bits before they meet the weights and the hidden states (float16: scaled into its range first).
 
-    Rows should start at multiples of 16 bytes, with D a multiple of 16 bytes; others are copied first.  At most 2^20 rows, 1024 tokens
-    a row.
+    Rows should start at multiples of 4 bytes (16 serve best), with one stride between them; others are copied first.  At most 2^20 rows, 1024
+    tokens a row.
     """
     _check_head(hidden, weight, bias, tokens)
     if tokens is None and complement:
