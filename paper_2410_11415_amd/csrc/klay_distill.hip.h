@@ -40,7 +40,7 @@ struct MassRun {
 constexpr int kChunk = 64;                  // vectors of a thread whose bits are held at a time
 
 // Few rows: a workgroup of sixteen waves each, whose first one puts the row together (FINISH).  Many: four waves each, which leave a row's sums, and a wave a
-// row afterwards, since the 64-bit arithmetic takes twice the registers of the run over the row (4096 x 131072 bf16 in one / in two: 334 / @@ us).
+// row afterwards, since the 64-bit arithmetic takes twice the registers of the run over the row (4096 x 131072 bf16 in one / in two: 334 / 212 us).
 template <typename T, int THREADS, bool FINISH>
 __global__ void __launch_bounds__(THREADS, FINISH ? 4 : 6) distill_row_kernel(DistillArgs g) {
     constexpr int N = 16 / sizeof(T), U = 4;

@@ -121,6 +121,7 @@ ProductPlan product_plan(klay::HeadTile tile, int64_t rows, int64_t columns, int
 constexpr int64_t kRowBlock = 16384;        // rows whose tiles' sums are held at a time
 constexpr int64_t kPieceElements = 1 << 25; // adjoints of logits that are held at a time, about
 constexpr int64_t kMostPiece = 1 << 20;
+constexpr int64_t kSmallCopy = 1 << 22;     // bytes of weights that are copied in as much time as a launch of its own takes
 constexpr int64_t kSmallProduct = 1ll << 30;    // up to here (rows x width x tokens) the two products are one launch, whatever tiles they would take alone
 
 struct HeadPlan {
@@ -166,7 +167,7 @@ HeadPlan head_plan(const klay_head_args* a, bool back) {
         p.tile = logits_tile(a->rows, columns);
         p.coefs = take(a->rows * sizeof(float4));
         p.entries = take(asked * 4);
-        p.largest = take(4);
+        p.largest = take(8);
         p.g = take(a->rows * columns * s.bytes);
         p.clean_hidden = take(a->rows * p.padded * s.bytes);
         if (a->bias) p.clean_weight = take(columns * p.padded * s.bytes);
@@ -332,19 +333,25 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
     ad.coefs = static_cast<float4*>(in(workspace, p.coefs));
     ad.entries = static_cast<float*>(in(workspace, p.entries));
     operands();
-    if (a->dtype == KLAY_F16) ad.largest = packs.clear = static_cast<uint32_t*>(in(workspace, p.largest));
+    uint32_t* const words = static_cast<uint32_t*>(in(workspace, p.largest));
+    if (a->dtype == KLAY_F16) ad.largest = words;
     // A row without a gradient gives none, whatever it holds: its adjoints are zeros, so that only what is not finite has to go.  (In a row that has one
     // the logits, and with them the adjoints, are NaN then.)
     if (dweight) pack(a->hidden, a->hidden_rows, a->rows, p.clean_hidden).finite = 1;
+    // Nor does a token that the bias bars, whatever its weights hold.  Few weights are copied along; many only if the adjoints' launch has found something in
+    // them that is not finite, since that would be as much to read and write as the products have.
+    const bool whole = p.piece >= a->vocab;             // one piece
+    const bool few = whole && a->vocab * a->width * s.bytes <= kSmallCopy;
+    uint32_t* const odd = dhidden && a->bias && !few ? words + 1 : nullptr;
     const auto clean_weights = [&](int64_t first, int64_t count) {
-        if (a->bias) pack(static_cast<const char*>(a->weight) + first * a->weight_stride * s.bytes, weight_rows(), count, p.clean_weight).bias = a->bias + first;
+        pack(static_cast<const char*>(a->weight) + first * a->weight_stride * s.bytes, weight_rows(), count, p.clean_weight).bias = a->bias + first;
     };
-    if (dhidden) clean_weights(0, std::min<int64_t>(p.piece, a->vocab));
+    if (dhidden && a->bias && few) clean_weights(0, a->vocab);
+    if (ad.largest || odd) packs.clear = words;
     KLAY_DO(run_packs());
     const dim3 row_grid((uint32_t)tiles(a->rows, 4));
     if (teacher) KLAY_LAUNCH(klay::head_distill_adjoint_kernel, row_grid, dim3(256), stream, ad);
     else KLAY_LAUNCH(klay::head_logprobs_adjoint_kernel, row_grid, dim3(256), stream, ad);
-    const bool whole = p.piece >= a->vocab;             // one piece
     klay::SumsArgs sums{};
     for (int64_t first = 0; first < a->vocab; first += p.piece) {
         const int64_t count = std::min(p.piece, a->vocab - first), columns = up(count, 8);
@@ -357,6 +364,7 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
         g.coefs = ad.coefs;
         g.entries = ad.entries;
         g.largest = ad.largest;
+        g.odd = odd;
         g.g = dhidden || dweight ? in(workspace, p.g) : nullptr;
         g.g_columns = columns;
         g.bias_partial = dbias ? static_cast<float*>(in(workspace, p.db_sums)) : nullptr;
@@ -365,15 +373,19 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
         klay::HeadTile job_tile[2];
         int n = 0;
         if (dhidden) {
-            if (first > 0) {
+            if (odd) {
                 clean_weights(first, count);
+                packs.only = odd;
                 KLAY_DO(run_packs());
             }
             klay::ProductJob& j = jobs[n];
             job_tile[n++] = p.dh.tile;
             j.a = klay::Operand{g.g, columns * s.bytes, a->rows, (int32_t)(columns / s.lot)};
-            j.b = a->bias ? klay::Operand{in(workspace, p.clean_weight), p.padded * s.bytes, a->width, (int32_t)count}
-                          : klay::Operand{g.weight.p, g.weight.stride, a->width, (int32_t)count};
+            j.odd = odd;
+            j.clean = in(workspace, p.clean_weight);
+            j.clean_stride = p.padded * s.bytes;
+            j.b = a->bias && few ? klay::Operand{j.clean, j.clean_stride, a->width, (int32_t)count}
+                                 : klay::Operand{g.weight.p, g.weight.stride, a->width, (int32_t)count};
             j.splits = (int32_t)std::min<int64_t>(p.dh.splits, stages_of(columns, s));
             j.rows = a->rows;
             j.columns = a->width;

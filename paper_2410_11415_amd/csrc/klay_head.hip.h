@@ -33,6 +33,7 @@ struct HeadArgs {
     const float4* coefs;                    // [rows]: ref (+inf: the row has no gradient), ln S log2 e, A, B ln 2
     const float* entries;                   // [rows, num_tokens]
     const uint32_t* largest;                // bits of the largest adjoint (fp16), or null
+    uint32_t* odd;                          // made 1 if a token that the bias bars may have weights that are not finite; or null
     void* g;                                // [rows, g_columns], or null
     int64_t g_columns;                      // a multiple of 8
     float* bias_partial;                    // [tiles of rows, g_columns], or null
@@ -41,6 +42,9 @@ struct HeadArgs {
 // One product of a launch: `splits` runs over its stages, each into fp32 sums of its own or, if it is the only one of all pieces, into `out`.
 struct ProductJob {
     Operand a, b;                           // b lies across, a where a_across
+    const uint32_t* odd;                    // null, or what decides whether b is rather a copy of it without what is not finite, `clean`, of this stride
+    const void* clean;
+    int64_t clean_stride;
     int32_t a_across, splits;
     int64_t rows, columns;
     void* out;                              // [rows, columns], or null
@@ -128,7 +132,8 @@ __device__ __forceinline__ void each_mark(const Tile& t, const M& marks, int j, 
 template <typename Tile>
 __device__ __forceinline__ bool some_bias(const HeadArgs& g, int64_t column0) { return g.bias != nullptr || column0 + Tile::kM > g.weight.rows; }
 template <typename Tile>
-__device__ __forceinline__ void add_bias(Tile& t, const HeadArgs& g, int64_t column0) {
+__device__ __forceinline__ bool add_bias(Tile& t, const HeadArgs& g, int64_t column0) {
+    bool odd = false;                       // (such a token's logits are not finite, whatever the row)
 #pragma unroll
     for (int i = 0; i < Tile::TM; ++i)
 #pragma unroll
@@ -136,8 +141,12 @@ __device__ __forceinline__ void add_bias(Tile& t, const HeadArgs& g, int64_t col
             const int64_t c = column0 + t.column(i) + 8 * (e >> 2) + (e & 3);
             const float b = c < g.weight.rows ? (g.bias ? g.bias[c] : 0.0f) : -INFINITY;
 #pragma unroll
-            for (int j = 0; j < Tile::TN; ++j) t.acc[i][j][e] = b == -INFINITY ? -INFINITY : t.acc[i][j][e] + b;
+            for (int j = 0; j < Tile::TN; ++j) {
+                odd |= b == -INFINITY && c < g.weight.rows && !(fabsf(t.acc[i][j][e]) < INFINITY);
+                t.acc[i][j][e] = b == -INFINITY ? -INFINITY : t.acc[i][j][e] + b;
+            }
         }
+    return odd;
 }
 
 // What the elements behind the last whole pieces add to the logits: through shared memory (`at`: 32 bytes a row and column), in fp32.
@@ -166,6 +175,7 @@ __device__ __forceinline__ void add_tail(Tile& t, const HeadArgs& g, int64_t row
                 for (int j = 0; j < Tile::TN; ++j) t.acc[i][j][e] = fmaf(x[j], y, t.acc[i][j][e]);
             }
     }
+    __syncthreads();
 }
 
 // ---- forward ---------------------------------------------------------------------------------------------------------
@@ -289,18 +299,15 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_adj
         if (g.num_tokens) sh.marks.make(g, row0, g.first + (int32_t)column0, threadIdx.x, Tile::kThreads);
     });
     if (g.tail) add_tail(t, g, row0, column0, reinterpret_cast<char*>(sh.stage));
-    if (some_bias<Tile>(g, column0)) add_bias(t, g, column0);
+    if (some_bias<Tile>(g, column0) && add_bias(t, g, column0) && g.odd) *g.odd = 1;
     const bool last = column0 + COLUMNS > g.weight.rows;
     const float up = adjoint_scale(g.largest);
-    // where the tile lies: a lane's own offset, and one that is the same for all lanes
-    const Stretch out = stretch_at(g.g ? static_cast<T*>(g.g) + row0 * g.g_columns + column0 : nullptr);
-    const uint32_t wide = (uint32_t)(g.g_columns * sizeof(T)), lower = 4 * (t.lane >> 5);
+    const uint32_t lower = 4 * (t.lane >> 5);
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
         const int64_t r = row0 + t.row(j);
         const float4 c = r < g.rows ? g.coefs[r] : make_float4(INFINITY, 0.0f, 0.0f, 0.0f);
         const bool live = c.x < INFINITY;
-        const uint32_t at_out = g.g && r < g.rows ? t.row(j) * wide + lower * (uint32_t)sizeof(T) : kNoLane;
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             const uint32_t block = t.columns_from(i);
@@ -324,16 +331,14 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_adj
                 for (int e = 0; e < 16; ++e)
                     if (column0 + t.column(i) + 8 * (e >> 2) + (e & 3) >= g.weight.rows) t.acc[i][j][e] = 0.0f;
             }
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                if (column0 + block + 8 * q >= g.g_columns) break;      // (a multiple of 8)
-                float d[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) d[e] = t.acc[i][j][4 * q + e] * up;
-                store_row<4, T>(out, at_out, (block + 8 * q) * (uint32_t)sizeof(T), d);
-            }
         }
     }
+    if (g.g)
+        t.template each_line<T>(reinterpret_cast<char*>(sh.stage), up, [&](int row, int column, const typename Tile::template Line<T>& x) {
+            const int64_t r = row0 + row, c = column0 + column;
+            if (r < g.rows && c < g.g_columns)                    // (a multiple of 8: whole lines)
+                *reinterpret_cast<typename Tile::template Line<T>*>(static_cast<T*>(g.g) + r * g.g_columns + c) = x;
+        });
     if (g.bias_partial) {
 #pragma unroll
         for (int i = 0; i < TM; ++i)
@@ -370,51 +375,45 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_pro
     const int64_t row0 = tr * Tile::kN, column0 = tc * Tile::kM;
     const int64_t stages = job.a_across ? Tile::stages_across(job.a) : Tile::stages(job.a);
     const int32_t from = (int32_t)(stages * split / job.splits), to = (int32_t)(stages * (split + 1) / job.splits);
-    Tile t;
-    if (job.a_across) t.template run<true, true>(job.b, job.a, column0, row0, from, to, sh, [] {});
-    else t.template run<true, false>(job.b, job.a, column0, row0, from, to, sh, [] {});
-    const float down = 1.0f / adjoint_scale(g.largest);
-#pragma unroll
-    for (int j = 0; j < Tile::TN; ++j) {
-        const int64_t r = row0 + t.row(j);
-        if (r >= job.rows) continue;
-#pragma unroll
-        for (int i = 0; i < Tile::TM; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int64_t c = column0 + t.column(i) + 8 * q;
-                if (c >= job.columns) continue;
-                const bool four = c + 4 <= job.columns;
-                float x[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = t.acc[i][j][4 * q + e] * down;
-                if (job.out) {
-                    T* out = static_cast<T*>(job.out) + r * job.columns + c;
-                    if (four) {
-                        store_elements<4>(out, x);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 3; ++e)
-                            if (c + e < job.columns) out[e] = (T)x[e];
-                    }
-                    continue;
-                }
-                float* s = job.sums + ((int64_t)split * job.rows + r) * job.columns + c;
-                if (four) {
-                    if (job.add) {
-                        float before[4];
-                        load_elements<4>(before, s);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) x[e] += before[e];
-                    }
-                    store_elements<4>(s, x);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 3; ++e)
-                        if (c + e < job.columns) s[e] = job.add ? s[e] + x[e] : x[e];
-                }
-            }
+    Operand b = job.b;
+    if (job.odd && *job.odd) {
+        b.p = job.clean;
+        b.stride = job.clean_stride;
     }
+    Tile t;
+    if (job.a_across) t.template run<true, true>(b, job.a, column0, row0, from, to, sh, [] {});
+    else t.template run<true, false>(b, job.a, column0, row0, from, to, sh, [] {});
+    const float down = 1.0f / adjoint_scale(g.largest);
+    char* const lds = reinterpret_cast<char*>(sh);
+    if (job.out) {
+        t.template each_line<T>(lds, down, [&](int row, int column, const typename Tile::template Line<T>& x) {
+            const int64_t r = row0 + row, c = column0 + column;
+            if (r >= job.rows || c >= job.columns) return;
+            constexpr int N = 16 / sizeof(T);
+            T* out = static_cast<T*>(job.out) + r * job.columns + c;
+            if (c + N <= job.columns) {
+                *reinterpret_cast<typename Pieces<T, N>::Loose*>(out) = x;
+            } else {
+#pragma unroll
+                for (int e = 0; e < N - 1; ++e)
+                    if (c + e < job.columns) out[e] = x[e];
+            }
+        });
+        return;
+    }
+    t.template each_line<float>(lds, down, [&](int row, int column, const typename Tile::template Line<float>& x) {
+        const int64_t r = row0 + row, c = column0 + column;
+        if (r >= job.rows || c >= job.columns) return;
+        float* s = job.sums + ((int64_t)split * job.rows + r) * job.columns + c;
+        if (c + 4 <= job.columns) {
+            auto* four = reinterpret_cast<typename Pieces<float, 4>::Loose*>(s);
+            *four = job.add ? *four + x : x;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (c + e < job.columns) s[e] = job.add ? s[e] + x[e] : x[e];
+        }
+    });
 }
 
 // out[i] = sum over parts of from[part][i], in their order
@@ -452,10 +451,12 @@ struct PacksArgs {
     PackArgs copy[4];
     uint32_t until[4];
     int32_t copies;
-    uint32_t* clear;                        // a word that is made 0, or null
+    uint32_t* clear;                        // two words that are made 0, or null
+    const uint32_t* only;                   // null, or: nothing is copied if this is 0
 };
 template <typename T> __global__ void __launch_bounds__(256) head_pack_kernel(PacksArgs g) {
-    if (g.clear && blockIdx.x == 0 && threadIdx.x == 0) *g.clear = 0;
+    if (g.clear && blockIdx.x == 0 && threadIdx.x < 2) g.clear[threadIdx.x] = 0;
+    if (g.only && *g.only == 0) return;
     uint32_t first = 0;
     for (int i = 0; i < g.copies; ++i) {
         if (blockIdx.x < g.until[i]) {
@@ -478,7 +479,7 @@ template <typename T> struct HeadLaunch {
     static klay_status adjoint(HeadTile tile, const HeadArgs& g, void* stream);
     static klay_status products(HeadTile tile, const ProductArgs& g, void* stream);
     static klay_status sums(const SumsArgs& g, void* stream);
-    static klay_status pack(PacksArgs& g, void* stream);      // (copies, copy, clear given)
+    static klay_status pack(PacksArgs& g, void* stream);      // (copies, copy, clear, only given)
 };
 
 }  // namespace klay

@@ -171,7 +171,7 @@ template <> struct Fragment<f32> {
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e / 4][e % 4] = *reinterpret_cast<const float*>(lds + at + half * KS * LONG + (16 * s + e) * LONG + block * 128);
     }
-    // Cut, not rounded: masks, subtractions and moves of bytes only, five and a half a number (conversions are slower: 760 us for 4096 x 1024 x 16384, @@).
+    // Cut, not rounded: masks, subtractions and moves of bytes only, five and a half a number (conversions are slower: 4096 x 1024 x 16384: 743 us with them, 712 so).
     __device__ __forceinline__ void take_apart() {
         typedef uint32_t Words __attribute__((ext_vector_type(4)));
         Words w[3];
@@ -241,6 +241,47 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
     // where a wave's i-th blocks of columns, its j-th of rows start
     __device__ __forceinline__ int columns_from(int i) const { return i / HA * (BM / kHalves) + (wm * HA + i % HA) * 32; }
     __device__ __forceinline__ int rows_from(int j) const { return j / HB * (BN / kHalves) + (wn * HB + j % HB) * 32; }
+
+    // The tile's elements, times `scale`, as U: put(row, column, x), x sixteen bytes of a row of the tile, neighbouring lanes next to each other.  Through the
+    // wave's own part of shared memory, which nothing else may be in: a lane's own elements are 8 or 16 bytes of 32 rows each, which costs a store of them as
+    // many cycles (the product of 16 rows' adjoints into 131072 x 4096 bf16: 522 us so, 378 through shared memory).
+    template <typename U> using Line = typename Pieces<U, 16 / sizeof(U)>::Vec;
+    template <typename U, typename F> __device__ __forceinline__ void each_line(char* lds, float scale, F&& put) const {
+        constexpr int N = 16 / sizeof(U), LINES = HA * 32 / N, LONG = LINES * 16, SAME = LONG < 256 ? 256 / LONG : 1;        // (SAME: rows in all banks)
+        static_assert(32 * LONG * kWaves <= S * sizeof(Shared), "rows of a block fit");
+        char* const mine = lds + wave * (32 * LONG);
+        const auto place = [](int row, int line) { return row * LONG + (line ^ ((row / SAME) & (LINES - 1))) * 16; };
+        const int to = lane & 31;
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+#pragma unroll
+                for (int i = 0; i < HA; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        float x[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] = acc[h * HA + i][j][4 * q + e] * scale;
+                        const int at = 32 * i + 8 * q + 4 * (lane >> 5);
+                        *reinterpret_cast<typename Pieces<U, 4>::Vec*>(mine + place(to, at / N) + at % N * sizeof(U)) = rounded<U, 4>(x);
+                    }
+                written();
+#pragma unroll
+                for (int k = 0; k < LINES / 2; ++k) {
+                    const int row = (64 * k + lane) / LINES, line = lane % LINES;
+                    put(rows_from(j) + row, columns_from(h * HA) + line * N, *reinterpret_cast<const Line<U>*>(mine + place(row, line)));
+                }
+                written();
+            }
+    }
+    // (a wave's accesses to shared memory keep their order: the compiler must, too)
+    static __device__ __forceinline__ void written() {
+#ifdef __HIP_DEVICE_COMPILE__
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+#endif
+    }
 
     // What a matrix instruction of each block takes: sixteen k's.
     struct Fragments {

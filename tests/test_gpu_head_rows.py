@@ -1,0 +1,151 @@
+"""Heads whose rows begin and end anywhere (GPU): starts and strides of single elements, widths behind whole pieces of 16 bytes, memory of others around
+the inputs and the gradients; weights that the bias bars, many and few; two calls at once; all of the operators in one step of training."""
+import pytest
+import torch
+
+from paper_2410_11415_amd import binding, operators
+from tests import head_ref as ref
+from tests.test_gpu_head import DTYPES, adjoints, check_distill, check_tokens, ids, klay, make
+
+pytestmark = pytest.mark.gpu
+
+
+def among(t, start, extra, fill=float("nan")):
+    """t in memory of others: its first element `start` behind a multiple of 256 bytes, its rows `extra` elements apart"""
+    rows, width = t.shape
+    stride = width + extra
+    big = torch.full((start + rows * stride + 64,), fill, dtype=t.dtype, device="cuda")
+    view = big.as_strided((rows, width), (stride, 1), start)
+    view.copy_(t)
+    return view
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("width", [1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15, 17, 30, 31, 33, 62, 63, 66, 71, 127, 129])
+def test_widths(width, dtype):
+    hidden, weight, bias, tokens, g = make(37, width, 141, 2, dtype, 40)
+    check_tokens(hidden, weight, bias, tokens, g)
+    check_distill(hidden, weight, bias, tokens, g, temperature=0.7)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("width", [3, 8, 21, 66])
+@pytest.mark.parametrize("hidden_at,weight_at", [((0, 0), (1, 0)), ((1, 1), (0, 2)), ((2, 0), (2, 2)), ((3, 4), (6, 0)), ((2, 6), (5, 3)), ((4, 1), (0, 1)), ((0, 3), (0, 8))])
+def test_rows_anywhere(hidden_at, weight_at, width, dtype):
+    """nothing of what lies around a row is taken for a part of it"""
+    hidden, weight, bias, tokens, g = make(41, width, 150, 3, dtype, 41)
+    given = among(hidden, *hidden_at), among(weight, *weight_at)
+    check_tokens(hidden, weight, bias, tokens, g, given=given)
+    check_distill(hidden, weight, bias, tokens, g, given=given, rest=True)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("rows,width,vocab", [(300, 45, 9000), (600, 130, 3001), (40, 1027, 2000)])
+def test_large_tiles_of_odd_widths(rows, width, vocab, dtype):
+    hidden, weight, bias, tokens, g = make(rows, width, vocab, 2, dtype, 42)
+    given = among(hidden, 2, 2 + width % 2), among(weight, 4, 2 + width % 2)
+    check_tokens(hidden, weight, bias, tokens, g, given=given)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("rows,width,vocab", [(5, 3, 7), (33, 19, 130), (70, 66, 257), (300, 45, 9000)])
+def test_gradients_end_where_they_end(rows, width, vocab, dtype):
+    """what lies behind the gradients stays as it was"""
+    hidden, weight, bias, tokens, g = make(rows, width, vocab, 1, dtype, 43)
+    args, _ = operators._head_args(hidden, weight, bias, tokens)
+    logp, kept = torch.empty(rows, 1, device="cuda"), operators._kept(hidden, args)
+    work, size = operators._workspace(hidden, args, False)
+    stream = operators._stream(args.device)
+    binding.klay_head_forward(args, logp.data_ptr(), None, None, kept.data_ptr(), work.data_ptr(), size, stream)
+    d = torch.randn(rows, 1, generator=g, device="cuda")
+    room = [torch.full((t.numel() + 100,), 7.0, dtype=t.dtype, device="cuda") for t in (hidden, weight, bias)]
+    work, size = operators._workspace(hidden, args, True)
+    binding.klay_head_backward(args, kept.data_ptr(), d.data_ptr(), None, None, *(t.data_ptr() for t in room), work.data_ptr(), size, stream)
+    inputs = [t.detach().requires_grad_(True) for t in (hidden, weight, bias)]
+    want = torch.autograd.grad(klay().head_logprobs(inputs[0], inputs[1], tokens, inputs[2]).logp, inputs, d)
+    for got, grad in zip(room, want):
+        assert torch.equal(got[:grad.numel()].view(grad.shape), grad) and bool((got[grad.numel():] == 7).all())
+
+
+# weights of a few bytes, which are copied along; of more than 4 MB, which are only if need be; in several pieces of the vocabulary
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("rows,width,vocab", [(30, 40, 500), (40, 520, 9001), (21, 1101, 4003), (2100, 121, 20011)])
+@pytest.mark.parametrize("first", [0, 0.9])
+def test_barred_weights_hold_anything(first, rows, width, vocab, dtype):
+    hidden, weight, bias, tokens, g = make(rows, width, vocab, 1, dtype, 44)
+    gone = torch.rand(vocab, generator=g, device="cuda") < 0.3
+    gone[:int(first * vocab)] = False
+    bias[gone] = -torch.inf
+    d = torch.randn(rows, 1, generator=g, device="cuda")
+    out = []
+    for hole in (0.0, float("nan"), float("inf"), -float("inf")):
+        w = weight.clone()
+        w[gone, :: 7] = hole
+        inputs = [t.detach().requires_grad_(True) for t in (hidden, w, bias)]
+        r = klay().head_logprobs(inputs[0], inputs[1], tokens, inputs[2])
+        grads = torch.autograd.grad(r.logp, inputs, d)
+        assert all(bool(torch.isfinite(t).all()) for t in grads)
+        out.append((r.logp, *grads))
+    for other in out[1:]:
+        for a, b in zip(out[0], other):
+            assert torch.equal(a, b)
+
+
+def test_calls_on_two_streams_at_once():
+    made = [make(rows, 130, 5000, 2, torch.bfloat16, 45) for rows in (70, 300)]
+    streams = [torch.cuda.Stream() for _ in made]
+
+    def step(hidden, weight, bias, tokens, grad):
+        inputs = [t.detach().requires_grad_(True) for t in (hidden, weight, bias)]
+        r = klay().head_logprobs(inputs[0], inputs[1], tokens, inputs[2], entropy=True)
+        return (r.logp, *torch.autograd.grad([r.logp, r.entropy], inputs, grad))
+    grads = [adjoints(m[4], m[3].shape, m[3].shape[:1]) for m in made]
+    want = [step(*m[:4], d) for m, d in zip(made, grads)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(4):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(step(*made[i][:4], grads[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for turn in got[i]:
+            for a, b in zip(turn, want[i]):
+                assert torch.equal(a, b)
+
+
+def test_the_same_index_twice_and_the_same_tensor_as_both():
+    """tokens listed twice count twice; weights that are the hidden states themselves get both gradients"""
+    x = torch.randn(24, 40, device="cuda")
+    t = torch.tensor([[3, 3, 5]], device="cuda").expand(24, 3)
+    a = x.clone().requires_grad_(True)
+    both, = torch.autograd.grad(klay().head_logprobs(a, a, t).logp.sum(), a)
+    b, c = x.clone().requires_grad_(True), x.clone().requires_grad_(True)
+    one, other = torch.autograd.grad(klay().head_logprobs(b, c, t).logp.sum(), (b, c))
+    assert torch.equal(both, one + other)
+    z = torch.tensor([[1.0, 1.0, -1.0]], device="cuda").expand(24, 3)
+    check_distill(x, x.clone(), None, t.contiguous(), torch.Generator(device="cuda").manual_seed(3))
+    assert bool(torch.isfinite(klay().head_distill(x, x, t, z)).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+def test_a_step_of_training_from_a_teacher(dtype):
+    """the teacher's top tokens, the student's divergence from them, its own answers' log probabilities: as they are used together"""
+    hidden, weight, bias, tokens, g = make(60, 48, 700, 1, dtype, 46)
+    teacher = hidden.float() @ weight.float().t() + 0.5 * torch.randn(60, 700, generator=g, device="cuda")
+    top = klay().token_logprobs(teacher, top=8)
+    inputs = [t.detach().requires_grad_(True) for t in (hidden, weight, bias)]
+    loss = klay().head_distill(inputs[0], inputs[1], top.top_tokens, top.top_logp, inputs[2], rest=True).mean() - \
+        klay().head_logprobs(inputs[0], inputs[1], tokens, inputs[2]).logp.mean()
+    got = torch.autograd.grad(loss, inputs)
+    x, slip = ref.logits_of(hidden, weight, bias)
+    up = torch.full((60,), 1 / 60.0, device="cuda").double()
+    a, dx_a, tol_a = ref.distill(x, top.top_tokens, top.top_logp, 1.0, True, slip, up)
+    b, dx_b, tol_b = ref.tokens(x, tokens, slip, -up[:, None])
+    want = ref.gradients(dx_a, tol_a, hidden, weight), ref.gradients(dx_b, tol_b, hidden, weight)
+    for grad, name in zip(got, ("dhidden", "dweight", "dbias")):
+        (va, ta), (vb, tb) = want[0][name], want[1][name]
+        # two gradients rounded to the type, and their sum, no larger than both
+        half = torch.finfo(grad.dtype).eps / 2
+        most = va.abs() + vb.abs() + ta + tb
+        assert bool(((grad.double() - va - vb).abs() <= ta + tb + 2 * half * (1 + half) * most + 3 * ref.TINY[grad.dtype]).all()), name
