@@ -106,9 +106,10 @@ struct ProductPlan {
     int32_t splits;
 };
 // The largest tile of which there are as many as CUs, its stages shared out where need be, at least eight each.
-klay::HeadTile product_tile(int64_t rows, int64_t columns, int64_t stages) {
+klay::HeadTile product_tile(int64_t rows, int64_t columns, int64_t stages, const Sizes& s) {
     if (rows <= 32) return klay::TILE_32;
     if (rows <= 64) return klay::TILE_64;
+    if (stages == 1 && s.bytes == 2) return klay::TILE_ONE;
     const int64_t large = tiles(rows, klay::kTileSizes[klay::TILE_256].rows) * tiles(columns, klay::kTileSizes[klay::TILE_256].columns);
     return rows > 128 && columns > 128 && large * std::min<int64_t>(stages / 8, 8) >= 192 ? klay::TILE_256 : klay::TILE_128;
 }
@@ -172,7 +173,7 @@ HeadPlan head_plan(const klay_head_args* a, bool back) {
         p.clean_hidden = take(a->rows * p.padded * s.bytes);
         if (a->bias) p.clean_weight = take(columns * p.padded * s.bytes);
         const int64_t dw_rows = std::min<int64_t>(p.piece, a->vocab), dh_stages = stages_of(columns, s), dw_stages = stages_of(a->rows, s);
-        klay::HeadTile dh = product_tile(a->rows, a->width, dh_stages), dw = product_tile(dw_rows, a->width, dw_stages);
+        klay::HeadTile dh = product_tile(a->rows, a->width, dh_stages, s), dw = product_tile(dw_rows, a->width, dw_stages, s);
         if (a->rows * a->width * dw_rows < kSmallProduct) dh = dw = std::min(dh, dw);
         p.dh = product_plan(dh, a->rows, a->width, dh_stages);
         p.dw = product_plan(dw, dw_rows, a->width, dw_stages);
@@ -406,6 +407,7 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
             j.columns = a->width;
             void* out = static_cast<char*>(dweight) + first * a->width * s.bytes;
             j.out = j.splits == 1 ? out : nullptr;
+            j.stream = a->width * s.bytes % 128 == 0 && reinterpret_cast<uintptr_t>(out) % 128 == 0;
             j.sums = static_cast<float*>(in(workspace, p.dw_sums));
             j.add = 0;
             if (!j.out) sums.sum[sums.sums++] = klay::SumArgs{j.sums, count * a->width, count * a->width, j.splits, 1, out};

@@ -48,6 +48,7 @@ struct ProductJob {
     int32_t a_across, splits;
     int64_t rows, columns;
     void* out;                              // [rows, columns], or null
+    int32_t stream;                         // out past the caches: its rows are whole lines of 128 bytes
     float* sums;                            // [splits, rows, columns]
     int32_t add;                            // to what is there
 };
@@ -386,34 +387,41 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_pro
     const float down = 1.0f / adjoint_scale(g.largest);
     char* const lds = reinterpret_cast<char*>(sh);
     if (job.out) {
-        t.template each_line<T>(lds, down, [&](int row, int column, const typename Tile::template Line<T>& x) {
+        auto put = [&](int row, int column, const typename Tile::template Line<T>& x, auto past) {
             const int64_t r = row0 + row, c = column0 + column;
             if (r >= job.rows || c >= job.columns) return;
             constexpr int N = 16 / sizeof(T);
             T* out = static_cast<T*>(job.out) + r * job.columns + c;
             if (c + N <= job.columns) {
-                *reinterpret_cast<typename Pieces<T, N>::Loose*>(out) = x;
+                auto* line = reinterpret_cast<typename Pieces<T, N>::Loose*>(out);
+                if constexpr (past) __builtin_nontemporal_store(x, line);
+                else *line = x;
             } else {
 #pragma unroll
                 for (int e = 0; e < N - 1; ++e)
                     if (c + e < job.columns) out[e] = x[e];
             }
-        });
+        };
+        if (Tile::kStages == 1 && job.stream)
+            t.template each_line<T>(lds, down, [&](int row, int column, const auto& x) { put(row, column, x, std::true_type{}); });
+        else
+            t.template each_line<T>(lds, down, [&](int row, int column, const auto& x) { put(row, column, x, std::false_type{}); });
         return;
     }
-    t.template each_line<float>(lds, down, [&](int row, int column, const typename Tile::template Line<float>& x) {
-        const int64_t r = row0 + row, c = column0 + column;
-        if (r >= job.rows || c >= job.columns) return;
-        float* s = job.sums + ((int64_t)split * job.rows + r) * job.columns + c;
-        if (c + 4 <= job.columns) {
-            auto* four = reinterpret_cast<typename Pieces<float, 4>::Loose*>(s);
-            *four = job.add ? *four + x : x;
-        } else {
+    if constexpr (Tile::kStages > 1)                              // (a single stage: the only sum)
+        t.template each_line<float>(lds, down, [&](int row, int column, const typename Tile::template Line<float>& x) {
+            const int64_t r = row0 + row, c = column0 + column;
+            if (r >= job.rows || c >= job.columns) return;
+            float* s = job.sums + ((int64_t)split * job.rows + r) * job.columns + c;
+            if (c + 4 <= job.columns) {
+                auto* four = reinterpret_cast<typename Pieces<float, 4>::Loose*>(s);
+                *four = job.add ? *four + x : x;
+            } else {
 #pragma unroll
-            for (int e = 0; e < 3; ++e)
-                if (c + e < job.columns) s[e] = job.add ? s[e] + x[e] : x[e];
-        }
-    });
+                for (int e = 0; e < 3; ++e)
+                    if (c + e < job.columns) s[e] = job.add ? s[e] + x[e] : x[e];
+            }
+        });
 }
 
 // out[i] = sum over parts of from[part][i], in their order
@@ -468,11 +476,11 @@ template <typename T> __global__ void __launch_bounds__(256) head_pack_kernel(Pa
 }
 
 // ---- launches of a type, each type in a translation unit of its own -------------------------------------------------
-enum HeadTile : int { TILE_32, TILE_64, TILE_128, TILE_256 };
+enum HeadTile : int { TILE_32, TILE_64, TILE_128, TILE_256, TILE_ONE };    // (TILE_ONE: products of a single stage, 128 x 128)
 struct TileSize {
     int rows, columns;
 };
-constexpr TileSize kTileSizes[] = {{32, 128}, {64, 128}, {128, 128}, {256, 256}};
+constexpr TileSize kTileSizes[] = {{32, 128}, {64, 128}, {128, 128}, {256, 256}, {128, 128}};
 
 template <typename T> struct HeadLaunch {
     static klay_status forward(HeadTile tile, const HeadArgs& g, bool entropy, void* stream);

@@ -10,6 +10,10 @@ namespace klay {
 
 template <typename T> using Tile32 = Tile<T, 128, 32, 4, 1, 3, 128>;
 template <typename T> using Tile64 = Tile<T, 128, 64, 4, 1, 3, 128>;
+// The weights' gradient of at most 64 rows is all writing: little shared memory, for more workgroups at a time, and rows of 256 bytes a wave, past the caches
+// where they are whole lines (16 x 4096 x 131072 bf16: 280 us; 318 through the caches, 378 by Tile128.  Rows that share lines take twice the time past the
+// caches; fp32 takes 448 us by it and 395 by Tile128, 20 x 3214 x 96569).
+template <typename T> using TileOne = Tile<T, 128, 128, 1, 4, 1, 128>;
 template <typename T> struct Large {
     typedef Tile<T, 128, 128, 2, 2, 2, 128> Tile128;
     typedef Tile<T, 256, 256, 2, 4, 2, 128> Tile256;
@@ -67,6 +71,8 @@ template <typename T> klay_status HeadLaunch<T>::adjoint(HeadTile tile, const He
     }
 }
 template <typename T> klay_status HeadLaunch<T>::products(HeadTile tile, const ProductArgs& g, void* stream) {
+    if constexpr (sizeof(T) == 2)
+        if (tile == TILE_ONE) return run_products<TileOne<T>>(g, stream);
     switch (tile) {
         case TILE_32: return run_products<Tile32<T>>(g, stream);
         case TILE_64: return run_products<Tile64<T>>(g, stream);
@@ -105,3 +111,4 @@ template <typename T> klay_status HeadLaunch<T>::pack(PacksArgs& g, void* stream
     KLAY_HEAD_TILE(klay::Tile128<klay::T>)    \
     KLAY_HEAD_TILE(klay::Tile256<klay::T>)    \
     template struct klay::HeadLaunch<klay::T>;
+#define KLAY_HEAD_ONE(T) template __global__ void klay::head_product_kernel<klay::TileOne<klay::T>>(klay::ProductArgs, int64_t);

@@ -362,13 +362,14 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
                 for (int part = 0; part < kParts; ++part) {
                     fetch<AA, BA>(f, sh[s], part);
                     if (part == kParts - 1 && kt + s + 1 < to) {
-                        arrived<(S - 2) * kLoads>();
+                        arrived<(S > 1 ? S - 2 : 0) * kLoads>();
                         la.load(0, kt + s + S, sh[s].a, wave);
                         lb.load(0, kt + s + S, sh[s].b, wave);
                     }
                     multiply(f);
                 }
                 if (kt + s + 1 >= to) break;
+                if constexpr (S == 1) arrived<0>();
             }
         }
     }

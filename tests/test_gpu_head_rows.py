@@ -48,6 +48,13 @@ def test_large_tiles_of_odd_widths(rows, width, vocab, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("rows,width,vocab", [(64, 1024, 16400), (64, 1027, 16400), (33, 2240, 16001), (65, 1024, 16384)])
+def test_few_rows_of_large_weights(rows, width, vocab, dtype):
+    hidden, weight, bias, tokens, g = make(rows, width, vocab, 1, dtype, 47)
+    check_tokens(hidden, weight, bias, tokens, g)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
 @pytest.mark.parametrize("rows,width,vocab", [(5, 3, 7), (33, 19, 130), (70, 66, 257), (300, 45, 9000)])
 def test_gradients_end_where_they_end(rows, width, vocab, dtype):
     """what lies behind the gradients stays as it was"""
