@@ -132,12 +132,23 @@ struct HeadPlan {
     klay::HeadTile tile = klay::TILE_32;
     // backward
     int64_t piece = 0;
+    int64_t cut = 1;                        // numbers of the operands' type that an adjoint is held in
     ProductPlan dh{}, dw{};
     // bytes from the start of the workspace
     size_t hidden = 0, weight = 0, partial = 0, kept = 0, coefs = 0, entries = 0, largest = 0, g = 0, clean_hidden = 0, clean_weight = 0,
            dh_sums = 0, dw_sums = 0, db_sums = 0, bytes = 0;
 };
 int64_t stages_of(int64_t elements, const Sizes& s) { return tiles(elements * s.bytes, klay::kMostStageBytes); }
+
+// Adjoints of 16-bit heads are rounded to 16 bits as the products' operands.  Over many entries that makes 1.41 times the error that the results' own rounding
+// makes; where a few entries make a result (a row's own tokens, mostly) or equal ones do, it can be 2.5 times.  There what the rounding leaves is held as well,
+// as rows of its own: for 16 rows and for small products it costs next to nothing (bf16, a step of training, 16 x 4096 x 131072: 869 us, 856 without),
+// otherwise up to a quarter (64 and 128 rows: 1127 and 1430, 883 and 1179 without), and up to 256 entries.
+constexpr int64_t kFewEntries = 256, kSmallCut = 1ll << 32;     // (entries; rows x width x tokens)
+int64_t cut_of(const klay_head_args* a, const Sizes& s) {
+    const bool few = a->rows <= 16 || a->rows * std::max(a->num_tokens, 1) <= kFewEntries || (double)a->rows * a->width * a->vocab < kSmallCut;
+    return s.bytes == 2 && few ? 2 : 1;
+}
 
 HeadPlan head_plan(const klay_head_args* a, bool back) {
     const Sizes s(a->dtype);
@@ -165,19 +176,21 @@ HeadPlan head_plan(const klay_head_args* a, bool back) {
         const int64_t all = up(a->vocab, 256);
         p.piece = std::min({all, kMostPiece, std::max<int64_t>(256, kPieceElements / up(a->rows, 256) / 256 * 256)});
         const int64_t columns = up(std::min<int64_t>(p.piece, a->vocab), 8);
+        p.cut = cut_of(a, s);
+        const int64_t rows = p.cut * a->rows;       // of the adjoints
         p.tile = logits_tile(a->rows, columns);
         p.coefs = take(a->rows * sizeof(float4));
         p.entries = take(asked * 4);
         p.largest = take(8);
-        p.g = take(a->rows * columns * s.bytes);
-        p.clean_hidden = take(a->rows * p.padded * s.bytes);
+        p.g = take(rows * columns * s.bytes);
+        p.clean_hidden = take(rows * p.padded * s.bytes);
         if (a->bias) p.clean_weight = take(columns * p.padded * s.bytes);
-        const int64_t dw_rows = std::min<int64_t>(p.piece, a->vocab), dh_stages = stages_of(columns, s), dw_stages = stages_of(a->rows, s);
-        klay::HeadTile dh = product_tile(a->rows, a->width, dh_stages, s), dw = product_tile(dw_rows, a->width, dw_stages, s);
+        const int64_t dw_rows = std::min<int64_t>(p.piece, a->vocab), dh_stages = stages_of(columns, s), dw_stages = stages_of(rows, s);
+        klay::HeadTile dh = product_tile(rows, a->width, dh_stages, s), dw = product_tile(dw_rows, a->width, dw_stages, s);
         if (a->rows * a->width * dw_rows < kSmallProduct) dh = dw = std::min(dh, dw);
-        p.dh = product_plan(dh, a->rows, a->width, dh_stages);
+        p.dh = product_plan(dh, rows, a->width, dh_stages);
         p.dw = product_plan(dw, dw_rows, a->width, dw_stages);
-        p.dh_sums = take(p.dh.splits * a->rows * a->width * 4);
+        p.dh_sums = take(p.dh.splits * rows * a->width * 4);
         p.dw_sums = take(p.dw.splits == 1 ? 0 : p.dw.splits * columns * a->width * 4);
         p.db_sums = take(tiles(a->rows, klay::kTileSizes[p.tile].rows) * columns * 4);
     }
@@ -338,7 +351,7 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
     if (a->dtype == KLAY_F16) ad.largest = words;
     // A row without a gradient gives none, whatever it holds: its adjoints are zeros, so that only what is not finite has to go.  (In a row that has one
     // the logits, and with them the adjoints, are NaN then.)
-    if (dweight) pack(a->hidden, a->hidden_rows, a->rows, p.clean_hidden).finite = 1;
+    for (int64_t i = 0; dweight && i < p.cut; ++i) pack(a->hidden, a->hidden_rows, a->rows, p.clean_hidden + i * a->rows * p.padded * s.bytes).finite = 1;
     // Nor does a token that the bias bars, whatever its weights hold.  Few weights are copied along; many only if the adjoints' launch has found something in
     // them that is not finite, since that would be as much to read and write as the products have.
     const bool whole = p.piece >= a->vocab;             // one piece
@@ -367,6 +380,7 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
         g.largest = ad.largest;
         g.odd = odd;
         g.g = dhidden || dweight ? in(workspace, p.g) : nullptr;
+        g.g_low = g.g && p.cut == 2 ? static_cast<char*>(g.g) + a->rows * columns * s.bytes : nullptr;
         g.g_columns = columns;
         g.bias_partial = dbias ? static_cast<float*>(in(workspace, p.db_sums)) : nullptr;
         KLAY_DO(klay::HeadLaunch<T>::adjoint(p.tile, g, stream));
@@ -381,27 +395,27 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
             }
             klay::ProductJob& j = jobs[n];
             job_tile[n++] = p.dh.tile;
-            j.a = klay::Operand{g.g, columns * s.bytes, a->rows, (int32_t)(columns / s.lot)};
+            j.a = klay::Operand{g.g, columns * s.bytes, p.cut * a->rows, (int32_t)(columns / s.lot)};
             j.odd = odd;
             j.clean = in(workspace, p.clean_weight);
             j.clean_stride = p.padded * s.bytes;
             j.b = a->bias && few ? klay::Operand{j.clean, j.clean_stride, a->width, (int32_t)count}
                                  : klay::Operand{g.weight.p, g.weight.stride, a->width, (int32_t)count};
             j.splits = (int32_t)std::min<int64_t>(p.dh.splits, stages_of(columns, s));
-            j.rows = a->rows;
+            j.rows = p.cut * a->rows;
             j.columns = a->width;
-            j.out = whole && j.splits == 1 ? dhidden : nullptr;
+            j.out = whole && j.splits * p.cut == 1 ? dhidden : nullptr;
             j.sums = static_cast<float*>(in(workspace, p.dh_sums));
             j.add = first > 0;
             const int64_t all = a->rows * a->width;
-            if (first + p.piece >= a->vocab && !j.out) sums.sum[sums.sums++] = klay::SumArgs{j.sums, all, all, whole ? j.splits : p.dh.splits, 1, dhidden};
+            if (first + p.piece >= a->vocab && !j.out) sums.sum[sums.sums++] = klay::SumArgs{j.sums, all, all, (int32_t)((whole ? j.splits : p.dh.splits) * p.cut), 1, dhidden};
         }
         if (dweight) {
             klay::ProductJob& j = jobs[n];
             job_tile[n++] = p.dw.tile;
             j.a_across = 1;
-            j.a = klay::Operand{g.g, columns * s.bytes, columns, (int32_t)a->rows};
-            j.b = klay::Operand{in(workspace, p.clean_hidden), p.padded * s.bytes, a->width, (int32_t)a->rows};
+            j.a = klay::Operand{g.g, columns * s.bytes, columns, (int32_t)(p.cut * a->rows)};
+            j.b = klay::Operand{in(workspace, p.clean_hidden), p.padded * s.bytes, a->width, (int32_t)(p.cut * a->rows)};
             j.splits = p.dw.splits;
             j.rows = count;
             j.columns = a->width;

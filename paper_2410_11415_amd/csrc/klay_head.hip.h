@@ -4,9 +4,10 @@
 // into the adjoint of the logits, which in all of these losses has the form
 //   G_ij = s_ij (A_i + B_i ln s_ij),  s_ij = e^((x_ij - ref_i) / T - ln S_i),
 // with an entry of its own for a listed token; then dH = G W, dW = G^T H, db = sum_i G_i, W, H and G^T read across from memory
-// that holds their rows.  G is rounded to the type of the operands (bf16: 2^-8 of an entry,
-// independent from entry to entry, as large as the rounding of the result; fp16: under a power of two taken from the largest entry, so that small
-// adjoints stay in its range; fp32: the three parts of all operands).  Sums over tokens and rows are in fp32, in an order that the sizes alone decide.
+// that holds their rows.  G is rounded to the type of the operands
+// (bf16: 2^-8 of an entry at most, independent from entry to entry, so that a sum of many is off by as much again as its own rounding; of few entries a second
+// number of the type holds what the first leaves; fp16: under a power of two taken from the largest entry, so that small adjoints stay in its range; fp32: the
+// three parts of all operands).  Sums over tokens and rows are in fp32, in an order that the sizes alone decide.
 #pragma once
 
 #include "klay_lists.hip.h"
@@ -35,6 +36,7 @@ struct HeadArgs {
     const uint32_t* largest;                // bits of the largest adjoint (fp16), or null
     uint32_t* odd;                          // made 1 if a token that the bias bars may have weights that are not finite; or null
     void* g;                                // [rows, g_columns], or null
+    void* g_low;                            // likewise: what the rounding has left of g, or null
     int64_t g_columns;                      // a multiple of 8
     float* bias_partial;                    // [tiles of rows, g_columns], or null
 };
@@ -334,12 +336,14 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_adj
             }
         }
     }
-    if (g.g)
-        t.template each_line<T>(reinterpret_cast<char*>(sh.stage), up, [&](int row, int column, const typename Tile::template Line<T>& x) {
+    const auto write = [&](void* to, float scale) {
+        t.template each_line<T>(reinterpret_cast<char*>(sh.stage), scale, [&](int row, int column, const typename Tile::template Line<T>& x) {
             const int64_t r = row0 + row, c = column0 + column;
             if (r < g.rows && c < g.g_columns)                    // (a multiple of 8: whole lines)
-                *reinterpret_cast<typename Tile::template Line<T>*>(static_cast<T*>(g.g) + r * g.g_columns + c) = x;
+                *reinterpret_cast<typename Tile::template Line<T>*>(static_cast<T*>(to) + r * g.g_columns + c) = x;
         });
+    };
+    if (g.g) write(g.g, up);
     if (g.bias_partial) {
 #pragma unroll
         for (int i = 0; i < TM; ++i)
@@ -359,6 +363,19 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kThreads / 256) head_adj
             if (column0 + c < g.g_columns) g.bias_partial[tr * g.g_columns + column0 + c] = s;
         }
     }
+    if constexpr (sizeof(T) == 2)
+        if (g.g_low) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float d = t.acc[i][j][e] * up, low = d - (float)(T)d;
+                        t.acc[i][j][e] = low == low ? low : 0.0f;          // (of an infinity nothing is left)
+                    }
+            write(g.g_low, 1.0f);
+        }
 }
 
 template <typename Tile>
@@ -456,8 +473,8 @@ __global__ void __launch_bounds__(256) head_sums_kernel(SumsArgs g) {
 
 // Copies of a launch: workgroups until[i - 1] .. until[i] - 1 make copy i.
 struct PacksArgs {
-    PackArgs copy[4];
-    uint32_t until[4];
+    PackArgs copy[5];
+    uint32_t until[5];
     int32_t copies;
     uint32_t* clear;                        // two words that are made 0, or null
     const uint32_t* only;                   // null, or: nothing is copied if this is 0

@@ -156,3 +156,23 @@ def test_a_step_of_training_from_a_teacher(dtype):
         half = torch.finfo(grad.dtype).eps / 2
         most = va.abs() + vb.abs() + ta + tb
         assert bool(((grad.double() - va - vb).abs() <= ta + tb + 2 * half * (1 + half) * most + 3 * ref.TINY[grad.dtype]).all()), name
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("rows,vocab", [(20, 2), (60, 2), (200, 4000), (900, 20000)])
+def test_long_sums_lean_to_no_side(rows, vocab, dtype):
+    """The mean error of many logits, each a sum of 8192 terms most of which have its sign.  A row's sum is rounded once every sixteen k's, by half a step of
+    at most the sum, 2^-24: spread like a walk of 512 steps of 2^-24 / sqrt(3), 7.8e-7 of it, and their mean over the rows 1 / sqrt(rows) of that, five times
+    of which are allowed; to this the products of parts of fp32 that are not made, 2^-24, and a rounding of the result."""
+    g = torch.Generator(device="cuda").manual_seed(48)
+    w0 = torch.randn(8192, generator=g, device="cuda")
+    hidden = (torch.randn(rows, 8192, generator=g, device="cuda") + 0.5 * w0).to(dtype)
+    weight = torch.zeros(vocab, 8192, dtype=dtype, device="cuda")
+    weight[0] = (w0 * (80 / 8192)).to(dtype)
+    x = hidden.double() @ weight[0].double()
+    assert float(x.min()) > 30
+    tokens = torch.zeros(rows, 1, dtype=torch.int64, device="cuda")
+    got = -klay().head_logprobs(hidden, weight, tokens, complement=True).neg[:, 0].double()     # ln(1 + e^x / (V - 1))
+    want = x - torch.log(torch.tensor(vocab - 1.0).double()) + torch.log1p((vocab - 1) * torch.exp(-x))
+    mean = ((got - want) / x).mean().abs()
+    assert float(mean) <= 5 * 7.8e-7 / rows ** 0.5 + 2.0 ** -24 + 2.0 ** -24
