@@ -106,10 +106,9 @@ struct ProductPlan {
     int32_t splits;
 };
 // The largest tile of which there are as many as CUs, its stages shared out where need be, at least eight each.
-klay::HeadTile product_tile(int64_t rows, int64_t columns, int64_t stages, const Sizes& s) {
+klay::HeadTile product_tile(int64_t rows, int64_t columns, int64_t stages) {
     if (rows <= 32) return klay::TILE_32;
     if (rows <= 64) return klay::TILE_64;
-    if (stages == 1 && s.bytes == 2) return klay::TILE_ONE;
     const int64_t large = tiles(rows, klay::kTileSizes[klay::TILE_256].rows) * tiles(columns, klay::kTileSizes[klay::TILE_256].columns);
     return rows > 128 && columns > 128 && large * std::min<int64_t>(stages / 8, 8) >= 192 ? klay::TILE_256 : klay::TILE_128;
 }
@@ -186,8 +185,9 @@ HeadPlan head_plan(const klay_head_args* a, bool back) {
         p.clean_hidden = take(rows * p.padded * s.bytes);
         if (a->bias) p.clean_weight = take(columns * p.padded * s.bytes);
         const int64_t dw_rows = std::min<int64_t>(p.piece, a->vocab), dh_stages = stages_of(columns, s), dw_stages = stages_of(rows, s);
-        klay::HeadTile dh = product_tile(rows, a->width, dh_stages, s), dw = product_tile(dw_rows, a->width, dw_stages, s);
+        klay::HeadTile dh = product_tile(rows, a->width, dh_stages), dw = product_tile(dw_rows, a->width, dw_stages);
         if (a->rows * a->width * dw_rows < kSmallProduct) dh = dw = std::min(dh, dw);
+        else if (dw_stages == 1 && dw_rows > 64 && s.bytes == 2) dw = klay::TILE_ONE;      // (always a single sum, stored as it is)
         p.dh = product_plan(dh, rows, a->width, dh_stages);
         p.dw = product_plan(dw, dw_rows, a->width, dw_stages);
         p.dh_sums = take(p.dh.splits * rows * a->width * 4);
@@ -408,7 +408,8 @@ klay_status Head<T>::backward(const klay_teacher* teacher, const Kept& kept, con
             j.sums = static_cast<float*>(in(workspace, p.dh_sums));
             j.add = first > 0;
             const int64_t all = a->rows * a->width;
-            if (first + p.piece >= a->vocab && !j.out) sums.sum[sums.sums++] = klay::SumArgs{j.sums, all, all, (int32_t)((whole ? j.splits : p.dh.splits) * p.cut), 1, dhidden};
+            const int32_t parts = (int32_t)((whole ? j.splits : p.dh.splits) * p.cut);
+            if (first + p.piece >= a->vocab && !j.out) sums.sum[sums.sums++] = klay::SumArgs{j.sums, all, all, parts, 1, dhidden};
         }
         if (dweight) {
             klay::ProductJob& j = jobs[n];

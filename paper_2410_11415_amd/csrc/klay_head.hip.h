@@ -162,7 +162,8 @@ __device__ __forceinline__ void add_tail(Tile& t, const HeadArgs& g, int64_t row
         const int r = i / MOST, d = i % MOST;
         const Operand& o = r < ROWS ? g.hidden : g.weight;
         const int64_t row = r < ROWS ? row0 + r : column0 + r - ROWS;
-        h[r][d] = d < g.tail && row < o.rows ? (float)reinterpret_cast<const T*>(static_cast<const char*>(o.p) + row * o.stride + (int64_t)o.pieces * 16)[d] : 0.0f;
+        const T* from = reinterpret_cast<const T*>(static_cast<const char*>(o.p) + row * o.stride + (int64_t)o.pieces * 16);
+        h[r][d] = d < g.tail && row < o.rows ? (float)from[d] : 0.0f;
     }
     __syncthreads();
     for (int d = 0; d < g.tail; ++d) {
@@ -493,7 +494,7 @@ template <typename T> __global__ void __launch_bounds__(256) head_pack_kernel(Pa
 }
 
 // ---- launches of a type, each type in a translation unit of its own -------------------------------------------------
-enum HeadTile : int { TILE_32, TILE_64, TILE_128, TILE_256, TILE_ONE };    // (TILE_ONE: products of a single stage, 128 x 128)
+enum HeadTile : int { TILE_32, TILE_64, TILE_128, TILE_256, TILE_ONE };    // (TILE_ONE: weights' gradients of a single stage, 128 x 128)
 struct TileSize {
     int rows, columns;
 };

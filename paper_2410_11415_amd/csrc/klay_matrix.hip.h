@@ -19,7 +19,7 @@ constexpr int kMostStageBytes = 128;
 constexpr uint32_t kMostStride = 1u << 23;  // bytes from row to row: 256 rows lie within 31 bits
 
 // One side of a product: rows with k next to each other; or, `across`, rows of k with the side's own rows next to each other.  Rows start at multiples of 4
-// bytes, and no byte behind the last one's end is read.
+// bytes, and nothing is read behind the four bytes that the last one ends in.
 struct Operand {
     const void* p;
     int64_t stride;                         // bytes from row to row (across: from k to k), a multiple of 4, as long as a row at least, at most kMostStride
@@ -171,7 +171,8 @@ template <> struct Fragment<f32> {
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e / 4][e % 4] = *reinterpret_cast<const float*>(lds + at + half * KS * LONG + (16 * s + e) * LONG + block * 128);
     }
-    // Cut, not rounded: masks, subtractions and moves of bytes only, five and a half a number (conversions are slower: 4096 x 1024 x 16384: 743 us with them, 712 so).
+    // Cut, not rounded: masks, subtractions and moves of bytes only, five and a half a number (with conversions the loop of 4096 x 1024 x 16384 took 743
+    // us for 712).
     __device__ __forceinline__ void take_apart() {
         typedef uint32_t Words __attribute__((ext_vector_type(4)));
         Words w[3];

@@ -48,7 +48,8 @@ def test_large_tiles_of_odd_widths(rows, width, vocab, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=ids)
-@pytest.mark.parametrize("rows,width,vocab", [(64, 1024, 16400), (64, 1027, 16400), (33, 2240, 16001), (65, 1024, 16384)])
+@pytest.mark.parametrize("rows,width,vocab", [(64, 1024, 16400), (64, 1027, 16400), (33, 2240, 16001), (65, 1024, 16384), (32, 2560, 16384), (20000, 1024, 60),
+                                             (24, 40000, 2000), (16, 550000, 130)])
 def test_few_rows_of_large_weights(rows, width, vocab, dtype):
     hidden, weight, bias, tokens, g = make(rows, width, vocab, 1, dtype, 47)
     check_tokens(hidden, weight, bias, tokens, g)
