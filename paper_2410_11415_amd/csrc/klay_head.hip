@@ -140,13 +140,12 @@ struct HeadPlan {
 int64_t stages_of(int64_t elements, const Sizes& s) { return tiles(elements * s.bytes, klay::kMostStageBytes); }
 
 // Adjoints of 16-bit heads are rounded to 16 bits as the products' operands.  Over many entries that makes 1.41 times the error that the results' own rounding
-// makes; where a few entries make a result (a row's own tokens, mostly) or equal ones do, it can be 2.5 times.  There what the rounding leaves is held as well,
-// as rows of its own: for 16 rows and for small products it costs next to nothing (bf16, a step of training, 16 x 4096 x 131072: 869 us, 856 without),
-// otherwise up to a quarter (64 and 128 rows: 1127 and 1430, 883 and 1179 without), and up to 256 entries.
-constexpr int64_t kFewEntries = 256, kSmallCut = 1ll << 32;     // (entries; rows x width x tokens)
+// makes; where a few entries make a result (one of a row's own tokens, mostly) or equal ones do, it can be 2.5 times.  There what the rounding leaves is held as
+// well, as rows of its own: for 16 rows and for small products it costs next to nothing (bf16, a step of training, 16 x 4096 x 131072: 863 us, 856 without),
+// otherwise a quarter or more (64 and 128 rows: 1132 and 1421, 883 and 1179 without; 512 would be 3211, 2302 without), which 256 rows are worth.
+constexpr int64_t kFewRows = 256, kSmallCut = 1ll << 32;     // (rows x width x tokens)
 int64_t cut_of(const klay_head_args* a, const Sizes& s) {
-    const bool few = a->rows <= 16 || a->rows * std::max(a->num_tokens, 1) <= kFewEntries || (double)a->rows * a->width * a->vocab < kSmallCut;
-    return s.bytes == 2 && few ? 2 : 1;
+    return s.bytes == 2 && (a->rows <= kFewRows || (double)a->rows * a->width * a->vocab < kSmallCut) ? 2 : 1;
 }
 
 HeadPlan head_plan(const klay_head_args* a, bool back) {
@@ -187,7 +186,7 @@ HeadPlan head_plan(const klay_head_args* a, bool back) {
         const int64_t dw_rows = std::min<int64_t>(p.piece, a->vocab), dh_stages = stages_of(columns, s), dw_stages = stages_of(rows, s);
         klay::HeadTile dh = product_tile(rows, a->width, dh_stages), dw = product_tile(dw_rows, a->width, dw_stages);
         if (a->rows * a->width * dw_rows < kSmallProduct) dh = dw = std::min(dh, dw);
-        else if (dw_stages == 1 && dw_rows > 64 && s.bytes == 2) dw = klay::TILE_ONE;      // (always a single sum, stored as it is)
+        else if (dw_stages == 1 && dw_rows > 64) dw = klay::TILE_ONE;      // (always a single sum, stored as it is)
         p.dh = product_plan(dh, rows, a->width, dh_stages);
         p.dw = product_plan(dw, dw_rows, a->width, dw_stages);
         p.dh_sums = take(p.dh.splits * rows * a->width * 4);

@@ -10,21 +10,24 @@ namespace klay {
 
 template <typename T> using Tile32 = Tile<T, 128, 32, 4, 1, 3, 128>;
 template <typename T> using Tile64 = Tile<T, 128, 64, 4, 1, 3, 128>;
-// The weights' gradient of at most 64 rows is all writing: little shared memory, for more workgroups at a time, and rows of 256 bytes a wave, past the caches
-// where they are whole lines (16 x 4096 x 131072 bf16: 280 us; 318 through the caches, 378 by Tile128.  Rows that share lines take twice the time past the
-// caches; fp32 takes 448 us by it and 395 by Tile128, 20 x 3214 x 96569).
-template <typename T> using TileOne = Tile<T, 128, 128, 1, 4, 1, 128>;
+// TileOne: the weights' gradient of at most 64 rows (fp32: 32) is all writing: little shared memory, for more workgroups at a time, and in 16 bits rows of 256
+// bytes a wave, past the caches where they are whole lines (16 x 4096 x 131072 bf16: 280 us; 318 through the caches, 378 by Tile128.  Rows that share lines take
+// twice the time past the caches).
 template <typename T> struct Large {
     typedef Tile<T, 128, 128, 2, 2, 2, 128> Tile128;
     typedef Tile<T, 256, 256, 2, 4, 2, 128> Tile256;
+    typedef Tile<T, 128, 128, 1, 4, 1, 128> TileOne;
 };
-// fp32: six products a pair of elements, so that a quarter of the k's are as long a stage
+// fp32: six products a pair of elements, so that a quarter of the k's is as long a stage for the largest tile; the next one adds its sums half as often with
+// 32 k's a stage (1183 x 3272 x 7032: 477 us, 528 with sixteen), and writes better with sixteen (20 x 3214 x 96569: 395, 447 with 32, 448 in a single stage).
 template <> struct Large<f32> {
-    typedef Tile<f32, 128, 128, 2, 2, 2, 64> Tile128;
+    typedef Tile<f32, 128, 128, 2, 2, 2, 128> Tile128;
     typedef Tile<f32, 256, 256, 2, 4, 2, 64> Tile256;
+    typedef Tile<f32, 128, 128, 2, 2, 2, 64> TileOne;
 };
 template <typename T> using Tile128 = typename Large<T>::Tile128;
 template <typename T> using Tile256 = typename Large<T>::Tile256;
+template <typename T> using TileOne = typename Large<T>::TileOne;
 
 template <typename Tile> Tiles tiles_of(int64_t rows, int64_t columns) {
     return Tiles{(rows + Tile::kN - 1) / Tile::kN, (columns + Tile::kM - 1) / Tile::kM};
@@ -71,12 +74,11 @@ template <typename T> klay_status HeadLaunch<T>::adjoint(HeadTile tile, const He
     }
 }
 template <typename T> klay_status HeadLaunch<T>::products(HeadTile tile, const ProductArgs& g, void* stream) {
-    if constexpr (sizeof(T) == 2)
-        if (tile == TILE_ONE) return run_products<TileOne<T>>(g, stream);
     switch (tile) {
         case TILE_32: return run_products<Tile32<T>>(g, stream);
         case TILE_64: return run_products<Tile64<T>>(g, stream);
         case TILE_128: return run_products<Tile128<T>>(g, stream);
+        case TILE_ONE: return run_products<TileOne<T>>(g, stream);
         default: return run_products<Tile256<T>>(g, stream);
     }
 }
@@ -110,5 +112,5 @@ template <typename T> klay_status HeadLaunch<T>::pack(PacksArgs& g, void* stream
     KLAY_HEAD_TILE(klay::Tile64<klay::T>)     \
     KLAY_HEAD_TILE(klay::Tile128<klay::T>)    \
     KLAY_HEAD_TILE(klay::Tile256<klay::T>)    \
+    template __global__ void klay::head_product_kernel<klay::TileOne<klay::T>>(klay::ProductArgs, int64_t); \
     template struct klay::HeadLaunch<klay::T>;
-#define KLAY_HEAD_ONE(T) template __global__ void klay::head_product_kernel<klay::TileOne<klay::T>>(klay::ProductArgs, int64_t);

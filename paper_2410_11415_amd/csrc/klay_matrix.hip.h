@@ -197,7 +197,7 @@ template <> struct Fragment<f32> {
 // The products of a pair of fragments, by `first` and then `all`, which make one of them for all pairs.  fp32: into a sum of their own from the smallest ones on,
 // which joins the others' in one addition.  By themselves the small ones are below half a step of a long sum and all of the sign of the terms, as the parts
 // are cut: a sum over 4096 loses 5e-6 of itself then, and is 2.4e-7 off so (as by multiply-adds one after the other).  The additions cost: 4096 x 1024 x 16384
-// 690 us without them, 812 so.  Sums over two stages of the smaller tile, for which there should be registers, spilled.
+// 690 us without them, 812 so.
 template <typename T, typename First, typename All> __device__ __forceinline__ void products(First&& first, All&& all) {
     typedef Fragment<T> F;
     if constexpr (std::is_same_v<T, f32>) {
@@ -416,10 +416,10 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
                 for (auto& x : row) x.take_apart();
     }
     template <int FROM, int TO> __device__ __forceinline__ void multiply(const HalfA& a, const HalfB& b, int ha, int hb) {
+        Acc sum[HA][HB];
+        const auto at = [&](int i, int j) -> Acc& { return kApartSums ? sum[i][j] : acc[ha * HA + i][hb * HB + j]; };
 #pragma unroll
         for (int s = FROM; s < TO; ++s) {
-            Acc sum[HA][HB];
-            const auto at = [&](int i, int j) -> Acc& { return kApartSums ? sum[i][j] : acc[ha * HA + i][hb * HB + j]; };
             const auto all = [&](auto&& one) {
 #pragma unroll
                 for (int i = 0; i < HA; ++i)
@@ -430,15 +430,15 @@ template <typename T, int BM, int BN, int WM, int WN, int S, int SB> struct Tile
 #pragma unroll
                 for (int i = 0; i < HA; ++i)
 #pragma unroll
-                    for (int j = 0; j < HB; ++j) at(i, j) = one(a.x[i][s], b.x[j][s], kApartSums ? Acc{} : at(i, j));
+                    for (int j = 0; j < HB; ++j) at(i, j) = one(a.x[i][s], b.x[j][s], kApartSums && s == FROM ? Acc{} : at(i, j));
             };
             products<T>(first, all);
-            if constexpr (kApartSums) {
+        }
+        if constexpr (kApartSums) {
 #pragma unroll
-                for (int i = 0; i < HA; ++i)
+            for (int i = 0; i < HA; ++i)
 #pragma unroll
-                    for (int j = 0; j < HB; ++j) acc[ha * HA + i][hb * HB + j] += sum[i][j];
-            }
+                for (int j = 0; j < HB; ++j) acc[ha * HA + i][hb * HB + j] += sum[i][j];
         }
     }
     // One phase; `others` asks for the half that is free now and reads `next`, the one that is needed later.  fp32: which is taken apart between the matrix
