@@ -177,3 +177,61 @@ def test_long_sums_lean_to_no_side(rows, vocab, dtype):
     want = x - torch.log(torch.tensor(vocab - 1.0).double()) + torch.log1p((vocab - 1) * torch.exp(-x))
     mean = ((got - want) / x).mean().abs()
     assert float(mean) <= 5 * 7.8e-7 / rows ** 0.5 + 2.0 ** -24 + 2.0 ** -24
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("rows,width,vocab", [(5, 24, 300), (70, 65, 1000), (300, 48, 9000)])
+def test_biases_of_the_lowest_value(rows, width, vocab, dtype):
+    """A bias of fp32's lowest value bars a token as -inf does, to the last bit; where it is everywhere, all tokens are alike."""
+    hidden, weight, bias, tokens, g = make(rows, width, vocab, 2, dtype, 49)
+    gone = torch.rand(vocab, generator=g, device="cuda") < 0.5
+    gone[0] = False
+    tokens = torch.where(gone[tokens], 0, tokens)
+    low = torch.finfo(torch.float32).min
+    d = adjoints(g, (rows, 2), (rows, 2), (rows,))
+    out = []
+    for least in (low, -torch.inf):
+        inputs = [t.detach().requires_grad_(True) for t in (hidden, weight, torch.where(gone, least, bias))]
+        r = klay().head_logprobs(inputs[0], inputs[1], tokens, inputs[2], complement=True, entropy=True)
+        out.append((*r, *torch.autograd.grad(list(r), inputs, d)))
+    for a, b in zip(*out):
+        assert torch.equal(a, b)
+    inputs = [t.detach().requires_grad_(True) for t in (hidden, weight, torch.full_like(bias, low))]
+    r = klay().head_logprobs(inputs[0], inputs[1], tokens, inputs[2], complement=True, entropy=True)
+    ln_v = torch.tensor(float(vocab)).double().log().item()
+    # (ln V from sums of V ones: one rounding of the result and of V's logarithm in it)
+    assert float((r.logp.double() + ln_v).abs().max()) <= 4 * 2.0 ** -24 * ln_v
+    assert float((r.entropy.double() - ln_v).abs().max()) <= 4 * 2.0 ** -24 * ln_v
+    assert all(bool(torch.isfinite(t).all()) for t in torch.autograd.grad(list(r), inputs, d))
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+def test_barred_weights_change_under_a_graph(dtype):
+    """whether the weights have to be copied is found out at every replay"""
+    hidden, weight, bias, tokens, g = make(40, 520, 9001, 1, dtype, 50)
+    gone = torch.rand(9001, generator=g, device="cuda") < 0.3
+    bias[gone] = -torch.inf
+    ins = [t.detach().clone().requires_grad_(True) for t in (hidden, weight, bias)]
+    ones = torch.ones(40, 1, device="cuda")
+
+    def step():
+        r = klay().head_logprobs(ins[0], ins[1], tokens, ins[2])
+        return [r.logp.detach(), *torch.autograd.grad(r.logp, ins, ones)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for turn, hole in enumerate((0.5, float("nan"), 0.25, float("inf"), float("nan"), 0.0)):
+        with torch.no_grad():
+            ins[0].copy_(torch.randn(hidden.shape, generator=g, device="cuda"))
+            ins[1][gone, ::5] = hole
+        want = step()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b), turn
+        assert all(bool(torch.isfinite(t).all()) for t in out[1:])         # (a barred token's own logp is -inf)
