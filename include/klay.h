@@ -432,8 +432,8 @@ klay_status klay_head_forward(const klay_head_args* args, float* logp, float* ne
  *   dlogp, dneg, dentropy   device, shaped as the outputs; each may be NULL (no adjoint)
  *   dhidden     device [rows, width] contiguous, of `dtype`; dweight device [vocab, width] contiguous, of `dtype`; dbias device [vocab]
  *               fp32; each may be NULL (not wanted); every entry is written (nothing where rows = 0)
- * The adjoints of the logits are made again in pieces of the vocabulary and rounded to `dtype` on their way into the two products (fp16: under a
- * power of two common to all); sums are fp32, and the same inputs give the same bits.  A row all of whose adjoints are exactly 0, or that
+ * The adjoints of the logits are made again in pieces of the vocabulary and go into the two products as two numbers of `dtype`, where it has 16 bits (fp16: under
+ * a power of two common to all); sums are fp32, and the same inputs give the same bits.  A row all of whose adjoints are exactly 0, or that
  * allows nothing, has no gradient and gives none, whatever it holds.
  */
 klay_status klay_head_backward(const klay_head_args* args, const void* kept, const float* dlogp, const float* dneg, const float* dentropy,

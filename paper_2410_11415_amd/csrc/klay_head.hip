@@ -119,7 +119,7 @@ ProductPlan product_plan(klay::HeadTile tile, int64_t rows, int64_t columns, int
 }
 
 constexpr int64_t kRowBlock = 16384;        // rows whose tiles' sums are held at a time
-constexpr int64_t kPieceElements = 1 << 25; // adjoints of logits that are held at a time, about
+constexpr int64_t kPieceElements = 1 << 25; // adjoints of logits that are held at a time, about: 128 MB
 constexpr int64_t kMostPiece = 1 << 20;
 constexpr int64_t kSmallCopy = 1 << 22;     // bytes of weights that are copied in as much time as a launch of its own takes
 constexpr int64_t kSmallProduct = 1ll << 30;    // up to here (rows x width x tokens) the two products are one launch, whatever tiles they would take alone
@@ -139,14 +139,11 @@ struct HeadPlan {
 };
 int64_t stages_of(int64_t elements, const Sizes& s) { return tiles(elements * s.bytes, klay::kMostStageBytes); }
 
-// Adjoints of 16-bit heads are rounded to 16 bits as the products' operands.  Over many entries that makes 1.41 times the error that the results' own rounding
-// makes; where a few entries make a result (one of a row's own tokens, mostly) or equal ones do, it can be 2.5 times.  There what the rounding leaves is held as
-// well, as rows of its own: for 16 rows and for small products it costs next to nothing (bf16, a step of training, 16 x 4096 x 131072: 863 us, 856 without),
-// otherwise a quarter or more (64 and 128 rows: 1132 and 1421, 883 and 1179 without; 512 would be 3211, 2302 without), which 256 rows are worth.
-constexpr int64_t kFewRows = 256, kSmallCut = 1ll << 32;     // (rows x width x tokens)
-int64_t cut_of(const klay_head_args* a, const Sizes& s) {
-    return s.bytes == 2 && (a->rows <= kFewRows || (double)a->rows * a->width * a->vocab < kSmallCut) ? 2 : 1;
-}
+// Adjoints of 16-bit heads are held in two numbers of the type as the products' operands, the second, of what the first's rounding leaves, as rows of its own:
+// rounded once they would make as large an error as the results' own rounding, and of few entries (one of a row's own tokens, mostly) or equal ones 1.5 times
+// it.  It costs what products of twice the terms cost (bf16, a step of training of 4096 features and 131072 tokens, with / without: 16 rows 863 / 856 us, 64
+// 1132 / 883, 512 3211 / 2302, 4096 22.2 / 14.7 ms).
+int64_t cut_of(const Sizes& s) { return s.bytes == 2 ? 2 : 1; }
 
 HeadPlan head_plan(const klay_head_args* a, bool back) {
     const Sizes s(a->dtype);
@@ -174,7 +171,7 @@ HeadPlan head_plan(const klay_head_args* a, bool back) {
         const int64_t all = up(a->vocab, 256);
         p.piece = std::min({all, kMostPiece, std::max<int64_t>(256, kPieceElements / up(a->rows, 256) / 256 * 256)});
         const int64_t columns = up(std::min<int64_t>(p.piece, a->vocab), 8);
-        p.cut = cut_of(a, s);
+        p.cut = cut_of(s);
         const int64_t rows = p.cut * a->rows;       // of the adjoints
         p.tile = logits_tile(a->rows, columns);
         p.coefs = take(a->rows * sizeof(float4));

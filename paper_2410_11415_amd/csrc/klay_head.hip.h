@@ -4,10 +4,9 @@
 // into the adjoint of the logits, which in all of these losses has the form
 //   G_ij = s_ij (A_i + B_i ln s_ij),  s_ij = e^((x_ij - ref_i) / T - ln S_i),
 // with an entry of its own for a listed token; then dH = G W, dW = G^T H, db = sum_i G_i, W, H and G^T read across from memory
-// that holds their rows.  G is rounded to the type of the operands
-// (bf16: 2^-8 of an entry at most, independent from entry to entry, so that a sum of many is off by as much again as its own rounding; of few entries a second
-// number of the type holds what the first leaves; fp16: under a power of two taken from the largest entry, so that small adjoints stay in its range; fp32: the
-// three parts of all operands).  Sums over tokens and rows are in fp32, in an order that the sizes alone decide.
+// that holds their rows.  G goes into the products as two numbers of the type of 16-bit operands, what the first one's rounding leaves in the second (bf16: off by
+// 2^-16 of an entry at most; fp16: 2^-22, under a power of two taken from the largest entry, so that small adjoints stay in its range), or as the three parts of all
+// operands of fp32.  Sums over tokens and rows are in fp32, in an order that the sizes alone decide.
 #pragma once
 
 #include "klay_lists.hip.h"
@@ -36,7 +35,7 @@ struct HeadArgs {
     const uint32_t* largest;                // bits of the largest adjoint (fp16), or null
     uint32_t* odd;                          // made 1 if a token that the bias bars may have weights that are not finite; or null
     void* g;                                // [rows, g_columns], or null
-    void* g_low;                            // likewise: what the rounding has left of g, or null
+    void* g_low;                            // likewise: what the rounding has left of g (16 bits), or null
     int64_t g_columns;                      // a multiple of 8
     float* bias_partial;                    // [tiles of rows, g_columns], or null
 };

@@ -10,7 +10,7 @@ namespace klay {
 
 template <typename T> using Tile32 = Tile<T, 128, 32, 4, 1, 3, 128>;
 template <typename T> using Tile64 = Tile<T, 128, 64, 4, 1, 3, 128>;
-// TileOne: the weights' gradient of at most 64 rows (fp32: 32) is all writing: little shared memory, for more workgroups at a time, and in 16 bits rows of 256
+// TileOne: the weights' gradient of at most 32 rows is all writing: little shared memory, for more workgroups at a time, and in 16 bits rows of 256
 // bytes a wave, past the caches where they are whole lines (16 x 4096 x 131072 bf16: 280 us; 318 through the caches, 378 by Tile128.  Rows that share lines take
 // twice the time past the caches).
 template <typename T> struct Large {

@@ -299,9 +299,8 @@ def head_logprobs(hidden, weight, tokens=None, bias=None, *, complement=False, e
 
     ``logp[..., K]``, with ``complement`` ``neg[..., K]``, with ``entropy`` the entropies ``[...]``, all float32 and differentiable with
     respect to ``hidden``, ``weight`` and ``bias`` (backward only: tensors with tangents are refused).  A bias of -inf is a token that is
-    not allowed; a negative token asks for nothing, a token >= V gives NaN.  The gradients have the types of their inputs.  With 16-bit types the
-    logits' adjoints are rounded to those bits before they meet the weights and the hidden states (float16: scaled into its range first); for up
-    to 256 rows, and for small products, what the rounding leaves is taken along.
+    not allowed; a negative token asks for nothing, a token >= V gives NaN.  The gradients have the types of their inputs
+    and are rounded once: 16-bit types hold the logits' adjoints in two numbers on their way to the weights and the hidden states.
 
     Rows should start at multiples of 4 bytes (16 serve best), with one stride between them; others are copied first.  At most 2^20 rows, 1024
     tokens a row.
