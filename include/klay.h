@@ -444,7 +444,8 @@ klay_status klay_head_backward(const klay_head_args* args, const void* kept, con
  *   p = softmax(x / temperature);  q = softmax(teacher / temperature) over the listed tokens
  *   loss = sum_k q_k (ln q_k - ln p_{t_k})
  *   rest: the teacher gives log probabilities, q_k = exp(teacher_k), and all tokens that are not listed are one more answer, q_r = 1 - sum q
- *   (0 where that is negative, or no such token is allowed): + q_r (ln q_r - ln(1 - sum of p over the listed tokens))
+ *   (0 where that is negative, or no such token is allowed: the q then add up to what the list has): + q_r (ln q_r - ln(1 - sum of p over the
+ *   listed tokens))
  *   args        logits and tokens as for klay_tokens_forward, top = 0, num_tokens >= 1.  A negative token lists nothing; a token >= vocab
  *               gives NaN; of a token listed more than once the q add up in the gradient
  *   teacher     logits: device fp32 [rows, num_tokens], placed by rows and stride (elements); 0.001 <= temperature <= 1000

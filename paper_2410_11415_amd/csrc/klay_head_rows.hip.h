@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(256) head_lists_kernel(ListArgs g) {
 struct AdjointArgs {
     const float* stats;                     // [rows, kRowFloats]
     const int32_t *sorted, *slots;
-    const float* values;                    // forward's: logits of the listed tokens; of a distillation p - q
+    const float* values;                    // forward's: logits of the listed tokens; of a distillation Q p - q
     const float *dlogp, *dneg, *dentropy;   // or null
     const float* dloss;
     float inverse_temperature;

@@ -184,7 +184,8 @@ __device__ __forceinline__ void finish_logprobs(const RowOut& out, int64_t r, in
 // ---- divergence from a teacher's list ------------------------------------------------------------------------------
 //   q = softmax of the listed teacher logits / T (rest: e^teacher, and q_r = 1 - sum q for all other tokens together), p = softmax(x / T)
 //   loss = sum q_k (ln q_k - ln p_k) + q_r (ln q_r - ln (1 - P)),  P = sum of p over the listed tokens
-//   T dx_j = p_j - sum_{k: t_k = j} q_k for a listed token, p_j (1 - q_r / (1 - P)) for the others
+//   T dx_j = Q p_j - sum_{k: t_k = j} q_k for a listed token, p_j (Q - q_r / (1 - P)) for the others, Q the sum of all q: 1 but with `rest` where the
+//   list has more than 1, or has less and no other token is allowed (q_r is 0 then)
 struct TeachArgs {
     const float* teacher;                   // placed by these; row r of the call is its row first + r
     RowMap teacher_rows;
@@ -194,10 +195,10 @@ struct TeachArgs {
     int32_t rest;
     float* loss;                            // [rows]
     float* stats;                           // [rows, kRowFloats], or null
-    float* moved;                           // [rows, num_tokens]: of a sorted token its entry of the gradient, p - q; or null
+    float* moved;                           // [rows, num_tokens]: of a sorted token its entry of the gradient, Q p - q; or null
 };
 struct TeachStats {
-    float ref, ref_log, others;             // others: (1 - P) - q_r, which the tokens that are not listed have by their shares of 1 - P
+    float ref, ref_log, others;             // others: Q (1 - P) - q_r, which the tokens that are not listed have by their shares of 1 - P
     int32_t live;                           // 0: nothing is listed, or nothing allowed: no gradient
     float unused[4];
 };
@@ -240,6 +241,7 @@ __device__ __forceinline__ void finish_distill(const TeachArgs& t, int64_t r, in
     const double log_s = log(s), log_z = t.rest ? 0.0 : log(zs);
     const bool others = o.max > -INFINITY;
     const double q_rest = t.rest && others ? fmax(0.0, 1.0 - zs) : 0.0;
+    const double q_all = t.rest && !(q_rest > 0.0) ? zs : 1.0;
     const bool empty = M == -INFINITY && s == 0.0, nan = bad > 0.0f || M == INFINITY || s != s;
     double loss = 0.0, q0 = 0.0;                              // q0: of entry `lane`
     for (int32_t k = lane; k < K; k += 64) {
@@ -267,7 +269,7 @@ __device__ __forceinline__ void finish_distill(const TeachArgs& t, int64_t r, in
                 }
             }
             const double lp = there && x[u] > -INFINITY ? ((double)x[u] - at) * inv - log_s : -INFINITY;
-            if (u < K) t.moved[r * K + u] = !there ? 0.0f : nan ? NAN : (float)(exp(lp) - taken);
+            if (u < K) t.moved[r * K + u] = !there ? 0.0f : nan ? NAN : (float)(q_all * exp(lp) - taken);
         }
     }
     loss = wave_sum(loss);
@@ -282,7 +284,7 @@ __device__ __forceinline__ void finish_distill(const TeachArgs& t, int64_t r, in
         st.ref = others ? o.max : 0.0f;
         st.ref_log = (float)log_o;
         st.live = teaches && !empty;
-        st.others = !st.live ? 0.0f : nan ? NAN : (float)(o_mass / s - q_rest);
+        st.others = !st.live ? 0.0f : nan ? NAN : (float)(q_all * (o_mass / s) - q_rest);
         reinterpret_cast<TeachStats*>(t.stats)[r] = st;
     }
 }

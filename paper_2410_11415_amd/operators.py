@@ -364,7 +364,7 @@ def token_distill(logits, tokens, teacher, *, temperature=1.0, rest=False):
         loss = sum_k q_k (ln q_k - ln p_{t_k}),  p = softmax(logits / temperature),  q = softmax(teacher / temperature) over the list.
 
     With ``rest`` ``teacher`` holds log probabilities, q_k = exp(teacher_k), and all tokens that are not listed are one more answer with what
-    the list leaves, q_r = 1 - sum q (0 where no such token is allowed): the loss gets + q_r (ln q_r - ln p_r).
+    the list leaves, q_r = 1 - sum q (0 where no such token is allowed, or the list has more than 1): the loss gets + q_r (ln q_r - ln p_r).
 
     A negative token lists nothing (lists of different lengths), a row that lists nothing has loss 0; a token >= V gives NaN.  A logit of -inf is a
     token that is not allowed.  Differentiable with respect to ``logits`` (backward only: tensors with tangents are refused); the teacher is a

@@ -116,6 +116,8 @@ def distill(x, t, teacher, temperature, rest, slip, dloss=None):
     share = torch.where(left > 0, q_left / left, 0.0)[:, None] * others
     on = some[:, None]
     g = dloss[:, None] / T
+    # each q pulls its own answer up against all of them: p counts as often as the q add up to (1 but for lists of more, and for ones that no rest completes)
+    p = p * (q.sum(1) + q_left)[:, None]
     dx = torch.where(on, (p - target - share) * g, 0.0)
     mass = torch.where(on, (p + target + share) * g.abs(), 0.0)
     steps = torch.where(p > 0, 4 * U * _safe(lp), 0.0)
