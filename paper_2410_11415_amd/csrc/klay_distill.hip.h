@@ -170,12 +170,13 @@ __global__ void __launch_bounds__(THREADS, FINISH ? 4 : 6) distill_row_kernel(Di
     }
 }
 __global__ void __launch_bounds__(256) distill_finish_kernel(DistillArgs g) {
-    const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), at = r * g.list.num_tokens;
-    if (r >= g.list.rows) return;
-    Others o;
-    o.max = g.sums[r * kRowFloats];
-    o.sum = g.sums[r * kRowFloats + 1];
-    finish_distill(g.teach, r, g.list.num_tokens, g.list.sorted + at, g.list.slots + at, g.teach.moved + at, o);
+    for (int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); r < g.list.rows; r += (int64_t)gridDim.x * 4) {
+        const int64_t at = r * g.list.num_tokens;
+        Others o;
+        o.max = g.sums[r * kRowFloats];
+        o.sum = g.sums[r * kRowFloats + 1];
+        finish_distill(g.teach, r, g.list.num_tokens, g.list.sorted + at, g.list.slots + at, g.teach.moved + at, o);
+    }
 }
 
 // Rows of at most 512: a wave each, the logits in its registers; lists of at most LISTED.
@@ -188,49 +189,53 @@ __global__ void __launch_bounds__(256) distill_short_kernel(DistillArgs g) {
     __shared__ uint32_t bits[4][kShortDistill / 32];
     const int w = threadIdx.x >> 6;
     const int32_t lane = threadIdx.x & 63, K = g.list.num_tokens;
-    const int64_t r = (int64_t)blockIdx.x * 4 + w;
-    const bool there = r < g.list.rows;
-    const T* row = static_cast<const T*>(g.logits) + (there ? g.logit_rows.at(r) : 0);
-    float x[E];
+    for (int64_t first_row = (int64_t)blockIdx.x * 4; first_row < g.list.rows; first_row += (int64_t)gridDim.x * 4) {
+        const int64_t r = first_row + w;
+        const bool there = r < g.list.rows;
+        const T* row = static_cast<const T*>(g.logits) + (there ? g.logit_rows.at(r) : 0);
+        float x[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = there && lane + 64 * e < g.list.vocab ? (float)row[lane + 64 * e] : -INFINITY;
-    if (lane < kShortDistill / 32) bits[w][lane] = 0;
-    if constexpr (LISTED <= 64) {
-        bool first;
-        const int32_t token = there && lane < K ? token_of(g.list, r, lane) : kNothing, slot = slot_in_wave(token, K, first);
-        if (lane < K) {
-            slots[w][lane] = slot;
-            sorted[w][lane] = kNoToken;
+        for (int e = 0; e < E; ++e) x[e] = there && lane + 64 * e < g.list.vocab ? (float)row[lane + 64 * e] : -INFINITY;
+        if (lane < kShortDistill / 32) bits[w][lane] = 0;
+        if constexpr (LISTED <= 64) {
+            bool first;
+            const int32_t token = there && lane < K ? token_of(g.list, r, lane) : kNothing, slot = slot_in_wave(token, K, first);
+            if (lane < K) {
+                slots[w][lane] = slot;
+                sorted[w][lane] = kNoToken;
+            }
+            __syncthreads();
+            if (first) sorted[w][slot] = token;
+            __syncthreads();
+        } else {
+            make_list(g.list, r, there, lane, 64, mark[w], sorted[w], slots[w]);
+        }
+        for (int32_t u = lane; u < K; u += 64) {
+            const int32_t j = sorted[w][u];
+            if (j == kNoToken) continue;
+            listed[w][u] = (float)row[j];
+            atomicOr(&bits[w][j >> 5], 1u << (j & 31));
         }
         __syncthreads();
-        if (first) sorted[w][slot] = token;
-        __syncthreads();
-    } else {
-        make_list(g.list, r, there, lane, 64, mark[w], sorted[w], slots[w]);
-    }
-    for (int32_t u = lane; u < K; u += 64) {
-        const int32_t j = sorted[w][u];
-        if (j == kNoToken) continue;
-        listed[w][u] = (float)row[j];
-        atomicOr(&bits[w][j >> 5], 1u << (j & 31));
-    }
-    __syncthreads();
-    if (!there) return;
-    Others o;
+        if (there) {
+            Others o;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const int32_t j = lane + 64 * e;
-        if (bits[w][j >> 5] >> (j & 31) & 1u) x[e] = -INFINITY;
-        o.max = fmaxf(o.max, x[e]);
-    }
-    o.max = wave_max(o.max);
-    const float to = fmaxf(o.max, -kTokFltMax);
-    float s = 0.0f;
+            for (int e = 0; e < E; ++e) {
+                const int32_t j = lane + 64 * e;
+                if (bits[w][j >> 5] >> (j & 31) & 1u) x[e] = -INFINITY;
+                o.max = fmaxf(o.max, x[e]);
+            }
+            o.max = wave_max(o.max);
+            const float to = fmaxf(o.max, -kTokFltMax);
+            float s = 0.0f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) s += exp2_of((x[e] - to) * g.scale);
-    o.sum = group_sum<64>(s);
-    finish_distill(g.teach, r, K, sorted[w], slots[w], listed[w], o);
-    for (int32_t u = lane; u < K; u += 64) g.list.sorted[r * K + u] = sorted[w][u];
+            for (int e = 0; e < E; ++e) s += exp2_of((x[e] - to) * g.scale);
+            o.sum = group_sum<64>(s);
+            finish_distill(g.teach, r, K, sorted[w], slots[w], listed[w], o);
+            for (int32_t u = lane; u < K; u += 64) g.list.sorted[r * K + u] = sorted[w][u];
+        }
+        __syncthreads();                    // shared memory is free again
+    }
 }
 
 // dx_j = A s_j, then the listed tokens' entries.  A workgroup a row part.

@@ -473,6 +473,7 @@ klay_status head_backward(const klay_head_args* a, const klay_teacher* teacher, 
 
 // ---- divergence of given logits -----------------------------------------------------------------------------------------
 constexpr int64_t kManyRows = 2 * klay::kComputeUnits;
+// (a launch has less than 2^32 threads; the kernels run through what is left)
 uint32_t capped_grid(int64_t units) { return (uint32_t)std::min<int64_t>(units, 1 << 20); }
 
 klay::DistillArgs distill_args(const klay_tokens_args* a, const klay_teacher* t) {
@@ -485,7 +486,7 @@ klay::DistillArgs distill_args(const klay_tokens_args* a, const klay_teacher* t)
     return g;
 }
 template <typename T> klay_status run_distill(const klay::DistillArgs& g, void* stream) {
-    const dim3 grid(capped_grid(g.list.rows)), waves((uint32_t)tiles(g.list.rows, 4));
+    const dim3 grid(capped_grid(g.list.rows)), waves(capped_grid(tiles(g.list.rows, 4)));
     if (g.list.vocab <= klay::kShortDistill) {
         if (g.list.num_tokens <= 64) KLAY_LAUNCH((klay::distill_short_kernel<T, 64>), waves, dim3(256), stream, g);
         else KLAY_LAUNCH((klay::distill_short_kernel<T, klay::kMaxListed>), waves, dim3(256), stream, g);
