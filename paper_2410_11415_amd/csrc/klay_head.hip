@@ -118,7 +118,8 @@ ProductPlan product_plan(klay::HeadTile tile, int64_t rows, int64_t columns, int
     return ProductPlan{tile, (int32_t)std::max<int64_t>(1, std::min<int64_t>({want / count, stages / 8, 32}))};
 }
 
-constexpr int64_t kRowBlock = 16384;        // rows whose tiles' sums are held at a time
+constexpr int64_t kRowBlock = 16384;        // rows whose tiles' sums are held at a time, at most
+constexpr int64_t kMostSums = 1 << 22;      // such sums of 16 bytes, of more than one tile of rows: 16384 tiles of 256 x 256, 64 for every compute unit
 constexpr int64_t kPieceElements = 1 << 25; // adjoints of logits that are held at a time, about: 128 MB
 constexpr int64_t kMostPiece = 1 << 20;
 constexpr int64_t kSmallCopy = 1 << 22;     // bytes of weights that are copied in as much time as a launch of its own takes
@@ -162,9 +163,13 @@ HeadPlan head_plan(const klay_head_args* a, bool back) {
     if (p.copy_weight) p.weight = take(a->vocab * p.padded * s.bytes);
     const int64_t asked = a->rows * a->num_tokens;
     if (!back) {
-        p.row_block = std::min(a->rows, kRowBlock);
-        p.tile = logits_tile(p.row_block, a->vocab);
-        p.tiles_n = tiles(a->vocab, klay::kTileSizes[p.tile].columns);
+        const auto block = [&](int64_t rows) {
+            p.row_block = rows;
+            p.tile = logits_tile(rows, a->vocab);
+            p.tiles_n = tiles(a->vocab, klay::kTileSizes[p.tile].columns);
+        };
+        block(std::min(a->rows, kRowBlock));
+        if (p.row_block > 256 && p.row_block * p.tiles_n > kMostSums) block(std::max<int64_t>(256, kMostSums / p.tiles_n / 256 * 256));
         p.partial = take(p.row_block * p.tiles_n * sizeof(float4));
         p.kept = take(kept_bytes(a->rows, a->num_tokens));
     } else {
