@@ -58,10 +58,11 @@ __global__ void __launch_bounds__(THREADS, FINISH ? 4 : 6) distill_row_kernel(Di
                 if (tid < K) {
                     slots[tid] = slot;
                     sorted[tid] = kNoToken;
-                    if (first) {
-                        sorted[slot] = token;
-                        listed[slot] = (float)row[token];
-                    }
+                }
+                wave_ordered();             // (a lane's token may belong where another lane has just said that there is none)
+                if (first) {
+                    sorted[slot] = token;
+                    listed[slot] = (float)row[token];
                 }
             }
             __syncthreads();

@@ -50,8 +50,7 @@ __device__ __forceinline__ bool list_of_one(const FinishArgs& g, int64_t r, One*
         g.sorted[r] = one->sorted;
         g.slots[r] = one->slot;
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+    wave_ordered();
     return true;
 }
 __global__ void __launch_bounds__(256) head_logprobs_finish_kernel(FinishArgs g, RowOut out) {

@@ -69,6 +69,12 @@ __device__ __forceinline__ int32_t slot_in_wave(int32_t token, int32_t K, bool& 
     return token < 0 ? token : place;
 }
 
+// What a wave's lanes have written into shared memory before is there for all of them.
+__device__ __forceinline__ void wave_ordered() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // ---- sums over a wave ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ double lane_of(double x, int lane) {
     return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(x), lane), __builtin_amdgcn_readlane(__double2loint(x), lane));
