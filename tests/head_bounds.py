@@ -50,3 +50,26 @@ def worst(got, want, dtype):
     """The largest error in units of what is allowed: the tolerance and one rounding."""
     value, tol = want
     return float(((got.double() - value).abs() / (tol + REL[dtype] * (value.abs() + tol) + TINY[dtype])).max())
+
+
+def slip_by_sums(hidden, weight, bias=None):
+    """What a row's logits may be off by, from the sums themselves: sixteen terms at a time join a sum S of fp32, with four roundings of S and of the magnitude of
+    what joins it; fp32 operands go through as several products of their parts, twice that.  (Of wide rows the magnitudes of all terms say little: S is some
+    steps of a walk, its terms together hundreds of times that.)"""
+    h, w = hidden.double(), weight.double()
+    s = torch.zeros(h.shape[0], w.shape[0], dtype=torch.float64, device=h.device)
+    run = torch.zeros_like(s)
+    for k in range(0, h.shape[1], 16):
+        a, b = h[:, k:k + 16], w[:, k:k + 16].t().contiguous()
+        s += a @ b
+        run += s.abs() + a.abs() @ b.abs()
+    slip = 4 * U * (2 if hidden.dtype == torch.float32 else 1) * run.amax(1)
+    return slip if bias is None else slip + 2 * U * (s.abs().amax(1) + bias.double().abs().max())
+
+
+def negated(x, t, slip, terms):
+    """(log(1 - p) of row i's tokens, its tolerance): what p / (1 - p) of a change of the logarithm makes of it, and no more than all others together change."""
+    p = torch.log_softmax(x, 1).exp()
+    r = torch.stack([p.scatter(1, t[:, k:k + 1], 0.0).sum(1) for k in range(t.shape[1])], 1)
+    neg = r.log()
+    return neg, (p.gather(1, t) / r).clamp(max=1.0) * (4 * slip[:, None] + terms) + 8 * U * neg.abs()
