@@ -122,8 +122,13 @@ constexpr int64_t kRowBlock = 16384;        // rows whose tiles' sums are held a
 constexpr int64_t kMostSums = 1 << 22;      // such sums of 16 bytes, of more than one tile of rows: 16384 tiles of 256 x 256, 64 for every compute unit
 constexpr int64_t kPieceElements = 1 << 25; // adjoints of logits that are held at a time, about: 128 MB
 constexpr int64_t kMostPiece = 1 << 20;
-constexpr int64_t kSmallCopy = 1 << 22;     // bytes of weights that are copied in as much time as a launch of its own takes
-constexpr int64_t kSmallProduct = 1ll << 30;    // up to here (rows x width x tokens) the two products are one launch, whatever tiles they would take alone
+// Bytes of weights that are copied with the hidden states, which saves a launch: longer ones cost more than that (backward of 256 rows of 1024 features in
+// bf16, in a graph, copied / only if need be: 1 MB 38.5 / 38.6 us, 2 MB 43.6 / 41.9, 4 MB 48.1 / 45.0, 8 MB 53.5 / 49.1).
+constexpr int64_t kSmallCopy = 1 << 20;
+// Up to here (rows x width x tokens) the two products are one launch, by the smaller of the tiles that they would take alone: a launch less, and as fast or
+// faster (32 x 1024 x 8192 bf16 40.2 us, 43.0 in two; 2^26 to 2^30 terms of 64 to 512 rows within 1%); beyond, the smaller tiles cost more (16 x 4096 x 16384
+// 159.8 us, 103.2 in two).
+constexpr int64_t kSmallProduct = 1ll << 30;
 
 struct HeadPlan {
     bool copy_hidden = false, copy_weight = false;
@@ -251,7 +256,7 @@ template <typename T> struct Head {
     klay::PackArgs& pack(const void* from, const klay_rows& rows, int64_t count, size_t to) {
         klay::PackArgs& c = packs.copy[packs.copies++];
         c = copy(from, rows, count);
-        c.stride = c.padded = p.padded;
+        c.padded = p.padded;
         c.to = in(workspace, to);
         return c;
     }
@@ -283,7 +288,6 @@ template <typename T> struct Head {
         g.hidden = hidden;
         g.weight = weight;
         g.bias = a->bias;
-        g.vocab = a->vocab;
         g.tail = tail;
         g.rows = a->rows;
         g.num_tokens = a->num_tokens;

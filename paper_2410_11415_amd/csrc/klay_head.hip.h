@@ -18,7 +18,7 @@ namespace klay {
 struct HeadArgs {
     Operand hidden, weight;                 // [rows, width], [tokens of this launch, width]
     const float* bias;                      // of these tokens, or null
-    int32_t first, vocab;                   // the first of these tokens; how many tokens there are in all
+    int32_t first;                          // the first of these tokens
     int64_t rows;
     int32_t tail;                           // elements of a row behind its last whole piece of 16 bytes
     int32_t num_tokens;

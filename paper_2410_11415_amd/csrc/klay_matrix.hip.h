@@ -535,7 +535,6 @@ struct PackArgs {
     int64_t inner;
     int64_t count, columns;                 // rows and columns taken
     void* to;
-    int64_t stride;                         // of the copy, elements
     int64_t padded;                         // elements of a row of the copy; zeros behind what is taken
     int32_t finite;                         // 1: only what is finite is taken, zeros for the rest
     const float* bias;                      // of a row whose entry is -inf likewise; null: of none
@@ -558,7 +557,7 @@ __device__ __forceinline__ void pack_rows(const PackArgs& g, int64_t block, int6
 #pragma unroll
             for (int e = 0; e < N; ++e) out[e] = fabsf((float)out[e]) < INFINITY ? out[e] : (T)0.0f;
         }
-        *reinterpret_cast<typename Pieces<T, N>::Vec*>(static_cast<T*>(g.to) + r * g.stride + c) = out;
+        *reinterpret_cast<typename Pieces<T, N>::Vec*>(static_cast<T*>(g.to) + r * g.padded + c) = out;
     }
 }
 
