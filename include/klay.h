@@ -406,7 +406,10 @@ klay_status klay_tokens_backward(const klay_tokens_args* args, const float* stat
  *   kept        device, 16-byte aligned, klay_list_kept_bytes(rows, num_tokens) bytes: what klay_head_backward needs of the rows; NULL: not kept
  *   workspace   device, 16-byte aligned, klay_head_workspace_bytes(args, 0) bytes (for klay_head_backward: args, 1)
  * Rows are read where they lie if they have one stride, and their first and that stride are at multiples of 4 bytes; others are copied into the
- * workspace first.  A row whose hidden state, or any allowed token's weights, holds a NaN or an infinity may get NaN in every value.
+ * workspace first.  A forward call's workspace holds the sums of tiles (64 MB, or those of 256 rows) and what `kept` would; a backward one's the
+ * adjoints of a piece of the vocabulary (about 2^25 of them, 128 MB; of 256 tokens at least), fp32 sums of dhidden, a copy of hidden (two of 16
+ * bits) and, with a bias, room for the piece's weights (of 256 rows or fewer those of 131072 tokens).
+ * A row whose hidden state, or any allowed token's weights, holds a NaN or an infinity may get NaN in every value.
  * Errors: KLAY_EINVAL (sizes out of range: 1 <= vocab <= 2^31 - 4097, 1 <= width <= 2^20, 0 <= num_tokens <= 1024, 0 <= rows <= 2^20; null or
  * unknown arguments), KLAY_ENOMEM (workspace too small), KLAY_EHIP.
  */

@@ -121,7 +121,6 @@ ProductPlan product_plan(klay::HeadTile tile, int64_t rows, int64_t columns, int
 constexpr int64_t kRowBlock = 16384;        // rows whose tiles' sums are held at a time, at most
 constexpr int64_t kMostSums = 1 << 22;      // such sums of 16 bytes, of more than one tile of rows: 16384 tiles of 256 x 256, 64 for every compute unit
 constexpr int64_t kPieceElements = 1 << 25; // adjoints of logits that are held at a time, about: 128 MB
-constexpr int64_t kMostPiece = 1 << 20;
 // Bytes of weights that are copied with the hidden states, which saves a launch: longer ones cost more than that (backward of 256 rows of 1024 features in
 // bf16, in a graph, copied / only if need be: 1 MB 38.5 / 38.6 us, 2 MB 43.6 / 41.9, 4 MB 48.1 / 45.0, 8 MB 53.5 / 49.1).
 constexpr int64_t kSmallCopy = 1 << 20;
@@ -179,7 +178,7 @@ HeadPlan head_plan(const klay_head_args* a, bool back) {
         p.kept = take(kept_bytes(a->rows, a->num_tokens));
     } else {
         const int64_t all = up(a->vocab, 256);
-        p.piece = std::min({all, kMostPiece, std::max<int64_t>(256, kPieceElements / up(a->rows, 256) / 256 * 256)});
+        p.piece = std::min(all, std::max<int64_t>(256, kPieceElements / up(a->rows, 256) / 256 * 256));
         const int64_t columns = up(std::min<int64_t>(p.piece, a->vocab), 8);
         p.cut = cut_of(s);
         const int64_t rows = p.cut * a->rows;       // of the adjoints
@@ -189,6 +188,8 @@ HeadPlan head_plan(const klay_head_args* a, bool back) {
         p.largest = take(8);
         p.g = take(rows * columns * s.bytes);
         p.clean_hidden = take(rows * p.padded * s.bytes);
+        // (Room for the piece's weights, of few rows all weights.  In pieces of 256 MB of them steps cost more: 16 x 4096 x 131072 bf16 680 / 761 us, 256 rows 1482 /
+        // 1670, 16 x 4096 x 65536 fp32 688 / 894.)
         if (a->bias) p.clean_weight = take(columns * p.padded * s.bytes);
         const int64_t dw_rows = std::min<int64_t>(p.piece, a->vocab), dh_stages = stages_of(columns, s), dw_stages = stages_of(rows, s);
         klay::HeadTile dh = product_tile(rows, a->width, dh_stages), dw = product_tile(dw_rows, a->width, dw_stages);

@@ -295,7 +295,8 @@ def _check_tokens(tokens, of, name):
 def head_logprobs(hidden, weight, tokens=None, bias=None, *, complement=False, entropy=False) -> HeadLogprobs:
     """:func:`token_logprobs` of the logits ``hidden @ weight.T + bias``, which are never in memory: ``hidden[..., D]``, ``weight[V, D]``
     (both float32, bfloat16 or float16), ``bias[V]`` float32 or None, ``tokens[..., K]`` int64.  The logits are made in pieces on the chip,
-    in float32, forward and once more backward, so that a call needs memory for a few thousand columns of them at a time.
+    in float32, forward and once more backward, so that a call needs memory for a piece of them at a time (backward about 2^25 logits,
+    and with a bias room for the weights of as many tokens).
 
     ``logp[..., K]``, with ``complement`` ``neg[..., K]``, with ``entropy`` the entropies ``[...]``, all float32 and differentiable with
     respect to ``hidden``, ``weight`` and ``bias`` (backward only: tensors with tangents are refused).  A bias of -inf is a token that is
